@@ -179,6 +179,37 @@ int r3_combine(const r3_layer_desc *desc, const void *Yp, const float *gates,
                const int32_t *inv_perm, void *y, void *stream);
 
 /*
+ * Gradients of r3_combine and of r3_permute's rows as calls of their own, for
+ * expert networks that are not this library's (adapters, other activations or
+ * number formats): r3_permute, the caller's experts on the rows of Xp,
+ * r3_combine; back: r3_combine_backward, the caller's gradients, then
+ * r3_permute_backward.  (r3_moe_backward has the two in its own steps.)
+ *
+ * r3_combine_backward: given dy [T,d], for the K slots of every token
+ *   dYp[inv_perm[t*K+j]] = gates[t,j] dy[t]              ([T*K,d], one rounding)
+ *   dgates[t,j] = <dy[t], Yp[inv_perm[t*K+j]]>           ([T,K] f32, f32 sums)
+ *   dz[t,j] = gates[t,j] (dgates[t,j] - sum_i gates[t,i] dgates[t,i])
+ * dz [T,K] f32 is the gradient of the K selected logits where the gates are
+ * r3_replay_gate's softmax of them.  dYp, dgates and dz may each be NULL, but
+ * not all three; Yp is needed (and read) for dgates and dz only.  dYp may be
+ * Yp itself (not a part of it).
+ *
+ * r3_permute_backward: dx[t] = add[t] + sum_j dXp[inv_perm[t*K+j]], j
+ * ascending, f32 sums, one rounding.  dXp [T*K,d], dx [T,d], add [T,d] (act) or
+ * NULL; add is for what else reaches x (the router's dz W_r^T, a residual), and
+ * may be dx itself (not a part of it).
+ *
+ * A row outside [0, T*K) in inv_perm (a bad record) is left out: nothing is
+ * read or written for the slot and its dgates is 0.  desc->flags and the
+ * record's fields are ignored.  No workspace.  R3_ERR_UNSUPPORTED where
+ * T * ceil(d * sizeof(act) / 1024) exceeds 2^25 - 4.
+ */
+int r3_combine_backward(const r3_layer_desc *desc, const void *dy, const void *Yp, const float *gates,
+                        const int32_t *inv_perm, void *dYp, float *dgates, float *dz, void *stream);
+int r3_permute_backward(const r3_layer_desc *desc, const void *dXp, const int32_t *inv_perm,
+                        const void *add, void *dx, void *stream);
+
+/*
  * The replayed forward in one call (Section 4.1: router logits, replay gate,
  * and the replay-output equation y = sum_i g_i E_i(x) over the recorded
  * experts).  Same results as r3_replay_gate, r3_permute (without the gathered
@@ -272,6 +303,58 @@ int r3_policy_discrepancy(int64_t n, const float *logp_train, const float *logp_
                           const float *tau, double *kl_out, double *frac_out, void *ws,
                           size_t ws_bytes, void *stream);
 size_t r3_policy_workspace_bytes(void);
+
+/*
+ * Log-probabilities of given tokens under a row of logits each, with entropy
+ * and the most probable alternatives: what the recompute and update stages
+ * (Section 5.1) need of the model's head, and r3_policy_discrepancy's input.
+ * logits: device [n, V], row i at logits + i*ld elements (ld >= V; rows may
+ * start at any element), dtype R3_BF16 or R3_F32.  scale = 1 / temperature, in
+ * [1e-6, 1e6].  With m = max_v z_v, S = sum_v exp(scale (z_v - m)) and
+ * l_v = scale (z_v - m) - log S, row i's outputs (f32, each may be NULL, but
+ * not all) are
+ *   logp[i] = l_target[i],  entropy[i] = -sum_v exp(l_v) l_v,
+ *   stats[i] = {m, S} ([n,2]; what r3_token_logprobs_backward reads),
+ *   top_logp[i], top_id[i] ([n,top]): the `top` largest l_v, descending, and
+ *     their ids; ties go to the lower id, -0 equals +0.
+ * target: device int32 [n], or NULL (every row counts; logp must be NULL).
+ * Row i is left out if target[i] is -1 (prompt, padding): its logits are not
+ * read, its logp, entropy and stats are 0 and it has no alternatives.  Other
+ * values outside [0, V) do the same and set R3_DATA_IDX_RANGE.
+ * A logit of -inf is a masked token: probability 0, logp -inf, never an
+ * alternative (missing ones: id -1, logp -inf).  The lowest finite value is an
+ * ordinary logit.  A row of nothing but -inf: logp -inf, entropy 0, stats
+ * {-inf, 0}.  A NaN or +inf in a row sets R3_DATA_NONFINITE and makes its
+ * floating outputs NaN and its ids -1.
+ * Sums are f32.  Few long rows are cut over several work-groups and joined by
+ * a second launch; a row's last bits can depend on how it is cut, that is on n
+ * and V.
+ * top <= R3_MAX_TOP; 0: top_logp and top_id are not read.  n = 0 is a no-op.
+ * ws: device workspace of r3_token_logprobs_workspace_bytes(n, V, top) (0 is
+ * possible; then ws may be NULL).
+ *
+ * r3_token_logprobs_backward: the gradient of sum_i (dlogp[i] logp[i] +
+ * dentropy[i] entropy[i]) with respect to the logits,
+ *   dlogits[i,v] = scale ([v = target[i]] dlogp[i]
+ *                         - exp(l_v) (dlogp[i] + dentropy[i] (l_v + entropy[i]))),
+ * from the forward's logits, target, scale, stats and entropy.  dlogp, dentropy
+ * [n] f32: one may be NULL (then zero); entropy is needed with dentropy, target
+ * with dlogp.  dlogits: [n, V] of the logits' dtype, row i at dlogits + i*ldd,
+ * one rounding; columns past V are not written.  Rows left out and rows of
+ * nothing but -inf get zeros; a masked token gets [v = target] dlogp scale.
+ * dlogits may be logits itself with ldd = ld; any other overlap of the two is
+ * refused (R3_ERR_INVALID_ARG).
+ */
+#define R3_MAX_TOP 32
+size_t r3_token_logprobs_workspace_bytes(int64_t n, int64_t V, int top);
+int r3_token_logprobs(int64_t n, int64_t V, int dtype, const void *logits, int64_t ld, float scale,
+                      const int32_t *target, float *logp, float *entropy, float *stats, int top,
+                      float *top_logp, int32_t *top_id, int32_t *status_word, void *ws, size_t ws_bytes,
+                      void *stream);
+int r3_token_logprobs_backward(int64_t n, int64_t V, int dtype, const void *logits, int64_t ld, float scale,
+                               const int32_t *target, const float *stats, const float *entropy,
+                               const float *dlogp, const float *dentropy, void *dlogits, int64_t ldd,
+                               void *stream);
 
 /*
  * Router-mask cache (Section 4.2: routing masks stored with the KV cache per

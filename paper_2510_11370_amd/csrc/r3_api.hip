@@ -36,6 +36,10 @@ int check_desc(const r3_layer_desc *D, Dims &m) {
 }
 
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
+// whether two arrays share bytes (one that is not given shares none)
+bool overlap(const void *p, size_t np, const void *q, size_t nq) {
+    return p && q && (uintptr_t)p < (uintptr_t)q + nq && (uintptr_t)q < (uintptr_t)p + np;
+}
 bool force_simt() {
     const char *v = getenv("R3_FORCE_SIMT");
     return v && v[0] == '1';
@@ -257,6 +261,34 @@ int r3_combine(const r3_layer_desc *desc, const void *Yp, const float *gates, co
     return hip_rc(launch_combine(m.T, m.d, m.K, m.act, Yp, gates, inv_perm, y, (hipStream_t)stream));
 }
 
+int r3_combine_backward(const r3_layer_desc *desc, const void *dy, const void *Yp, const float *gates, const int32_t *inv_perm,
+                        void *dYp, float *dgates, float *dz, void *stream) {
+    Dims m;
+    int rc = check_desc(desc, m);
+    if (rc) return rc;
+    if (!dy || !gates || !inv_perm || (!dYp && !dgates && !dz) || ((dgates || dz) && !Yp)) return R3_ERR_INVALID_ARG;
+    if (!aligned(dy, 16) || !aligned(Yp, 16) || !aligned(dYp, 16) || !aligned(gates, 4) || !aligned(inv_perm, 4) ||
+        !aligned(dgates, 4) || !aligned(dz, 4))
+        return R3_ERR_INVALID_ARG;
+    const size_t rows = (size_t)m.S * m.d * m.eb, tokens = (size_t)m.T * m.d * m.eb, slots = (size_t)m.S * sizeof(float);
+    if ((Yp != dYp && overlap(Yp, rows, dYp, rows)) || overlap(dy, tokens, dYp, rows) || overlap(dgates, slots, dz, slots))
+        return R3_ERR_INVALID_ARG;
+    if (!route_backward_supported(m.T, m.d, m.act)) return R3_ERR_UNSUPPORTED;
+    return hip_rc(launch_combine_backward(m.T, m.d, m.K, m.act, dy, Yp, gates, inv_perm, dYp, dgates, dz, (hipStream_t)stream));
+}
+
+int r3_permute_backward(const r3_layer_desc *desc, const void *dXp, const int32_t *inv_perm, const void *add, void *dx, void *stream) {
+    Dims m;
+    int rc = check_desc(desc, m);
+    if (rc) return rc;
+    if (!dXp || !inv_perm || !dx) return R3_ERR_INVALID_ARG;
+    if (!aligned(dXp, 16) || !aligned(add, 16) || !aligned(dx, 16) || !aligned(inv_perm, 4)) return R3_ERR_INVALID_ARG;
+    const size_t rows = (size_t)m.S * m.d * m.eb, tokens = (size_t)m.T * m.d * m.eb;
+    if (overlap(dXp, rows, dx, tokens) || (add != dx && overlap(add, tokens, dx, tokens))) return R3_ERR_INVALID_ARG;
+    if (!route_backward_supported(m.T, m.d, m.act)) return R3_ERR_UNSUPPORTED;
+    return hip_rc(launch_permute_backward(m.T, m.d, m.K, m.act, dXp, inv_perm, add, dx, (hipStream_t)stream));
+}
+
 int r3_moe_forward(const r3_layer_desc *desc, const void *x, const void *W_r, const float *bias, const void *idx,
                    const void *W_gate, const void *W_up, const void *W_down, void *y, float *gates, int32_t *counts,
                    int32_t *offsets, int32_t *inv_perm, int32_t *perm, void *Yp, void *H, void *FA_save,
@@ -438,6 +470,56 @@ int r3_policy_discrepancy(int64_t n, const float *logp_train, const float *logp_
     if (!ws || ws_bytes < policy_ws_bytes() || !aligned(ws, 256)) return R3_ERR_WORKSPACE;
     return hip_rc(launch_policy_discrepancy(n, logp_train, logp_infer, ntau, tau, kl_out, frac_out, ws,
                                             (hipStream_t)stream));
+}
+
+static int check_logits(int64_t n, int64_t V, int dtype, const void *logits, int64_t ld, float scale) {
+    if (n < 0 || V <= 0 || (dtype != R3_BF16 && dtype != R3_F32) || (n > 0 && !logits) || ld < V) return R3_ERR_INVALID_ARG;
+    if (!(scale >= 1e-6f && scale <= 1e6f) || !aligned(logits, dtype == R3_BF16 ? 2 : 4)) return R3_ERR_INVALID_ARG;
+    // ids are int32 (and a row's index with a work-group's reach beyond it stays one); rows are addressed in 64 bits
+    if (n > 0x7fffffffll || V > 0x7fffffffll - 65536 || ld > 0xffffffffll) return R3_ERR_UNSUPPORTED;
+    return R3_OK;
+}
+
+size_t r3_token_logprobs_workspace_bytes(int64_t n, int64_t V, int top) {
+    if (n <= 0 || V <= 0 || n > 0x7fffffffll || V > 0x7fffffffll - 65536 || top < 0 || top > R3_MAX_TOP) return 0;
+    return token_logprobs_ws_bytes(n, V, top);
+}
+
+int r3_token_logprobs(int64_t n, int64_t V, int dtype, const void *logits, int64_t ld, float scale, const int32_t *target,
+                      float *logp, float *entropy, float *stats, int top, float *top_logp, int32_t *top_id,
+                      int32_t *status_word, void *ws, size_t ws_bytes, void *stream) {
+    const int rc = check_logits(n, V, dtype, logits, ld, scale);
+    if (rc) return rc;
+    if (top < 0 || top > R3_MAX_TOP || (n > 0 && ((top > 0 && (!top_logp || !top_id)) || (!logp && !entropy && !stats && top == 0) ||
+                                                  (logp && !target))))
+        return R3_ERR_INVALID_ARG;
+    if (!aligned(target, 4) || !aligned(logp, 4) || !aligned(entropy, 4) || !aligned(stats, 4) ||
+        (top > 0 && (!aligned(top_logp, 4) || !aligned(top_id, 4))) || !aligned(status_word, 4))
+        return R3_ERR_INVALID_ARG;
+    if (n == 0) return R3_OK;
+    const size_t need = token_logprobs_ws_bytes(n, V, top);
+    if (need && (!ws || ws_bytes < need || !aligned(ws, 256))) return R3_ERR_WORKSPACE;
+    return hip_rc(launch_token_logprobs(n, V, dtype, logits, ld, scale, target, logp, entropy, stats, top, top_logp, top_id, status_word,
+                                        ws, (hipStream_t)stream));
+}
+
+int r3_token_logprobs_backward(int64_t n, int64_t V, int dtype, const void *logits, int64_t ld, float scale, const int32_t *target,
+                               const float *stats, const float *entropy, const float *dlogp, const float *dentropy, void *dlogits,
+                               int64_t ldd, void *stream) {
+    const int rc = check_logits(n, V, dtype, logits, ld, scale);
+    if (rc) return rc;
+    if (ldd < V || !aligned(dlogits, dtype == R3_BF16 ? 2 : 4)) return R3_ERR_INVALID_ARG;
+    if (ldd > 0xffffffffll) return R3_ERR_UNSUPPORTED;
+    if (!aligned(target, 4) || !aligned(stats, 4) || !aligned(entropy, 4) || !aligned(dlogp, 4) || !aligned(dentropy, 4))
+        return R3_ERR_INVALID_ARG;
+    if (n == 0) return R3_OK;
+    if (!stats || !dlogits || (!dlogp && !dentropy) || (dlogp && !target) || (dentropy && !entropy)) return R3_ERR_INVALID_ARG;
+    const size_t eb = dtype == R3_BF16 ? 2 : 4;
+    if (!(dlogits == logits && ldd == ld) &&
+        overlap(logits, ((size_t)(n - 1) * ld + V) * eb, dlogits, ((size_t)(n - 1) * ldd + V) * eb))
+        return R3_ERR_INVALID_ARG;
+    return hip_rc(launch_token_logprobs_backward(n, V, dtype, logits, ld, scale, target, stats, entropy, dlogp, dentropy, dlogits, ldd,
+                                                 (hipStream_t)stream));
 }
 
 static int check_cache(int idx_dtype, int L, int K, int P, const void *pages, int64_t num_pages,

@@ -9,7 +9,8 @@ namespace r3 {
 enum ProfTag {
     PROF_RECORD = 0, PROF_LOGITS, PROF_GATE, PROF_PERMUTE_INDEX, PROF_GATHER_ROWS, PROF_FFN1, PROF_FFN2,
     PROF_COMBINE, PROF_GATE_BWD, PROF_DWR, PROF_DH, PROF_WGRAD, PROF_DXP, PROF_DX_FINISH, PROF_WGRAD_PAIR,
-    PROF_ROUTING_DIFF, PROF_POLICY, PROF_CACHE_APPEND, PROF_CACHE_GATHER, PROF_AGREEMENT, PROF_NTAGS
+    PROF_ROUTING_DIFF, PROF_POLICY, PROF_CACHE_APPEND, PROF_CACHE_GATHER, PROF_AGREEMENT, PROF_LOGPROBS, PROF_LOGPROBS_BWD,
+    PROF_COMBINE_BWD, PROF_PERMUTE_BWD, PROF_NTAGS
 };
 struct ProfScope {
     int tag, slot;
@@ -62,6 +63,22 @@ hipError_t launch_routing_diff(int T, int K, int L, const void *a, const void *b
                                int32_t *token_choices, int32_t *token_routers, double *seq_mean, hipStream_t s);
 hipError_t launch_policy_discrepancy(int64_t n, const float *lt, const float *li, int ntau, const float *tau_host,
                                      double *kl, double *frac, void *ws, hipStream_t s);
+
+// r3_logprobs.hip
+size_t token_logprobs_ws_bytes(int64_t n, int64_t V, int top);
+hipError_t launch_token_logprobs(int64_t n, int64_t V, int dtype, const void *logits, int64_t ld, float scale, const int32_t *target,
+                                 float *logp, float *entropy, float *stats, int top, float *top_logp, int32_t *top_id, int32_t *status,
+                                 void *ws, hipStream_t s);
+hipError_t launch_token_logprobs_backward(int64_t n, int64_t V, int dtype, const void *logits, int64_t ld, float scale,
+                                          const int32_t *target, const float *stats, const float *entropy, const float *dlogp,
+                                          const float *dentropy, void *dlogits, int64_t ldd, hipStream_t s);
+
+// r3_route_bwd.hip (a grid has less than 2^32 threads; Yp is not read where dgates and dz are NULL)
+bool route_backward_supported(int T, int d, int act);
+hipError_t launch_combine_backward(int T, int d, int K, int act, const void *dy, const void *Yp, const float *gates, const int32_t *inv_perm,
+                                   void *dYp, float *dgates, float *dz, hipStream_t s);
+hipError_t launch_permute_backward(int T, int d, int K, int act, const void *dXp, const int32_t *inv_perm, const void *add, void *dx,
+                                   hipStream_t s);
 
 // r3_cache.hip
 hipError_t launch_cache_append(int idx_bytes, int L, int K, int P, void *pages, int64_t num_pages,

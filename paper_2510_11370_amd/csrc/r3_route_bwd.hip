@@ -1,0 +1,229 @@
+// Gradients of the weighted combination and of the dispatch, each as a call of its own, for experts that are not this
+// library's:
+//   y_t = sum_j g_tj Yp[r_tj]:   dYp[r_tj] = g_tj dy_t,  dg_tj = <dy_t, Yp[r_tj]>,
+//                                dz_tj = g_tj (dg_tj - sum_i g_ti dg_ti)   (the gates are a softmax of the selected logits)
+//   Xp[r_tj] = x_t:              dx_t = sum_j dXp[r_tj]  (+ add_t)
+// Both move rows and compute next to nothing: HBM-bound.
+#include "r3_kernels.h"
+#include "r3_vec.h"
+
+namespace r3 {
+namespace {
+
+// A row of d elements is `units` pieces: whole vectors, then single elements.
+struct Width {
+    int d, nvec, units;
+};
+template <typename T> Width width(int d) {
+    constexpr int N = Row<T>::kVec;
+    return {d, d / N, d / N + d % N};
+}
+
+template <class F> void by_rows(int K, F f) {   // rows in flight together: all K where K is one of these, else eight
+    switch (K) {
+        case 1: f(std::integral_constant<int, 1>{}); break;
+        case 2: f(std::integral_constant<int, 2>{}); break;
+        case 4: f(std::integral_constant<int, 4>{}); break;
+        case 6: f(std::integral_constant<int, 6>{}); break;
+        default: f(std::integral_constant<int, 8>{});
+    }
+}
+
+struct CombineBwd {
+    int T, K;
+    int64_t S;
+    Width w;
+    const void *dy, *Yp;
+    const float *gates;
+    const int32_t *inv_perm;
+    void *dYp;
+    float *dgates, *dz;
+};
+
+// W waves to a token, four waves to a work-group.  dYp may be Yp: an element is read and written by one thread.
+template <typename T, int G, int W>
+__global__ void __launch_bounds__(256)
+combine_backward_kernel(CombineBwd a) {
+    typedef Row<T> R;
+    constexpr int N = R::kVec;
+    __shared__ float part[W > 1 ? W : 1][kMaxK];
+    const int wave = threadIdx.x / kWave, lane = lane_id();
+    const int t = __builtin_amdgcn_readfirstlane(W > 1 ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave);
+    if (t >= a.T) return;
+    const T *dy = (const T *)a.dy + (int64_t)t * a.w.d;
+    const int32_t *rows = a.inv_perm + (int64_t)t * a.K;
+    const float *gates = a.gates + (int64_t)t * a.K;
+    const bool dots = a.Yp != nullptr;
+    float mine = 0.0f;   // lane j: the dot product of slot j over this wave's columns
+    for (int j0 = 0; j0 < a.K; j0 += G) {
+        int64_t at[G];
+        float g[G], dot[G];
+        bool in[G];
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+            const int32_t r = j0 + j < a.K ? rows[j0 + j] : -1;
+            in[j] = r >= 0 && r < a.S;
+            at[j] = in[j] ? (int64_t)r * a.w.d : 0;
+            g[j] = j0 + j < a.K ? gates[j0 + j] : 0.0f;
+            dot[j] = 0.0f;
+        }
+        for (int c = (W > 1 ? (int)threadIdx.x : lane); c < a.w.units; c += W * kWave) {
+            if (c < a.w.nvec) {
+                float x[N];
+                typename R::V v[G];
+                R::unpack(R::load(dy + c * N), x);
+                if (dots) {
+#pragma unroll
+                    for (int j = 0; j < G; ++j) v[j] = R::load_once((const T *)a.Yp + at[j] + c * N);
+                }
+#pragma unroll
+                for (int j = 0; j < G; ++j) {
+                    if (dots) {
+                        float y[N];
+                        R::unpack(v[j], y);
+#pragma unroll
+                        for (int u = 0; u < N; ++u) dot[j] = fmaf(x[u], y[u], dot[j]);
+                    }
+                    if (a.dYp && in[j]) {
+                        float o[N];
+#pragma unroll
+                        for (int u = 0; u < N; ++u) o[u] = g[j] * x[u];
+                        R::store((T *)a.dYp + at[j] + c * N, o);
+                    }
+                }
+            } else {
+                const int e = a.w.nvec * N + (c - a.w.nvec);
+                const float x = Elem<T>::ld(dy + e);
+#pragma unroll
+                for (int j = 0; j < G; ++j) {
+                    if (dots) dot[j] = fmaf(x, Elem<T>::ld((const T *)a.Yp + at[j] + e), dot[j]);
+                    if (a.dYp && in[j]) Elem<T>::st((T *)a.dYp + at[j] + e, g[j] * x);
+                }
+            }
+        }
+        if (dots) {
+#pragma unroll
+            for (int j = 0; j < G; ++j) {
+                const float s = wave_sum(in[j] ? dot[j] : 0.0f);
+                if (lane == j0 + j) mine = s;
+            }
+        }
+    }
+    if (!dots) return;
+    if constexpr (W > 1) {
+        part[wave][lane] = mine;
+        __syncthreads();
+        if (wave > 0) return;
+        mine = 0.0f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) mine += part[i][lane];
+    }
+    const float g = lane < a.K ? gates[lane] : 0.0f;
+    const float mix = wave_sum(lane < a.K ? g * mine : 0.0f);
+    if (lane < a.K) {
+        if (a.dgates) a.dgates[(int64_t)t * a.K + lane] = mine;
+        if (a.dz) a.dz[(int64_t)t * a.K + lane] = g * (mine - mix);
+    }
+}
+
+struct PermuteBwd {
+    int T, K, chunks;
+    int64_t S;
+    Width w;
+    const void *dXp, *add;
+    const int32_t *inv_perm;
+    void *dx;
+};
+
+// A wave to 64 pieces of a token's row.  dx may be add.
+template <typename T, int G>
+__global__ void __launch_bounds__(256)
+permute_backward_kernel(PermuteBwd a) {
+    typedef Row<T> R;
+    constexpr int N = R::kVec;
+    const int64_t item = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+    const int t = __builtin_amdgcn_readfirstlane((int)(item / a.chunks));
+    if (t >= a.T) return;
+    const int c = __builtin_amdgcn_readfirstlane((int)(item % a.chunks)) * kWave + lane_id();
+    if (c >= a.w.units) return;
+    const int32_t *rows = a.inv_perm + (int64_t)t * a.K;
+    const T *dXp = (const T *)a.dXp, *add = a.add ? (const T *)a.add + (int64_t)t * a.w.d : nullptr;
+    T *dx = (T *)a.dx + (int64_t)t * a.w.d;
+    if (c < a.w.nvec) {
+        float acc[N];
+#pragma unroll
+        for (int u = 0; u < N; ++u) acc[u] = 0.0f;
+        if (add) R::unpack(R::load(add + c * N), acc);
+        for (int j0 = 0; j0 < a.K; j0 += G) {
+            typename R::V v[G];
+            bool in[G];
+#pragma unroll
+            for (int j = 0; j < G; ++j) {
+                const int32_t r = j0 + j < a.K ? rows[j0 + j] : -1;
+                in[j] = r >= 0 && r < a.S;
+                v[j] = R::load_once(dXp + (in[j] ? (int64_t)r * a.w.d : 0) + c * N);
+            }
+#pragma unroll
+            for (int j = 0; j < G; ++j) {
+                float f[N];
+                R::unpack(v[j], f);
+                if (in[j]) {
+#pragma unroll
+                    for (int u = 0; u < N; ++u) acc[u] += f[u];
+                }
+            }
+        }
+        R::store(dx + c * N, acc);
+    } else {
+        const int e = a.w.nvec * N + (c - a.w.nvec);
+        float acc = add ? Elem<T>::ld(add + e) : 0.0f;
+        for (int j = 0; j < a.K; ++j) {
+            const int32_t r = rows[j];
+            if (r >= 0 && r < a.S) acc += Elem<T>::ld(dXp + (int64_t)r * a.w.d + e);
+        }
+        Elem<T>::st(dx + e, acc);
+    }
+}
+
+}  // namespace
+
+bool route_backward_supported(int T, int d, int act) {
+    const int per = 1024 / (act == R3_BF16 ? 2 : 4);   // elements of 64 vectors; single elements may take 64 pieces more
+    return (int64_t)T * (((int64_t)d + per - 1) / per) <= (1 << 25) - 4;
+}
+
+hipError_t launch_combine_backward(int T, int d, int K, int act, const void *dy, const void *Yp, const float *gates, const int32_t *inv_perm,
+                                   void *dYp, float *dgates, float *dz, hipStream_t s) {
+    ProfScope ps(PROF_COMBINE_BWD, s);
+    CombineBwd a = {T, K, (int64_t)T * K, {}, dy, dgates || dz ? Yp : nullptr, gates, inv_perm, dYp, dgates, dz};
+    auto go = [&](auto type) {
+        typedef decltype(type) E;
+        a.w = width<E>(d);
+        by_rows(K, [&](auto g) {
+            constexpr int G = decltype(g)::value;
+            if (T >= 4096 || a.w.units <= kWave) combine_backward_kernel<E, G, 1><<<(T + 3) / 4, 256, 0, s>>>(a);
+            else combine_backward_kernel<E, G, 4><<<T, 256, 0, s>>>(a);
+        });
+    };
+    if (act == R3_BF16) go(bf16_t{});
+    else go(float{});
+    return hipGetLastError();
+}
+
+hipError_t launch_permute_backward(int T, int d, int K, int act, const void *dXp, const int32_t *inv_perm, const void *add, void *dx,
+                                   hipStream_t s) {
+    ProfScope ps(PROF_PERMUTE_BWD, s);
+    PermuteBwd a = {T, K, 0, (int64_t)T * K, {}, dXp, add, inv_perm, dx};
+    auto go = [&](auto type) {
+        typedef decltype(type) E;
+        a.w = width<E>(d);
+        a.chunks = (a.w.units + kWave - 1) / kWave;
+        const unsigned blocks = (unsigned)(((int64_t)T * a.chunks + 3) / 4);
+        by_rows(K, [&](auto g) { permute_backward_kernel<E, decltype(g)::value><<<blocks, 256, 0, s>>>(a); });
+    };
+    if (act == R3_BF16) go(bf16_t{});
+    else go(float{});
+    return hipGetLastError();
+}
+
+}  // namespace r3

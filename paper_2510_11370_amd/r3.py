@@ -23,7 +23,10 @@ EXPORTS = ["r3_version", "r3_workspace_bytes", "r3_record_topk", "r3_replay_gate
            "r3_permute_static", "r3_grouped_ffn", "r3_combine", "r3_moe_forward", "r3_moe_backward", "r3_profile_enable", "r3_profile_tags",
            "r3_profile_name", "r3_profile_read", "r3_profile_copy",
            "r3_profile_mfma", "r3_profile_mfma_flops", "r3_profile_gemm_mix", "r3_routing_diff", "r3_policy_discrepancy",
-           "r3_policy_workspace_bytes", "r3_mask_cache_append", "r3_mask_cache_gather"]
+           "r3_policy_workspace_bytes", "r3_mask_cache_append", "r3_mask_cache_gather",
+           "r3_combine_backward", "r3_permute_backward", "r3_token_logprobs_workspace_bytes", "r3_token_logprobs",
+           "r3_token_logprobs_backward"]
+MAX_TOP = 32
 
 
 class LayerDesc(C.Structure):
@@ -55,6 +58,13 @@ def lib():
         L.r3_profile_name.restype = C.c_char_p
         L.r3_profile_mfma_flops.restype = C.c_double
         L.r3_policy_workspace_bytes.restype = C.c_size_t
+        p, i64, i32, f32 = C.c_void_p, C.c_int64, C.c_int, C.c_float
+        L.r3_combine_backward.argtypes = [C.POINTER(LayerDesc)] + [p] * 8
+        L.r3_permute_backward.argtypes = [C.POINTER(LayerDesc)] + [p] * 5
+        L.r3_token_logprobs_workspace_bytes.restype = C.c_size_t
+        L.r3_token_logprobs_workspace_bytes.argtypes = [i64, i64, i32]
+        L.r3_token_logprobs.argtypes = [i64, i64, i32, p, i64, f32, p, p, p, p, i32, p, p, p, p, C.c_size_t, p]
+        L.r3_token_logprobs_backward.argtypes = [i64, i64, i32, p, i64, f32] + [p] * 6 + [i64, p]
         _lib = L
     return _lib
 
@@ -169,6 +179,88 @@ def policy_discrepancy(logp_train, logp_infer, taus, kl_out, frac_out, ws=None):
     _check(lib().r3_policy_discrepancy(C.c_int64(logp_train.numel()), _p(logp_train), _p(logp_infer),
                                        C.c_int(len(taus)), tau, _p(kl_out), _p(frac_out), _p(ws),
                                        C.c_size_t(ws.numel()), _stream()), "r3_policy_discrepancy")
+
+
+def _have(what, device, **tensors):
+    """Refuses what the C call would take for something else: {name: (tensor or None, shape, dtype)}, dense unless the
+    shape is None, on the current device.  Returns their addresses, 0 for None."""
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise R3Error("%s: tensors on %s, which is not the current GPU" % (what, device))
+    out = []
+    for name, (t, shape, dtype) in tensors.items():
+        if t is None:
+            out.append(0)
+            continue
+        if t.dtype != dtype or t.device != device or (shape is not None and (tuple(t.shape) != shape or not t.is_contiguous())):
+            raise R3Error("%s: %s has to be a dense %s tensor of shape %s on %s" % (what, name, dtype, shape, device))
+        out.append(t.data_ptr())
+    return out
+
+
+def combine_backward(D, dy, Yp, gates, inv_perm, dYp=None, dgates=None, dz=None):
+    """Gradient of combine: rows dYp [T*K,d], gates dgates [T,K], selected logits dz [T,K]; each may be None, and Yp with
+    dgates and dz.  dYp may be Yp."""
+    a, T, K, d, f = act_dtype(D), D.T, D.K, D.d, torch.float32
+    ptr = _have("combine_backward", dy.device, dy=(dy, (T, d), a), Yp=(Yp, (T * K, d), a), gates=(gates, (T, K), f),
+                inv_perm=(inv_perm, (T * K,), torch.int32), dYp=(dYp, (T * K, d), a), dgates=(dgates, (T, K), f),
+                dz=(dz, (T, K), f))
+    _check(lib().r3_combine_backward(C.byref(D), *ptr, torch.cuda.current_stream().cuda_stream), "r3_combine_backward")
+
+
+def permute_backward(D, dXp, inv_perm, dx, add=None):
+    """Gradient of permute's rows: dx [T,d] = add + the sum of each token's K rows of dXp [T*K,d].  add may be dx."""
+    a = act_dtype(D)
+    ptr = _have("permute_backward", dXp.device, dXp=(dXp, (D.T * D.K, D.d), a), inv_perm=(inv_perm, (D.T * D.K,), torch.int32),
+                add=(add, (D.T, D.d), a), dx=(dx, (D.T, D.d), a))
+    _check(lib().r3_permute_backward(C.byref(D), *ptr, torch.cuda.current_stream().cuda_stream), "r3_permute_backward")
+
+
+def token_logprobs_workspace(n, V, top=0, device="cuda"):
+    """A workspace tensor for token_logprobs on [n, V] logits, or None where none is needed."""
+    b = lib().r3_token_logprobs_workspace_bytes(n, V, top)
+    return torch.empty(b, dtype=torch.uint8, device=device) if b else None
+
+
+def _logits(what, t):
+    if t.dim() != 2 or t.dtype not in (torch.bfloat16, torch.float32) or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise R3Error("%s: logits and their gradient are [n, V], bfloat16 or float32, with dense rows" % what)
+    n, V = t.shape
+    return n, V, BF16 if t.dtype == torch.bfloat16 else F32, t.stride(0) if n > 1 else max(V, t.stride(0))
+
+
+def token_logprobs(logits, target, logp=None, entropy=None, stats=None, top_logp=None, top_id=None, scale=1.0, status=None,
+                   ws=None):
+    """Of each row of logits [n,V] (rows may be strided): logp [n] of target [n] (int32; -1 leaves a row out), entropy [n],
+    stats [n,2] (for the backward), top_logp and top_id [n,top] the most probable alternatives.  scale: 1 / temperature.
+    ws: token_logprobs_workspace(n, V, top); made here where it is needed and not given."""
+    n, V, dt, ld = _logits("token_logprobs", logits)
+    top = 0 if top_id is None else top_id.shape[-1]
+    f, i = torch.float32, torch.int32
+    z, tg, lp, en, st, tl, ti, sw = _have(
+        "token_logprobs", logits.device, logits=(logits, None, logits.dtype), target=(target, (n,), i), logp=(logp, (n,), f),
+        entropy=(entropy, (n,), f), stats=(stats, (n, 2), f), top_logp=(top_logp, (n, top), f), top_id=(top_id, (n, top), i),
+        status=(status, (1,), i))
+    if ws is None:
+        ws = token_logprobs_workspace(n, V, top, logits.device)
+    _check(lib().r3_token_logprobs(n, V, dt, z, ld, scale, tg, lp, en, st, top, tl, ti, sw, 0 if ws is None else ws.data_ptr(),
+                                   0 if ws is None else ws.numel(), torch.cuda.current_stream().cuda_stream),
+           "r3_token_logprobs")
+
+
+def token_logprobs_backward(logits, target, stats, dlogits, dlogp=None, entropy=None, dentropy=None, scale=1.0):
+    """Gradient of sum(dlogp * logp + dentropy * entropy) with respect to the logits, from token_logprobs' stats and (with
+    dentropy) entropy.  dlogits may be logits."""
+    n, V, dt, ld = _logits("token_logprobs_backward", logits)
+    n2, V2, dt2, ldd = _logits("token_logprobs_backward", dlogits)
+    if (n, V, dt) != (n2, V2, dt2):
+        raise R3Error("token_logprobs_backward: dlogits has to be of the logits' shape and type")
+    f = torch.float32
+    z, dz, tg, st, en, dl, de = _have(
+        "token_logprobs_backward", logits.device, logits=(logits, None, logits.dtype), dlogits=(dlogits, None, logits.dtype),
+        target=(target, (n,), torch.int32), stats=(stats, (n, 2), f), entropy=(entropy, (n,), f), dlogp=(dlogp, (n,), f),
+        dentropy=(dentropy, (n,), f))
+    _check(lib().r3_token_logprobs_backward(n, V, dt, z, ld, scale, tg, st, en, dl, de, dz, ldd,
+                                            torch.cuda.current_stream().cuda_stream), "r3_token_logprobs_backward")
 
 
 def _idx_code(t):

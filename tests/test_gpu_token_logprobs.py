@@ -1,0 +1,353 @@
+"""r3_token_logprobs and r3_token_logprobs_backward against oracle/operators.py (64 bits): sizes from one element, rows that
+are cut and not, odd and padded strides, masks, ties, rows of nothing, non-finite logits, rows left out; what the calls must
+not touch; other streams, graphs, addresses past 2^31 elements."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as ref
+from paper_2510_11370_amd import r3
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}   # half a step, relative
+
+
+def _logits(n, V, dtype, pad=0, seed=0, spread=2.0):
+    g = torch.Generator().manual_seed(seed)
+    full = (torch.randn(n, V + pad, generator=g) * spread)
+    t = torch.randint(0, V, (n,), generator=g, dtype=torch.int32)
+    full[torch.arange(n), t.long()] += 5.0
+    full = full.to(dtype)
+    if pad:
+        full[:, V:] = math.nan         # columns past V are nobody's
+    return full, t
+
+
+def _np(z):
+    return z.double().numpy()
+
+
+def _run(full, V, target, top=0, scale=1.0, want=("logp", "entropy", "stats"), guard=2):
+    """Runs with outputs inside larger ones, whose rows behind the last must stay as they were."""
+    n = full.shape[0]
+    z = full.to(DEV)[:, :V]
+    shapes = {"logp": ((), torch.float32), "entropy": ((), torch.float32), "stats": ((2,), torch.float32),
+              "top_logp": ((top,), torch.float32), "top_id": ((top,), torch.int32)}
+    names = list(want) + (["top_logp", "top_id"] if top else [])
+    big = {k: torch.full((n + guard,) + shapes[k][0], 77, dtype=shapes[k][1], device=DEV) for k in names}
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    r3.token_logprobs(z, None if target is None else target.to(DEV), scale=scale, status=status, **{k: v[:n] for k, v in big.items()})
+    torch.cuda.synchronize()
+    for k, v in big.items():
+        assert (v[n:] == 77).all(), k
+    return {k: v[:n].cpu().double().numpy() for k, v in big.items()}, int(status.item()), z
+
+
+def _check(got, want, what=""):
+    def near(x, y, tol, name):
+        # a result below the lowest float (-2^128 + 2^104) by half a step or more rounds to -inf
+        y = np.where(y <= -(2.0 ** 128 - 2.0 ** 103), -np.inf, y)
+        with np.errstate(invalid="ignore"):
+            bad = ~((np.abs(x - y) <= tol) | (x == y) | (np.isnan(x) & np.isnan(y)))
+        assert not bad.any(), (what, name, np.argwhere(bad)[:3].tolist(), x[bad][:3], y[bad][:3], np.broadcast_to(tol, x.shape)[bad][:3])
+    if "logp" in got:
+        near(got["logp"], want["logp"], want["tol_logp"], "logp")
+    if "entropy" in got:
+        near(got["entropy"], want["entropy"], want["tol_entropy"], "entropy")
+    if "stats" in got:
+        near(got["stats"][:, 0], want["stats"][:, 0], 0.0, "m")
+        near(got["stats"][:, 1], want["stats"][:, 1], want["tol_S"] * np.abs(want["stats"][:, 1]), "S")
+    if "top_id" in got:
+        assert np.array_equal(got["top_id"], want["top_id"]), (what, np.argwhere(got["top_id"] != want["top_id"])[:3].tolist())
+        near(got["top_logp"], want["top_logp"], want["tol_top"], "top_logp")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,V,top,pad,scale", [
+    (1, 1, 1, 0, 1.0), (3, 7, 5, 0, 1.0), (2, 64, 32, 1, 0.5), (5, 20, 32, 0, 1.0), (9, 513, 20, 3, 1.7), (7, 4096, 32, 0, 1.0),
+    (4, 4097, 20, 0, 1.0), (1300, 300, 1, 5, 1.0), (1030, 5000, 3, 0, 1 / 0.6), (3, 32769, 20, 7, 1.0), (40, 9001, 8, 0, 1.0),
+    (64, 50257, 8, 0, 1 / 0.6), (1, 151936, 20, 0, 1.0), (2, 262147, 32, 0, 1.0), (600, 40009, 5, 2, 1.0)])
+def test_against_64_bits(n, V, top, pad, scale, dtype):
+    full, t = _logits(n, V, dtype, pad, seed=n + V)
+    got, status, _ = _run(full, V, t, top, scale)
+    assert status == 0
+    _check(got, ref.token_logprobs(_np(full[:, :V]), t.numpy(), scale, top))
+
+
+@pytest.mark.parametrize("want,top,target", [(("logp",), 0, True), (("entropy",), 0, False), (("stats",), 0, True), ((), 4, False),
+                                             (("logp", "stats"), 4, True)])
+@pytest.mark.parametrize("n,V", [(5, 700), (3, 20001)])
+def test_outputs_that_are_not_wanted(n, V, want, top, target):
+    full, t = _logits(n, V, torch.bfloat16, seed=3)
+    got, _, _ = _run(full, V, t if target else None, top, want=want)
+    _check(got, ref.token_logprobs(_np(full), t.numpy() if target else None, 1.0, top))
+
+
+def _special(V):
+    """Rows where something can go wrong, and their names."""
+    rng = np.random.default_rng(V)
+    base = rng.normal(0, 2, V).astype(np.float32)
+    low = float(torch.finfo(torch.bfloat16).min)
+    rows = {}
+    rows["all masked"] = np.full(V, -np.inf, np.float32)
+    r = np.full(V, -np.inf, np.float32); r[V // 2] = 3.0
+    rows["one token left"] = r
+    r = np.full(V, -np.inf, np.float32); r[rng.choice(V, min(V, 9), replace=False)] = rng.normal(0, 1, min(V, 9))
+    rows["nine tokens left"] = r
+    r = base.copy(); r[rng.random(V) < 0.5] = -np.inf
+    rows["half masked"] = r
+    rows["all equal"] = np.full(V, 1.5, np.float32)
+    rows["all lowest"] = np.full(V, low, np.float32)
+    r = np.full(V, low, np.float32); r[rng.choice(V, min(V, 3), replace=False)] = 2.0
+    rows["all lowest but three"] = r
+    rows["three values"] = rng.integers(0, 3, V).astype(np.float32)
+    rows["zeros of both signs"] = np.where(rng.random(V) < 0.5, 0.0, -0.0).astype(np.float32)
+    rows["ascending"] = np.linspace(-8, 8, V).astype(np.float32)
+    rows["descending"] = np.linspace(8, -8, V).astype(np.float32)
+    # the large values all belong to a few threads, whatever the number of threads and the elements of a load
+    rows["every 512th run of eight"] = np.where((np.arange(V) // 8) % 64 == 0, base + 20, base).astype(np.float32)
+    rows["every 256th run of four"] = np.where((np.arange(V) // 4) % 64 == 0, base + 20, base).astype(np.float32)
+    rows["far apart"] = (base * 1e4).astype(np.float32)
+    rows["huge"] = np.where(rng.random(V) < 0.5, 3e38, -3e38).astype(np.float32)
+    rows["offset 1e5"] = (base + 1e5).astype(np.float32)
+    r = base.copy(); r[V - 1] = 30.0
+    rows["one certain token"] = r
+    r = base.copy(); r[V // 3] = np.nan
+    rows["a NaN"] = r
+    r = base.copy(); r[0] = np.inf
+    rows["an infinity"] = r
+    rows["all NaN"] = np.full(V, np.nan, np.float32)
+    rows["plain"] = base
+    return rows
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V,copies", [(5, 1), (900, 1), (4097, 60), (6001, 1), (50257, 1), (50257, 50), (151936, 50)])
+def test_rows_where_something_can_go_wrong(V, copies, dtype):
+    """copies: other rows beside them, so that rows are not cut."""
+    rows = _special(V)
+    names = list(rows)
+    z = torch.tensor(np.stack(list(rows.values()))).to(dtype)
+    k = len(names)
+    t = torch.tensor([(i * 7919) % V for i in range(k)], dtype=torch.int32)
+    t[names.index("one token left")] = V // 2
+    t[names.index("one certain token")] = V - 1
+    many, tm = z.repeat(copies, 1), t.repeat(copies)
+    for top, scale in ((32, 1.0), (3, 0.25)):
+        got, status, _ = _run(many, V, tm, top, scale)
+        want = ref.token_logprobs(_np(z), t.numpy(), scale, top)
+        assert status == r3.DATA_NONFINITE
+        for c in (0, copies - 1):
+            for i, name in enumerate(names):
+                row = {a: b[c * k + i:c * k + i + 1] for a, b in got.items()}
+                _check(row, {a: b[i:i + 1] for a, b in want.items()}, (name, top, c))
+
+
+def test_rows_left_out_are_not_read():
+    for n, V in ((40, 1000), (9, 30011), (1200, 300)):
+        full, t = _logits(n, V, torch.bfloat16, seed=5)
+        t[::3] = -1
+        full[::3] = math.nan
+        got, status, _ = _run(full, V, t, 6)
+        assert status == 0
+        _check(got, ref.token_logprobs(_np(full), t.numpy(), 1.0, 6))
+        t[1] = V
+        t[4] = -2
+        got, status, _ = _run(full, V, t, 6)
+        assert status == r3.DATA_IDX_RANGE
+        _check(got, ref.token_logprobs(_np(full), t.numpy(), 1.0, 6))
+
+
+def test_the_same_bits_twice_and_no_rows():
+    full, t = _logits(30, 50257, torch.bfloat16, seed=6)
+    a, _, _ = _run(full, 50257, t, 20)
+    b, _, _ = _run(full, 50257, t, 20)
+    for k in a:
+        assert np.array_equal(a[k], b[k]), k
+    got, status, _ = _run(full[:0], 50257, t[:0], 4)
+    assert status == 0 and got["logp"].shape == (0,)
+    r3.token_logprobs_backward(full[:0].to(DEV), t[:0].to(DEV), torch.empty(0, 2, device=DEV), full[:0].to(DEV),
+                               dlogp=torch.empty(0, device=DEV))
+
+
+# ---------------------------------------------------------------- gradient
+def _backward(full, V, t, dtype, dl, dh, scale=1.0, out="own", pad_out=0):
+    n = full.shape[0]
+    f = lambda a: None if a is None else torch.tensor(a, dtype=torch.float32, device=DEV)  # noqa: E731
+    keep = full.to(DEV)
+    z = keep[:, :V]
+    tg = None if t is None else t.to(DEV)
+    stats, H = torch.empty(n, 2, device=DEV), torch.empty(n, device=DEV)
+    r3.token_logprobs(z, tg, entropy=H, stats=stats, scale=scale)
+    big = keep if out == "in place" else torch.full((n + 1, V + pad_out), 77, dtype=dtype, device=DEV)
+    dz = big[:n, :V]
+    before = big[:, V:].clone()
+    r3.token_logprobs_backward(z, tg, stats, dz, dlogp=f(dl), entropy=H if dh is not None else None, dentropy=f(dh), scale=scale)
+    torch.cuda.synchronize()
+    same = (big[:, V:] == before) | (big[:, V:].isnan() & before.isnan())
+    assert same.all() and (out == "in place" or (big[n:] == 77).all())
+    return dz.cpu().double().numpy()
+
+
+def _check_grad(got, full, V, t, scale, dl, dh, dtype, what=""):
+    f32 = lambda a: None if a is None else np.asarray(a, np.float32).astype(np.float64)  # noqa: E731
+    want, tol = ref.token_logprobs_backward(_np(full[:, :V]), None if t is None else t.numpy(), scale, f32(dl), f32(dh), HALF[dtype])
+    bad = ~((np.abs(got - want) <= tol) | (np.isnan(got) & np.isnan(want)))
+    assert not bad.any(), (what, np.argwhere(bad)[:3].tolist(), got[bad][:3], want[bad][:3], tol[bad][:3])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,V,pad,pad_out,scale,which", [
+    (1, 1, 0, 0, 1.0, "both"), (3, 7, 0, 0, 1.0, "both"), (5, 64, 3, 0, 0.5, "logp"), (9, 515, 0, 5, 1.7, "entropy"),
+    (700, 300, 1, 1, 1.0, "both"), (6, 8192, 0, 0, 1.0, "both"), (5, 8193, 8, 8, 1 / 0.6, "both"), (3, 50257, 0, 3, 1.0, "both"),
+    (2, 151936, 0, 0, 1.0, "logp")])
+def test_gradient_against_64_bits(n, V, pad, pad_out, scale, which, dtype):
+    full, t = _logits(n, V, dtype, pad, seed=n * V)
+    rng = np.random.default_rng(n + V)
+    dl = rng.normal(0, 1, n) if which != "entropy" else None
+    dh = rng.normal(0, 0.2, n) if which != "logp" else None
+    if n > 4:
+        t[2] = -1
+    got = _backward(full, V, t, dtype, dl, dh, scale, pad_out=pad_out)
+    _check_grad(got, full, V, t, scale, dl, dh, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,V,pad", [(7, 1001, 0), (4, 50257, 3)])
+def test_gradient_in_the_logits_place(n, V, pad, dtype):
+    full, t = _logits(n, V, dtype, pad, seed=9)
+    t[1] = -1
+    dl, dh = np.linspace(-1, 1, n), np.linspace(0.3, 0.1, n)
+    got = _backward(full, V, t, dtype, dl, dh, out="in place")
+    _check_grad(got, full, V, t, 1.0, dl, dh, dtype)
+    assert np.array_equal(got, _backward(full, V, t, dtype, dl, dh))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [5, 900, 50257])
+def test_gradient_of_rows_where_something_can_go_wrong(V, dtype):
+    rows = _special(V)
+    names = [k for k in rows if k not in ("a NaN", "an infinity", "all NaN")]
+    z = torch.tensor(np.stack([rows[k] for k in names])).to(dtype)
+    z = torch.where(torch.isinf(z) & (z > 0), torch.full_like(z, torch.finfo(dtype).max), z)
+    t = torch.tensor([(i * 7919) % V for i in range(len(names))], dtype=torch.int32)
+    dl, dh = np.linspace(-1, 1, len(names)), np.linspace(0.5, -0.5, len(names))
+    got = _backward(z, V, t, dtype, dl, dh)
+    for i, name in enumerate(names):
+        _check_grad(got[i:i + 1], z[i:i + 1], V, t[i:i + 1], 1.0, dl[i:i + 1], dh[i:i + 1], dtype, name)
+    # a row with a NaN or an infinity gives NaN, the rows beside it do not
+    bad = torch.tensor(np.stack([rows["plain"], rows["a NaN"], rows["an infinity"], rows["plain"]])).to(dtype)
+    got = _backward(bad, V, t[:4], dtype, dl[:4], dh[:4])
+    assert np.isnan(got[1:3]).all() and np.isfinite(got[[0, 3]]).all()
+
+
+def test_gradient_against_differences():
+    n, V, scale = 3, 40, 1.25
+    full, t = _logits(n, V, torch.float32, seed=12)
+    dl, dh = np.array([1.0, -0.5, 0.25]), np.array([0.1, -0.2, 0.3])
+    got = _backward(full, V, t, torch.float32, dl, dh, scale)
+    h, z = 1e-5, _np(full)
+
+    def loss(a):
+        f = ref.token_logprobs(a, t.numpy(), scale)
+        return (dl * f["logp"] + dh * f["entropy"]).sum()
+
+    for i in range(n):
+        for v in (0, V - 1, int(t[i])):
+            a, b = z.copy(), z.copy()
+            a[i, v] += h
+            b[i, v] -= h
+            # differences: error h^2 and 1e-16 / h; the kernel's: some 1e2 half steps of values of size 1
+            assert abs((loss(a) - loss(b)) / (2 * h) - got[i, v]) < 1e-5, (i, v)
+
+
+# ---------------------------------------------------------------- streams, graphs, large offsets
+def test_on_another_stream():
+    full, t = _logits(20, 50257, torch.bfloat16, seed=14)
+    want = ref.token_logprobs(_np(full), t.numpy(), 1.0, 8)
+    side = torch.cuda.Stream()
+    z, tg = full.to(DEV), t.to(DEV)
+    lp, tl, ti = torch.empty(20, device=DEV), torch.empty(20, 8, device=DEV), torch.empty(20, 8, dtype=torch.int32, device=DEV)
+    ws = r3.token_logprobs_workspace(20, 50257, 8)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        r3.token_logprobs(z, tg, lp, top_logp=tl, top_id=ti, ws=ws)
+    side.synchronize()
+    _check({"logp": lp.cpu().double().numpy(), "top_logp": tl.cpu().double().numpy(), "top_id": ti.cpu().numpy()}, want)
+
+
+def test_two_graphs_that_share_a_workspace():
+    """A decode step's call on cut rows and a training step's forward and gradient, each captured, replayed in turn with
+    eager work between."""
+    V = 40009
+    fa, ta = _logits(3, V, torch.bfloat16, seed=15)
+    fb, tb = _logits(5, V, torch.bfloat16, seed=16)
+    ws = r3.token_logprobs_workspace(5, V, 16)
+    need = max(r3.lib().r3_token_logprobs_workspace_bytes(k, V, 16) for k in (3, 5))
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    st = []
+    for f, t in ((fa, ta), (fb, tb)):
+        n = f.shape[0]
+        st.append(dict(z=f.to(DEV), t=t.to(DEV), logp=torch.empty(n, device=DEV), entropy=torch.empty(n, device=DEV),
+                       stats=torch.empty(n, 2, device=DEV), top_logp=torch.empty(n, 16, device=DEV),
+                       top_id=torch.empty(n, 16, dtype=torch.int32, device=DEV), dl=torch.linspace(-1, 1, n, device=DEV),
+                       dh=torch.linspace(0.2, 0.1, n, device=DEV), dz=torch.empty(n, V, dtype=torch.bfloat16, device=DEV)))
+    outs = ("logp", "entropy", "stats", "top_logp", "top_id", "dz")
+
+    def step(s):
+        r3.token_logprobs(s["z"], s["t"], s["logp"], s["entropy"], s["stats"], s["top_logp"], s["top_id"], ws=ws)
+        r3.token_logprobs_backward(s["z"], s["t"], s["stats"], s["dz"], dlogp=s["dl"], entropy=s["entropy"], dentropy=s["dh"])
+
+    eager = []
+    for s in st:
+        step(s)
+        torch.cuda.synchronize()
+        eager.append({k: s[k].clone() for k in outs})
+    side, graphs = torch.cuda.Stream(), []
+    side.wait_stream(torch.cuda.current_stream())
+    for s in st:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side):
+            step(s)
+            side.synchronize()
+            with torch.cuda.graph(g, stream=side):
+                step(s)
+        graphs.append(g)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    for replay in range(3):
+        for s, g, e in zip(st, graphs, eager):
+            for k in outs:
+                s[k].zero_()
+            torch.randn(1 << 18, device=DEV).sum().item()
+            g.replay()
+            torch.cuda.synchronize()
+            for k in outs:
+                assert torch.equal(s[k], e[k]), (k, replay)
+        step(st[replay % 2])           # eager calls on the same workspace between
+    # new logits in the captured tensors: the replay computes them anew
+    st[0]["z"].copy_(fb[:3].to(DEV))
+    st[0]["t"].copy_(tb[:3].to(DEV))
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    _check({k: st[0][k].cpu().double().numpy() for k in ("logp", "entropy", "stats", "top_logp", "top_id")},
+           ref.token_logprobs(_np(fb[:3]), tb[:3].numpy(), 1.0, 16))
+
+
+def test_offsets_past_32_bits():
+    """Rows 2^30 + 6 elements apart: the third starts past 2^31 elements (4 GB), and so does its gradient."""
+    n, V, ld = 3, 1003, (1 << 30) + 6
+    full, t = _logits(n, V, torch.bfloat16, seed=17)
+    flat = torch.empty(2 * ld + V, dtype=torch.bfloat16, device=DEV)
+    z = flat.as_strided((n, V), (ld, 1))
+    z.copy_(full.to(DEV))
+    lp, st, H = torch.empty(n, device=DEV), torch.empty(n, 2, device=DEV), torch.empty(n, device=DEV)
+    r3.token_logprobs(z, t.to(DEV), lp, entropy=H, stats=st)
+    want = ref.token_logprobs(_np(full), t.numpy(), 1.0)
+    _check({"logp": lp.cpu().double().numpy(), "stats": st.cpu().double().numpy(), "entropy": H.cpu().double().numpy()}, want)
+    dl = np.array([1.0, -1.0, 0.5])
+    r3.token_logprobs_backward(z, t.to(DEV), st, z, dlogp=torch.tensor(dl, dtype=torch.float32, device=DEV))
+    _check_grad(z.cpu().double().numpy(), full, V, t, 1.0, dl, None, torch.bfloat16)
