@@ -318,8 +318,8 @@ size_t r3_policy_workspace_bytes(void);
  *   top_logp[i], top_id[i] ([n,top]): the `top` largest l_v, descending, and
  *     their ids; ties go to the lower id, -0 equals +0.
  * target: device int32 [n], or NULL (every row counts; logp must be NULL).
- * Row i is left out if target[i] is -1 (prompt, padding): its logits are not
- * read, its logp, entropy and stats are 0 and it has no alternatives.  Other
+ * Row i is left out if target[i] is -1 (prompt, padding): its logits do not
+ * matter, its logp, entropy and stats are 0 and it has no alternatives.  Other
  * values outside [0, V) do the same and set R3_DATA_IDX_RANGE.
  * A logit of -inf is a masked token: probability 0, logp -inf, never an
  * alternative (missing ones: id -1, logp -inf).  The lowest finite value is an

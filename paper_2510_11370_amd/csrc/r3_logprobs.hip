@@ -24,55 +24,101 @@ __device__ __forceinline__ float wave_max_nan(float v) {
     return v;
 }
 
-// Running statistics over some of a row's elements: m their maximum, s = sum 2^x, q = sum 2^x x with
-// x = c (z - m), c = s log2(e).  m = -inf, s = q = 0: nothing yet, or nothing but -inf.
+// Running statistics over some of a row's elements: m their maximum, s = sum 2^x, q = sum 2^x x with x = c z - r,
+// c = scale log2(e).  The sums refer to a logit b that was the maximum when it was taken, r = c b, and stay with it until a
+// logit exceeds `most` = b + 64 / c: one fused multiply-add to an exponent, with the one rounding, and no change of reference
+// in the loop.  Where b is not a moderate number (nothing but -inf so far, 1e30 and beyond), most = -inf, r = b and
+// x = c (z - b).  Elements come in pieces: `where` is the piece that holds m, m2 the largest of the other pieces.
 struct Stat {
-    float m, s, q;
+    float m, s, q, r, most, m2;
+    int where;
 };
-// the same sums for another maximum, which is at least a.m (or NaN)
-template <bool ENT> __device__ __forceinline__ void rebase(Stat &a, float m, float c) {
-    const float d = fmaxf((a.m - m) * c, -kFar), f = __builtin_amdgcn_exp2f(d);   // (-inf less -inf: -kFar, f = 0)
+__device__ __forceinline__ Stat no_stat() { return {-INFINITY, 0.0f, 0.0f, -INFINITY, -INFINITY, -INFINITY, 0}; }
+// a piece's name: its first vector, and whether it is two vectors (NT apart), one, or one of the loose elements
+enum { kPair = 0, kOne = 1, kLoose = 2 };
+// s and q for exponents less by d
+template <bool ENT> __device__ __forceinline__ void shift(Stat &a, float d) {
+    const float f = __builtin_amdgcn_exp2f(d);
     if constexpr (ENT) a.q = fmaf(a.s, d, a.q) * f;
     a.s *= f;
-    a.m = m;
+}
+// s and q for x = c (z - m) instead; m is at least the reference (or NaN)
+template <bool ENT> __device__ __forceinline__ void refer_to(Stat &a, float m, float c) {
+    shift<ENT>(a, fmaxf(a.most > -INFINITY ? fmaf(-m, c, a.r) : (a.r - m) * c, -kFar));   // (-inf less -inf: -kFar)
 }
 
-// N more elements.
-template <int N, bool ENT> __device__ __forceinline__ void take(Stat &a, const float (&z)[N], float c) {
+// N more elements, a piece of the name given.
+template <bool ENT, bool TOP, int N>
+__device__ __forceinline__ void take(Stat &a, const float (&z)[N], float c, float span, int name) {
     float hi = z[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) hi = max_nan(hi, z[i]);
-    rebase<ENT>(a, max_nan(a.m, hi), c);
+    if constexpr (TOP) {
+        a.m2 = __builtin_amdgcn_fmed3f(a.m, hi, a.m2);
+        a.where = hi > a.m ? name : a.where;
+    }
+    a.m = max_nan(a.m, hi);
+    if (!(hi <= a.most)) {   // the first ones, a much larger one, a NaN
+        refer_to<ENT>(a, a.m, c);
+        const bool moderate = fabsf(a.m) <= 1e30f;
+        a.most = moderate ? a.m + span : -INFINITY;
+        a.r = moderate ? a.m * c : a.m;
+        if (moderate) shift<ENT>(a, fmaf(a.m, c, -a.r));   // from x = c (z - b) to x = c z - r
+    }
+    if (a.most > -INFINITY) {
+        float s = a.s, q = a.q;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float x = fmaf(z[i], c, -a.r), e = __builtin_amdgcn_exp2f(x);
+            s += e;
+            if constexpr (ENT) q = fmaf(e, x, q);
+        }
+        if (!ENT || q == q) {   // (an x of -inf makes q a NaN)
+            a.s = s;
+            a.q = q;
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float x = fmaxf(fmaf(z[i], c, -a.r), -kFar), e = __builtin_amdgcn_exp2f(x);
+            a.s += e;
+            a.q = fmaf(e, x, a.q);
+        }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float x = fmaxf((z[i] - a.m) * c, -kFar), e = __builtin_amdgcn_exp2f(x);
+        const float x = fmaxf((z[i] - a.r) * c, -kFar), e = __builtin_amdgcn_exp2f(x);
         a.s += e;
         if constexpr (ENT) a.q = fmaf(e, x, a.q);
     }
 }
 
+// What is kept of a part of a row: maximum and sums for x = c (z - m).
+struct Part {
+    float m, s, q;
+};
+
 // A logit and its place in one whole number: larger logits first, then lower places.  0: none.
 typedef unsigned long long key_t;
-__device__ __forceinline__ key_t make_key(float z, int v) {
-    const uint32_t b = __float_as_uint(z + 0.0f);   // -0 equals +0
-    const uint32_t o = (b & 0x80000000u) ? ~b : b | 0x80000000u;
-    return ((key_t)o << 32) | (0xffffffffu - (uint32_t)v);
+__device__ __forceinline__ uint32_t order_of(float z) {   // of finite numbers and infinities
+    const uint32_t b = __float_as_uint(z + 0.0f);         // -0 equals +0
+    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ float key_logit(key_t k) {
-    const uint32_t o = (uint32_t)(k >> 32);
-    return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
-}
+__device__ __forceinline__ float of_order(uint32_t o) { return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o); }
+__device__ __forceinline__ key_t make_key(float z, int v) { return ((key_t)order_of(z) << 32) | (0xffffffffu - (uint32_t)v); }
+__device__ __forceinline__ float key_logit(key_t k) { return of_order((uint32_t)(k >> 32)); }
 __device__ __forceinline__ int key_place(key_t k) { return (int)(0xffffffffu - (uint32_t)k); }
 
 struct Args {
     int64_t n, ld, row0;            // rows row0 .. n - 1
     int V, top, nsplit, seg;        // seg: elements of one part of a row
-    float scale, c;
+    float scale, c, span;           // c = scale log2(e), span = 64 / c
     const void *logits;
     const int32_t *target;
     float *logp, *entropy, *stats, *top_logp;
     int32_t *top_id, *status;
-    Stat *part;                     // [n][nsplit], and
+    Part *part;                     // [n][nsplit], and
     key_t *part_keys;               // [n][nsplit][top], where rows are cut
 };
 
@@ -83,7 +129,7 @@ __device__ __forceinline__ float log_odds(float z, float m, float scale) {
 }
 
 // What a row comes to, by the thread that has it.
-__device__ __forceinline__ void put_row(const Args &a, int64_t row, const Stat &r, float zt) {
+__device__ __forceinline__ void put_row(const Args &a, int64_t row, const Part &r, float zt) {
     const float ls = logf(r.s), nan = __uint_as_float(0x7fc00000u);
     const bool bad = !(r.m < INFINITY), none = r.m == -INFINITY;
     if (bad && a.status) atomicOr(a.status, R3_DATA_NONFINITE);
@@ -115,27 +161,39 @@ __device__ __forceinline__ void put_left_out(const Args &a, int64_t row, int t, 
     put_no_top(a, row, tid, -INFINITY);
 }
 
+// How many of the count keys of buf (room for kBuf) are above k: eight reads in flight.
+template <int kBuf> __device__ __forceinline__ int rank_of(const key_t *buf, int count, key_t k) {
+    int rank = 0;
+    for (int q = 0; q < count; q += 8) {
+        key_t v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = buf[min(q + u, kBuf - 1)];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) rank += q + u < count && v[u] > k;
+    }
+    return rank;
+}
 // Of the candidates in buf[0..count) the `top` largest, each to its rank; keys are distinct (0 is none).
-template <int NT, class F> __device__ __forceinline__ void rank_out(const key_t *buf, int count, int top, int tid, F put) {
+template <int NT, int kBuf, class F> __device__ __forceinline__ void rank_out(const key_t *buf, int count, int top, int tid, F put) {
     for (int i = tid; i < count; i += NT) {
         const key_t k = buf[i];
-        int rank = 0;
-        for (int q = 0; q < count; ++q) rank += buf[q] > k;
+        const int rank = rank_of<kBuf>(buf, count, k);
         if (rank < top) put(rank, k);
     }
     for (int i = count + tid; i < top; i += NT) put(i, (key_t)0);
 }
 
-// The k-th largest of the lanes' values: each lane counts those above its own, and the smallest value with less than k
-// above it is the one.
-__device__ __forceinline__ float kth_of_wave(float v, int k) {
-    int above = 0;
-#pragma unroll 8
-    for (int i = 0; i < kWave; ++i) above += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), i)) > v;
-    float t = above < k ? v : INFINITY;
+// A number that at least k of the lanes' values reach, and all but the last bits of the largest such: the upper 16 bits of
+// the values' order (what a bf16 has), one at a time by counting lanes.  -inf where fewer than k lanes have more.
+__device__ __forceinline__ float reached_by(float v, int k) {
+    const uint32_t o = order_of(v);
+    uint32_t t = 0;
 #pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) t = fminf(t, __shfl_xor(t, o, kWave));
-    return t;
+    for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t c = t | 1u << bit;
+        t = __popcll(__ballot(o >= c)) >= k ? c : t;
+    }
+    return t <= order_of(-INFINITY) ? -INFINITY : of_order(t);
 }
 
 // NT threads to a row (or to one of a.nsplit parts of it); NT = 64: four rows to a work-group, nothing shared between its
@@ -143,21 +201,21 @@ __device__ __forceinline__ float kth_of_wave(float v, int k) {
 //
 // Alternatives: a thread knows the maximum of its own elements anyway.  The 64 maxima over the threads of one lane number
 // are 64 elements of the row, so the k-th largest of them has k elements at or above it: a bound from below for the k-th
-// largest element, met by some 64 ln(64 / (64 - k)) elements of a row in random order (24 for k = 20).  Only the threads
-// whose maximum reaches it are read again, by whole waves, from L2.  Rows that keep more candidates than fit (many equal
+// largest element, met by some 64 ln(64 / (64 - k)) elements of a row in random order (24 for k = 20).  A thread whose maximum reaches
+// it has that piece read again, and all of its elements if another of its pieces reaches it too.  Rows that keep more candidates than fit (many equal
 // values) are gone through once more in order with the k-th best so far as the bound.
 template <typename T, int NT, bool ENT, bool TOP>
 __global__ void __launch_bounds__(NT < 256 ? 256 : NT)
 token_logprobs_kernel(Args a) {
     typedef Row<T> R;
-    constexpr int N = R::kVec, U = 4, W = NT / kWave, kRows = NT == kWave ? 4 : 1;
+    constexpr int N = R::kVec, U = TOP ? 2 : 4, W = NT / kWave, kRows = NT == kWave ? 4 : 1;
     constexpr int kBuf = 2 * NT;   // room for the k best and one more element from every thread
     static_assert(kBuf >= NT + kMaxTop, "");
-    __shared__ float max_s[kRows][W][kWave], sum_s[kRows][2][W], thr_s[kRows];
-    __shared__ int count_s[kRows][2];
+    __shared__ float max_s[kRows][W][kWave], sum_s[kRows][2][W];
+    __shared__ int count_s[kRows][3];
     __shared__ int sel_s[TOP ? kRows : 1][TOP ? NT : 1];
     __shared__ key_t buf_s[TOP ? kRows : 1][TOP ? kBuf : 1];
-    const int lane = lane_id(), slot = kRows > 1 ? (int)threadIdx.x / kWave : 0;
+    const int lane = lane_id(), slot = kRows > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) : 0;
     const int tid = kRows > 1 ? lane : (int)threadIdx.x, w = tid / kWave;
     auto sync = [] {
         if constexpr (W > 1) __syncthreads();
@@ -171,61 +229,93 @@ token_logprobs_kernel(Args a) {
     const int split = (int)(item - row * a.nsplit);
     if (row >= a.n) return;
     const int t = a.target ? a.target[row] : 0;
-    if (t < 0 || t >= a.V) {
-        if (split == 0) put_left_out(a, row, t, tid);
+    // Short rows and few long ones wait for latencies: there the target is not waited for, and a row left out is found to
+    // be one at the end.
+    const bool left_out = t < 0 || t >= a.V, late = W == 1 || a.nsplit > 1;
+    if (left_out && !late) {
+        put_left_out(a, row, t, tid);
         return;
     }
     const T *z = (const T *)a.logits + row * a.ld;
-    const int lo = split * a.seg, len = min(a.seg, a.V - lo), nvec = len / N;
+    const int lo = split * a.seg, len = min(a.seg, a.V - lo);
+    // elements before the first whole vector at a 16-byte address and behind the last one: a thread each
     const T *zp = z + lo;
-    float zt = 0.0f;
+    const int head = min(len, (int)((0 - (uintptr_t)zp) % 16 / sizeof(T))), nvec = (len - head) / N, rest = head + nvec * N;
+    const int nloose = head + len - rest;
+    const T *zv = zp + head;
+    auto loose = [&](int i) { return i < head ? i : rest + i - head; };
     if (tid == 0) {
-        zt = Elem<T>::ld(z + t);
-        count_s[slot][0] = count_s[slot][1] = 0;
+        count_s[slot][0] = count_s[slot][1] = count_s[slot][2] = 0;
     }
-    Stat st = {-INFINITY, 0.0f, 0.0f};
+    Stat run = no_stat();
+    // U loads of a thread on their way, consumed two at a time and replaced at once
     int j = tid;
-    for (; j + (U - 1) * NT < nvec; j += U * NT) {
+    if (j + (U - 1) * NT < nvec) {
         typename R::V v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = R::load(zp + (int64_t)(j + u * NT) * N);
-        float f[U * N];
+        for (int u = 0; u < U; ++u) v[u] = R::load_once(zv + (int64_t)(j + u * NT) * N);
+        for (; j + (2 * U - 1) * NT < nvec; j += U * NT) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) R::unpack(v[u], f + u * N);
-        take<U * N, ENT>(st, f, a.c);
+            for (int u = 0; u < U; u += 2) {
+                float f[2 * N];
+                R::unpack(v[u], f);
+                R::unpack(v[u + 1], f + N);
+                v[u] = R::load_once(zv + (int64_t)(j + (u + U) * NT) * N);
+                v[u + 1] = R::load_once(zv + (int64_t)(j + (u + 1 + U) * NT) * N);
+                take<ENT, TOP>(run, f, a.c, a.span, 4 * (j + u * NT) + kPair);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; u += 2) {
+            float f[2 * N];
+            R::unpack(v[u], f);
+            R::unpack(v[u + 1], f + N);
+            take<ENT, TOP>(run, f, a.c, a.span, 4 * (j + u * NT) + kPair);
+        }
+        j += U * NT;
     }
     for (; j < nvec; j += NT) {
         float f[N];
-        R::unpack(R::load(zp + (int64_t)j * N), f);
-        take<N, ENT>(st, f, a.c);
+        R::unpack(R::load_once(zv + (int64_t)j * N), f);
+        take<ENT, TOP>(run, f, a.c, a.span, 4 * j + kOne);
     }
-    if (tid < len - nvec * N) {
-        const float f[1] = {Elem<T>::ld(zp + nvec * N + tid)};
-        take<1, ENT>(st, f, a.c);
+    if (tid < nloose) {
+        const float f[1] = {Elem<T>::ld(zp + loose(tid))};
+        take<ENT, TOP>(run, f, a.c, a.span, 4 * tid + kLoose);
     }
 
-    const float mine = st.m;
+    float zt = 0.0f;
+    if (tid == 0 && !left_out) zt = Elem<T>::ld(z + t);
+
+    const float mine = run.m;
     float top64 = mine;   // the largest of the threads with this lane's number
     if constexpr (W > 1) {
         max_s[slot][w][lane] = mine;
         sync();
 #pragma unroll
         for (int i = 0; i < W; ++i) top64 = max_nan(top64, max_s[slot][i][lane]);
+    } else if constexpr (TOP) {
+        sync();
     }
     const float m = wave_max_nan(top64);
-    rebase<ENT>(st, m, a.c);
-    st.s = wave_sum(st.s);
-    if constexpr (ENT) st.q = wave_sum(st.q);
+    const bool search = TOP && m > -INFINITY && m < INFINITY;   // (the same in every thread)
+    float thr = 0.0f;
+    int *sel = sel_s[TOP ? slot : 0];
+    key_t *buf = buf_s[TOP ? slot : 0];
+    if (search) {
+        thr = reached_by(top64, a.top);
+        if (mine >= thr && mine > -INFINITY) {   // from below: threads read as a whole; from above: those of one piece
+            if (run.m2 >= thr && run.m2 > -INFINITY) sel[atomicAdd(&count_s[slot][0], 1)] = tid;
+            else sel[NT - 1 - atomicAdd(&count_s[slot][2], 1)] = run.where;
+        }
+    }
+    refer_to<ENT>(run, m, a.c);
+    Part st = {m, wave_sum(run.s), ENT ? wave_sum(run.q) : 0.0f};
     if constexpr (W > 1) {
         if (lane == 0) {
             sum_s[slot][0][w] = st.s;
             sum_s[slot][1][w] = st.q;
         }
-    }
-    const bool search = TOP && m > -INFINITY && m < INFINITY;   // (the same in every thread)
-    if (search && w == 0) {
-        const float b = kth_of_wave(top64, a.top);
-        if (lane == 0) thr_s[slot] = b;
     }
     if constexpr (W > 1 || TOP) sync();
     if constexpr (W > 1) {
@@ -235,6 +325,10 @@ token_logprobs_kernel(Args a) {
             st.s += sum_s[slot][0][i];
             st.q += sum_s[slot][1][i];
         }
+    }
+    if (W == 1 && left_out) {
+        put_left_out(a, row, t, tid);
+        return;
     }
     if (tid == 0) {
         if (a.nsplit == 1) put_row(a, row, st, zt);
@@ -251,28 +345,43 @@ token_logprobs_kernel(Args a) {
             else if (tid < a.top) a.part_keys[item * a.top + tid] = 0;
             return;
         }
-        const float thr = thr_s[slot];
-        int *sel = sel_s[slot];
-        key_t *buf = buf_s[slot];
-        if (mine >= thr && mine > -INFINITY) sel[atomicAdd(&count_s[slot][0], 1)] = tid;
-        sync();
-        const int nsel = count_s[slot][0];
+        const int nsel = count_s[slot][0], none = count_s[slot][2];
         auto offer = [&](float x, int place) {
             if (x >= thr && x > -INFINITY) {
                 const int at = atomicAdd(&count_s[slot][1], 1);
                 if (at < kBuf) buf[at] = make_key(x, lo + place);
             }
         };
-        for (int i = w; i < nsel; i += W) {
-            const int who = sel[i];
-            for (int q = who + lane * NT; q < nvec; q += kWave * NT) {
-                float f[N];
-                R::unpack(R::load(zp + (int64_t)q * N), f);
-#pragma unroll
-                for (int u = 0; u < N; ++u) offer(f[u], q * N + u);
+        // the pieces' vectors and all of the other threads', dealt to all threads, two in flight
+        const int per = (nvec + NT - 1) / NT, all = 2 * none + nsel * per;
+        auto vector_of = [&](int p) {   // (nvec: none)
+            if (p >= all) return nvec;
+            if (p < 2 * none) {
+                const int name = sel[NT - 1 - p / 2], second = p & 1, kind = name & 3;
+                return kind == kLoose || (second && kind == kOne) ? nvec : name / 4 + second * NT;
             }
-            if (lane == 0 && who < len - nvec * N) offer(Elem<T>::ld(zp + nvec * N + who), nvec * N + who);
+            p -= 2 * none;
+            return min(nvec, sel[p / per] + p % per * NT);
+        };
+        for (int i = tid; i < all; i += 2 * NT) {
+            const int q[2] = {vector_of(i), vector_of(i + NT)};
+            typename R::V v[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (q[h] < nvec) v[h] = R::load(zv + (int64_t)q[h] * N);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (q[h] < nvec) {
+                    float f[N];
+                    R::unpack(v[h], f);
+#pragma unroll
+                    for (int u = 0; u < N; ++u) offer(f[u], head + q[h] * N + u);
+                }
         }
+        for (int i = tid; i < none; i += NT)
+            if (const int name = sel[NT - 1 - i]; (name & 3) == kLoose) offer(Elem<T>::ld(zp + loose(name / 4)), loose(name / 4));
+        for (int i = tid; i < nsel; i += NT)
+            if (sel[i] < nloose) offer(Elem<T>::ld(zp + loose(sel[i])), loose(sel[i]));
         sync();
         int count = count_s[slot][1];
         if (count > kBuf) {
@@ -294,8 +403,7 @@ token_logprobs_kernel(Args a) {
                     for (int u = 0; u < kBuf / NT; ++u) {
                         const int i = tid + u * NT;
                         best[u] = i < count ? buf[i] : 0;
-                        rank[u] = i < count ? 0 : kBuf;
-                        for (int q = 0; q < count; ++q) rank[u] += buf[q] > best[u];
+                        rank[u] = i < count ? rank_of<kBuf>(buf, count, best[u]) : kBuf;
                     }
                     sync();
 #pragma unroll
@@ -308,7 +416,7 @@ token_logprobs_kernel(Args a) {
                 }
             }
         }
-        rank_out<NT>(buf, count, a.top, tid, put);
+        rank_out<NT, kBuf>(buf, count, a.top, tid, put);
     }
 }
 
@@ -321,14 +429,16 @@ token_logprobs_join_kernel(Args a) {
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, lane = lane_id();
     const int t = a.target ? a.target[row] : 0;
-    if (t < 0 || t >= a.V) return;   // written by the row's first part
-    Stat st = {-INFINITY, 0.0f, 0.0f};
+    Part st = {-INFINITY, 0.0f, 0.0f};
     if (lane < a.nsplit) st = a.part[row * a.nsplit + lane];
+    if (t < 0 || t >= a.V) {
+        put_left_out(a, row, t, tid);
+        return;
+    }
     const float zt = tid == 0 ? Elem<T>::ld((const T *)a.logits + row * a.ld + t) : 0.0f;
     const float m = wave_max_nan(st.m);
-    rebase<true>(st, m, a.c);
-    st.s = wave_sum(st.s);
-    st.q = wave_sum(st.q);
+    const float d = fmaxf((st.m - m) * a.c, -kFar), f = __builtin_amdgcn_exp2f(d);
+    st = {m, wave_sum(st.s * f), wave_sum(fmaf(st.s, d, st.q) * f)};
     if (tid == 0) put_row(a, row, st, zt);
     if (a.top == 0) return;
     if (!(m > -INFINITY && m < INFINITY)) {
@@ -360,7 +470,7 @@ token_logprobs_join_kernel(Args a) {
     }
     __syncthreads();
     const float ls = logf(st.s);
-    rank_out<256>(buf, count_s, a.top, tid, [&](int rank, key_t k) { put_top(a, row, rank, k, m, ls); });
+    rank_out<256, kMaxSplit * kMaxTop>(buf, count_s, a.top, tid, [&](int rank, key_t k) { put_top(a, row, rank, k, m, ls); });
 }
 
 struct BackArgs {
@@ -433,14 +543,14 @@ Plan plan(int64_t n, int64_t V) {
     const int64_t seg = ((V + k - 1) / k + 7) / 8 * 8;
     return {(int)((V + seg - 1) / seg), (int)seg};
 }
-size_t stat_bytes(int64_t n, const Plan &p) { return align_up((size_t)n * p.nsplit * sizeof(Stat), 256); }
+size_t part_bytes(int64_t n, const Plan &p) { return align_up((size_t)n * p.nsplit * sizeof(Part), 256); }
 
 }  // namespace
 
 size_t token_logprobs_ws_bytes(int64_t n, int64_t V, int top) {
     const Plan p = plan(n, V);
     if (p.nsplit == 1) return 0;
-    return stat_bytes(n, p) + align_up((size_t)n * p.nsplit * top * sizeof(key_t), 256);
+    return part_bytes(n, p) + align_up((size_t)n * p.nsplit * top * sizeof(key_t), 256);
 }
 
 hipError_t launch_token_logprobs(int64_t n, int64_t V, int dtype, const void *logits, int64_t ld, float scale, const int32_t *target,
@@ -449,12 +559,12 @@ hipError_t launch_token_logprobs(int64_t n, int64_t V, int dtype, const void *lo
     const Plan p = plan(n, V);
     Args a = {};
     a.n = n; a.ld = ld; a.V = (int)V; a.top = top; a.nsplit = p.nsplit; a.seg = p.seg;
-    a.scale = scale; a.c = (float)((double)scale * 1.4426950408889634);
+    a.scale = scale; a.c = (float)((double)scale * 1.4426950408889634); a.span = 64.0f / a.c;
     a.logits = logits; a.target = target;
     a.logp = logp; a.entropy = entropy; a.stats = stats; a.top_logp = top_logp; a.top_id = top_id; a.status = status;
     if (p.nsplit > 1) {
-        a.part = (Stat *)ws;
-        a.part_keys = (key_t *)((char *)ws + stat_bytes(n, p));
+        a.part = (Part *)ws;
+        a.part_keys = (key_t *)((char *)ws + part_bytes(n, p));
     }
     ProfScope ps(PROF_LOGPROBS, s);
     auto go = [&](auto type, auto nt) {
@@ -469,8 +579,9 @@ hipError_t launch_token_logprobs(int64_t n, int64_t V, int dtype, const void *lo
         if (p.nsplit > 1) token_logprobs_join_kernel<T><<<(unsigned)n, 256, 0, s>>>(a);
     };
     auto by_size = [&](auto type) {
+        const int64_t bytes = V * (int64_t)sizeof(type);
         if (V <= 4096) go(type, std::integral_constant<int, 64>{});
-        else if (V <= 32768) go(type, std::integral_constant<int, 256>{});
+        else if (bytes <= (top > 0 ? 131072 : 65536)) go(type, std::integral_constant<int, 256>{});
         else go(type, std::integral_constant<int, 512>{});
     };
     if (dtype == R3_BF16) by_size(bf16_t{});

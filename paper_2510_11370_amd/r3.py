@@ -181,38 +181,45 @@ def policy_discrepancy(logp_train, logp_infer, taus, kl_out, frac_out, ws=None):
                                        C.c_size_t(ws.numel()), _stream()), "r3_policy_discrepancy")
 
 
-def _have(what, device, **tensors):
-    """Refuses what the C call would take for something else: {name: (tensor or None, shape, dtype)}, dense unless the
-    shape is None, on the current device.  Returns their addresses, 0 for None."""
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise R3Error("%s: tensors on %s, which is not the current GPU" % (what, device))
-    out = []
-    for name, (t, shape, dtype) in tensors.items():
-        if t is None:
-            out.append(0)
-            continue
-        if t.dtype != dtype or t.device != device or (shape is not None and (tuple(t.shape) != shape or not t.is_contiguous())):
-            raise R3Error("%s: %s has to be a dense %s tensor of shape %s on %s" % (what, name, dtype, shape, device))
-        out.append(t.data_ptr())
-    return out
+def _device(what, t):
+    """The current GPU's number, which has to be the tensor's."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise R3Error("%s: tensors on %s, which is not the current GPU" % (what, t.device))
+    return dev
+
+
+def _at(what, name, t, dev, dtype, shape):
+    """Address of a dense tensor (0 for None); refuses one that the C call would take for something else."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+        raise R3Error("%s: %s has to be a dense %s tensor of shape %s on cuda:%d" % (what, name, dtype, tuple(shape), dev))
+    return t.data_ptr()
+
+
+def _raw_stream(dev):
+    return torch._C._cuda_getCurrentRawStream(dev)   # torch.cuda.current_stream() makes an object: 2.8 us of a 10 us call
 
 
 def combine_backward(D, dy, Yp, gates, inv_perm, dYp=None, dgates=None, dz=None):
     """Gradient of combine: rows dYp [T*K,d], gates dgates [T,K], selected logits dz [T,K]; each may be None, and Yp with
     dgates and dz.  dYp may be Yp."""
-    a, T, K, d, f = act_dtype(D), D.T, D.K, D.d, torch.float32
-    ptr = _have("combine_backward", dy.device, dy=(dy, (T, d), a), Yp=(Yp, (T * K, d), a), gates=(gates, (T, K), f),
-                inv_perm=(inv_perm, (T * K,), torch.int32), dYp=(dYp, (T * K, d), a), dgates=(dgates, (T, K), f),
-                dz=(dz, (T, K), f))
-    _check(lib().r3_combine_backward(C.byref(D), *ptr, torch.cuda.current_stream().cuda_stream), "r3_combine_backward")
+    w, dev, a, f = "combine_backward", _device("combine_backward", dy), act_dtype(D), torch.float32
+    tok, rows, slots = (D.T, D.d), (D.T * D.K, D.d), (D.T, D.K)
+    _check(lib().r3_combine_backward(
+        C.byref(D), _at(w, "dy", dy, dev, a, tok), _at(w, "Yp", Yp, dev, a, rows), _at(w, "gates", gates, dev, f, slots),
+        _at(w, "inv_perm", inv_perm, dev, torch.int32, rows[:1]), _at(w, "dYp", dYp, dev, a, rows),
+        _at(w, "dgates", dgates, dev, f, slots), _at(w, "dz", dz, dev, f, slots), _raw_stream(dev)), "r3_combine_backward")
 
 
 def permute_backward(D, dXp, inv_perm, dx, add=None):
     """Gradient of permute's rows: dx [T,d] = add + the sum of each token's K rows of dXp [T*K,d].  add may be dx."""
-    a = act_dtype(D)
-    ptr = _have("permute_backward", dXp.device, dXp=(dXp, (D.T * D.K, D.d), a), inv_perm=(inv_perm, (D.T * D.K,), torch.int32),
-                add=(add, (D.T, D.d), a), dx=(dx, (D.T, D.d), a))
-    _check(lib().r3_permute_backward(C.byref(D), *ptr, torch.cuda.current_stream().cuda_stream), "r3_permute_backward")
+    w, dev, a = "permute_backward", _device("permute_backward", dXp), act_dtype(D)
+    tok, rows = (D.T, D.d), (D.T * D.K, D.d)
+    _check(lib().r3_permute_backward(
+        C.byref(D), _at(w, "dXp", dXp, dev, a, rows), _at(w, "inv_perm", inv_perm, dev, torch.int32, rows[:1]),
+        _at(w, "add", add, dev, a, tok), _at(w, "dx", dx, dev, a, tok), _raw_stream(dev)), "r3_permute_backward")
 
 
 def token_logprobs_workspace(n, V, top=0, device="cuda"):
@@ -222,10 +229,14 @@ def token_logprobs_workspace(n, V, top=0, device="cuda"):
 
 
 def _logits(what, t):
-    if t.dim() != 2 or t.dtype not in (torch.bfloat16, torch.float32) or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise R3Error("%s: logits and their gradient are [n, V], bfloat16 or float32, with dense rows" % what)
+    """n, V, the library's type, the rows' stride"""
+    if t.dim() != 2 or (t.dtype is not torch.bfloat16 and t.dtype is not torch.float32):
+        raise R3Error("%s: logits and their gradient are [n, V], bfloat16 or float32" % what)
     n, V = t.shape
-    return n, V, BF16 if t.dtype == torch.bfloat16 else F32, t.stride(0) if n > 1 else max(V, t.stride(0))
+    ld, one = t.stride()
+    if V > 1 and one != 1:
+        raise R3Error("%s: the rows of logits and of their gradient are dense" % what)
+    return n, V, BF16 if t.dtype is torch.bfloat16 else F32, ld if n > 1 else max(V, ld)
 
 
 def token_logprobs(logits, target, logp=None, entropy=None, stats=None, top_logp=None, top_id=None, scale=1.0, status=None,
@@ -233,34 +244,35 @@ def token_logprobs(logits, target, logp=None, entropy=None, stats=None, top_logp
     """Of each row of logits [n,V] (rows may be strided): logp [n] of target [n] (int32; -1 leaves a row out), entropy [n],
     stats [n,2] (for the backward), top_logp and top_id [n,top] the most probable alternatives.  scale: 1 / temperature.
     ws: token_logprobs_workspace(n, V, top); made here where it is needed and not given."""
-    n, V, dt, ld = _logits("token_logprobs", logits)
+    w = "token_logprobs"
+    n, V, dt, ld = _logits(w, logits)
+    dev, f, i = _device(w, logits), torch.float32, torch.int32
     top = 0 if top_id is None else top_id.shape[-1]
-    f, i = torch.float32, torch.int32
-    z, tg, lp, en, st, tl, ti, sw = _have(
-        "token_logprobs", logits.device, logits=(logits, None, logits.dtype), target=(target, (n,), i), logp=(logp, (n,), f),
-        entropy=(entropy, (n,), f), stats=(stats, (n, 2), f), top_logp=(top_logp, (n, top), f), top_id=(top_id, (n, top), i),
-        status=(status, (1,), i))
     if ws is None:
         ws = token_logprobs_workspace(n, V, top, logits.device)
-    _check(lib().r3_token_logprobs(n, V, dt, z, ld, scale, tg, lp, en, st, top, tl, ti, sw, 0 if ws is None else ws.data_ptr(),
-                                   0 if ws is None else ws.numel(), torch.cuda.current_stream().cuda_stream),
-           "r3_token_logprobs")
+    elif ws.get_device() != dev or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        raise R3Error("%s: ws has to be a dense uint8 tensor on cuda:%d" % (w, dev))
+    _check(lib().r3_token_logprobs(
+        n, V, dt, logits.data_ptr(), ld, scale, _at(w, "target", target, dev, i, (n,)), _at(w, "logp", logp, dev, f, (n,)),
+        _at(w, "entropy", entropy, dev, f, (n,)), _at(w, "stats", stats, dev, f, (n, 2)), top,
+        _at(w, "top_logp", top_logp, dev, f, (n, top)), _at(w, "top_id", top_id, dev, i, (n, top)),
+        _at(w, "status", status, dev, i, (1,)), 0 if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
+        _raw_stream(dev)), "r3_token_logprobs")
 
 
 def token_logprobs_backward(logits, target, stats, dlogits, dlogp=None, entropy=None, dentropy=None, scale=1.0):
     """Gradient of sum(dlogp * logp + dentropy * entropy) with respect to the logits, from token_logprobs' stats and (with
     dentropy) entropy.  dlogits may be logits."""
-    n, V, dt, ld = _logits("token_logprobs_backward", logits)
-    n2, V2, dt2, ldd = _logits("token_logprobs_backward", dlogits)
-    if (n, V, dt) != (n2, V2, dt2):
-        raise R3Error("token_logprobs_backward: dlogits has to be of the logits' shape and type")
-    f = torch.float32
-    z, dz, tg, st, en, dl, de = _have(
-        "token_logprobs_backward", logits.device, logits=(logits, None, logits.dtype), dlogits=(dlogits, None, logits.dtype),
-        target=(target, (n,), torch.int32), stats=(stats, (n, 2), f), entropy=(entropy, (n,), f), dlogp=(dlogp, (n,), f),
-        dentropy=(dentropy, (n,), f))
-    _check(lib().r3_token_logprobs_backward(n, V, dt, z, ld, scale, tg, st, en, dl, de, dz, ldd,
-                                            torch.cuda.current_stream().cuda_stream), "r3_token_logprobs_backward")
+    w = "token_logprobs_backward"
+    n, V, dt, ld = _logits(w, logits)
+    n2, V2, dt2, ldd = _logits(w, dlogits)
+    dev, f = _device(w, logits), torch.float32
+    if (n, V, dt, dev) != (n2, V2, dt2, dlogits.get_device()):
+        raise R3Error("%s: dlogits has to be of the logits' shape, type and device" % w)
+    _check(lib().r3_token_logprobs_backward(
+        n, V, dt, logits.data_ptr(), ld, scale, _at(w, "target", target, dev, torch.int32, (n,)),
+        _at(w, "stats", stats, dev, f, (n, 2)), _at(w, "entropy", entropy, dev, f, (n,)), _at(w, "dlogp", dlogp, dev, f, (n,)),
+        _at(w, "dentropy", dentropy, dev, f, (n,)), dlogits.data_ptr(), ldd, _raw_stream(dev)), "r3_token_logprobs_backward")
 
 
 def _idx_code(t):
