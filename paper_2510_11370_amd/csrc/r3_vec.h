@@ -26,6 +26,7 @@ template <> struct Row<bf16_t> {
         return v;
     }
     static __device__ __forceinline__ void store(bf16_t *p, const float *f) { *(U *)p = pack(f); }
+    static __device__ __forceinline__ void store_once(bf16_t *p, const float *f) { __builtin_nontemporal_store(pack(f), (U *)p); }
 };
 template <> struct Row<float> {
     static constexpr int kVec = 4;
@@ -39,6 +40,7 @@ template <> struct Row<float> {
     }
     static __device__ __forceinline__ V pack(const float *f) { return V{f[0], f[1], f[2], f[3]}; }
     static __device__ __forceinline__ void store(float *p, const float *f) { *(U *)p = pack(f); }
+    static __device__ __forceinline__ void store_once(float *p, const float *f) { __builtin_nontemporal_store(pack(f), (U *)p); }
 };
 
 }  // namespace r3
