@@ -10,13 +10,13 @@
 namespace r3 {
 namespace {
 
-// A row of d elements is `units` pieces: whole vectors, then single elements.
+// A row of d elements: nvec whole vectors, then rest single elements.
 struct Width {
-    int d, nvec, units;
+    int d, nvec, rest;
 };
 template <typename T> Width width(int d) {
     constexpr int N = Row<T>::kVec;
-    return {d, d / N, d / N + d % N};
+    return {d, d / N, d % N};
 }
 
 template <class F> void by_rows(int K, F f) {   // rows in flight together: all K where K is one of these, else eight
@@ -46,16 +46,18 @@ __global__ void __launch_bounds__(256)
 combine_backward_kernel(CombineBwd a) {
     typedef Row<T> R;
     constexpr int N = R::kVec;
-    __shared__ float part[W > 1 ? W : 1][kMaxK];
-    const int wave = threadIdx.x / kWave, lane = lane_id();
-    const int t = __builtin_amdgcn_readfirstlane(W > 1 ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave);
-    if (t >= a.T) return;
+    constexpr int kTok = 4 / W;   // tokens of a work-group
+    __shared__ float part[4][kMaxK];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
+    const int t = blockIdx.x * kTok + wave / W;
+    const bool some = t < a.T;   // (waves of the last work-group may have no token, and still meet the others)
+    if (W == 1 && !some) return;
     const T *dy = (const T *)a.dy + (int64_t)t * a.w.d;
     const int32_t *rows = a.inv_perm + (int64_t)t * a.K;
     const float *gates = a.gates + (int64_t)t * a.K;
     const bool dots = a.Yp != nullptr;
     float mine = 0.0f;   // lane j: the dot product of slot j over this wave's columns
-    for (int j0 = 0; j0 < a.K; j0 += G) {
+    for (int j0 = some ? 0 : a.K; j0 < a.K; j0 += G) {
         int64_t at[G];
         float g[G], dot[G];
         bool in[G];
@@ -67,38 +69,38 @@ combine_backward_kernel(CombineBwd a) {
             g[j] = j0 + j < a.K ? gates[j0 + j] : 0.0f;
             dot[j] = 0.0f;
         }
-        for (int c = (W > 1 ? (int)threadIdx.x : lane); c < a.w.units; c += W * kWave) {
-            if (c < a.w.nvec) {
-                float x[N];
-                typename R::V v[G];
-                R::unpack(R::load(dy + c * N), x);
+        const int first = W > 1 ? (int)threadIdx.x % (W * kWave) : lane;
+        for (int c = first; c < a.w.nvec; c += W * kWave) {
+            float x[N];
+            typename R::V v[G];
+            R::unpack(R::load(dy + c * N), x);
+            if (dots) {
+#pragma unroll
+                for (int j = 0; j < G; ++j) v[j] = R::load_once((const T *)a.Yp + at[j] + c * N);
+            }
+#pragma unroll
+            for (int j = 0; j < G; ++j) {
                 if (dots) {
+                    float y[N];
+                    R::unpack(v[j], y);
 #pragma unroll
-                    for (int j = 0; j < G; ++j) v[j] = R::load_once((const T *)a.Yp + at[j] + c * N);
+                    for (int u = 0; u < N; ++u) dot[j] = fmaf(x[u], y[u], dot[j]);
                 }
+                if (a.dYp && in[j]) {
+                    float o[N];
 #pragma unroll
-                for (int j = 0; j < G; ++j) {
-                    if (dots) {
-                        float y[N];
-                        R::unpack(v[j], y);
-#pragma unroll
-                        for (int u = 0; u < N; ++u) dot[j] = fmaf(x[u], y[u], dot[j]);
-                    }
-                    if (a.dYp && in[j]) {
-                        float o[N];
-#pragma unroll
-                        for (int u = 0; u < N; ++u) o[u] = g[j] * x[u];
-                        R::store((T *)a.dYp + at[j] + c * N, o);
-                    }
+                    for (int u = 0; u < N; ++u) o[u] = g[j] * x[u];
+                    R::store_once((T *)a.dYp + at[j] + c * N, o);
                 }
-            } else {
-                const int e = a.w.nvec * N + (c - a.w.nvec);
-                const float x = Elem<T>::ld(dy + e);
+            }
+        }
+        if (first < a.w.rest) {
+            const int e = a.w.nvec * N + first;
+            const float x = Elem<T>::ld(dy + e);
 #pragma unroll
-                for (int j = 0; j < G; ++j) {
-                    if (dots) dot[j] = fmaf(x, Elem<T>::ld((const T *)a.Yp + at[j] + e), dot[j]);
-                    if (a.dYp && in[j]) Elem<T>::st((T *)a.dYp + at[j] + e, g[j] * x);
-                }
+            for (int j = 0; j < G; ++j) {
+                if (dots) dot[j] = fmaf(x, Elem<T>::ld((const T *)a.Yp + at[j] + e), dot[j]);
+                if (a.dYp && in[j]) Elem<T>::st((T *)a.dYp + at[j] + e, g[j] * x);
             }
         }
         if (dots) {
@@ -113,10 +115,10 @@ combine_backward_kernel(CombineBwd a) {
     if constexpr (W > 1) {
         part[wave][lane] = mine;
         __syncthreads();
-        if (wave > 0) return;
+        if (wave % W > 0 || !some) return;
         mine = 0.0f;
 #pragma unroll
-        for (int i = 0; i < W; ++i) mine += part[i][lane];
+        for (int i = 0; i < W; ++i) mine += part[wave + i][lane];
     }
     const float g = lane < a.K ? gates[lane] : 0.0f;
     const float mix = wave_sum(lane < a.K ? g * mine : 0.0f);
@@ -127,7 +129,8 @@ combine_backward_kernel(CombineBwd a) {
 }
 
 struct PermuteBwd {
-    int T, K, chunks;
+    int T, K;
+    uint32_t chunks;   // of 64 vectors, in a row
     int64_t S;
     Width w;
     const void *dXp, *add;
@@ -135,24 +138,20 @@ struct PermuteBwd {
     void *dx;
 };
 
-// A wave to 64 pieces of a token's row.  dx may be add.
+// A wave to 64 vectors of a token's row, the last one of a row to the elements behind them too.  dx may be add.
 template <typename T, int G>
 __global__ void __launch_bounds__(256)
 permute_backward_kernel(PermuteBwd a) {
     typedef Row<T> R;
     constexpr int N = R::kVec;
-    const int64_t item = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
-    const int t = __builtin_amdgcn_readfirstlane((int)(item / a.chunks));
-    if (t >= a.T) return;
-    const int c = __builtin_amdgcn_readfirstlane((int)(item % a.chunks)) * kWave + lane_id();
-    if (c >= a.w.units) return;
+    const uint32_t item = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), t = item / a.chunks;
+    if (t >= (uint32_t)a.T) return;
+    const int chunk = item - t * a.chunks, c = chunk * kWave + lane_id();
     const int32_t *rows = a.inv_perm + (int64_t)t * a.K;
     const T *dXp = (const T *)a.dXp, *add = a.add ? (const T *)a.add + (int64_t)t * a.w.d : nullptr;
     T *dx = (T *)a.dx + (int64_t)t * a.w.d;
     if (c < a.w.nvec) {
-        float acc[N];
-#pragma unroll
-        for (int u = 0; u < N; ++u) acc[u] = 0.0f;
+        float acc[N] = {};
         if (add) R::unpack(R::load(add + c * N), acc);
         for (int j0 = 0; j0 < a.K; j0 += G) {
             typename R::V v[G];
@@ -174,8 +173,9 @@ permute_backward_kernel(PermuteBwd a) {
             }
         }
         R::store(dx + c * N, acc);
-    } else {
-        const int e = a.w.nvec * N + (c - a.w.nvec);
+    }
+    if (chunk == (int)a.chunks - 1 && lane_id() < a.w.rest) {
+        const int e = a.w.nvec * N + lane_id();
         float acc = add ? Elem<T>::ld(add + e) : 0.0f;
         for (int j = 0; j < a.K; ++j) {
             const int32_t r = rows[j];
@@ -188,7 +188,7 @@ permute_backward_kernel(PermuteBwd a) {
 }  // namespace
 
 bool route_backward_supported(int T, int d, int act) {
-    const int per = 1024 / (act == R3_BF16 ? 2 : 4);   // elements of 64 vectors; single elements may take 64 pieces more
+    const int per = 1024 / (act == R3_BF16 ? 2 : 4);   // elements of 64 vectors
     return (int64_t)T * (((int64_t)d + per - 1) / per) <= (1 << 25) - 4;
 }
 
@@ -201,7 +201,9 @@ hipError_t launch_combine_backward(int T, int d, int K, int act, const void *dy,
         a.w = width<E>(d);
         by_rows(K, [&](auto g) {
             constexpr int G = decltype(g)::value;
-            if (T >= 4096 || a.w.units <= kWave) combine_backward_kernel<E, G, 1><<<(T + 3) / 4, 256, 0, s>>>(a);
+            // as many waves to a token as its row has vectors for: no wave comes back for more
+            if (a.w.nvec <= kWave) combine_backward_kernel<E, G, 1><<<(T + 3) / 4, 256, 0, s>>>(a);
+            else if (a.w.nvec <= 2 * kWave) combine_backward_kernel<E, G, 2><<<(T + 1) / 2, 256, 0, s>>>(a);
             else combine_backward_kernel<E, G, 4><<<T, 256, 0, s>>>(a);
         });
     };
@@ -213,11 +215,11 @@ hipError_t launch_combine_backward(int T, int d, int K, int act, const void *dy,
 hipError_t launch_permute_backward(int T, int d, int K, int act, const void *dXp, const int32_t *inv_perm, const void *add, void *dx,
                                    hipStream_t s) {
     ProfScope ps(PROF_PERMUTE_BWD, s);
-    PermuteBwd a = {T, K, 0, (int64_t)T * K, {}, dXp, add, inv_perm, dx};
+    PermuteBwd a = {T, K, 1, (int64_t)T * K, {}, dXp, add, inv_perm, dx};
     auto go = [&](auto type) {
         typedef decltype(type) E;
         a.w = width<E>(d);
-        a.chunks = (a.w.units + kWave - 1) / kWave;
+        a.chunks = a.w.nvec > 0 ? (a.w.nvec + kWave - 1) / kWave : 1;
         const unsigned blocks = (unsigned)(((int64_t)T * a.chunks + 3) / 4);
         by_rows(K, [&](auto g) { permute_backward_kernel<E, decltype(g)::value><<<blocks, 256, 0, s>>>(a); });
     };
