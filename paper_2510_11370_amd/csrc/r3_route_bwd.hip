@@ -10,23 +10,22 @@
 namespace r3 {
 namespace {
 
-// A row of d elements: nvec whole vectors, then rest single elements.
+// A row of d elements: nvec whole vectors, then rest single elements.  `once`: the rows are marked as read once (non-temporal).
+// That is for rows of whole vectors (others share their lines: 30000 x 5 of 501 bf16, sums of rows, marked | not, 50 us | 43) and
+// for more of them than half of the 256 MB cache may still hold from whoever wrote them.  marked | not, T x 8 rows of 2048 bf16,
+// 33.5 MB for 1024 tokens: combine's gradient T = 1024 14.7 | 13.0 us, 3000 40.0 | 32.7, 4096 52.1 | 51.0, 8192 98.1 | 105.5;
+// permute's 3000 20.6 | 17.9, 4096 27.1 | 26.4, 6000 39.4 | 45.2, 16000 100 | 117.
 struct Width {
     int d, nvec, rest;
+    bool once;
 };
-template <typename T> Width width(int d) {
+template <typename T> Width width(int d, int64_t rows) {
     constexpr int N = Row<T>::kVec;
-    return {d, d / N, d % N};
+    return {d, d / N, d % N, d % N == 0 && rows * d * (int64_t)sizeof(T) > 128 << 20};
 }
-
-template <class F> void by_rows(int K, F f) {   // rows in flight together: all K where K is one of these, else eight
-    switch (K) {
-        case 1: f(std::integral_constant<int, 1>{}); break;
-        case 2: f(std::integral_constant<int, 2>{}); break;
-        case 4: f(std::integral_constant<int, 4>{}); break;
-        case 6: f(std::integral_constant<int, 6>{}); break;
-        default: f(std::integral_constant<int, 8>{});
-    }
+template <bool ONCE, typename T> __device__ __forceinline__ typename Row<T>::V load_row(const T *p) {
+    if constexpr (ONCE) return Row<T>::load_once(p);
+    else return Row<T>::load(p);
 }
 
 struct CombineBwd {
@@ -40,24 +39,29 @@ struct CombineBwd {
     float *dgates, *dz;
 };
 
-// W waves to a token, four waves to a work-group.  dYp may be Yp: an element is read and written by one thread.
-template <typename T, int G, int W>
-__global__ void __launch_bounds__(256)
+// W waves to the columns of a token's rows, a vector of 16 bytes to a lane at a time, times P waves to its slots, G slots at a
+// time.  Two rows a wave and two waves to the slots: with more rows in one wave the loads and stores of fewer, longer waves move
+// less (65536 x 8 of 2048 bf16, 8 x 1 | 4 x 2 | 2 x 4 | 2 x 2: 898 | 884 | 886 | 882 us; 30000 x 6 of 1000 178 | 176 | 173 | 172;
+// 30000 x 5 of 501 103 | 105 | 97 | 92; 30000 x 4 of 1024 f32 204 | 217 | 226 | 183), and the dot products of a token meet once,
+// in LDS.  dYp may be Yp: an element is read and written by one thread.
+template <typename T, int G, int W, int P, bool ONCE>
+__global__ void __launch_bounds__(W * P > 4 ? W * P * kWave : 256)
 combine_backward_kernel(CombineBwd a) {
     typedef Row<T> R;
     constexpr int N = R::kVec;
-    constexpr int kTok = 4 / W;   // tokens of a work-group
-    __shared__ float part[4][kMaxK];
+    constexpr int kTok = W * P < 4 ? 4 / (W * P) : 1;   // tokens of a work-group
+    __shared__ float part[kTok * W * P][kMaxK];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
-    const int t = blockIdx.x * kTok + wave / W;
+    const int t = blockIdx.x * kTok + wave / (W * P);
     const bool some = t < a.T;   // (waves of the last work-group may have no token, and still meet the others)
-    if (W == 1 && !some) return;
+    if (W * P == 1 && !some) return;
+    const int first_slot = wave / W % P * G, first = wave % W * kWave + lane;
     const T *dy = (const T *)a.dy + (int64_t)t * a.w.d;
     const int32_t *rows = a.inv_perm + (int64_t)t * a.K;
     const float *gates = a.gates + (int64_t)t * a.K;
     const bool dots = a.Yp != nullptr;
     float mine = 0.0f;   // lane j: the dot product of slot j over this wave's columns
-    for (int j0 = some ? 0 : a.K; j0 < a.K; j0 += G) {
+    for (int j0 = some ? first_slot : a.K; j0 < a.K; j0 += G * P) {
         int64_t at[G];
         float g[G], dot[G];
         bool in[G];
@@ -69,14 +73,13 @@ combine_backward_kernel(CombineBwd a) {
             g[j] = j0 + j < a.K ? gates[j0 + j] : 0.0f;
             dot[j] = 0.0f;
         }
-        const int first = W > 1 ? (int)threadIdx.x % (W * kWave) : lane;
         for (int c = first; c < a.w.nvec; c += W * kWave) {
             float x[N];
             typename R::V v[G];
             R::unpack(R::load(dy + c * N), x);
             if (dots) {
 #pragma unroll
-                for (int j = 0; j < G; ++j) v[j] = R::load_once((const T *)a.Yp + at[j] + c * N);
+                for (int j = 0; j < G; ++j) v[j] = load_row<ONCE>((const T *)a.Yp + at[j] + c * N);
             }
 #pragma unroll
             for (int j = 0; j < G; ++j) {
@@ -112,13 +115,13 @@ combine_backward_kernel(CombineBwd a) {
         }
     }
     if (!dots) return;
-    if constexpr (W > 1) {
+    if constexpr (W * P > 1) {
         part[wave][lane] = mine;
         __syncthreads();
-        if (wave % W > 0 || !some) return;
+        if (wave % (W * P) > 0 || !some) return;
         mine = 0.0f;
 #pragma unroll
-        for (int i = 0; i < W; ++i) mine += part[wave + i][lane];
+        for (int i = 0; i < W * P; ++i) mine += part[wave + i][lane];
     }
     const float g = lane < a.K ? gates[lane] : 0.0f;
     const float mix = wave_sum(lane < a.K ? g * mine : 0.0f);
@@ -138,8 +141,10 @@ struct PermuteBwd {
     void *dx;
 };
 
-// A wave to 64 vectors of a token's row, the last one of a row to the elements behind them too.  dx may be add.
-template <typename T, int G>
+// A wave to 64 vectors of a token's row, the last one of a row to the elements behind them too.  Two rows at a time: with all
+// K on their way at once 65536 x 8 of 2048 bf16 take 488 us, four at a time 484, two 476; 30000 x 6 of 1000 82 | 82 | 77 (many
+// waves keep enough loads on their way).  dx may be add.
+template <typename T, int G, bool ONCE>
 __global__ void __launch_bounds__(256)
 permute_backward_kernel(PermuteBwd a) {
     typedef Row<T> R;
@@ -160,7 +165,7 @@ permute_backward_kernel(PermuteBwd a) {
             for (int j = 0; j < G; ++j) {
                 const int32_t r = j0 + j < a.K ? rows[j0 + j] : -1;
                 in[j] = r >= 0 && r < a.S;
-                v[j] = R::load_once(dXp + (in[j] ? (int64_t)r * a.w.d : 0) + c * N);
+                v[j] = load_row<ONCE>(dXp + (in[j] ? (int64_t)r * a.w.d : 0) + c * N);
             }
 #pragma unroll
             for (int j = 0; j < G; ++j) {
@@ -198,14 +203,19 @@ hipError_t launch_combine_backward(int T, int d, int K, int act, const void *dy,
     CombineBwd a = {T, K, (int64_t)T * K, {}, dy, dgates || dz ? Yp : nullptr, gates, inv_perm, dYp, dgates, dz};
     auto go = [&](auto type) {
         typedef decltype(type) E;
-        a.w = width<E>(d);
-        by_rows(K, [&](auto g) {
-            constexpr int G = decltype(g)::value;
-            // as many waves to a token as its row has vectors for: no wave comes back for more
-            if (a.w.nvec <= kWave) combine_backward_kernel<E, G, 1><<<(T + 3) / 4, 256, 0, s>>>(a);
-            else if (a.w.nvec <= 2 * kWave) combine_backward_kernel<E, G, 2><<<(T + 1) / 2, 256, 0, s>>>(a);
-            else combine_backward_kernel<E, G, 4><<<T, 256, 0, s>>>(a);
-        });
+        a.w = width<E>(d, a.S);
+        auto launch = [&](auto g, auto w, auto p) {
+            constexpr int G = decltype(g)::value, W = decltype(w)::value, P = decltype(p)::value, kTok = W * P < 4 ? 4 / (W * P) : 1;
+            auto k = a.w.once ? combine_backward_kernel<E, G, W, P, true> : combine_backward_kernel<E, G, W, P, false>;
+            k<<<(T + kTok - 1) / kTok, kTok * W * P * kWave, 0, s>>>(a);
+        };
+        auto by_width = [&](auto g, auto p) {
+            if (a.w.nvec <= kWave) launch(g, std::integral_constant<int, 1>{}, p);
+            else if (a.w.nvec <= 2 * kWave) launch(g, std::integral_constant<int, 2>{}, p);
+            else launch(g, std::integral_constant<int, 4>{}, p);
+        };
+        if (K == 1) by_width(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{});
+        else by_width(std::integral_constant<int, 2>{}, std::integral_constant<int, 2>{});
     };
     if (act == R3_BF16) go(bf16_t{});
     else go(float{});
@@ -218,10 +228,12 @@ hipError_t launch_permute_backward(int T, int d, int K, int act, const void *dXp
     PermuteBwd a = {T, K, 1, (int64_t)T * K, {}, dXp, add, inv_perm, dx};
     auto go = [&](auto type) {
         typedef decltype(type) E;
-        a.w = width<E>(d);
+        a.w = width<E>(d, a.S);
         a.chunks = a.w.nvec > 0 ? (a.w.nvec + kWave - 1) / kWave : 1;
         const unsigned blocks = (unsigned)(((int64_t)T * a.chunks + 3) / 4);
-        by_rows(K, [&](auto g) { permute_backward_kernel<E, decltype(g)::value><<<blocks, 256, 0, s>>>(a); });
+        auto k = K == 1 ? (a.w.once ? permute_backward_kernel<E, 1, true> : permute_backward_kernel<E, 1, false>)
+                        : (a.w.once ? permute_backward_kernel<E, 2, true> : permute_backward_kernel<E, 2, false>);
+        k<<<blocks, 256, 0, s>>>(a);
     };
     if (act == R3_BF16) go(bf16_t{});
     else go(float{});
