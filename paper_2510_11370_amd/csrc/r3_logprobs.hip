@@ -173,12 +173,24 @@ template <int kBuf> __device__ __forceinline__ int rank_of(const key_t *buf, int
     }
     return rank;
 }
-// Of the candidates in buf[0..count) the `top` largest, each to its rank; keys are distinct (0 is none).
+// Of the candidates in buf[0..count) the `top` largest, each to its rank; keys are distinct (0 is none).  NT / 64
+// neighbouring lanes share a candidate's comparisons.
 template <int NT, int kBuf, class F> __device__ __forceinline__ void rank_out(const key_t *buf, int count, int top, int tid, F put) {
-    for (int i = tid; i < count; i += NT) {
+    constexpr int P = NT / kWave;
+    const int share = tid % P;
+    for (int i = tid / P; i < count; i += kWave) {
         const key_t k = buf[i];
-        const int rank = rank_of<kBuf>(buf, count, k);
-        if (rank < top) put(rank, k);
+        int rank = 0;
+        for (int q = share; q < count; q += 4 * P) {
+            key_t v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = buf[min(q + u * P, kBuf - 1)];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) rank += q + u * P < count && v[u] > k;
+        }
+#pragma unroll
+        for (int o = 1; o < P; o <<= 1) rank += __shfl_xor(rank, o, kWave);
+        if (share == 0 && rank < top) put(rank, k);
     }
     for (int i = count + tid; i < top; i += NT) put(i, (key_t)0);
 }
@@ -248,8 +260,23 @@ token_logprobs_kernel(Args a) {
         count_s[slot][0] = count_s[slot][1] = count_s[slot][2] = 0;
     }
     Stat run = no_stat();
-    // U loads of a thread on their way, consumed two at a time and replaced at once
     int j = tid;
+    typename R::V kept[2];   // a short row's (or part's) vectors stay with their threads
+    const bool brief = TOP && nvec <= 2 * NT;
+    if (brief) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            if (j + u * NT < nvec) kept[u] = R::load_once(zv + (int64_t)(j + u * NT) * N);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            if (j + u * NT < nvec) {
+                float f[N];
+                R::unpack(kept[u], f);
+                take<ENT, TOP>(run, f, a.c, a.span, 0);
+            }
+        j = nvec;
+    }
+    // U loads of a thread on their way, consumed two at a time and replaced at once
     if (j + (U - 1) * NT < nvec) {
         typename R::V v[U];
 #pragma unroll
@@ -279,8 +306,10 @@ token_logprobs_kernel(Args a) {
         R::unpack(R::load_once(zv + (int64_t)j * N), f);
         take<ENT, TOP>(run, f, a.c, a.span, 4 * j + kOne);
     }
+    float odd = -INFINITY;
     if (tid < nloose) {
-        const float f[1] = {Elem<T>::ld(zp + loose(tid))};
+        odd = Elem<T>::ld(zp + loose(tid));
+        const float f[1] = {odd};
         take<ENT, TOP>(run, f, a.c, a.span, 4 * tid + kLoose);
     }
 
@@ -304,7 +333,7 @@ token_logprobs_kernel(Args a) {
     key_t *buf = buf_s[TOP ? slot : 0];
     if (search) {
         thr = reached_by(top64, a.top);
-        if (mine >= thr && mine > -INFINITY) {   // from below: threads read as a whole; from above: those of one piece
+        if (!brief && mine >= thr && mine > -INFINITY) {   // from below: threads read as a whole; from above: those of one piece
             if (run.m2 >= thr && run.m2 > -INFINITY) sel[atomicAdd(&count_s[slot][0], 1)] = tid;
             else sel[NT - 1 - atomicAdd(&count_s[slot][2], 1)] = run.where;
         }
@@ -346,12 +375,25 @@ token_logprobs_kernel(Args a) {
             return;
         }
         const int nsel = count_s[slot][0], none = count_s[slot][2];
+        // an element that reaches the bound is a candidate (few are: compacting a wave's with ballots costs more than their atomics,
+        // 64 x 151936 with 32 alternatives 19.6 us | 14.8)
         auto offer = [&](float x, int place) {
             if (x >= thr && x > -INFINITY) {
                 const int at = atomicAdd(&count_s[slot][1], 1);
                 if (at < kBuf) buf[at] = make_key(x, lo + place);
             }
         };
+        if (brief && mine >= thr) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (tid + h * NT < nvec) {
+                    float f[N];
+                    R::unpack(kept[h], f);
+#pragma unroll
+                    for (int u = 0; u < N; ++u) offer(f[u], head + (tid + h * NT) * N + u);
+                }
+            if (tid < nloose) offer(odd, loose(tid));
+        }
         // the pieces' vectors and all of the other threads', dealt to all threads, two in flight
         const int per = (nvec + NT - 1) / NT, all = 2 * none + nsel * per;
         auto vector_of = [&](int p) {   // (nvec: none)
@@ -424,13 +466,20 @@ token_logprobs_kernel(Args a) {
 template <typename T>
 __global__ void __launch_bounds__(256)
 token_logprobs_join_kernel(Args a) {
-    __shared__ key_t buf[kMaxSplit * kMaxTop], head_s[kWave];
+    constexpr int kKeys = kMaxSplit * kMaxTop, kPer = kKeys / 256;
+    __shared__ key_t key_s[kKeys], buf[kKeys];
     __shared__ int count_s;
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, lane = lane_id();
     const int t = a.target ? a.target[row] : 0;
     Part st = {-INFINITY, 0.0f, 0.0f};
     if (lane < a.nsplit) st = a.part[row * a.nsplit + lane];
+    // all keys of the row's parts, in registers and in LDS
+    const key_t *keys = a.part_keys + row * a.nsplit * a.top;
+    const int n = a.nsplit * a.top;
+    key_t k[kPer];
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) k[u] = tid + u * 256 < n ? keys[tid + u * 256] : 0;
     if (t < 0 || t >= a.V) {
         put_left_out(a, row, t, tid);
         return;
@@ -439,38 +488,27 @@ token_logprobs_join_kernel(Args a) {
     const float m = wave_max_nan(st.m);
     const float d = fmaxf((st.m - m) * a.c, -kFar), f = __builtin_amdgcn_exp2f(d);
     st = {m, wave_sum(st.s * f), wave_sum(fmaf(st.s, d, st.q) * f)};
-    if (tid == 0) put_row(a, row, st, zt);
-    if (a.top == 0) return;
-    if (!(m > -INFINITY && m < INFINITY)) {
+    if (a.top == 0 || !(m > -INFINITY && m < INFINITY)) {
+        if (tid == 0) put_row(a, row, st, zt);
         put_no_top(a, row, tid, m == -INFINITY ? -INFINITY : __uint_as_float(0x7fc00000u));
         return;
     }
-    // each part's keys come in descending order: the k-th largest of the 64 first ones over all parts bounds the k-th
-    // largest of all
-    const key_t *keys = a.part_keys + row * a.nsplit * a.top;
-    const int n = a.nsplit * a.top;
-    if (tid == 0) count_s = 0;
-    if (tid < kWave) {
-        const int p = tid % a.nsplit, at = tid / a.nsplit;
-        head_s[tid] = at < a.top ? keys[p * a.top + at] : 0;
-    }
-    __syncthreads();
-    const key_t mine = head_s[lane];
-    int above = 0;
-    for (int i = 0; i < kWave; ++i) above += head_s[i] > mine;
-    key_t thr = above < a.top ? mine : ~0ull;
 #pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) {
-        const key_t other = __shfl_xor(thr, o, kWave);
-        thr = other < thr ? other : thr;
-    }
-    for (int i = tid; i < n; i += 256) {
-        const key_t k = keys[i];
-        if (k && k >= thr) buf[atomicAdd(&count_s, 1)] = k;
-    }
+    for (int u = 0; u < kPer; ++u)
+        if (tid + u * 256 < n) key_s[tid + u * 256] = k[u];
+    if (tid == 0) count_s = 0;
+    __syncthreads();
+    // each part's keys come in descending order: what a.top of the 64 first ones over all parts reach bounds the row's
+    const int p = lane % a.nsplit, at = lane / a.nsplit;
+    const key_t first = at < a.top ? key_s[p * a.top + at] : 0;
+    const float thr = reached_by(first ? key_logit(first) : -INFINITY, a.top);
+#pragma unroll
+    for (int u = 0; u < kPer; ++u)
+        if (k[u] && key_logit(k[u]) >= thr) buf[atomicAdd(&count_s, 1)] = k[u];
     __syncthreads();
     const float ls = logf(st.s);
-    rank_out<256, kMaxSplit * kMaxTop>(buf, count_s, a.top, tid, [&](int rank, key_t k) { put_top(a, row, rank, k, m, ls); });
+    rank_out<256, kKeys>(buf, count_s, a.top, tid, [&](int rank, key_t key) { put_top(a, row, rank, key, m, ls); });
+    if (tid == 0) put_row(a, row, st, zt);
 }
 
 constexpr int kGradLoads = 2;
@@ -563,13 +601,14 @@ token_logprobs_backward_kernel(BackArgs g) {
 }
 
 // How a call cuts its rows.
+constexpr int kPartLeast = 4096;
 struct Plan {
     int nsplit, seg;
 };
 Plan plan(int64_t n, int64_t V) {
-    const int64_t least = 4096, want = n > 0 ? 1024 / n : 1;
-    int64_t k = std::min<int64_t>(std::min<int64_t>(want, kMaxSplit), V / least);
-    if (k <= 1) return {1, (int)V};
+    const int64_t most = (V + kPartLeast - 1) / kPartLeast;
+    const int64_t k = std::min(std::min<int64_t>(n > 0 ? 1024 / n : 1, kMaxSplit), most);
+    if (k <= 1 || V < 2 * kPartLeast) return {1, (int)V};
     const int64_t seg = ((V + k - 1) / k + 7) / 8 * 8;
     return {(int)((V + seg - 1) / seg), (int)seg};
 }
