@@ -601,8 +601,9 @@ token_logprobs_backward_kernel(BackArgs g) {
 }
 
 // How a call cuts its rows: up to 512 work-groups in all, parts of 4096 elements at least (smaller ones do not shorten the
-// chain of latencies that is left), and only rows long enough to pay for the join (about 4 us with its launch; a row of 10000
-// bf16 logits 8.9 us whole, 12 cut).  512 | 1024 work-groups, 151936 bf16 logits with 20 alternatives: 64 rows 13.5 | 14.0 us,
+// chain of latencies that is left), and only rows long enough to pay for the join and its launch: whole | cut, 64 rows of
+// 20000 bf16 logits 9.0 | 11.1 us, of 50257 f32 8.5 | 10.2, of 72000 11.1 | 11.7 and 11.4 | 10.2, of 151936 16.4 | 13.1 and
+// 18.8 | 11.5.  512 | 1024 work-groups, 151936 bf16 logits with 20 alternatives: 64 rows 13.5 | 14.0 us,
 // 256 rows 21.2 | 22.5, 400 rows 24.1 | 32.3, 512 rows 29.7 | 35.0; 2048: 19.6, 28.4, 33.2, 38.9.
 struct Plan {
     int nsplit, seg;
@@ -610,7 +611,7 @@ struct Plan {
 Plan plan(int64_t n, int64_t V) {
     constexpr int64_t kPart = 4096, kGroups = 512;
     const int64_t k = std::min(std::min<int64_t>(kGroups / n, kMaxSplit), (V + kPart - 1) / kPart);
-    if (k <= 1 || V < 4 * kPart) return {1, (int)V};
+    if (k <= 1 || V < 16 * kPart) return {1, (int)V};
     const int64_t seg = ((V + k - 1) / k + 7) / 8 * 8;
     return {(int)((V + seg - 1) / seg), (int)seg};
 }
