@@ -3,6 +3,7 @@
 //   dz_v = s ([v = t] dlogp - p_v (dlogp + dH (log p_v + H)))
 // Both read the logits once (and the gradient writes once): HBM-bound.
 #include <algorithm>
+#include <cfloat>
 
 #include "r3_kernels.h"
 #include "r3_vec.h"
@@ -332,9 +333,9 @@ token_logprobs_kernel(Args a) {
     int *sel = sel_s[TOP ? slot : 0];
     key_t *buf = buf_s[TOP ? slot : 0];
     if (search) {
-        thr = reached_by(top64, a.top);
-        if (!brief && mine >= thr && mine > -INFINITY) {   // from below: threads read as a whole; from above: those of one piece
-            if (run.m2 >= thr && run.m2 > -INFINITY) sel[atomicAdd(&count_s[slot][0], 1)] = tid;
+        thr = fmaxf(reached_by(top64, a.top), -FLT_MAX);   // (-inf is never a candidate)
+        if (!brief && mine >= thr) {   // from below: threads read as a whole; from above: those of one piece
+            if (run.m2 >= thr) sel[atomicAdd(&count_s[slot][0], 1)] = tid;
             else sel[NT - 1 - atomicAdd(&count_s[slot][2], 1)] = run.where;
         }
     }
@@ -378,7 +379,7 @@ token_logprobs_kernel(Args a) {
         // an element that reaches the bound is a candidate (few are: compacting a wave's with ballots costs more than their atomics,
         // 64 x 151936 with 32 alternatives 19.6 us | 14.8)
         auto offer = [&](float x, int place) {
-            if (x >= thr && x > -INFINITY) {
+            if (x >= thr) {
                 const int at = atomicAdd(&count_s[slot][1], 1);
                 if (at < kBuf) buf[at] = make_key(x, lo + place);
             }
