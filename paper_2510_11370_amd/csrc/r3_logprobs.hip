@@ -178,6 +178,18 @@ template <int kBuf> __device__ __forceinline__ int rank_of(const key_t *buf, int
 // neighbouring lanes share a candidate's comparisons.
 template <int NT, int kBuf, class F> __device__ __forceinline__ void rank_out(const key_t *buf, int count, int top, int tid, F put) {
     constexpr int P = NT / kWave;
+    if (P == 1 && count <= kWave) {   // a key to a lane (32000 rows of 1000 with 20 alternatives 41.8 -> 39.3 us)
+        const key_t k = tid < count ? buf[tid] : 0;
+        const int lo = (int)k, hi = (int)(k >> 32);
+        int rank = 0;
+        for (int q = 0; q < count; ++q) {
+            const key_t other = (key_t)(uint32_t)__builtin_amdgcn_readlane(hi, q) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, q);
+            rank += other > k;
+        }
+        if (tid < count && rank < top) put(rank, k);
+        if (tid >= count && tid < top) put(tid, (key_t)0);
+        return;
+    }
     const int share = tid % P;
     for (int i = tid / P; i < count; i += kWave) {
         const key_t k = buf[i];
@@ -214,9 +226,18 @@ __device__ __forceinline__ float reached_by(float v, int k) {
 //
 // Alternatives: a thread knows the maximum of its own elements anyway.  The 64 maxima over the threads of one lane number
 // are 64 elements of the row, so the k-th largest of them has k elements at or above it: a bound from below for the k-th
-// largest element, met by some 64 ln(64 / (64 - k)) elements of a row in random order (24 for k = 20).  A thread whose maximum reaches
-// it has that piece read again, and all of its elements if another of its pieces reaches it too.  Rows that keep more candidates than fit (many equal
-// values) are gone through once more in order with the k-th best so far as the bound.
+// largest element, met by some 64 ln(64 / (64 - k)) elements of a row in random order (24 for k = 20).  A thread whose maximum
+// reaches it has that piece read again, and all of its elements if another of its pieces reaches it too (all elements of all such
+// threads, a line of memory each, made 4096 x 151936 with 20 alternatives 204 us instead of 159).  Rows that keep more
+// candidates than fit (many equal values) are gone through once more in order with the k-th best so far as the bound.
+//
+// Bound by HBM: 16384 x 151936 bf16 725 us, 6.9 TB/s where a kernel that only reads reaches 7.1 (non-temporal loads; ordinary
+// ones 6.3), with the vector pipe about three quarters busy: 8.5 issue slots an element, four of them the exponential.  With
+// the maximum as the reference of every sum, as it changes, and guarded exponents it was 11 slots and 825 us.
+// Threads to a row: 64 up to 4096 logits (32768 x 4000 bf16 50 us, x 1000 19), 256 up to 64 KB a row, 128 KB with alternatives, whose
+// search keeps the others waiting (256 | 512: 4096 x 50257 bf16 71 | 67 us, with 20 alternatives 77 | 85; 8192 x 32000 86 | 89;
+// 16384 x 10000 56 | 88), 512 beyond (1024: 4096 x 151936 with alternatives 232 us | 159).  Loads on their way: four a thread,
+// two where alternatives need the registers (4 | 2: 256 x 151936 with 20 28.4 us | 24.9).
 template <typename T, int NT, bool ENT, bool TOP>
 __global__ void __launch_bounds__(NT < 256 ? 256 : NT)
 token_logprobs_kernel(Args a) {
@@ -237,13 +258,13 @@ token_logprobs_kernel(Args a) {
             __builtin_amdgcn_wave_barrier();
         }
     };
-    const int64_t item = a.row0 * a.nsplit + (int64_t)blockIdx.x * kRows + slot;
-    const int64_t row = item / a.nsplit;
-    const int split = (int)(item - row * a.nsplit);
+    const uint32_t nth = blockIdx.x * kRows + slot, nth_row = a.nsplit == 1 ? nth : nth / (uint32_t)a.nsplit;
+    const int split = nth - nth_row * a.nsplit;
+    const int64_t row = a.row0 + nth_row, item = row * a.nsplit + split;
     if (row >= a.n) return;
     const int t = a.target ? a.target[row] : 0;
     // Short rows and few long ones wait for latencies: there the target is not waited for, and a row left out is found to
-    // be one at the end.
+    // be one at the end (32768 x 1000 27 -> 20 us).
     const bool left_out = t < 0 || t >= a.V, late = W == 1 || a.nsplit > 1;
     if (left_out && !late) {
         put_left_out(a, row, t, tid);
@@ -257,9 +278,7 @@ token_logprobs_kernel(Args a) {
     const int nloose = head + len - rest;
     const T *zv = zp + head;
     auto loose = [&](int i) { return i < head ? i : rest + i - head; };
-    if (tid == 0) {
-        count_s[slot][0] = count_s[slot][1] = count_s[slot][2] = 0;
-    }
+    if (tid == 0) count_s[slot][0] = count_s[slot][1] = count_s[slot][2] = 0;
     Stat run = no_stat();
     int j = tid;
     typename R::V kept[2];   // a short row's (or part's) vectors stay with their threads
@@ -512,7 +531,7 @@ token_logprobs_join_kernel(Args a) {
     if (tid == 0) put_row(a, row, st, zt);
 }
 
-constexpr int kGradLoads = 2;
+constexpr int kGradLoads = 2;   // of 16 bytes, a thread's
 struct BackArgs {
     int64_t row0, ld, ldd;
     int V, nseg, seg;
@@ -564,15 +583,14 @@ token_logprobs_backward_kernel(BackArgs g) {
     const int nloose = head + len - rest, atv = at - head;
     const T *zv = z + head;
     T *dv = dz + head;
-    constexpr int U = kGradLoads;
     int j = threadIdx.x;
     if (live) {
-        for (; j + (U - 1) * NT < nvec; j += U * NT) {
-            typename R::V v[U];
+        for (; j + (kGradLoads - 1) * NT < nvec; j += kGradLoads * NT) {
+            typename R::V v[kGradLoads];
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = R::load(zv + (int64_t)(j + u * NT) * N);
+            for (int u = 0; u < kGradLoads; ++u) v[u] = R::load(zv + (int64_t)(j + u * NT) * N);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < kGradLoads; ++u) {
                 float f[N];
                 R::unpack(v[u], f);
 #pragma unroll

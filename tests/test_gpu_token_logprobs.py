@@ -351,3 +351,61 @@ def test_offsets_past_32_bits():
     dl = np.array([1.0, -1.0, 0.5])
     r3.token_logprobs_backward(z, t.to(DEV), st, z, dlogp=torch.tensor(dl, dtype=torch.float32, device=DEV))
     _check_grad(z.cpu().double().numpy(), full, V, t, 1.0, dl, None, torch.bfloat16)
+
+
+def test_two_calls_at_once_on_two_streams():
+    n, V, top = 6, 151936, 20
+    st = []
+    for k in range(2):
+        full, t = _logits(n, V, torch.bfloat16, seed=20 + k)
+        st.append(dict(want=ref.token_logprobs(_np(full), t.numpy(), 1.0, top), z=full.to(DEV), t=t.to(DEV), lp=torch.empty(n, device=DEV),
+                       tl=torch.empty(n, top, device=DEV), ti=torch.empty(n, top, dtype=torch.int32, device=DEV),
+                       ws=r3.token_logprobs_workspace(n, V, top), s=torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s in st:
+            with torch.cuda.stream(s["s"]):
+                r3.token_logprobs(s["z"], s["t"], s["lp"], top_logp=s["tl"], top_id=s["ti"], ws=s["ws"])
+    torch.cuda.synchronize()
+    for s in st:
+        _check({"logp": s["lp"].cpu().double().numpy(), "top_logp": s["tl"].cpu().double().numpy(), "top_id": s["ti"].cpu().numpy()},
+               s["want"])
+
+
+def test_gradient_of_the_entropy_without_targets():
+    n, V = 5, 3000
+    full, _ = _logits(n, V, torch.float32, seed=23)
+    dh = np.linspace(-0.5, 1.0, n)
+    got = _backward(full, V, None, torch.float32, None, dh)
+    _check_grad(got, full, V, None, 1.0, None, dh, torch.float32)
+
+
+def test_the_launch_timers_see_the_calls():
+    full, t = _logits(3, 200, torch.float32, seed=24)
+    z, tg, st, lp = full.to(DEV), t.to(DEV), torch.empty(3, 2, device=DEV), torch.ones(3, device=DEV)
+    r3.profile_enable(True)
+    r3.token_logprobs(z, tg, stats=st)
+    r3.token_logprobs_backward(z, tg, st, z, dlogp=lp)
+    D = r3.desc(4, 8, 8, 2, 16, "f32")
+    rows, tok, gates, inv = torch.ones(8, 8, device=DEV), torch.ones(4, 8, device=DEV), torch.ones(4, 2, device=DEV), torch.arange(8, dtype=torch.int32, device=DEV)
+    r3.combine_backward(D, tok, rows, gates, inv, dYp=rows)
+    r3.permute_backward(D, rows, inv, tok)
+    torch.cuda.synchronize()
+    prof = r3.profile_read()
+    r3.profile_enable(False)
+    assert {k: v[1] for k, v in prof.items()} == {"token_logprobs": 1, "token_logprobs_backward": 1, "combine_backward": 1, "permute_backward": 1}
+
+
+def test_a_workspace_that_is_too_small_is_refused():
+    z, lp = torch.zeros(1, 151936, device=DEV), torch.empty(1, device=DEV)
+    t = torch.zeros(1, dtype=torch.int32, device=DEV)
+    need = r3.lib().r3_token_logprobs_workspace_bytes(1, 151936, 0)
+    with pytest.raises(r3.R3Error, match="WORKSPACE"):
+        r3.token_logprobs(z, t, lp, ws=torch.empty(need - 256, dtype=torch.uint8, device=DEV))
+    for bad in (dict(logp=lp.double()), dict(logp=torch.empty(2, device=DEV)), dict(logp=lp.cpu()), dict(ws=torch.empty(need // 4, device=DEV)),
+                dict(top_logp=torch.empty(1, 3, device=DEV), top_id=torch.empty(1, 2, dtype=torch.int32, device=DEV)),
+                dict(top_id=torch.empty(1, 4, dtype=torch.int32, device=DEV)[:, ::2], top_logp=torch.empty(1, 4, device=DEV)[:, ::2])):
+        with pytest.raises(r3.R3Error):
+            r3.token_logprobs(z, t, **{"logp": lp, **bad})
+    with pytest.raises(r3.R3Error):
+        r3.token_logprobs(z, t.long(), lp)
