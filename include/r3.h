@@ -202,7 +202,7 @@ int r3_combine(const r3_layer_desc *desc, const void *Yp, const float *gates,
  * A row outside [0, T*K) in inv_perm (a bad record) is left out: nothing is
  * read or written for the slot and its dgates is 0.  desc->flags and the
  * record's fields are ignored.  No workspace.  R3_ERR_UNSUPPORTED where
- * T * ceil(d * sizeof(act) / 1024) exceeds 2^25 - 4.
+ * T * ceil(d * sizeof(act) / 1024) exceeds 2^24.
  */
 int r3_combine_backward(const r3_layer_desc *desc, const void *dy, const void *Yp, const float *gates,
                         const int32_t *inv_perm, void *dYp, float *dgates, float *dz, void *stream);

@@ -236,7 +236,9 @@ __device__ __forceinline__ float reached_by(float v, int k) {
 // the maximum as the reference of every sum, as it changes, and guarded exponents it was 11 slots and 825 us.
 // Threads to a row: 64 up to 4096 logits (32768 x 4000 bf16 50 us, x 1000 19), 256 up to 64 KB a row, 128 KB with alternatives, whose
 // search keeps the others waiting (256 | 512: 4096 x 50257 bf16 71 | 67 us, with 20 alternatives 77 | 85; 8192 x 32000 86 | 89;
-// 16384 x 10000 56 | 88), 512 beyond (1024: 4096 x 151936 with alternatives 232 us | 159).  Loads on their way: four a thread,
+// 16384 x 10000 56 | 88), 512 beyond (1024: 4096 x 151936 with alternatives 232 us | 159).  Up to 256 rows that are not cut have a
+// compute unit each: 512 threads from 16 KB on, 1024 from 64 KB (200 rows with 8 alternatives, before | so: 32000 bf16 10.1 | 8.7 us,
+// f32 13.4 | 10.0, 50257 bf16 12.6 | 9.4, f32 13.5 | 11.8).  Loads on their way: four a thread,
 // two where alternatives need the registers (4 | 2: 256 x 151936 with 20 28.4 us | 24.9).
 template <typename T, int NT, bool ENT, bool TOP>
 __global__ void __launch_bounds__(NT < 256 ? 256 : NT)
@@ -671,9 +673,11 @@ hipError_t launch_token_logprobs(int64_t n, int64_t V, int dtype, const void *lo
     };
     auto by_size = [&](auto type) {
         const int64_t bytes = V * (int64_t)sizeof(type);
+        const bool few = n <= 256 && p.nsplit == 1;   // a row has a compute unit to itself
         if (V <= 4096) go(type, std::integral_constant<int, 64>{});
-        else if (bytes <= (top > 0 ? 131072 : 65536)) go(type, std::integral_constant<int, 256>{});
-        else go(type, std::integral_constant<int, 512>{});
+        else if (bytes <= (few ? 16384 : top > 0 ? 131072 : 65536)) go(type, std::integral_constant<int, 256>{});
+        else if (bytes <= 65536 || !few) go(type, std::integral_constant<int, 512>{});
+        else go(type, std::integral_constant<int, 1024>{});
     };
     if (dtype == R3_BF16) by_size(bf16_t{});
     else by_size(float{});

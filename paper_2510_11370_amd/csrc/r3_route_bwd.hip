@@ -194,7 +194,7 @@ permute_backward_kernel(PermuteBwd a) {
 
 bool route_backward_supported(int T, int d, int act) {
     const int per = 1024 / (act == R3_BF16 ? 2 : 4);   // elements of 64 vectors
-    return (int64_t)T * (((int64_t)d + per - 1) / per) <= (1 << 25) - 4;
+    return (int64_t)T * (((int64_t)d + per - 1) / per) <= 1 << 24;   // a token takes 512 threads at most
 }
 
 hipError_t launch_combine_backward(int T, int d, int K, int act, const void *dy, const void *Yp, const float *gates, const int32_t *inv_perm,

@@ -161,7 +161,7 @@ def test_gradients_of_combine_and_permute_refuse():
     for bad in (dict(dXp=None), dict(inv=None), dict(dx=None), dict(add=_off(A[2], 8)), dict(dx=_off(A[3], 2)), dict(dx=A[0]),
                 dict(dx=_off(A[0], rows - 16)), dict(add=_off(A[3], 16))):
         assert pb(**bad) == INVALID, bad
-    wide = r3.desc(1 << 25, 512, 8, 1, 16, "bf16")
+    wide = r3.desc((1 << 24) + 1, 512, 8, 1, 16, "bf16")
     assert cb(D=wide, Yp=None, dg=None, dz=None, dYp=C.c_void_p(1 << 50), dy=C.c_void_p(1 << 55)) == UNSUPPORTED
     assert pb(D=wide, dXp=C.c_void_p(1 << 50), dx=C.c_void_p(1 << 55), add=None) == UNSUPPORTED
 
