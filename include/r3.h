@@ -307,7 +307,7 @@ size_t r3_policy_workspace_bytes(void);
 /*
  * Log-probabilities of given tokens under a row of logits each, with entropy
  * and the most probable alternatives: what the recompute and update stages
- * (Section 5.1) need of the model's head, and r3_policy_discrepancy's input.
+ * need of the model's head, and r3_policy_discrepancy's input.
  * logits: device [n, V], row i at logits + i*ld elements (ld >= V; rows may
  * start at any element), dtype R3_BF16 or R3_F32.  scale = 1 / temperature, in
  * [1e-6, 1e6].  With m = max_v z_v, S = sum_v exp(scale (z_v - m)) and

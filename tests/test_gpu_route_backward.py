@@ -243,3 +243,65 @@ def test_replays_from_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(o, e) for o, e in zip(outs, eager))
+
+
+@pytest.mark.parametrize("T,K,d,act", [(4300, 8, 2048, "bf16"), (4100, 8, 1100, "f32"), (70000, 1, 1024, "bf16")])
+def test_rows_past_the_caches(T, K, d, act):
+    """More than 128 MB of rows: read past the caches.  The reference is 64-bit torch."""
+    g = torch.Generator(device=DEV).manual_seed(T)
+    dt = torch.bfloat16 if act == "bf16" else torch.float32
+    r = lambda *s: torch.randn(*s, generator=g, device=DEV).to(dt)  # noqa: E731
+    dy, Yp, add, gates = r(T, d), r(T * K, d), r(T, d), torch.rand(T, K, generator=g, device=DEV)
+    inv = torch.randperm(T * K, generator=g, device=DEV).int()
+    D = r3.desc(T, d, 8, K, 16, act)
+    dYp, dg, dz, dx = torch.empty_like(Yp), torch.empty(T, K, device=DEV), torch.empty(T, K, device=DEV), torch.empty(T, d, dtype=dt, device=DEV)
+    r3.combine_backward(D, dy, Yp, gates, inv, dYp=dYp, dgates=dg, dz=dz)
+    r3.permute_backward(D, Yp, inv, dx, add=add)
+    row, U, half = inv.view(T, K).long(), 2.0 ** -24, HALF[act]
+    want_dx, size = add.double(), add.double().abs()
+    want_dg, tg = torch.empty(T, K, dtype=torch.float64, device=DEV), torch.empty(T, K, dtype=torch.float64, device=DEV)
+    for j in range(K):
+        y = Yp[row[:, j]].double()
+        want_dx, size = want_dx + y, size + y.abs()
+        v = dy.double() * gates[:, j:j + 1].double()
+        assert ((dYp[row[:, j]].double() - v).abs() <= (half + 2 * U) * v.abs() + 1e-37).all()
+        want_dg[:, j] = (y * dy.double()).sum(1)
+        tg[:, j] = U * (d / 64 + 24) * (y * dy.double()).abs().sum(1)
+    assert ((dg.double() - want_dg).abs() <= tg).all()
+    g64 = gates.double()
+    want_dz = g64 * (want_dg - (g64 * want_dg).sum(1, keepdim=True))
+    tz = g64 * (tg + (g64 * tg).sum(1, keepdim=True) + 12 * U * (g64 * want_dg.abs()).sum(1, keepdim=True) + 3 * U * want_dg.abs()) + 1e-37
+    assert ((dz.double() - want_dz).abs() <= tz).all()
+    t = U * (K + 1) * size
+    assert ((dx.double() - want_dx).abs() <= t + half * (want_dx.abs() + t) + 1e-37).all()
+
+
+def test_more_than_2_31_elements():
+    T, K, d = 132000, 8, 2048                       # 2.16e9 elements of rows, the last ones past 2^31
+    D = r3.desc(T, d, 8, K, 16, "bf16")
+    S = T * K
+    g = torch.Generator(device=DEV).manual_seed(9)
+    inv = torch.randperm(S, generator=g, device=DEV).int()
+    Yp = torch.zeros(S, d, dtype=torch.bfloat16, device=DEV)
+    col = torch.arange(d, device=DEV) % 7
+    Yp[-1000:] = (col - 3).bfloat16()               # small whole numbers: every sum is exact
+    Yp[:1000] = (col % 3).bfloat16()
+    dy = torch.zeros(T, d, dtype=torch.bfloat16, device=DEV)
+    dy[:] = (torch.arange(T, device=DEV) % 5 - 2).bfloat16()[:, None]
+    gates = torch.full((T, K), 0.5, device=DEV)
+    dYp, dg, dx = torch.empty_like(Yp), torch.empty(T, K, device=DEV), torch.empty_like(dy)
+    r3.combine_backward(D, dy, Yp, gates, inv, dYp=dYp, dgates=dg)
+    r3.permute_backward(D, Yp, inv, dx)
+    tok = torch.empty(S, dtype=torch.long, device=DEV)
+    tok[inv.long()] = torch.arange(S, device=DEV) // K
+    for rows in (slice(0, 1000), slice(S // 2, S // 2 + 1000), slice(S - 1000, S)):
+        assert torch.equal(dYp[rows], 0.5 * dy[tok[rows]])
+        slot = torch.full((S,), -1, dtype=torch.long, device=DEV)
+        slot[inv.long()] = torch.arange(S, device=DEV)
+        want = (Yp[rows].float().sum(1) * dy[tok[rows], 0].float())
+        assert torch.equal(dg.view(-1)[slot[rows]], want)
+    some = tok[S - 1000:].unique()
+    want = torch.zeros(len(some), d, device=DEV)
+    for j in range(K):
+        want += Yp[inv.view(T, K)[some, j].long()].float()
+    assert torch.equal(dx[some].float(), want)

@@ -69,7 +69,8 @@ def _check(got, want, what=""):
 @pytest.mark.parametrize("n,V,top,pad,scale", [
     (1, 1, 1, 0, 1.0), (3, 7, 5, 0, 1.0), (2, 64, 32, 1, 0.5), (5, 20, 32, 0, 1.0), (9, 513, 20, 3, 1.7), (7, 4096, 32, 0, 1.0),
     (4, 4097, 20, 0, 1.0), (1300, 300, 1, 5, 1.0), (1030, 5000, 3, 0, 1 / 0.6), (3, 32769, 20, 7, 1.0), (40, 9001, 8, 0, 1.0),
-    (64, 50257, 8, 0, 1 / 0.6), (1, 151936, 20, 0, 1.0), (2, 262147, 32, 0, 1.0), (600, 40009, 5, 2, 1.0)])
+    (64, 50257, 8, 0, 1 / 0.6), (1, 151936, 20, 0, 1.0), (2, 262147, 32, 0, 1.0), (600, 40009, 5, 2, 1.0),
+    (256, 65536, 5, 0, 1.0), (257, 65536, 5, 0, 1.0), (37, 65537, 32, 3, 0.7), (4, 65535, 32, 1, 1.0)])
 def test_against_64_bits(n, V, top, pad, scale, dtype):
     full, t = _logits(n, V, dtype, pad, seed=n + V)
     got, status, _ = _run(full, V, t, top, scale)
@@ -79,7 +80,7 @@ def test_against_64_bits(n, V, top, pad, scale, dtype):
 
 @pytest.mark.parametrize("want,top,target", [(("logp",), 0, True), (("entropy",), 0, False), (("stats",), 0, True), ((), 4, False),
                                              (("logp", "stats"), 4, True)])
-@pytest.mark.parametrize("n,V", [(5, 700), (3, 20001)])
+@pytest.mark.parametrize("n,V", [(5, 700), (3, 20001), (3, 70001)])
 def test_outputs_that_are_not_wanted(n, V, want, top, target):
     full, t = _logits(n, V, torch.bfloat16, seed=3)
     got, _, _ = _run(full, V, t if target else None, top, want=want)
@@ -125,7 +126,7 @@ def _special(V):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("V,copies", [(5, 1), (900, 1), (4097, 60), (6001, 1), (50257, 1), (50257, 50), (151936, 50)])
+@pytest.mark.parametrize("V,copies", [(5, 1), (900, 1), (4097, 60), (6001, 1), (50257, 1), (50257, 50), (151936, 1), (151936, 50)])
 def test_rows_where_something_can_go_wrong(V, copies, dtype):
     """copies: other rows beside them, so that rows are not cut."""
     rows = _special(V)
@@ -147,7 +148,7 @@ def test_rows_where_something_can_go_wrong(V, copies, dtype):
 
 
 def test_rows_left_out_are_not_read():
-    for n, V in ((40, 1000), (9, 30011), (1200, 300)):
+    for n, V in ((40, 1000), (9, 30011), (1200, 300), (9, 70001), (300, 70001)):
         full, t = _logits(n, V, torch.bfloat16, seed=5)
         t[::3] = -1
         full[::3] = math.nan
@@ -162,11 +163,13 @@ def test_rows_left_out_are_not_read():
 
 
 def test_the_same_bits_twice_and_no_rows():
-    full, t = _logits(30, 50257, torch.bfloat16, seed=6)
-    a, _, _ = _run(full, 50257, t, 20)
-    b, _, _ = _run(full, 50257, t, 20)
-    for k in a:
-        assert np.array_equal(a[k], b[k]), k
+    for n, V in ((30, 50257), (30, 80009), (600, 50257)):
+        full, t = _logits(n, V, torch.bfloat16, seed=6)
+        a, _, _ = _run(full, V, t, 20)
+        b, _, _ = _run(full, V, t, 20)
+        for k in a:
+            assert np.array_equal(a[k], b[k]), (n, V, k)
+    full = full[:, :50257]
     got, status, _ = _run(full[:0], 50257, t[:0], 4)
     assert status == 0 and got["logp"].shape == (0,)
     r3.token_logprobs_backward(full[:0].to(DEV), t[:0].to(DEV), torch.empty(0, 2, device=DEV), full[:0].to(DEV),
@@ -282,11 +285,11 @@ def test_on_another_stream():
 def test_two_graphs_that_share_a_workspace():
     """A decode step's call on cut rows and a training step's forward and gradient, each captured, replayed in turn with
     eager work between."""
-    V = 40009
+    V = 70001
     fa, ta = _logits(3, V, torch.bfloat16, seed=15)
     fb, tb = _logits(5, V, torch.bfloat16, seed=16)
-    ws = r3.token_logprobs_workspace(5, V, 16)
     need = max(r3.lib().r3_token_logprobs_workspace_bytes(k, V, 16) for k in (3, 5))
+    assert need > 0
     ws = torch.empty(need, dtype=torch.uint8, device=DEV)
     st = []
     for f, t in ((fa, ta), (fb, tb)):
@@ -351,6 +354,26 @@ def test_offsets_past_32_bits():
     dl = np.array([1.0, -1.0, 0.5])
     r3.token_logprobs_backward(z, t.to(DEV), st, z, dlogp=torch.tensor(dl, dtype=torch.float32, device=DEV))
     _check_grad(z.cpu().double().numpy(), full, V, t, 1.0, dl, None, torch.bfloat16)
+
+
+def test_more_rows_than_one_launch_takes():
+    n, V = (1 << 22) + 5, 3
+    g = torch.Generator(device=DEV).manual_seed(18)
+    z = torch.randn(n, V, generator=g, device=DEV)
+    t = torch.randint(-1, V, (n,), generator=g, device=DEV, dtype=torch.int32)
+    lp, st, ti, tl = torch.empty(n, device=DEV), torch.empty(n, 2, device=DEV), torch.empty(n, 1, dtype=torch.int32, device=DEV), torch.empty(n, 1, device=DEV)
+    r3.token_logprobs(z, t, lp, stats=st, top_logp=tl, top_id=ti)
+    p = torch.log_softmax(z.double(), 1)
+    live = t >= 0
+    at = t.clamp(min=0).long()[:, None]
+    # three exponentials: a dozen roundings of values below 16
+    assert (lp.double() - p.gather(1, at)[:, 0])[live].abs().max() < 16 * 12 * 2.0 ** -24 and (lp[~live] == 0).all()
+    assert torch.equal(ti[live, 0].long(), z.argmax(1)[live]) and (ti[~live] == -1).all()
+    dl = torch.randn(n, generator=g, device=DEV)
+    dz = torch.empty_like(z)
+    r3.token_logprobs_backward(z, t, st, dz, dlogp=dl)
+    want = dl.double()[:, None] * (torch.zeros_like(p).scatter_(1, at, 1.0) - p.exp())
+    assert (dz.double() - want)[live].abs().max() < dl.abs().max().item() * 16 * 2.0 ** -24 and (dz[~live] == 0).all()
 
 
 def test_two_calls_at_once_on_two_streams():
