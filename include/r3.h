@@ -199,6 +199,7 @@ int r3_combine(const r3_layer_desc *desc, const void *Yp, const float *gates,
  * NULL; add is for what else reaches x (the router's dz W_r^T, a residual), and
  * may be dx itself (not a part of it).
  *
+ * A token's results are the same bits whatever other tokens the call has.
  * A row outside [0, T*K) in inv_perm (a bad record) is left out: nothing is
  * read or written for the slot and its dgates is 0.  desc->flags and the
  * record's fields are ignored.  No workspace.  R3_ERR_UNSUPPORTED where
@@ -326,9 +327,11 @@ size_t r3_policy_workspace_bytes(void);
  * ordinary logit.  A row of nothing but -inf: logp -inf, entropy 0, stats
  * {-inf, 0}.  A NaN or +inf in a row sets R3_DATA_NONFINITE and makes its
  * floating outputs NaN and its ids -1.
- * Sums are f32.  Few long rows are cut over several work-groups and joined by
- * a second launch; a row's last bits can depend on how it is cut, that is on n
- * and V.
+ * Sums are f32.  With more than 256 rows, and for V <= 4096, a row's results are
+ * the same bits whatever other rows the call has (and wherever in a 16-byte
+ * unit it starts the same).  Fewer, longer rows get more threads and, from
+ * V = 65536 on, are cut over several work-groups and joined by a second launch:
+ * their last bits can depend on n.
  * top <= R3_MAX_TOP; 0: top_logp and top_id are not read.  n = 0 is a no-op.
  * ws: device workspace of r3_token_logprobs_workspace_bytes(n, V, top) (0 is
  * possible; then ws may be NULL).

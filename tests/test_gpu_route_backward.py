@@ -305,3 +305,23 @@ def test_more_than_2_31_elements():
     for j in range(K):
         want += Yp[inv.view(T, K)[some, j].long()].float()
     assert torch.equal(dx[some].float(), want)
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+def test_a_token_has_the_same_bits_in_another_batch(act):
+    T, K, d, n = 5000, 4, 4096, 7                   # many: rows past the caches
+    g = torch.Generator(device=DEV).manual_seed(3)
+    dt = torch.bfloat16 if act == "bf16" else torch.float32
+    r = lambda *s: torch.randn(*s, generator=g, device=DEV).to(dt)  # noqa: E731
+    dy, Yp, add, gates = r(T, d), r(T * K, d), r(T, d), torch.rand(T, K, generator=g, device=DEV)
+    out = []
+    for k in (T, n):
+        D = r3.desc(k, d, 8, K, 16, act)
+        inv = torch.arange(k * K, device=DEV, dtype=torch.int32)
+        dYp, dg, dz = torch.empty(k * K, d, dtype=dt, device=DEV), torch.empty(k, K, device=DEV), torch.empty(k, K, device=DEV)
+        dx = torch.empty(k, d, dtype=dt, device=DEV)
+        r3.combine_backward(D, dy[:k], Yp[:k * K], gates[:k], inv, dYp=dYp, dgates=dg, dz=dz)
+        r3.permute_backward(D, Yp[:k * K], inv, dx, add=add[:k])
+        out.append((dYp[:n * K], dg[:n], dz[:n], dx[:n]))
+    for a, b in zip(*out):
+        assert torch.equal(a, b)

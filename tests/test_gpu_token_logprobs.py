@@ -356,6 +356,16 @@ def test_offsets_past_32_bits():
     _check_grad(z.cpu().double().numpy(), full, V, t, 1.0, dl, None, torch.bfloat16)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V,n,m", [(3000, 2, 700), (4096, 1, 50), (20000, 257, 600), (50264, 300, 900), (151936, 257, 400)])
+def test_a_row_has_the_same_bits_in_another_batch(V, n, m, dtype):
+    full, t = _logits(m, V, dtype, seed=V)
+    few, _, _ = _run(full[:n], V, t[:n], 6)
+    many, _, _ = _run(full, V, t, 6)
+    for k in few:
+        assert np.array_equal(few[k], many[k][:n]), k
+
+
 def test_more_rows_than_one_launch_takes():
     n, V = (1 << 22) + 5, 3
     g = torch.Generator(device=DEV).manual_seed(18)
