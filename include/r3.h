@@ -187,7 +187,8 @@ int r3_combine(const r3_layer_desc *desc, const void *Yp, const float *gates,
  *
  * r3_combine_backward: given dy [T,d], for the K slots of every token
  *   dYp[inv_perm[t*K+j]] = gates[t,j] dy[t]              ([T*K,d], one rounding)
- *   dgates[t,j] = <dy[t], Yp[inv_perm[t*K+j]]>           ([T,K] f32, f32 sums)
+ *   dgates[t,j] = <dy[t], Yp[inv_perm[t*K+j]]>           ([T,K] f32, f32 sums;
+ *                 Yp as r3_combine takes it, without the gate)
  *   dz[t,j] = gates[t,j] (dgates[t,j] - sum_i gates[t,i] dgates[t,i])
  * dz [T,K] f32 is the gradient of the K selected logits where the gates are
  * r3_replay_gate's softmax of them.  dYp, dgates and dz may each be NULL, but
@@ -329,9 +330,9 @@ size_t r3_policy_workspace_bytes(void);
  * floating outputs NaN and its ids -1.
  * Sums are f32.  With more than 256 rows, and for V <= 4096, a row's results are
  * the same bits whatever other rows the call has (and wherever in a 16-byte
- * unit it starts the same).  Fewer, longer rows get more threads and, from
- * V = 65536 on, are cut over several work-groups and joined by a second launch:
- * their last bits can depend on n.
+ * unit it starts the same).  Fewer, longer rows get more threads, and up to 128
+ * rows of 256 KB and more are cut over several work-groups and joined by a
+ * second launch: their last bits can depend on n.
  * top <= R3_MAX_TOP; 0: top_logp and top_id are not read.  n = 0 is a no-op.
  * ws: device workspace of r3_token_logprobs_workspace_bytes(n, V, top) (0 is
  * possible; then ws may be NULL).

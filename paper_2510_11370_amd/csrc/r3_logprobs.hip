@@ -637,18 +637,18 @@ token_logprobs_backward_kernel(BackArgs g) {
     }
 }
 
-// How a call cuts its rows: up to 512 work-groups in all, parts of 4096 elements at least (smaller ones do not shorten the
-// chain of latencies that is left), and only rows long enough to pay for the join and its launch: whole | cut, 64 rows of
-// 20000 bf16 logits 9.0 | 11.1 us, of 50257 f32 8.5 | 10.2, of 72000 11.1 | 11.7 and 11.4 | 10.2, of 151936 16.4 | 13.1 and
-// 18.8 | 11.5.  512 | 1024 work-groups, 151936 bf16 logits with 20 alternatives: 64 rows 13.5 | 14.0 us,
-// 256 rows 21.2 | 22.5, 400 rows 24.1 | 32.3, 512 rows 29.7 | 35.0; 2048: 19.6, 28.4, 33.2, 38.9.
+// How a call cuts its rows: up to 128 of them, of 256 KB and more, into up to 512 work-groups in all, parts of 4096 elements at
+// least (smaller ones do not shorten the chain of latencies that is left).  Others have 1024 threads and a compute unit each,
+// which takes some 20 bytes a nanosecond, where a join and its launch cost 4 us and more.  Cut | whole, bf16 with 20 alternatives:
+// 96 rows of 66000 13.1 | 10.4 us, of 100000 13.6 | 12.4, of 151936 14.7 | 15.4, of 256000 16.8 | 21.9; 200 rows 14.8 | 10.9,
+// 16.4 | 12.6, 19.5 | 15.2, 25.3 | 22.2.  512 | 1024 work-groups: 64 rows of 151936 13.5 | 14.0.
 struct Plan {
     int nsplit, seg;
 };
-Plan plan(int64_t n, int64_t V) {
+Plan plan(int64_t n, int64_t V, int elem_bytes) {
     constexpr int64_t kPart = 4096, kGroups = 512;
+    if (n > 128 || V * elem_bytes < 262144) return {1, (int)V};
     const int64_t k = std::min(std::min<int64_t>(kGroups / n, kMaxSplit), (V + kPart - 1) / kPart);
-    if (k <= 1 || V < 16 * kPart) return {1, (int)V};
     const int64_t seg = ((V + k - 1) / k + 7) / 8 * 8;
     return {(int)((V + seg - 1) / seg), (int)seg};
 }
@@ -657,7 +657,7 @@ size_t part_bytes(int64_t n, const Plan &p) { return align_up((size_t)n * p.nspl
 }  // namespace
 
 size_t token_logprobs_ws_bytes(int64_t n, int64_t V, int top) {
-    const Plan p = plan(n, V);
+    const Plan p = plan(n, V, 4);   // (two-byte logits are cut alike or not at all)
     if (p.nsplit == 1) return 0;
     return part_bytes(n, p) + align_up((size_t)n * p.nsplit * top * sizeof(key_t), 256);
 }
@@ -665,7 +665,7 @@ size_t token_logprobs_ws_bytes(int64_t n, int64_t V, int top) {
 hipError_t launch_token_logprobs(int64_t n, int64_t V, int dtype, const void *logits, int64_t ld, float scale, const int32_t *target,
                                  float *logp, float *entropy, float *stats, int top, float *top_logp, int32_t *top_id, int32_t *status,
                                  void *ws, hipStream_t s) {
-    const Plan p = plan(n, V);
+    const Plan p = plan(n, V, dtype == R3_BF16 ? 2 : 4);
     Args a = {};
     a.n = n; a.ld = ld; a.V = (int)V; a.top = top; a.nsplit = p.nsplit; a.seg = p.seg;
     a.scale = scale; a.c = (float)((double)scale * 1.4426950408889634); a.span = 64.0f / a.c;

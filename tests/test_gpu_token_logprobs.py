@@ -70,7 +70,8 @@ def _check(got, want, what=""):
     (1, 1, 1, 0, 1.0), (3, 7, 5, 0, 1.0), (2, 64, 32, 1, 0.5), (5, 20, 32, 0, 1.0), (9, 513, 20, 3, 1.7), (7, 4096, 32, 0, 1.0),
     (4, 4097, 20, 0, 1.0), (1300, 300, 1, 5, 1.0), (1030, 5000, 3, 0, 1 / 0.6), (3, 32769, 20, 7, 1.0), (40, 9001, 8, 0, 1.0),
     (64, 50257, 8, 0, 1 / 0.6), (1, 151936, 20, 0, 1.0), (2, 262147, 32, 0, 1.0), (600, 40009, 5, 2, 1.0),
-    (256, 65536, 5, 0, 1.0), (257, 65536, 5, 0, 1.0), (37, 65537, 32, 3, 0.7), (4, 65535, 32, 1, 1.0)])
+    (256, 65536, 5, 0, 1.0), (257, 65536, 5, 0, 1.0), (37, 65537, 32, 3, 0.7), (4, 65535, 32, 1, 1.0),
+    (128, 131072, 5, 0, 1.0), (129, 131072, 5, 0, 1.0), (5, 131071, 32, 0, 1.0), (3, 131080, 32, 1, 1.0)])
 def test_against_64_bits(n, V, top, pad, scale, dtype):
     full, t = _logits(n, V, dtype, pad, seed=n + V)
     got, status, _ = _run(full, V, t, top, scale)
@@ -80,7 +81,7 @@ def test_against_64_bits(n, V, top, pad, scale, dtype):
 
 @pytest.mark.parametrize("want,top,target", [(("logp",), 0, True), (("entropy",), 0, False), (("stats",), 0, True), ((), 4, False),
                                              (("logp", "stats"), 4, True)])
-@pytest.mark.parametrize("n,V", [(5, 700), (3, 20001), (3, 70001)])
+@pytest.mark.parametrize("n,V", [(5, 700), (3, 20001), (3, 140001)])
 def test_outputs_that_are_not_wanted(n, V, want, top, target):
     full, t = _logits(n, V, torch.bfloat16, seed=3)
     got, _, _ = _run(full, V, t if target else None, top, want=want)
@@ -148,7 +149,7 @@ def test_rows_where_something_can_go_wrong(V, copies, dtype):
 
 
 def test_rows_left_out_are_not_read():
-    for n, V in ((40, 1000), (9, 30011), (1200, 300), (9, 70001), (300, 70001)):
+    for n, V in ((40, 1000), (9, 30011), (1200, 300), (9, 140001), (300, 70001)):
         full, t = _logits(n, V, torch.bfloat16, seed=5)
         t[::3] = -1
         full[::3] = math.nan
@@ -163,7 +164,7 @@ def test_rows_left_out_are_not_read():
 
 
 def test_the_same_bits_twice_and_no_rows():
-    for n, V in ((30, 50257), (30, 80009), (600, 50257)):
+    for n, V in ((30, 50257), (30, 140009), (600, 50257)):
         full, t = _logits(n, V, torch.bfloat16, seed=6)
         a, _, _ = _run(full, V, t, 20)
         b, _, _ = _run(full, V, t, 20)
@@ -285,7 +286,7 @@ def test_on_another_stream():
 def test_two_graphs_that_share_a_workspace():
     """A decode step's call on cut rows and a training step's forward and gradient, each captured, replayed in turn with
     eager work between."""
-    V = 70001
+    V = 140001
     fa, ta = _logits(3, V, torch.bfloat16, seed=15)
     fb, tb = _logits(5, V, torch.bfloat16, seed=16)
     need = max(r3.lib().r3_token_logprobs_workspace_bytes(k, V, 16) for k in (3, 5))
