@@ -8,12 +8,15 @@ import numpy as np
 U = 2.0 ** -24
 
 
+REF = 8 * np.log(2.0)   # how far the reference of a sum may be below the row's maximum
+
+
 def _chain(V):
-    """Roundings a sum over V elements may pass: the longest chain of one thread (64 threads share a row of at most 4096,
-    256 or more a longer one), the trees that join the threads, and for each piece of a row (16 elements at least, and up
-    to eight short ones) six more where the running maximum changes."""
-    per = V / (64 if V <= 4096 else 256)
-    return 80 + per + 6 * (8 + per / 16)
+    """Roundings a sum over V elements may pass.  64 threads share a row of at most 4096, 256 or more a longer one; a thread
+    adds pieces of at most 16 elements (8 of four bytes), and a piece and up to eight short ones more may each change the
+    sum's reference, six roundings; trees over the threads and the parts of a row."""
+    pieces = 8 + V / (64 if V <= 4096 else 256) / 8
+    return 16 + pieces + 6 * pieces + 36
 
 
 def token_logprobs(z, target, scale, top=0):
@@ -47,13 +50,14 @@ def token_logprobs(z, target, scale, top=0):
         out["logp"][i] = x[t] - ls
         out["entropy"][i] = ls - (p * x0).sum()
         out["stats"][i] = (m, S)
-        # x carries three roundings, its exponential the relative error ln-wise plus two; sums as above
+        # x carries three roundings, its exponential the relative error ln-wise plus two; sums as above.  The entropy's sum of
+        # e x has x relative to the reference, so that its terms are larger by REF until it is referred to the maximum.
         A, A2, L = (p * -x0).sum(), (p * x0 * x0).sum(), _chain(V)
         ts = U * (L + 3 * A + 4)
         out["tol_S"][i] = ts
         lp = lambda v: ts + U * (3 * abs(v) + 4 * abs(ls) + abs(v - ls))  # noqa: E731
         out["tol_logp"][i] = lp(x[t]) if np.isfinite(x[t]) else 0.0
-        out["tol_entropy"][i] = ts + U * (3 * A2 + (2 * L + 16) * A + 4 * ls)
+        out["tol_entropy"][i] = ts + U * (3 * A2 + (2 * L + 16) * (A + REF) + 4 * ls)
         if top:
             r0 = r + 0.0
             order = np.lexsort((np.arange(V), -r0))[:top]

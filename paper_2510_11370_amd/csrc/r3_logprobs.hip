@@ -15,6 +15,7 @@ constexpr int kMaxTop = R3_MAX_TOP;
 constexpr int kMaxSplit = 64;       // parts of a row: one lane each when they are joined
 constexpr float kFar = 1e4f;        // 2^-kFar is 0: exponents are kept above -kFar, so that 0 x (-inf) never arises
 constexpr int64_t kRowsAtOnce = 1 << 22;   // work-groups of a launch: a grid has less than 2^32 threads
+constexpr float kSpan = 8.0f;       // in powers of two
 constexpr float kLn2 = 0.693147180559945309f;
 
 // The larger of two numbers; NaN if one is NaN (v_maximum3_f32), so that a row's maximum says whether it holds one.
@@ -27,8 +28,10 @@ __device__ __forceinline__ float wave_max_nan(float v) {
 
 // Running statistics over some of a row's elements: m their maximum, s = sum 2^x, q = sum 2^x x with x = c z - r,
 // c = scale log2(e).  The sums refer to a logit b that was the maximum when it was taken, r = c b, and stay with it until a
-// logit exceeds `most` = b + 64 / c: one fused multiply-add to an exponent, with the one rounding, and no change of reference
-// in the loop.  Where b is not a moderate number (nothing but -inf so far, 1e30 and beyond), most = -inf, r = b and
+// logit exceeds `most` = b + kSpan / c: one fused multiply-add to an exponent, with the one rounding, and hardly a change of
+// reference in the loop.  q loses what cancels when it is referred to the row's maximum in the end: at most kSpan times the
+// rounding of s, and the sums of a piece are made apart, so that few roundings are that large (16384 x 151936, entropies off by
+// at most: kSpan = 64, one chain 4e-6 of their size, 64 4e-7, 8 2e-7, 0 2e-7; the time is the same within 1 %).  Where b is not a moderate number (nothing but -inf so far, 1e30 and beyond), most = -inf, r = b and
 // x = c (z - b).  Elements come in pieces: `where` is the piece that holds m, m2 the largest of the other pieces.  `masked`: a
 // piece has held -inf.
 struct Stat {
@@ -73,7 +76,7 @@ __device__ __forceinline__ void take(Stat &a, const float (&z)[N], float c, floa
         // bf16, half of it masked, 227 -> 198 us; 188 unmasked).  Not beside the search for alternatives, where the test
         // costs unmasked rows as much as it gives masked ones (200 -> 209, 240 -> 215).
         if (TOP || !__any(a.masked)) {
-            float s = a.s, q = a.q;
+            float s = 0.0f, q = 0.0f;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float x = fmaf(z[i], c, -a.r), e = __builtin_amdgcn_exp2f(x);
@@ -81,18 +84,21 @@ __device__ __forceinline__ void take(Stat &a, const float (&z)[N], float c, floa
                 if constexpr (ENT) q = fmaf(e, x, q);
             }
             if (!ENT || q == q) {   // (an x of -inf makes q a NaN)
-                a.s = s;
-                a.q = q;
+                a.s += s;
+                a.q += q;
                 return;
             }
             a.masked = true;
         }
+        float s = 0.0f, q = 0.0f;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float x = fmaxf(fmaf(z[i], c, -a.r), -kFar), e = __builtin_amdgcn_exp2f(x);
-            a.s += e;
-            a.q = fmaf(e, x, a.q);
+            s += e;
+            q = fmaf(e, x, q);
         }
+        a.s += s;
+        a.q += q;
         return;
     }
 #pragma unroll
@@ -668,7 +674,7 @@ hipError_t launch_token_logprobs(int64_t n, int64_t V, int dtype, const void *lo
     const Plan p = plan(n, V, dtype == R3_BF16 ? 2 : 4);
     Args a = {};
     a.n = n; a.ld = ld; a.V = (int)V; a.top = top; a.nsplit = p.nsplit; a.seg = p.seg;
-    a.scale = scale; a.c = (float)((double)scale * 1.4426950408889634); a.span = 64.0f / a.c;
+    a.scale = scale; a.c = (float)((double)scale * 1.4426950408889634); a.span = kSpan / a.c;
     a.logits = logits; a.target = target;
     a.logp = logp; a.entropy = entropy; a.stats = stats; a.top_logp = top_logp; a.top_id = top_id; a.status = status;
     if (p.nsplit > 1) {

@@ -367,6 +367,23 @@ def test_a_row_has_the_same_bits_in_another_batch(V, n, m, dtype):
         assert np.array_equal(few[k], many[k][:n]), k
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_entropies_of_peaked_rows(dtype):
+    """One logit far above the others, met late: what the sums held before it must not cost the entropy its digits.  Some 25
+    roundings of values up to 8 ln 2 + 1 = 6.5 in the thread that meets it, each 2^-24 / sqrt(3) of them by root mean square:
+    1.1e-6, and five times that for the largest of 2000 rows.  (One sum over all of a thread's elements: 2e-5.)"""
+    n, V = 2000, 50257
+    g = torch.Generator(device=DEV).manual_seed(31)
+    z = torch.randn(n, V, generator=g, device=DEV) * 2
+    t = torch.randint(0, V, (n,), generator=g, device=DEV, dtype=torch.int32)
+    z[torch.arange(n, device=DEV), t.long()] += torch.linspace(0, 16, n, device=DEV)
+    z = z.to(dtype)
+    H = torch.empty(n, device=DEV)
+    r3.token_logprobs(z, t, entropy=H)
+    want = torch.cat([-(torch.softmax(p.double(), 1) * torch.log_softmax(p.double(), 1)).sum(1) for p in z.split(200)])
+    assert (H.double() - want).abs().max() < 5.5e-6
+
+
 def test_more_rows_than_one_launch_takes():
     n, V = (1 << 22) + 5, 3
     g = torch.Generator(device=DEV).manual_seed(18)
