@@ -202,8 +202,8 @@ int r3_combine(const r3_layer_desc *desc, const void *Yp, const float *gates,
  *
  * A token's results are the same bits whatever other tokens the call has.
  * A row outside [0, T*K) in inv_perm (a bad record) is left out: nothing is
- * read or written for the slot and its dgates is 0.  desc->flags and the
- * record's fields are ignored.  No workspace.  R3_ERR_UNSUPPORTED where
+ * written for the slot, it adds nothing and its dgates is 0.  desc->flags and
+ * the record's fields are ignored.  No workspace.  R3_ERR_UNSUPPORTED where
  * T * ceil(d * sizeof(act) / 1024) exceeds 2^24.
  */
 int r3_combine_backward(const r3_layer_desc *desc, const void *dy, const void *Yp, const float *gates,
