@@ -21,9 +21,7 @@ constexpr float kLn2 = 0.693147180559945309f;
 // The larger of two numbers; NaN if one is NaN (v_maximum3_f32), so that a row's maximum says whether it holds one.
 __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 __device__ __forceinline__ float wave_max_nan(float v) {
-#pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) v = max_nan(v, __shfl_xor(v, o, kWave));
-    return v;
+    return over_wave(v, -INFINITY, [](float a, float b) { return max_nan(a, b); });
 }
 
 // Running statistics over some of a row's elements: m their maximum, s = sum 2^x, q = sum 2^x x with x = c z - r,
@@ -143,9 +141,9 @@ __device__ __forceinline__ float log_odds(float z, float m, float scale) {
     return d + d;
 }
 
-// What a row comes to, by the thread that has it.
-__device__ __forceinline__ void put_row(const Args &a, int64_t row, const Part &r, float zt) {
-    const float ls = logf(r.s), nan = __uint_as_float(0x7fc00000u);
+// What a row comes to, by the thread that has it; ls = log r.s.
+__device__ __forceinline__ void put_row(const Args &a, int64_t row, const Part &r, float ls, float zt) {
+    const float nan = __uint_as_float(0x7fc00000u);
     const bool bad = !(r.m < INFINITY), none = r.m == -INFINITY;
     if (bad && a.status) atomicOr(a.status, R3_DATA_NONFINITE);
     if (a.logp) a.logp[row] = bad ? nan : none ? -INFINITY : log_odds(zt, r.m, a.scale) - ls;
@@ -383,7 +381,7 @@ token_logprobs_kernel(Args a) {
         }
     }
     refer_to<ENT>(run, m, a.c);
-    Part st = {m, wave_sum(run.s), ENT ? wave_sum(run.q) : 0.0f};
+    Part st = {m, wave_total(run.s), ENT ? wave_total(run.q) : 0.0f};
     if constexpr (W > 1) {
         if (lane == 0) {
             sum_s[slot][0][w] = st.s;
@@ -403,12 +401,12 @@ token_logprobs_kernel(Args a) {
         put_left_out(a, row, t, tid);
         return;
     }
+    const float ls = logf(st.s);
     if (tid == 0) {
-        if (a.nsplit == 1) put_row(a, row, st, zt);
+        if (a.nsplit == 1) put_row(a, row, st, ls, zt);
         else a.part[item] = st;
     }
     if constexpr (TOP) {
-        const float ls = logf(st.s);
         auto put = [&](int rank, key_t k) {
             if (a.nsplit == 1) put_top(a, row, rank, k, m, ls);
             else a.part_keys[item * a.top + rank] = k;
@@ -531,9 +529,10 @@ token_logprobs_join_kernel(Args a) {
     const float zt = tid == 0 ? Elem<T>::ld((const T *)a.logits + row * a.ld + t) : 0.0f;
     const float m = wave_max_nan(st.m);
     const float d = fmaxf((st.m - m) * a.c, -kFar), f = __builtin_amdgcn_exp2f(d);
-    st = {m, wave_sum(st.s * f), wave_sum(fmaf(st.s, d, st.q) * f)};
+    st = {m, wave_total(st.s * f), wave_total(fmaf(st.s, d, st.q) * f)};
+    const float ls = logf(st.s);
     if (a.top == 0 || !(m > -INFINITY && m < INFINITY)) {
-        if (tid == 0) put_row(a, row, st, zt);
+        if (tid == 0) put_row(a, row, st, ls, zt);
         put_no_top(a, row, tid, m == -INFINITY ? -INFINITY : __uint_as_float(0x7fc00000u));
         return;
     }
@@ -550,9 +549,8 @@ token_logprobs_join_kernel(Args a) {
     for (int u = 0; u < kPer; ++u)
         if (k[u] && key_logit(k[u]) >= thr) buf[atomicAdd(&count_s, 1)] = k[u];
     __syncthreads();
-    const float ls = logf(st.s);
     rank_out<256, kKeys>(buf, count_s, a.top, tid, [&](int rank, key_t key) { put_top(a, row, rank, key, m, ls); });
-    if (tid == 0) put_row(a, row, st, zt);
+    if (tid == 0) put_row(a, row, st, ls, zt);
 }
 
 constexpr int kGradLoads = 2;   // of 16 bytes, a thread's

@@ -109,7 +109,7 @@ combine_backward_kernel(CombineBwd a) {
         if (dots) {
 #pragma unroll
             for (int j = 0; j < G; ++j) {
-                const float s = wave_sum(in[j] ? dot[j] : 0.0f);
+                const float s = wave_total(in[j] ? dot[j] : 0.0f);
                 if (lane == j0 + j) mine = s;
             }
         }
@@ -124,7 +124,7 @@ combine_backward_kernel(CombineBwd a) {
         for (int i = 0; i < W * P; ++i) mine += part[wave + i][lane];
     }
     const float g = lane < a.K ? gates[lane] : 0.0f;
-    const float mix = wave_sum(lane < a.K ? g * mine : 0.0f);
+    const float mix = wave_total(lane < a.K ? g * mine : 0.0f);
     if (lane < a.K) {
         if (a.dgates) a.dgates[(int64_t)t * a.K + lane] = mine;
         if (a.dz) a.dz[(int64_t)t * a.K + lane] = g * (mine - mix);

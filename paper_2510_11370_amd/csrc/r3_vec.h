@@ -1,5 +1,5 @@
 // Rows of elements in loads and stores of 16 bytes at any element's address: rows of odd widths and strides start
-// anywhere, and the hardware takes such addresses.
+// anywhere, and the hardware takes such addresses.  Reductions over a wave.
 #pragma once
 #include "r3_common.h"
 
@@ -42,5 +42,23 @@ template <> struct Row<float> {
     static __device__ __forceinline__ void store(float *p, const float *f) { *(U *)p = pack(f); }
     static __device__ __forceinline__ void store_once(float *p, const float *f) { __builtin_nontemporal_store(pack(f), (U *)p); }
 };
+
+// A value over all 64 lanes, in every lane: six moves within the vector pipe (a row's neighbours 1, 2, 4, 8 on, the last lane
+// of a row to the next row, of the first half to the second) instead of six trips through LDS.  `none`: what f leaves alone.
+template <int CTRL, int ROWS> __device__ __forceinline__ float lane_move(float v, float none) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+template <class F> __device__ __forceinline__ float over_wave(float v, float none, F f) {
+    v = f(v, lane_move<0x111, 0xf>(v, none));
+    v = f(v, lane_move<0x112, 0xf>(v, none));
+    v = f(v, lane_move<0x114, 0xf>(v, none));
+    v = f(v, lane_move<0x118, 0xf>(v, none));
+    v = f(v, lane_move<0x142, 0xa>(v, none));
+    v = f(v, lane_move<0x143, 0xc>(v, none));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), kWave - 1));
+}
+__device__ __forceinline__ float wave_total(float v) {
+    return over_wave(v, 0.0f, [](float a, float b) { return a + b; });
+}
 
 }  // namespace r3
