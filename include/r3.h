@@ -334,6 +334,7 @@ size_t r3_policy_workspace_bytes(void);
  * rows of 256 KB and more are cut over several work-groups and joined by a
  * second launch: their last bits can depend on n.
  * top <= R3_MAX_TOP; 0: top_logp and top_id are not read.  n = 0 is a no-op.
+ * n < 2^31, V < 2^31 - 65536, n * ld <= 2^48, else R3_ERR_UNSUPPORTED.
  * ws: device workspace of r3_token_logprobs_workspace_bytes(n, V, top) (0 is
  * possible; then ws may be NULL).
  *
@@ -346,8 +347,8 @@ size_t r3_policy_workspace_bytes(void);
  * with dlogp.  dlogits: [n, V] of the logits' dtype, row i at dlogits + i*ldd,
  * one rounding; columns past V are not written.  Rows left out and rows of
  * nothing but -inf get zeros; a masked token gets [v = target] dlogp scale.
- * dlogits may be logits itself with ldd = ld; any other overlap of the two is
- * refused (R3_ERR_INVALID_ARG).
+ * dlogits may be logits itself with ldd = ld; other arrays whose address ranges
+ * meet are refused (R3_ERR_INVALID_ARG).
  */
 #define R3_MAX_TOP 32
 size_t r3_token_logprobs_workspace_bytes(int64_t n, int64_t V, int top);

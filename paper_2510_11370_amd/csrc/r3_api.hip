@@ -472,11 +472,14 @@ int r3_policy_discrepancy(int64_t n, const float *logp_train, const float *logp_
                                             (hipStream_t)stream));
 }
 
+// n rows ld elements apart reach past 2^48 elements
+static bool rows_too_far(int64_t n, int64_t ld) { return ld > (1ll << 48) / (n > 0 ? n : 1); }
+
 static int check_logits(int64_t n, int64_t V, int dtype, const void *logits, int64_t ld, float scale) {
     if (n < 0 || V <= 0 || (dtype != R3_BF16 && dtype != R3_F32) || (n > 0 && !logits) || ld < V) return R3_ERR_INVALID_ARG;
     if (!(scale >= 1e-6f && scale <= 1e6f) || !aligned(logits, dtype == R3_BF16 ? 2 : 4)) return R3_ERR_INVALID_ARG;
     // ids are int32 (and a row's index with a work-group's reach beyond it stays one); rows are addressed in 64 bits
-    if (n > 0x7fffffffll || V > 0x7fffffffll - 65536 || ld > 0xffffffffll) return R3_ERR_UNSUPPORTED;
+    if (n > 0x7fffffffll || V > 0x7fffffffll - 65536 || rows_too_far(n, ld)) return R3_ERR_UNSUPPORTED;
     return R3_OK;
 }
 
@@ -509,7 +512,7 @@ int r3_token_logprobs_backward(int64_t n, int64_t V, int dtype, const void *logi
     const int rc = check_logits(n, V, dtype, logits, ld, scale);
     if (rc) return rc;
     if (ldd < V || !aligned(dlogits, dtype == R3_BF16 ? 2 : 4)) return R3_ERR_INVALID_ARG;
-    if (ldd > 0xffffffffll) return R3_ERR_UNSUPPORTED;
+    if (rows_too_far(n, ldd)) return R3_ERR_UNSUPPORTED;
     if (!aligned(target, 4) || !aligned(stats, 4) || !aligned(entropy, 4) || !aligned(dlogp, 4) || !aligned(dentropy, 4))
         return R3_ERR_INVALID_ARG;
     if (n == 0) return R3_OK;

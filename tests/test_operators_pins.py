@@ -118,6 +118,7 @@ def test_log_probabilities_refuse():
                 dict(logp=None, entropy=None, stats=None, top=0)):
         assert _lp(**bad) == INVALID, bad
     assert _lp(n=1 << 31) == UNSUPPORTED and _lp(V=(1 << 31) - 1, ld=1 << 31) == UNSUPPORTED
+    assert _lp(n=1 << 30, ld=1 << 30) == UNSUPPORTED and _lp(n=2, ld=(1 << 47) + 1) == UNSUPPORTED
     need = r3.lib().r3_token_logprobs_workspace_bytes(1, 151936, 20)
     assert need > 0 and need % 256 == 0
     cut = dict(n=1, V=151936, ld=151936, top=20)
@@ -138,7 +139,7 @@ def test_gradient_of_the_logits_refuses():
                 dict(dlogits=_off(A[0], 2 * 399)),              # the last element alone
                 dict(dlogits=_off(A[0], -2 * 399))):
         assert _lb(**bad) == INVALID, bad
-    assert _lb(n=1 << 31) == UNSUPPORTED and _lb(ldd=1 << 33) == UNSUPPORTED
+    assert _lb(n=1 << 31) == UNSUPPORTED and _lb(ldd=1 << 47) == UNSUPPORTED and _lb(ld=1 << 47) == UNSUPPORTED
     assert _lb(n=0, logits=None, stats=None, dlogits=None) == OK
 
 
