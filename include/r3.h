@@ -328,6 +328,7 @@ size_t r3_policy_workspace_bytes(void);
  * ordinary logit.  A row of nothing but -inf: logp -inf, entropy 0, stats
  * {-inf, 0}.  A NaN or +inf in a row sets R3_DATA_NONFINITE and makes its
  * floating outputs NaN and its ids -1.
+ * No logp is above 0, no entropy below 0, whatever rounding does.
  * Sums are f32.  With more than 256 rows, and for V <= 4096, a row's results are
  * the same bits whatever other rows the call has (and wherever in a 16-byte
  * unit it starts the same).  Fewer, longer rows get more threads, and up to 128

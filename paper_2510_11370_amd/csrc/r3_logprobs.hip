@@ -141,13 +141,18 @@ __device__ __forceinline__ float log_odds(float z, float m, float scale) {
     return d + d;
 }
 
+// The largest term of s is 1, whatever rounding says: no log-probability is above 0, no entropy (below) under it.
+__device__ __forceinline__ void settle(Part &r) {
+    if (r.m > -INFINITY) r.s = fmaxf(r.s, 1.0f);
+}
+
 // What a row comes to, by the thread that has it; ls = log r.s.
 __device__ __forceinline__ void put_row(const Args &a, int64_t row, const Part &r, float ls, float zt) {
     const float nan = __uint_as_float(0x7fc00000u);
     const bool bad = !(r.m < INFINITY), none = r.m == -INFINITY;
     if (bad && a.status) atomicOr(a.status, R3_DATA_NONFINITE);
     if (a.logp) a.logp[row] = bad ? nan : none ? -INFINITY : log_odds(zt, r.m, a.scale) - ls;
-    if (a.entropy) a.entropy[row] = bad ? nan : none ? 0.0f : ls - r.q * kLn2 / r.s;
+    if (a.entropy) a.entropy[row] = bad ? nan : none ? 0.0f : fmaxf(ls - r.q * kLn2 / r.s, 0.0f);
     if (a.stats) {
         a.stats[2 * row] = bad ? nan : r.m;
         a.stats[2 * row + 1] = bad ? nan : r.s;
@@ -401,6 +406,7 @@ token_logprobs_kernel(Args a) {
         put_left_out(a, row, t, tid);
         return;
     }
+    if (a.nsplit == 1) settle(st);
     const float ls = logf(st.s);
     if (tid == 0) {
         if (a.nsplit == 1) put_row(a, row, st, ls, zt);
@@ -530,6 +536,7 @@ token_logprobs_join_kernel(Args a) {
     const float m = wave_max_nan(st.m);
     const float d = fmaxf((st.m - m) * a.c, -kFar), f = __builtin_amdgcn_exp2f(d);
     st = {m, wave_total(st.s * f), wave_total(fmaf(st.s, d, st.q) * f)};
+    settle(st);
     const float ls = logf(st.s);
     if (a.top == 0 || !(m > -INFINITY && m < INFINITY)) {
         if (tid == 0) put_row(a, row, st, ls, zt);

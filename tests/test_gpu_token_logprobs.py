@@ -53,6 +53,11 @@ def _check(got, want, what=""):
         with np.errstate(invalid="ignore"):
             bad = ~((np.abs(x - y) <= tol) | (x == y) | (np.isnan(x) & np.isnan(y)))
         assert not bad.any(), (what, name, np.argwhere(bad)[:3].tolist(), x[bad][:3], y[bad][:3], np.broadcast_to(tol, x.shape)[bad][:3])
+    # whatever rounding does: no log-probability above 0, no entropy below, no sum below its largest term
+    for k in ("logp", "top_logp"):
+        assert k not in got or not (got[k] > 0).any(), (what, k)
+    assert "entropy" not in got or not (got["entropy"] < 0).any(), what
+    assert "stats" not in got or not ((got["stats"][:, 1] < 1) & (got["stats"][:, 1] != 0)).any(), what
     if "logp" in got:
         near(got["logp"], want["logp"], want["tol_logp"], "logp")
     if "entropy" in got:
@@ -382,6 +387,18 @@ def test_entropies_of_peaked_rows(dtype):
     r3.token_logprobs(z, t, entropy=H)
     want = torch.cat([-(torch.softmax(p.double(), 1) * torch.log_softmax(p.double(), 1)).sum(1) for p in z.split(200)])
     assert (H.double() - want).abs().max() < 5.5e-6
+
+
+@pytest.mark.parametrize("n,V", [(3000, 300), (700, 50257), (3, 140001), (900, 3)])
+def test_certain_tokens_are_not_more_than_certain(n, V):
+    g = torch.Generator().manual_seed(33)
+    z = torch.randn(n, V, generator=g)
+    t = torch.randint(0, V, (n,), generator=g, dtype=torch.int32)
+    z[torch.arange(n), t.long()] = torch.linspace(15, 60, n) + torch.rand(n, generator=g)
+    for scale in (1.0, 0.7, 1.3):
+        got, status, _ = _run(z, V, t, 3, scale)
+        assert status == 0 and not (got["logp"] > 0).any() and not (got["entropy"] < 0).any() and not (got["top_logp"] > 0).any()
+        assert (got["stats"][:, 1] >= 1).all() and (got["top_id"][:, 0] == t.numpy()).all()
 
 
 def test_more_rows_than_one_launch_takes():
