@@ -331,9 +331,10 @@ size_t r3_policy_workspace_bytes(void);
  * No logp is above 0, no entropy below 0, whatever rounding does.
  * Sums are f32.  With more than 256 rows, and for V <= 4096, a row's results are
  * the same bits whatever other rows the call has (where the same outputs are
- * asked for and the row starts at the same place of a 16-byte unit).  Fewer, longer rows get more threads, and up to 128
- * rows of 256 KB and more are cut over several work-groups and joined by a
- * second launch: their last bits can depend on n.
+ * asked for and the row starts at the same place of a 16-byte unit).  Fewer,
+ * longer rows get more threads, and up to 128 rows of 256 KB and more are cut
+ * over several work-groups and joined by a second launch: their last bits can
+ * depend on n.
  * top <= R3_MAX_TOP; 0: top_logp and top_id are not read.  n = 0 is a no-op.
  * n < 2^31, V < 2^31 - 65536, n * ld <= 2^48, else R3_ERR_UNSUPPORTED.
  * ws: device workspace of r3_token_logprobs_workspace_bytes(n, V, top) (0 is
