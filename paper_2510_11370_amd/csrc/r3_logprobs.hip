@@ -141,9 +141,10 @@ __device__ __forceinline__ float log_odds(float z, float m, float scale) {
     return d + d;
 }
 
-// The largest term of s is 1, whatever rounding says: no log-probability is above 0, no entropy (below) under it.
+// The largest term of s is 1, whatever rounding says: no log-probability is above 0, no entropy (below) under it.  A sum that is
+// a NaN stays one (fmaxf would make it 1).
 __device__ __forceinline__ void settle(Part &r) {
-    if (r.m > -INFINITY) r.s = fmaxf(r.s, 1.0f);
+    if (r.m > -INFINITY) r.s = r.s < 1.0f ? 1.0f : r.s;
 }
 
 // What a row comes to, by the thread that has it; ls = log r.s.
@@ -152,7 +153,10 @@ __device__ __forceinline__ void put_row(const Args &a, int64_t row, const Part &
     const bool bad = !(r.m < INFINITY), none = r.m == -INFINITY;
     if (bad && a.status) atomicOr(a.status, R3_DATA_NONFINITE);
     if (a.logp) a.logp[row] = bad ? nan : none ? -INFINITY : log_odds(zt, r.m, a.scale) - ls;
-    if (a.entropy) a.entropy[row] = bad ? nan : none ? 0.0f : fmaxf(ls - r.q * kLn2 / r.s, 0.0f);
+    if (a.entropy) {
+        const float h = ls - r.q * kLn2 / r.s;
+        a.entropy[row] = bad ? nan : none || h < 0.0f ? 0.0f : h;
+    }
     if (a.stats) {
         a.stats[2 * row] = bad ? nan : r.m;
         a.stats[2 * row + 1] = bad ? nan : r.s;

@@ -477,3 +477,31 @@ def test_a_workspace_that_is_too_small_is_refused():
             r3.token_logprobs(z, t, **{"logp": lp, **bad})
     with pytest.raises(r3.R3Error):
         r3.token_logprobs(z, t.long(), lp)
+
+
+# ---------------------------------------------------------------- finite logits of any size
+def _finite_masks(V, value, n=5, few=100, seed=0):
+    """Rows whose logits are a finite mask value but for a run of ordinary ones in some place each."""
+    rng = np.random.default_rng(seed + V)
+    z = np.full((n, V), value, np.float32)
+    at = []
+    for i in range(n):
+        k = min(few, max(1, V // 4))
+        a = int(rng.integers(0, V - k + 1))
+        z[i, a:a + k] = rng.normal(0, 2, k)
+        at.append(a + k // 2)
+    return torch.tensor(z), torch.tensor(at, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("n,V", [(5, 4096), (5, 50257), (300, 20000), (5, 151936)])
+def test_a_sum_that_is_not_a_number_is_not_made_one(n, V):
+    """Whatever a row's sums come to, no result is a plausible wrong one: right, or NaN with all that follows from it."""
+    for value in (-1e10, -1e20, -1e30):
+        full, t = _finite_masks(V, value, n)
+        got, _, _ = _run(full, V, t, 4)
+        want = ref.token_logprobs(_np(full), t.numpy(), 1.0, 4)
+        for k, tol in (("logp", "tol_logp"), ("entropy", "tol_entropy"), ("top_logp", "tol_top")):
+            near = np.isnan(got[k]) | (np.abs(got[k] - want[k]) <= want[tol])
+            assert near.all(), (value, k, got[k][~near][:3], want[k][~near][:3])
+        S, at = got["stats"][:, 1], want["stats"][:, 1]
+        assert (np.isnan(S) | (np.abs(S - at) <= want["tol_S"] * at)).all(), (value, S[:3], at[:3])
