@@ -16,6 +16,7 @@ constexpr int kMaxSplit = 64;       // parts of a row: one lane each when they a
 constexpr float kFar = 1e4f;        // 2^-kFar is 0: exponents are kept above -kFar, so that 0 x (-inf) never arises
 constexpr int64_t kRowsAtOnce = 1 << 22;   // work-groups of a launch: a grid has less than 2^32 threads
 constexpr float kSpan = 8.0f;       // in powers of two
+constexpr float kMostRef = 16777216.0f;   // 2^24
 constexpr float kLn2 = 0.693147180559945309f;
 
 // The larger of two numbers; NaN if one is NaN (v_maximum3_f32), so that a row's maximum says whether it holds one.
@@ -29,8 +30,10 @@ __device__ __forceinline__ float wave_max_nan(float v) {
 // logit exceeds `most` = b + kSpan / c: one fused multiply-add to an exponent, with the one rounding, and hardly a change of
 // reference in the loop.  q loses what cancels when it is referred to the row's maximum in the end: at most kSpan times the
 // rounding of s, and the sums of a piece are made apart, so that few roundings are that large (16384 x 151936, entropies off by
-// at most: kSpan = 64, one chain 4e-6 of their size, 64 4e-7, 8 2e-7, 0 2e-7; the time is the same within 1 %).  Where b is not a moderate number (nothing but -inf so far, 1e30 and beyond), most = -inf, r = b and
-// x = c (z - b).  Elements come in pieces: `where` is the piece that holds m, m2 the largest of the other pieces.  `masked`: a
+// at most: kSpan = 64, one chain 4e-6 of their size, 64 4e-7, 8 2e-7, 0 2e-7; the time is the same within 1 %).  r carries the
+// rounding of c b into every exponent, and out again in the end: half a unit in c b's last place, 1/2 at kMostRef, but past a
+// float's largest exponent from 2^32 on.  Where |c b| is above kMostRef (mask values like -1e9 are), or there is nothing but -inf so far,
+// most = -inf, r = b and x = c (z - b).  Elements come in pieces: `where` is the piece that holds m, m2 the largest of the other pieces.  `masked`: a
 // piece has held -inf.
 struct Stat {
     float m, s, q, r, most, m2;
@@ -64,9 +67,10 @@ __device__ __forceinline__ void take(Stat &a, const float (&z)[N], float c, floa
     a.m = max_nan(a.m, hi);
     if (!(hi <= a.most)) {   // the first ones, a much larger one, a NaN
         refer_to<ENT>(a, a.m, c);
-        const bool moderate = fabsf(a.m) <= 1e30f;
+        const float r = a.m * c;
+        const bool moderate = fabsf(r) <= kMostRef;
         a.most = moderate ? a.m + span : -INFINITY;
-        a.r = moderate ? a.m * c : a.m;
+        a.r = moderate ? r : a.m;
         if (moderate) shift<ENT>(a, fmaf(a.m, c, -a.r));   // from x = c (z - b) to x = c z - r
     }
     if (a.most > -INFINITY) {
@@ -99,12 +103,15 @@ __device__ __forceinline__ void take(Stat &a, const float (&z)[N], float c, floa
         a.q += q;
         return;
     }
+    float s = 0.0f, q = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const float x = fmaxf((z[i] - a.r) * c, -kFar), e = __builtin_amdgcn_exp2f(x);
-        a.s += e;
-        if constexpr (ENT) a.q = fmaf(e, x, a.q);
+        s += e;
+        if constexpr (ENT) q = fmaf(e, x, q);
     }
+    a.s += s;
+    a.q += q;
 }
 
 // What is kept of a part of a row: maximum and sums for x = c (z - m).
@@ -126,7 +133,7 @@ __device__ __forceinline__ int key_place(key_t k) { return (int)(0xffffffffu - (
 struct Args {
     int64_t n, ld, row0;            // rows row0 .. n - 1
     int V, top, nsplit, seg;        // seg: elements of one part of a row
-    float scale, c, span;           // c = scale log2(e), span = 64 / c
+    float scale, c, span;           // c = scale log2(e), span = kSpan / c
     const void *logits;
     const int32_t *target;
     float *logp, *entropy, *stats, *top_logp;

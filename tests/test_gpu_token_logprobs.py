@@ -505,3 +505,68 @@ def test_a_sum_that_is_not_a_number_is_not_made_one(n, V):
             assert near.all(), (value, k, got[k][~near][:3], want[k][~near][:3])
         S, at = got["stats"][:, 1], want["stats"][:, 1]
         assert (np.isnan(S) | (np.abs(S - at) <= want["tol_S"] * at)).all(), (value, S[:3], at[:3])
+
+
+def _of_any_size(V):
+    """Finite rows whose largest logit times scale log2(e) is anything from the ordinary to 1e30, and their names."""
+    rng = np.random.default_rng(V)
+    base = rng.normal(0, 2, V).astype(np.float32)
+    rows = {}
+    for value in (-1e4, -1e7, -1e9, -1e10, -1e15, -1e20, -1e30):
+        rows["all %g" % value] = np.full(V, value, np.float32)
+        for few in (1, 9, 300):
+            r = np.full(V, value, np.float32)
+            k = min(few, V)
+            a = int(rng.integers(0, V - k + 1))
+            r[a:a + k] = rng.normal(0, 2, k)
+            rows["%g but %d" % (value, few)] = r
+        r = base.copy(); r[rng.random(V) < 0.5] = value
+        rows["half %g" % value] = r
+        r = base.copy(); r[V // 2:] = value
+        rows["second half %g" % value] = r
+        r = base.copy(); r[:V // 2] = value
+        rows["first half %g" % value] = r
+    for value in (3000.0, 3e6, 1e9, 1e10, 1e20, 1e30):
+        r = np.full(V, value, np.float32); r[rng.random(V) < 0.5] *= np.float32(0.75)
+        rows["ties at %g" % value] = r
+        r = base.copy(); r[V // 3] = value
+        rows["one of %g" % value] = r
+    for value in (1e5, 1e6, 5e6, 1.3e7, 4e7):   # around the largest size that an exponent is taken as one fused multiply-add at
+        rows["offset %g" % value] = (base + value).astype(np.float32)
+        rows["offset %g" % -value] = (base - value).astype(np.float32)
+    return rows
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V,copies,scales", [(5, 1, (1.0, 1 / 0.6, 1e6, 1e-6)), (900, 1, (1.0, 1 / 0.7, 1e6, 1e-6)), (4096, 6, (1.0, 1 / 0.6)),
+                                             (20000, 6, (1.0, 1 / 0.7)), (50257, 1, (1.0, 1 / 0.6)), (151936, 1, (1.0, 1 / 0.6))])
+def test_finite_logits_of_any_size(V, copies, scales, dtype):
+    """copies: other rows beside them, so that more than 256 are in the call.  Rows of 151936 are cut."""
+    rows = _of_any_size(V)
+    names = list(rows)
+    k = len(names)
+    z = torch.tensor(np.stack(list(rows.values()))).to(dtype)
+    t = torch.tensor([(i * 7919) % V for i in range(k)], dtype=torch.int32)
+    t[1::2] = z.float().argmax(1).int()[1::2]
+    for scale in scales:
+        want = ref.token_logprobs(_np(z), t.numpy(), scale, 32)
+        for top in (32, 0):
+            got, status, _ = _run(z.repeat(copies, 1), V, t.repeat(copies), top, scale)
+            assert status == 0
+            for c in {0, copies - 1}:
+                for i, name in enumerate(names):
+                    row = {a: b[c * k + i:c * k + i + 1] for a, b in got.items()}
+                    _check(row, {a: b[i:i + 1] for a, b in want.items()}, (name, scale, top, c))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V,scale", [(5, 1.0), (900, 1e6), (4096, 1 / 0.6), (20000, 1.0), (140001, 1 / 0.7)])
+def test_gradient_of_finite_logits_of_any_size(V, scale, dtype):
+    rows = _of_any_size(V)
+    names = list(rows)
+    z = torch.tensor(np.stack(list(rows.values()))).to(dtype)
+    t = torch.tensor([(i * 7919) % V for i in range(len(names))], dtype=torch.int32)
+    dl, dh = np.linspace(-1, 1, len(names)), np.linspace(0.5, -0.5, len(names))
+    got = _backward(z, V, t, dtype, dl, dh, scale)
+    for i, name in enumerate(names):
+        _check_grad(got[i:i + 1], z[i:i + 1], V, t[i:i + 1], scale, dl[i:i + 1], dh[i:i + 1], dtype, (name, scale))
