@@ -349,8 +349,8 @@ size_t r3_policy_workspace_bytes(void);
  * with dlogp.  dlogits: [n, V] of the logits' dtype, row i at dlogits + i*ldd,
  * one rounding; columns past V are not written.  Rows left out and rows of
  * nothing but -inf get zeros; a masked token gets [v = target] dlogp scale.
- * dlogits may be logits itself with ldd = ld; other arrays whose address ranges
- * meet are refused (R3_ERR_INVALID_ARG).
+ * dlogits may be logits itself with ldd = ld; otherwise no array that is read may
+ * lie between dlogits' first element and its last (R3_ERR_INVALID_ARG).
  */
 #define R3_MAX_TOP 32
 size_t r3_token_logprobs_workspace_bytes(int64_t n, int64_t V, int top);

@@ -517,9 +517,12 @@ int r3_token_logprobs_backward(int64_t n, int64_t V, int dtype, const void *logi
         return R3_ERR_INVALID_ARG;
     if (n == 0) return R3_OK;
     if (!stats || !dlogits || (!dlogp && !dentropy) || (dlogp && !target) || (dentropy && !entropy)) return R3_ERR_INVALID_ARG;
-    const size_t eb = dtype == R3_BF16 ? 2 : 4;
-    if (!(dlogits == logits && ldd == ld) &&
-        overlap(logits, ((size_t)(n - 1) * ld + V) * eb, dlogits, ((size_t)(n - 1) * ldd + V) * eb))
+    // a row's work-groups read what is the row's while others write: nothing that is read may lie in dlogits
+    const size_t eb = dtype == R3_BF16 ? 2 : 4, written = ((size_t)(n - 1) * ldd + V) * eb, word = (size_t)n * 4;
+    if (!(dlogits == logits && ldd == ld) && overlap(logits, ((size_t)(n - 1) * ld + V) * eb, dlogits, written))
+        return R3_ERR_INVALID_ARG;
+    if (overlap(stats, 2 * word, dlogits, written) || overlap(target, word, dlogits, written) || overlap(dlogp, word, dlogits, written) ||
+        overlap(dentropy, word, dlogits, written) || (dentropy && overlap(entropy, word, dlogits, written)))
         return R3_ERR_INVALID_ARG;
     return hip_rc(launch_token_logprobs_backward(n, V, dtype, logits, ld, scale, target, stats, entropy, dlogp, dentropy, dlogits, ldd,
                                                  (hipStream_t)stream));

@@ -184,3 +184,14 @@ def test_the_binding_refuses_what_the_library_cannot_see():
                  lambda: r3.permute_backward(D, rows, inv, tok)):
         with pytest.raises(r3.R3Error):
             call()
+
+
+def test_the_gradient_of_the_logits_refuses_to_write_over_what_it_reads():
+    """dlogits of 4 x 100 bf16 at A[6], 800 bytes: an array that begins in its last four bytes, or ends in its first four."""
+    hip_build.build()
+    size = dict(target=16, stats=32, entropy=16, dlogp=16, dentropy=16)
+    for name, nbytes in size.items():
+        for at in (A[6], _off(A[6], 796), _off(A[6], 4 - nbytes)):
+            assert _lb(**{name: at}) == INVALID, (name, at)
+    # rows apart: what lies between two of them counts as theirs
+    assert _lb(ldd=1000, stats=_off(A[6], 4 * 1000 * 2 - 1900)) == INVALID
