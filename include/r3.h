@@ -193,12 +193,14 @@ int r3_combine(const r3_layer_desc *desc, const void *Yp, const float *gates,
  * dz [T,K] f32 is the gradient of the K selected logits where the gates are
  * r3_replay_gate's softmax of them.  dYp, dgates and dz may each be NULL, but
  * not all three; Yp is needed (and read) for dgates and dz only.  dYp may be
- * Yp itself (not a part of it).
+ * Yp itself, and dgates or dz may be gates itself (not a part of it); otherwise
+ * no output may share bytes with another array.
  *
  * r3_permute_backward: dx[t] = add[t] + sum_j dXp[inv_perm[t*K+j]], j
  * ascending, f32 sums, one rounding.  dXp [T*K,d], dx [T,d], add [T,d] (act) or
  * NULL; add is for what else reaches x (the router's dz W_r^T, a residual), and
- * may be dx itself (not a part of it).
+ * may be dx itself (not a part of it); dx may share no bytes with another array.
+ * Both refuse arrays that do (R3_ERR_INVALID_ARG).
  *
  * A token's results are the same bits whatever other tokens the call has.
  * A row outside [0, T*K) in inv_perm (a bad record) is left out: nothing is

@@ -271,8 +271,13 @@ int r3_combine_backward(const r3_layer_desc *desc, const void *dy, const void *Y
         !aligned(dgates, 4) || !aligned(dz, 4))
         return R3_ERR_INVALID_ARG;
     const size_t rows = (size_t)m.S * m.d * m.eb, tokens = (size_t)m.T * m.d * m.eb, slots = (size_t)m.S * sizeof(float);
-    if ((Yp != dYp && overlap(Yp, rows, dYp, rows)) || overlap(dy, tokens, dYp, rows) || overlap(dgates, slots, dz, slots))
+    if ((Yp != dYp && overlap(Yp, rows, dYp, rows)) || overlap(dy, tokens, dYp, rows) || overlap(gates, slots, dYp, rows) ||
+        overlap(inv_perm, slots, dYp, rows) || overlap(dgates, slots, dz, slots))
         return R3_ERR_INVALID_ARG;
+    for (const float *out : {dgates, dz})   // (gates: a token's are read before its own results are written)
+        if ((out != gates && overlap(out, slots, gates, slots)) || overlap(out, slots, inv_perm, slots) || overlap(out, slots, dy, tokens) ||
+            overlap(out, slots, Yp, rows) || overlap(out, slots, dYp, rows))
+            return R3_ERR_INVALID_ARG;
     if (!route_backward_supported(m.T, m.d, m.act)) return R3_ERR_UNSUPPORTED;
     return hip_rc(launch_combine_backward(m.T, m.d, m.K, m.act, dy, Yp, gates, inv_perm, dYp, dgates, dz, (hipStream_t)stream));
 }
@@ -284,7 +289,9 @@ int r3_permute_backward(const r3_layer_desc *desc, const void *dXp, const int32_
     if (!dXp || !inv_perm || !dx) return R3_ERR_INVALID_ARG;
     if (!aligned(dXp, 16) || !aligned(add, 16) || !aligned(dx, 16) || !aligned(inv_perm, 4)) return R3_ERR_INVALID_ARG;
     const size_t rows = (size_t)m.S * m.d * m.eb, tokens = (size_t)m.T * m.d * m.eb;
-    if (overlap(dXp, rows, dx, tokens) || (add != dx && overlap(add, tokens, dx, tokens))) return R3_ERR_INVALID_ARG;
+    if (overlap(dXp, rows, dx, tokens) || (add != dx && overlap(add, tokens, dx, tokens)) ||
+        overlap(inv_perm, (size_t)m.S * sizeof(int32_t), dx, tokens))
+        return R3_ERR_INVALID_ARG;
     if (!route_backward_supported(m.T, m.d, m.act)) return R3_ERR_UNSUPPORTED;
     return hip_rc(launch_permute_backward(m.T, m.d, m.K, m.act, dXp, inv_perm, add, dx, (hipStream_t)stream));
 }

@@ -325,3 +325,18 @@ def test_a_token_has_the_same_bits_in_another_batch(act):
         out.append((dYp[:n * K], dg[:n], dz[:n], dx[:n]))
     for a, b in zip(*out):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("T,K,d", [(1, 1, 1), (700, 1, 512), (9, 2, 2055), (130, 7, 24), (40, 8, 2048), (5000, 2, 515), (3, 64, 130)])
+def test_gradients_in_the_gates_place(T, K, d, act):
+    dy, Yp, gates, inv, _ = _case(T, K, d, act, seed=6)
+    D = r3.desc(T, d, max(K, 8), K, 16, act)
+    c = [t.to(DEV) for t in (dy, Yp, gates, inv)]
+    want = [torch.empty_like(c[1]), torch.empty(T, K, device=DEV), torch.empty(T, K, device=DEV)]
+    r3.combine_backward(D, *c, dYp=want[0], dgates=want[1], dz=want[2])
+    for which in (1, 2):
+        out = [torch.empty_like(w) for w in want]
+        out[which] = c[2].clone()
+        r3.combine_backward(D, c[0], c[1], out[which], c[3], dYp=out[0], dgates=out[1], dz=out[2])
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), which

@@ -195,3 +195,23 @@ def test_the_gradient_of_the_logits_refuses_to_write_over_what_it_reads():
             assert _lb(**{name: at}) == INVALID, (name, at)
     # rows apart: what lies between two of them counts as theirs
     assert _lb(ldd=1000, stats=_off(A[6], 4 * 1000 * 2 - 1900)) == INVALID
+
+
+def test_gradients_of_combine_and_permute_refuse_outputs_that_share_bytes():
+    hip_build.build()
+    D = r3.desc(16, 8, 8, 2, 16, "bf16")
+    given = dict(dy=(A[0], 256), Yp=(A[1], 512), gates=(A[2], 128), inv=(A[3], 128), dYp=(A[4], 512), dg=(A[5], 128), dz=(A[6], 128))
+
+    def cb(**at):
+        p = [at.get(k, v[0]) for k, v in given.items()]
+        return r3.lib().r3_combine_backward(C.byref(D), *p, None)
+
+    for out in ("dYp", "dg", "dz"):
+        for other, (at, nbytes) in given.items():
+            if other == out:
+                continue
+            step = 16 if out == "dYp" else 4
+            for where in (_off(at, nbytes - step), _off(at, step - given[out][1])) + (() if (out, other) in (("dYp", "Yp"), ("dg", "gates"), ("dz", "gates")) else (at,)):
+                assert cb(**{out: where}) == INVALID, (out, other, where)
+    for dx in (A[1], _off(A[1], 112), _off(A[1], -240)):
+        assert r3.lib().r3_permute_backward(C.byref(D), A[0], A[1], A[2], dx, None) == INVALID, dx
