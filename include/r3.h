@@ -341,6 +341,7 @@ size_t r3_policy_workspace_bytes(void);
  * n < 2^31, V < 2^31 - 65536, n * ld <= 2^48, else R3_ERR_UNSUPPORTED.
  * ws: device workspace of r3_token_logprobs_workspace_bytes(n, V, top) (0 is
  * possible; then ws may be NULL).
+ * No output, nor ws, may share bytes with another array (R3_ERR_INVALID_ARG).
  *
  * r3_token_logprobs_backward: the gradient of sum_i (dlogp[i] logp[i] +
  * dentropy[i] entropy[i]) with respect to the logits,

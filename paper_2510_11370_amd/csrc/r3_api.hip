@@ -509,6 +509,13 @@ int r3_token_logprobs(int64_t n, int64_t V, int dtype, const void *logits, int64
     if (n == 0) return R3_OK;
     const size_t need = token_logprobs_ws_bytes(n, V, top);
     if (need && (!ws || ws_bytes < need || !aligned(ws, 256))) return R3_ERR_WORKSPACE;
+    const size_t word = (size_t)n * 4, best = word * top, eb = dtype == R3_BF16 ? 2 : 4;
+    const struct { const void *p; size_t bytes; } at[] = {   // seven that are written, two that are read
+        {logp, word}, {entropy, word}, {stats, 2 * word}, {top ? top_logp : nullptr, best}, {top ? top_id : nullptr, best},
+        {status_word, 4}, {need ? ws : nullptr, need}, {target, word}, {logits, ((size_t)(n - 1) * ld + V) * eb}};
+    for (int i = 0; i < 7; ++i)
+        for (int j = i + 1; j < 9; ++j)
+            if (overlap(at[i].p, at[i].bytes, at[j].p, at[j].bytes)) return R3_ERR_INVALID_ARG;
     return hip_rc(launch_token_logprobs(n, V, dtype, logits, ld, scale, target, logp, entropy, stats, top, top_logp, top_id, status_word,
                                         ws, (hipStream_t)stream));
 }

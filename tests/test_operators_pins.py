@@ -215,3 +215,20 @@ def test_gradients_of_combine_and_permute_refuse_outputs_that_share_bytes():
                 assert cb(**{out: where}) == INVALID, (out, other, where)
     for dx in (A[1], _off(A[1], 112), _off(A[1], -240)):
         assert r3.lib().r3_permute_backward(C.byref(D), A[0], A[1], A[2], dx, None) == INVALID, dx
+
+
+def test_log_probabilities_refuse_outputs_that_share_bytes():
+    hip_build.build()
+    n, V, top = 2, 140001, 5
+    need = r3.lib().r3_token_logprobs_workspace_bytes(n, V, top)
+    call = dict(n=n, V=V, ld=V + 7, top=top, ws_bytes=need)
+    size = dict(logp=8, entropy=8, stats=16, top_logp=40, top_id=40, status=4, ws=need, target=8, logits=(V + 7 + V) * 2)
+    place = dict(logits=A[0], target=A[1], logp=A[2], entropy=A[3], stats=A[4], top_logp=A[5], top_id=A[6], status=A[7], ws=A[8])
+    assert need > 0 and need % 256 == 0
+    for out in ("logp", "entropy", "stats", "top_logp", "top_id", "status"):
+        for other, at in place.items():
+            if other != out:
+                for where in (at, _off(at, size[other] - 4 & ~3), _off(at, 4 - size[out])):
+                    assert _lp(**call, **{out: where}) == INVALID, (out, other, where)
+    for other in ("logits", "target"):
+        assert _lp(**call, ws=place[other]) == INVALID, other
