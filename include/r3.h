@@ -340,7 +340,8 @@ size_t r3_policy_workspace_bytes(void);
  * top <= R3_MAX_TOP; 0: top_logp and top_id are not read.  n = 0 is a no-op.
  * n < 2^31, V < 2^31 - 65536, n * ld <= 2^48, else R3_ERR_UNSUPPORTED.
  * ws: device workspace of r3_token_logprobs_workspace_bytes(n, V, top) (0 is
- * possible; then ws may be NULL).
+ * possible; then, and for bf16 rows of fewer than 131072 logits, which are not
+ * cut, ws may be NULL).
  * No output, nor ws, may share bytes with another array (R3_ERR_INVALID_ARG).
  *
  * r3_token_logprobs_backward: the gradient of sum_i (dlogp[i] logp[i] +

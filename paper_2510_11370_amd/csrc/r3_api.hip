@@ -492,7 +492,7 @@ static int check_logits(int64_t n, int64_t V, int dtype, const void *logits, int
 
 size_t r3_token_logprobs_workspace_bytes(int64_t n, int64_t V, int top) {
     if (n <= 0 || V <= 0 || n > 0x7fffffffll || V > 0x7fffffffll - 65536 || top < 0 || top > R3_MAX_TOP) return 0;
-    return token_logprobs_ws_bytes(n, V, top);
+    return token_logprobs_ws_bytes(n, V, top, 4);   // (two-byte logits are cut as these are, or not at all)
 }
 
 int r3_token_logprobs(int64_t n, int64_t V, int dtype, const void *logits, int64_t ld, float scale, const int32_t *target,
@@ -507,9 +507,9 @@ int r3_token_logprobs(int64_t n, int64_t V, int dtype, const void *logits, int64
         (top > 0 && (!aligned(top_logp, 4) || !aligned(top_id, 4))) || !aligned(status_word, 4))
         return R3_ERR_INVALID_ARG;
     if (n == 0) return R3_OK;
-    const size_t need = token_logprobs_ws_bytes(n, V, top);
+    const size_t eb = dtype == R3_BF16 ? 2 : 4, need = token_logprobs_ws_bytes(n, V, top, (int)eb);
     if (need && (!ws || ws_bytes < need || !aligned(ws, 256))) return R3_ERR_WORKSPACE;
-    const size_t word = (size_t)n * 4, best = word * top, eb = dtype == R3_BF16 ? 2 : 4;
+    const size_t word = (size_t)n * 4, best = word * top;
     const struct { const void *p; size_t bytes; } at[] = {   // seven that are written, two that are read
         {logp, word}, {entropy, word}, {stats, 2 * word}, {top ? top_logp : nullptr, best}, {top ? top_id : nullptr, best},
         {status_word, 4}, {need ? ws : nullptr, need}, {target, word}, {logits, ((size_t)(n - 1) * ld + V) * eb}};

@@ -65,7 +65,7 @@ hipError_t launch_policy_discrepancy(int64_t n, const float *lt, const float *li
                                      double *kl, double *frac, void *ws, hipStream_t s);
 
 // r3_logprobs.hip
-size_t token_logprobs_ws_bytes(int64_t n, int64_t V, int top);
+size_t token_logprobs_ws_bytes(int64_t n, int64_t V, int top, int elem_bytes);
 hipError_t launch_token_logprobs(int64_t n, int64_t V, int dtype, const void *logits, int64_t ld, float scale, const int32_t *target,
                                  float *logp, float *entropy, float *stats, int top, float *top_logp, int32_t *top_id, int32_t *status,
                                  void *ws, hipStream_t s);

@@ -678,8 +678,8 @@ size_t part_bytes(int64_t n, const Plan &p) { return align_up((size_t)n * p.nspl
 
 }  // namespace
 
-size_t token_logprobs_ws_bytes(int64_t n, int64_t V, int top) {
-    const Plan p = plan(n, V, 4);   // (two-byte logits are cut alike or not at all)
+size_t token_logprobs_ws_bytes(int64_t n, int64_t V, int top, int elem_bytes) {
+    const Plan p = plan(n, V, elem_bytes);
     if (p.nsplit == 1) return 0;
     return part_bytes(n, p) + align_up((size_t)n * p.nsplit * top * sizeof(key_t), 256);
 }

@@ -570,3 +570,25 @@ def test_gradient_of_finite_logits_of_any_size(V, scale, dtype):
     got = _backward(z, V, t, dtype, dl, dh, scale)
     for i, name in enumerate(names):
         _check_grad(got[i:i + 1], z[i:i + 1], V, t[i:i + 1], scale, dl[i:i + 1], dh[i:i + 1], dtype, (name, scale))
+
+
+@pytest.mark.parametrize("n,V,top", [(1, 65536, 5), (3, 100001, 20), (128, 131071, 0)])
+def test_two_byte_rows_that_are_not_cut_need_no_workspace(n, V, top):
+    """The query has no type and answers for four bytes a logit; a call with two is not refused for what it does not use."""
+    assert r3.lib().r3_token_logprobs_workspace_bytes(n, V, top) > 0
+    full, t = _logits(n, V, torch.bfloat16, seed=41)
+    z, tg = full.to(DEV), t.to(DEV)
+    lp, H = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    tl, ti = torch.empty(n, top, device=DEV), torch.empty(n, top, dtype=torch.int32, device=DEV)
+    stream = torch.cuda.current_stream().cuda_stream
+    best = (tl.data_ptr(), ti.data_ptr()) if top else (None, None)
+    rc = r3.lib().r3_token_logprobs(n, V, r3.BF16, z.data_ptr(), V, 1.0, tg.data_ptr(), lp.data_ptr(), H.data_ptr(), None, top, *best,
+                                    None, None, 0, stream)
+    assert rc == 0
+    got = {"logp": lp.cpu().double().numpy(), "entropy": H.cpu().double().numpy()}
+    if top:
+        got.update(top_logp=tl.cpu().double().numpy(), top_id=ti.cpu().numpy())
+    _check(got, ref.token_logprobs(_np(full), t.numpy(), 1.0, top))
+    zf = full.float().to(DEV)      # four bytes a logit: cut, and refused without a workspace
+    assert r3.lib().r3_token_logprobs(n, V, r3.F32, zf.data_ptr(), V, 1.0, tg.data_ptr(), lp.data_ptr(), H.data_ptr(), None, top, *best,
+                                      None, None, 0, stream) == 3
