@@ -35,6 +35,16 @@ int check_desc(const r3_layer_desc *D, Dims &m) {
     return R3_OK;
 }
 
+// of calls that deal with rows alone: the flags and the record's fields may hold anything
+int check_rows_desc(const r3_layer_desc *D, Dims &m) {
+    if (!D) return R3_ERR_INVALID_ARG;
+    r3_layer_desc rows = *D;
+    rows.flags = 0;
+    rows.idx = R3_IDX_U16;
+    rows.idx_token_stride = 0;
+    return check_desc(&rows, m);
+}
+
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 // whether two arrays share bytes (one that is not given shares none)
 bool overlap(const void *p, size_t np, const void *q, size_t nq) {
@@ -264,7 +274,7 @@ int r3_combine(const r3_layer_desc *desc, const void *Yp, const float *gates, co
 int r3_combine_backward(const r3_layer_desc *desc, const void *dy, const void *Yp, const float *gates, const int32_t *inv_perm,
                         void *dYp, float *dgates, float *dz, void *stream) {
     Dims m;
-    int rc = check_desc(desc, m);
+    int rc = check_rows_desc(desc, m);
     if (rc) return rc;
     if (!dy || !gates || !inv_perm || (!dYp && !dgates && !dz) || ((dgates || dz) && !Yp)) return R3_ERR_INVALID_ARG;
     if (!aligned(dy, 16) || !aligned(Yp, 16) || !aligned(dYp, 16) || !aligned(gates, 4) || !aligned(inv_perm, 4) ||
@@ -284,7 +294,7 @@ int r3_combine_backward(const r3_layer_desc *desc, const void *dy, const void *Y
 
 int r3_permute_backward(const r3_layer_desc *desc, const void *dXp, const int32_t *inv_perm, const void *add, void *dx, void *stream) {
     Dims m;
-    int rc = check_desc(desc, m);
+    int rc = check_rows_desc(desc, m);
     if (rc) return rc;
     if (!dXp || !inv_perm || !dx) return R3_ERR_INVALID_ARG;
     if (!aligned(dXp, 16) || !aligned(add, 16) || !aligned(dx, 16) || !aligned(inv_perm, 4)) return R3_ERR_INVALID_ARG;

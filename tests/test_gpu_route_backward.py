@@ -340,3 +340,16 @@ def test_gradients_in_the_gates_place(T, K, d, act):
         out[which] = c[2].clone()
         r3.combine_backward(D, c[0], c[1], out[which], c[3], dYp=out[0], dgates=out[1], dz=out[2])
         assert all(torch.equal(a, b) for a, b in zip(out, want)), which
+
+
+def test_more_experts_than_the_records_ids_can_name():
+    T, K, d = 50, 6, 96
+    dy, Yp, gates, inv, add = [t.to(DEV) for t in _case(T, K, d, "f32", seed=7)]
+    out = []
+    for ids in (torch.uint16, torch.uint8):
+        D = r3.desc(T, d, 384, K, 16, "f32", idx_dtype=ids)
+        o = [torch.empty_like(Yp), torch.empty(T, K, device=DEV), torch.empty(T, K, device=DEV), torch.empty_like(dy)]
+        r3.combine_backward(D, dy, Yp, gates, inv, dYp=o[0], dgates=o[1], dz=o[2])
+        r3.permute_backward(D, Yp, inv, o[3], add=add)
+        out.append(o)
+    assert all(torch.equal(a, b) for a, b in zip(*out))

@@ -232,3 +232,15 @@ def test_log_probabilities_refuse_outputs_that_share_bytes():
                     assert _lp(**call, **{out: where}) == INVALID, (out, other, where)
     for other in ("logits", "target"):
         assert _lp(**call, ws=place[other]) == INVALID, other
+
+
+def test_gradients_of_combine_and_permute_do_not_look_at_the_record():
+    """Flags, id type and stride of the record that the call has no use for: what is wrong with this one is its size alone."""
+    hip_build.build()
+    far = [C.c_void_p((i + 1) << 50) for i in range(4)]
+    for more in (dict(), dict(flags=r3.FLAG_GATED_H), dict(flags=64), dict(idx=7), dict(idx_token_stride=1), dict(idx_token_stride=-5)):
+        D = r3.desc((1 << 24) + 1, 512, 8, 2, 16, "bf16")
+        for k, v in more.items():
+            setattr(D, k, v)
+        assert r3.lib().r3_combine_backward(C.byref(D), far[0], None, far[1], far[2], far[3], None, None, None) == UNSUPPORTED, more
+        assert r3.lib().r3_permute_backward(C.byref(D), far[0], far[1], None, far[2], None) == UNSUPPORTED, more
