@@ -592,3 +592,84 @@ def test_two_byte_rows_that_are_not_cut_need_no_workspace(n, V, top):
     zf = full.float().to(DEV)      # four bytes a logit: cut, and refused without a workspace
     assert r3.lib().r3_token_logprobs(n, V, r3.F32, zf.data_ptr(), V, 1.0, tg.data_ptr(), lp.data_ptr(), H.data_ptr(), None, top, *best,
                                       None, None, 0, stream) == 3
+
+
+# ---------------------------------------------------------------- every element once; accuracy on ordinary rows
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,V,pad,start", [
+    (3, 5, 0, 1), (2000, 1003, 0, 0), (700, 4096, 3, 5), (1, 4097, 0, 0), (300, 9001, 0, 3), (200, 32771, 1, 0), (300, 32771, 1, 0),
+    (40, 65535, 0, 1), (40, 65537, 0, 0), (3, 65536, 0, 2), (128, 66000, 2, 0), (3, 131071, 0, 0), (3, 131072, 0, 0), (7, 131080, 1, 3),
+    (128, 131088, 0, 0), (129, 131088, 0, 0), (1, 151936, 0, 0), (17, 151936, 0, 7), (300, 151936, 0, 0), (5, 262147, 0, 0), (60, 250003, 5, 1),
+    (2, 1000003, 0, 1)])
+def test_every_logit_counts_once(n, V, pad, start, dtype):
+    """Zeros of both signs, half of them masked with -inf: every sum is a whole number below 2^24, so S is the number of logits
+    left, exactly, however a row is cut; one left out or read twice between two parts, before or behind the vectors, shows.
+    logp and entropy come to the logarithm of that, in 32 bits: four units in the last place.  The alternatives are the first
+    ids left."""
+    g = torch.Generator(device=DEV).manual_seed(n + V)
+    ld, top = V + pad, min(32, V)
+    flat = torch.full((start + n * ld,), math.nan, dtype=dtype, device=DEV)
+    z = flat[start:].as_strided((n, V), (ld, 1))
+    left = torch.rand(n, V, generator=g, device=DEV) < 0.5
+    left[:, V // 2] = True
+    left[n // 2] = True                                  # and a row with nothing masked
+    sign = torch.where(torch.rand(n, V, generator=g, device=DEV) < 0.5, -0.0, 0.0)
+    z.copy_(torch.where(left, sign, torch.full_like(sign, -math.inf)))
+    t = torch.full((n,), V // 2, dtype=torch.int32, device=DEV)
+    want = left.sum(1)
+    log = want.double().log()
+    ids = torch.where(left, torch.arange(V, device=DEV), V).topk(top, 1, largest=False).values.sort(1).values
+    for k in (0, top):
+        lp, H, st = torch.empty(n, device=DEV), torch.empty(n, device=DEV), torch.empty(n, 2, device=DEV)
+        tl, ti = torch.empty(n, top, device=DEV), torch.empty(n, top, dtype=torch.int32, device=DEV)
+        r3.token_logprobs(z, t, lp, entropy=H, stats=st, **(dict(top_logp=tl, top_id=ti) if k else {}))
+        assert (st[:, 0] == 0).all() and torch.equal(st[:, 1].double(), want.double()), (k, (st[:, 1] - want).nonzero()[:3])
+        assert ((lp.double() + log).abs() <= 2.0 ** -21 * log).all() and ((H.double() - log).abs() <= 2.0 ** -21 * log).all()
+        if k:
+            assert torch.equal(ti.long(), torch.where(ids < V, ids, -1))
+            assert ((tl.double() + log[:, None]).abs()[ids < V] <= (2.0 ** -21 * log[:, None]).expand_as(tl)[ids < V]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,V,top,scale", [(1000, 1000, 0, 1.0), (400, 4096, 20, 1 / 0.6), (300, 20000, 0, 1 / 0.6), (300, 50257, 8, 1.0), (100, 50257, 0, 0.5),
+                                           (300, 151936, 0, 1.0), (300, 151936, 20, 1 / 0.7), (100, 151936, 20, 1.0), (1, 151936, 20, 1 / 0.6),
+                                           (128, 262147, 0, 1.0), (64, 262147, 32, 0.5)])
+def test_accuracy_on_ordinary_rows(n, V, top, scale, dtype):
+    """What ordinary rows (a spread of 2 in random order) may be off by, tighter than the bound for any row: roundings add up as
+    independent ones do, U / sqrt(3) each (U half a step), five times that for the largest of all rows.
+
+    With x the logits' distances from the largest, A = sum p |x|, A2 = sum p x^2, U times:
+      c = scale log2(e) is rounded once for all: A in log S, A2 - A^2 in the entropy;
+      the exponential has a unit in the last place, counted in full: 2, and 2 A;
+      a thread's roundings (16 to a piece, one a piece, three changes of its reference by six) average over the threads and over
+      the elements that have the weight: f = sqrt(sum p^2 + 1/64) of sqrt(L1), and as much of an exponent's own rounding, A, A2;
+      a term of the entropy is up to x + REF before it is referred to the maximum;
+      the wave's tree (its early levels average: 2), up to 16 waves in a row (sum (i/16)^2 < 6) and the parts' tree (2), two more: 12;
+      logf two units in the last place, the target's distance three roundings, each result its own."""
+    g = torch.Generator(device=DEV).manual_seed(n + V + top)
+    z = (torch.randn(n, V, generator=g, device=DEV) * 2).to(dtype)
+    t = torch.randint(0, V, (n,), generator=g, device=DEV, dtype=torch.int32)
+    lp, H, st = torch.empty(n, device=DEV), torch.empty(n, device=DEV), torch.empty(n, 2, device=DEV)
+    more = dict(top_logp=torch.empty(n, top, device=DEV), top_id=torch.empty(n, top, dtype=torch.int32, device=DEV)) if top else {}
+    r3.token_logprobs(z, t, lp, entropy=H, stats=st, scale=scale, **more)
+    scale = float(np.float32(scale))
+    x = (z.double() - z.double().amax(1, keepdim=True)) * scale
+    S = x.exp().sum(1)
+    p = x.exp() / S[:, None]
+    ls = S.log()
+    A, A2, f = -(p * x).sum(1), (p * x * x).sum(1), ((p * p).sum(1) + 1 / 64).sqrt()
+    h = ls + A
+    N = 8 if dtype == torch.bfloat16 else 4
+    L1 = 16 + 8 + V / (64 if V <= 4096 else 256) / N + 18
+    r, L2 = 5 / 3 ** 0.5, 12
+    tol_S = ref.U * (A + 2 + r * (f * L1 ** 0.5 + L2 ** 0.5 + f * A))
+    tol_H = tol_S * (1 + A) + ref.U * (4 * ls + (A2 - A * A) + 2 * A + r * (f * L1 ** 0.5 * (A + ref.REF) + L2 ** 0.5 * A + f * A2) + 4 * A + 2 * h)
+    xt = x.gather(1, t.long()[:, None])[:, 0]
+    tol_lp = tol_S + ref.U * (3 * xt.abs() + 4 * ls + (xt - ls).abs())
+    for name, got, want, tol in (("S", st[:, 1] / S - 1, 0.0, tol_S), ("entropy", H, h, tol_H), ("logp", lp, xt - ls, tol_lp)):
+        err = (got.double() - want).abs()
+        assert (err <= tol).all(), (name, (err / tol).max().item(), tol.max().item())
+    if top:
+        best = x.topk(top, 1).values
+        tol = tol_S[:, None] + ref.U * (3 * best.abs() + 4 * ls[:, None] + (best - ls[:, None]).abs())
+        assert ((more["top_logp"].double() - (best - ls[:, None])).abs() <= tol).all()
