@@ -30,11 +30,15 @@ __device__ __forceinline__ float wave_max_nan(float v) {
 // logit exceeds `most` = b + kSpan / c: one fused multiply-add to an exponent, with the one rounding, and hardly a change of
 // reference in the loop.  q loses what cancels when it is referred to the row's maximum in the end: at most kSpan times the
 // rounding of s, and the sums of a piece are made apart, so that few roundings are that large (16384 x 151936, entropies off by
-// at most: kSpan = 64, one chain 4e-6 of their size, 64 4e-7, 8 2e-7, 0 2e-7; the time is the same within 1 %).  r carries the
-// rounding of c b into every exponent, and out again in the end: half a unit in c b's last place, 1/2 at kMostRef, but past a
-// float's largest exponent from 2^32 on.  Where |c b| is above kMostRef (mask values like -1e9 are), or there is nothing but -inf so far,
-// most = -inf, r = b and x = c (z - b).  Elements come in pieces: `where` is the piece that holds m, m2 the largest of the other pieces.  `masked`: a
-// piece has held -inf.
+// at most: kSpan = 64, one chain 4e-6 of their size, 64 4e-7, 8 2e-7, 0 2e-7; the time is the same within 1 %).
+//
+// r carries the rounding of c b into every exponent, and out again in the end: half a unit in c b's last place, 1/2 at kMostRef,
+// but past a float's largest exponent from 2^32 on.  Where |c b| is above kMostRef (mask values like -1e9 are), or there is
+// nothing but -inf so far, most = -inf, r = b and x = c (z - b) (4096 x 151936 bf16 with the first half at -1e9 183 us, random
+// halves 183; at -inf 187 and 188).
+//
+// Elements come in pieces: `where` is the piece that holds m, m2 the largest of the other pieces.  `masked`: a piece has held
+// -inf.
 struct Stat {
     float m, s, q, r, most, m2;
     int where;
@@ -660,8 +664,8 @@ token_logprobs_backward_kernel(BackArgs g) {
 }
 
 // How a call cuts its rows: up to 128 of them, of 256 KB and more, into up to 512 work-groups in all, parts of 4096 elements at
-// least (smaller ones do not shorten the chain of latencies that is left).  Others have 1024 threads and a compute unit each,
-// which takes some 20 bytes a nanosecond, where a join and its launch cost 4 us and more.  Cut | whole, bf16 with 20 alternatives:
+// least (smaller ones do not shorten the chain of latencies that is left).  Others have 1024 threads and a compute unit each, which
+// with their loads on the way, 32 KB, takes some 20 bytes a nanosecond, where a join and its launch cost 4 us and more.  Cut | whole, bf16 with 20 alternatives:
 // 96 rows of 66000 13.1 | 10.4 us, of 100000 13.6 | 12.4, of 151936 14.7 | 15.4, of 256000 16.8 | 21.9; 200 rows 14.8 | 10.9,
 // 16.4 | 12.6, 19.5 | 15.2, 25.3 | 22.2.  512 | 1024 work-groups: 64 rows of 151936 13.5 | 14.0.
 struct Plan {
