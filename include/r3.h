@@ -342,7 +342,8 @@ size_t r3_policy_workspace_bytes(void);
  * ws: device workspace of r3_token_logprobs_workspace_bytes(n, V, top) (0 is
  * possible; then, and for bf16 rows of fewer than 131072 logits, which are not
  * cut, ws may be NULL).
- * No output, nor ws, may share bytes with another array (R3_ERR_INVALID_ARG).
+ * No output, nor ws, may lie between another array's first element and its last,
+ * padding of the rows included (R3_ERR_INVALID_ARG).
  *
  * r3_token_logprobs_backward: the gradient of sum_i (dlogp[i] logp[i] +
  * dentropy[i] entropy[i]) with respect to the logits,

@@ -205,7 +205,7 @@ def _raw_stream(dev):
 
 def combine_backward(D, dy, Yp, gates, inv_perm, dYp=None, dgates=None, dz=None):
     """Gradient of combine: rows dYp [T*K,d], gates dgates [T,K], selected logits dz [T,K]; each may be None, and Yp with
-    dgates and dz.  dYp may be Yp."""
+    dgates and dz.  dYp may be Yp, dgates or dz may be gates."""
     w, dev, a, f = "combine_backward", _device("combine_backward", dy), act_dtype(D), torch.float32
     tok, rows, slots = (D.T, D.d), (D.T * D.K, D.d), (D.T, D.K)
     _check(lib().r3_combine_backward(
