@@ -664,10 +664,11 @@ token_logprobs_backward_kernel(BackArgs g) {
 }
 
 // How a call cuts its rows: up to 128 of them, of 256 KB and more, into up to 512 work-groups in all, parts of 4096 elements at
-// least (smaller ones do not shorten the chain of latencies that is left).  Others have 1024 threads and a compute unit each, which
-// with their loads on the way, 32 KB, takes some 20 bytes a nanosecond, where a join and its launch cost 4 us and more.  Cut | whole, bf16 with 20 alternatives:
-// 96 rows of 66000 13.1 | 10.4 us, of 100000 13.6 | 12.4, of 151936 14.7 | 15.4, of 256000 16.8 | 21.9; 200 rows 14.8 | 10.9,
-// 16.4 | 12.6, 19.5 | 15.2, 25.3 | 22.2.  512 | 1024 work-groups: 64 rows of 151936 13.5 | 14.0.
+// least (smaller ones do not shorten the chain of latencies that is left).  Others have 1024 threads and a compute unit each,
+// which with 32 KB of loads on their way takes some 20 bytes a nanosecond, where a join and its launch cost 4 us and more.
+// Cut | whole, bf16 with 20 alternatives: 96 rows of 66000 13.1 | 10.4 us, of 100000 13.6 | 12.4, of 151936 14.7 | 15.4, of
+// 256000 16.8 | 21.9; 200 rows 14.8 | 10.9, 16.4 | 12.6, 19.5 | 15.2, 25.3 | 22.2.  512 | 1024 work-groups: 64 rows of 151936
+// 13.5 | 14.0.
 struct Plan {
     int nsplit, seg;
 };
