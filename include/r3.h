@@ -369,6 +369,38 @@ int r3_token_logprobs_backward(int64_t n, int64_t V, int dtype, const void *logi
                                void *stream);
 
 /*
+ * Orthogonalised updates: a batch of gradients (dW_gate, dW_up, dW_down or dW_r
+ * as r3_moe_backward writes them, or momenta of them) by Newton-Schulz
+ * products, for optimisers whose update keeps a gradient's singular vectors and
+ * levels its singular values.  For each of `batch` matrices G [rows,cols],
+ *   X = G / (|G|_F + eps),  `steps` times  X <- a X + (b A + c A A) X,  A = X X^T,
+ *   out = scale X,
+ * which takes every singular value s of G to scale f(f(... s / (|G|_F + eps))),
+ * f(x) = a x + b x^3 + c x^5 (a tall matrix is worked on transposed; the result
+ * is the same).  coef: HOST pointer to {a, b, c}, or NULL for
+ * {3.4445, -4.775, 2.0315}, with which singular values of 0.005 and more come
+ * to lie in [0.68, 1.14] after five steps.
+ * G and out: dense [batch, rows, cols], dtype R3_BF16 or R3_F32 each.  The
+ * products' operands are f16 numbers with f32 sums; for dtype_out R3_F32 they
+ * are sums of two such, 22 bits.  Relative to each matrix (2-norm) a bf16 result
+ * is off by about 1e-3 beside its own rounding, an f32 one by 1e-6, as f32
+ * products are (more where most of G is within rounding of fewer dimensions).
+ * A matrix of zeros gives zeros.  A NaN or an infinity in a matrix makes its
+ * result NaN and sets R3_DATA_NONFINITE; the other matrices are as without it.
+ * A matrix's result is the same bits whatever other matrices the call has.
+ * rows, cols <= 32768, batch * rows * cols <= 2^46, and coefficients with which
+ * no element of X, A or b A + c A A can leave (-15, 15) (|G|_2 <= |G|_F bounds
+ * them), else R3_ERR_UNSUPPORTED.  1 <= steps <= R3_MAX_STEPS, eps >= 0.
+ * out may be G itself if the types are the same; otherwise no output, nor ws,
+ * may share bytes with another array.  batch = 0 is a no-op.
+ * ws: device workspace of r3_orthogonalize_workspace_bytes(), 256-byte aligned.
+ */
+#define R3_MAX_STEPS 64
+size_t r3_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, int dtype_out);
+int r3_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int dtype_in, const void *G, int dtype_out, void *out, int steps,
+                     const float *coef, float eps, float scale, int32_t *status_word, void *ws, size_t ws_bytes, void *stream);
+
+/*
  * Router-mask cache (Section 4.2: routing masks stored with the KV cache per
  * layer and token prefix, so that a prefix that hits the cache brings its masks
  * and is not prefilled again).  Masks live in `pages`, a device pool

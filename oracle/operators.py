@@ -136,3 +136,44 @@ def permute_backward(dXp, inv_perm, add, T, half_step):
         size += np.abs(v)
     t = U * (K + 1) * size
     return dx, t + half_step * (np.abs(dx) + t) + 1e-37
+
+
+def _f16(x):
+    return x.astype(np.float16).astype(np.float64)
+
+
+def _pair(x):
+    h = _f16(x)
+    return h + _f16(x - h)
+
+
+QUINTIC = (3.4445, -4.775, 2.0315)
+
+
+def orthogonalize(G, steps=5, coef=QUINTIC, eps=1e-7, scale=1.0, to="f32"):
+    """One matrix G: (the result in 64 bits, a bound on the 2-norm of the error).  The bound is three times what the roundings of
+    the documented number formats do to this matrix (X as pairs of f16, A and its polynomial as f16 or, for f32 results, as
+    pairs; all times 2^12), the chains of f32 sums, and the result's rounding."""
+    a, b, c = (float(np.float32(v)) for v in coef)
+    eps, scale = float(np.float32(eps)), float(np.float32(scale))
+    X = G if G.shape[0] <= G.shape[1] else G.T
+    n = np.linalg.norm(X) + eps
+    X = X / n if n > 0 else X
+    unit, small = 4096.0, _pair if to == "f32" else _f16
+    q, r = (lambda v: _pair(v * unit) / unit), (lambda v: small(v * unit) / unit)
+    Y, I = q(X), np.eye(len(X))
+    for k in range(steps):
+        apart = a + b + c if k >= steps - 2 else a
+        A = X @ X.T
+        X = a * X + (b * A + c * (A @ A)) @ X
+        H = r(Y)
+        A = r(H @ H.T)
+        Y = apart * Y + r((a - apart) * I + b * A + c * (A @ A)) @ H
+        Y = q(Y) if k + 1 < steps else Y
+    size, half = np.linalg.norm(X), 2.0 ** -8 if to == "bf16" else U
+    # 32 products to a rounding of a sum, the worst of a chain's roundings in one direction, for the three products of a step and
+    # growth by the quintic's steepest slope
+    chain = U * steps * 3 * (8 + max(G.shape) / 32) * abs(a)
+    tol = abs(scale) * (3 * np.linalg.norm(Y - X) + chain * size + half * size * 1.01 + 1e-30)
+    out = scale * (X if G.shape[0] <= G.shape[1] else X.T)
+    return out, tol

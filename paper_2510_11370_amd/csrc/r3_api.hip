@@ -552,6 +552,40 @@ int r3_token_logprobs_backward(int64_t n, int64_t V, int dtype, const void *logi
                                                  (hipStream_t)stream));
 }
 
+static const float kQuintic[3] = {3.4445f, -4.775f, 2.0315f};
+
+static bool ortho_sizes_ok(int64_t batch, int64_t rows, int64_t cols) {
+    return batch <= 0x7fffffffll && rows <= 32768 && cols <= 32768 && (batch == 0 || rows * cols <= (1ll << 46) / batch);
+}
+
+size_t r3_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, int dtype_out) {
+    if (batch <= 0 || rows <= 0 || cols <= 0 || !ortho_sizes_ok(batch, rows, cols) || (dtype_out != R3_BF16 && dtype_out != R3_F32)) return 0;
+    return orthogonalize_ws_bytes(batch, rows, cols, dtype_out);
+}
+
+int r3_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int dtype_in, const void *G, int dtype_out, void *out, int steps,
+                     const float *coef, float eps, float scale, int32_t *status_word, void *ws, size_t ws_bytes, void *stream) {
+    if (batch < 0 || rows <= 0 || cols <= 0 || (dtype_in != R3_BF16 && dtype_in != R3_F32) || (dtype_out != R3_BF16 && dtype_out != R3_F32))
+        return R3_ERR_INVALID_ARG;
+    if (steps < 1 || steps > R3_MAX_STEPS || !(eps >= 0.0f && eps <= 1e30f) || !(scale >= -1e30f && scale <= 1e30f)) return R3_ERR_INVALID_ARG;
+    const float *q = coef ? coef : kQuintic;
+    for (int i = 0; i < 3; ++i)
+        if (!(q[i] >= -1e30f && q[i] <= 1e30f)) return R3_ERR_INVALID_ARG;
+    const size_t ib = dtype_in == R3_BF16 ? 2 : 4, ob = dtype_out == R3_BF16 ? 2 : 4;
+    if (!aligned(G, ib) || !aligned(out, ob) || !aligned(status_word, 4)) return R3_ERR_INVALID_ARG;
+    if (!ortho_sizes_ok(batch, rows, cols) || !orthogonalize_in_range(steps, q)) return R3_ERR_UNSUPPORTED;
+    if (batch == 0) return R3_OK;
+    if (!G || !out) return R3_ERR_INVALID_ARG;
+    const size_t need = orthogonalize_ws_bytes(batch, rows, cols, dtype_out);
+    if (!ws || ws_bytes < need || !aligned(ws, 256)) return R3_ERR_WORKSPACE;
+    const size_t n = (size_t)batch * rows * cols;
+    if ((!(out == G && ib == ob) && overlap(G, n * ib, out, n * ob)) || overlap(G, n * ib, ws, need) || overlap(out, n * ob, ws, need) ||
+        overlap(status_word, 4, G, n * ib) || overlap(status_word, 4, out, n * ob) || overlap(status_word, 4, ws, need))
+        return R3_ERR_INVALID_ARG;
+    return hip_rc(launch_orthogonalize(batch, rows, cols, dtype_in, G, dtype_out, out, steps, q, eps, scale, status_word, ws,
+                                       (hipStream_t)stream));
+}
+
 static int check_cache(int idx_dtype, int L, int K, int P, const void *pages, int64_t num_pages,
                        const int32_t *block_table, int nseq, int max_blocks, int &idx_bytes) {
     if (idx_dtype != R3_IDX_U8 && idx_dtype != R3_IDX_U16) return R3_ERR_INVALID_ARG;

@@ -10,7 +10,7 @@ enum ProfTag {
     PROF_RECORD = 0, PROF_LOGITS, PROF_GATE, PROF_PERMUTE_INDEX, PROF_GATHER_ROWS, PROF_FFN1, PROF_FFN2,
     PROF_COMBINE, PROF_GATE_BWD, PROF_DWR, PROF_DH, PROF_WGRAD, PROF_DXP, PROF_DX_FINISH, PROF_WGRAD_PAIR,
     PROF_ROUTING_DIFF, PROF_POLICY, PROF_CACHE_APPEND, PROF_CACHE_GATHER, PROF_AGREEMENT, PROF_LOGPROBS, PROF_LOGPROBS_BWD,
-    PROF_COMBINE_BWD, PROF_PERMUTE_BWD, PROF_NTAGS
+    PROF_COMBINE_BWD, PROF_PERMUTE_BWD, PROF_ORTHO, PROF_NTAGS
 };
 struct ProfScope {
     int tag, slot;
@@ -79,6 +79,12 @@ hipError_t launch_combine_backward(int T, int d, int K, int act, const void *dy,
                                    void *dYp, float *dgates, float *dz, hipStream_t s);
 hipError_t launch_permute_backward(int T, int d, int K, int act, const void *dXp, const int32_t *inv_perm, const void *add, void *dx,
                                    hipStream_t s);
+
+// r3_ortho.hip
+size_t orthogonalize_ws_bytes(int64_t batch, int64_t rows, int64_t cols, int dtype_out);
+bool orthogonalize_in_range(int steps, const float *coef);   // of the f16 that it computes with
+hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int dtype_in, const void *G, int dtype_out, void *out, int steps,
+                                const float *coef, float eps, float scale, int32_t *status, void *ws, hipStream_t s);
 
 // r3_cache.hip
 hipError_t launch_cache_append(int idx_bytes, int L, int K, int P, void *pages, int64_t num_pages,

@@ -25,8 +25,9 @@ EXPORTS = ["r3_version", "r3_workspace_bytes", "r3_record_topk", "r3_replay_gate
            "r3_profile_mfma", "r3_profile_mfma_flops", "r3_profile_gemm_mix", "r3_routing_diff", "r3_policy_discrepancy",
            "r3_policy_workspace_bytes", "r3_mask_cache_append", "r3_mask_cache_gather",
            "r3_combine_backward", "r3_permute_backward", "r3_token_logprobs_workspace_bytes", "r3_token_logprobs",
-           "r3_token_logprobs_backward"]
+           "r3_token_logprobs_backward", "r3_orthogonalize_workspace_bytes", "r3_orthogonalize"]
 MAX_TOP = 32
+MAX_STEPS = 64
 
 
 class LayerDesc(C.Structure):
@@ -65,6 +66,9 @@ def lib():
         L.r3_token_logprobs_workspace_bytes.argtypes = [i64, i64, i32]
         L.r3_token_logprobs.argtypes = [i64, i64, i32, p, i64, f32, p, p, p, p, i32, p, p, p, p, C.c_size_t, p]
         L.r3_token_logprobs_backward.argtypes = [i64, i64, i32, p, i64, f32] + [p] * 6 + [i64, p]
+        L.r3_orthogonalize_workspace_bytes.restype = C.c_size_t
+        L.r3_orthogonalize_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.r3_orthogonalize.argtypes = [i64, i64, i64, i32, p, i32, p, i32, C.POINTER(f32), f32, f32, p, p, C.c_size_t, p]
         _lib = L
     return _lib
 
@@ -274,6 +278,40 @@ def token_logprobs_backward(logits, target, stats, dlogits, dlogp=None, entropy=
         n, V, dt, logits.data_ptr(), ld, scale, _at(w, "target", target, dev, torch.int32, (n,)),
         _at(w, "stats", stats, dev, f, (n, 2)), _at(w, "entropy", entropy, dev, f, (n,)), _at(w, "dlogp", dlogp, dev, f, (n,)),
         _at(w, "dentropy", dentropy, dev, f, (n,)), dlogits.data_ptr(), ldd, _raw_stream(dev)), "r3_token_logprobs_backward")
+
+
+_FLOATS = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _matrices(what, G, out):
+    """batch, rows, cols and the library's types of a dense batch of matrices (or one matrix) and of what becomes of it"""
+    if G.dim() not in (2, 3) or G.dtype not in _FLOATS or out.dtype not in _FLOATS:
+        raise R3Error("%s: matrices are [rows, cols] or [batch, rows, cols], bfloat16 or float32" % what)
+    b, r, c = (1, *G.shape) if G.dim() == 2 else G.shape
+    return b, r, c, _FLOATS[G.dtype], _FLOATS[out.dtype]
+
+
+def orthogonalize_workspace(G, out):
+    """A workspace tensor for orthogonalize(G, out)."""
+    b, r, c, _, to = _matrices("orthogonalize_workspace", G, out)
+    return torch.empty(max(lib().r3_orthogonalize_workspace_bytes(b, r, c, to), 256), dtype=torch.uint8, device=G.device)
+
+
+def orthogonalize(G, out, steps=5, coef=None, eps=1e-7, scale=1.0, status=None, ws=None):
+    """out = scale times G [rows,cols] or each of G [batch,rows,cols] after `steps` Newton-Schulz steps X <- a X + (b A + c A A) X,
+    A = X X^T, from X = G / (|G| + eps).  coef: (a, b, c).  out: G's shape, bfloat16 or float32 (more exact); may be G.
+    ws: orthogonalize_workspace(G, out); made here if it is not given."""
+    w = "orthogonalize"
+    b, r, c, src, to = _matrices(w, G, out)
+    dev = _device(w, G)
+    if ws is None:
+        ws = orthogonalize_workspace(G, out)
+    elif ws.get_device() != dev or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        raise R3Error("%s: ws has to be a dense uint8 tensor on cuda:%d" % (w, dev))
+    _check(lib().r3_orthogonalize(
+        b, r, c, src, _at(w, "G", G, dev, G.dtype, G.shape), to, _at(w, "out", out, dev, out.dtype, G.shape), steps,
+        None if coef is None else (C.c_float * 3)(*coef), eps, scale, _at(w, "status", status, dev, torch.int32, (1,)),
+        ws.data_ptr(), ws.numel(), _raw_stream(dev)), "r3_orthogonalize")
 
 
 def _idx_code(t):
