@@ -369,6 +369,88 @@ int r3_token_logprobs_backward(int64_t n, int64_t V, int dtype, const void *logi
                                void *stream);
 
 /*
+ * Clipped policy loss over packed sequences, and its gradient: between
+ * r3_token_logprobs, whose logp and entropy it reads, and
+ * r3_token_logprobs_backward, which takes its dlogp and dentropy.
+ * n tokens; sequence q has tokens seq_start[q] .. seq_start[q+1]-1 (device int32
+ * [nseq+1], ascending, within [0,n]; NULL: one sequence of all n, nseq ignored).
+ * Token i is live if it is in a sequence and target[i] >= 0 (target NULL: all
+ * are); what the other arrays hold for the rest does not matter.
+ * For a live token with advantage A (advantage [n], or [nseq] with
+ * R3_FLAG_SEQ_ADVANTAGE), all f32:
+ *   d = logp - logp_old (logp_old NULL: it is logp, d = 0);  R3_RATIO_SEQUENCE:
+ *       the mean of that over the sequence's live tokens;    r = exp(d)
+ *   used = min(r, 1 + clip_high) if A > 0, max(r, 1 - clip_low) if A < 0, and in
+ *       the latter case at most dual_clip unless that is 0
+ *   w = min(exp(logp_old - logp_infer), weight_cap), a constant; 1 without logp_infer
+ *   k = exp(q) - 1 - q, q = logp_ref - logp
+ *   l = -w used A + kl_coef k - entropy_coef entropy
+ *   loss = sum_i nu_i l_i;  nu = scale / live tokens (R3_MEAN_TOKENS), scale /
+ *       (sequences with live tokens * the sequence's live tokens)
+ *       (R3_MEAN_SEQUENCES), scale (R3_SUM)
+ *   dlogp = nu (-w A r [used = r] + kl_coef (1 - exp(q))); R3_RATIO_SEQUENCE: the
+ *       first part is the mean over the sequence's live tokens; where clipping
+ *       holds a token it has no part.   dentropy = -entropy_coef nu
+ * Borders are compared in 64 bits.  Tokens that are not live get 0.
+ * stats [8] f32: loss, sum nu (-w used A), sum nu k / scale, sum nu entropy /
+ * scale, share of live tokens that clipping holds, mean w, live tokens, sequences
+ * with live tokens (shares and means of nothing: 0).  Sums are made in 64 bits.
+ * kl_coef needs logp_ref, entropy_coef needs entropy, unless they are 0.  dlogp,
+ * dentropy [n]: may be NULL.  A live token whose loss or gradient is not finite
+ * sets R3_DATA_NONFINITE.  0 <= clip_low <= 1, clip_high >= 0, dual_clip 0 or > 1,
+ * weight_cap > 0; they and the coefficients finite, but for weight_cap, which may
+ * be infinite.  n = 0 gives stats of 0.  n < 2^31 - 2^16.
+ * No output, nor ws, may share bytes with another array.
+ * ws: device workspace of r3_policy_loss_workspace_bytes(desc), 256-byte aligned.
+ */
+enum { R3_RATIO_TOKEN = 0, R3_RATIO_SEQUENCE = 1 };
+enum { R3_MEAN_TOKENS = 0, R3_MEAN_SEQUENCES = 1, R3_SUM = 2 };
+enum { R3_FLAG_SEQ_ADVANTAGE = 1 };   /* r3_policy_desc.flags */
+typedef struct r3_policy_desc {
+    int64_t n;
+    int32_t nseq, ratio, norm, flags;
+    float clip_low, clip_high, dual_clip, weight_cap, kl_coef, entropy_coef, scale;
+} r3_policy_desc;
+size_t r3_policy_loss_workspace_bytes(const r3_policy_desc *desc);
+int r3_policy_loss(const r3_policy_desc *desc, const float *logp, const float *logp_old, const float *logp_infer,
+                   const float *logp_ref, const float *entropy, const float *advantage, const int32_t *target,
+                   const int32_t *seq_start, float *dlogp, float *dentropy, float *stats, int32_t *status_word, void *ws,
+                   size_t ws_bytes, void *stream);
+
+/*
+ * Load-balance loss of the recorded routing with the router's z-loss, and the
+ * gradient of the router's logits (r3_replay_gate's logits_out).  Groups: the
+ * nseq sequences of seq_start (as for r3_policy_loss), or with NULL the whole
+ * batch.  Of a group with N tokens:
+ *   counts[e] = slots of its tokens that the record gives expert e   (int32)
+ *   probs[e]  = mean over its tokens of p_te, p_t = softmax(logits[t])   (f32)
+ *   f_e = E counts[e] / (K N)
+ * loss = balance_coef * balance + z_coef * z, where balance is the mean over the
+ * groups that hold tokens of sum_e f_e probs[e] and z the mean over their tokens
+ * of the squared log-sum-exp of the logits.  f is a constant:
+ *   dlogits[t,e] = balance_coef / (groups N) p_te (f_e - sum_i f_i p_ti)
+ *                  + 2 z_coef / tokens lse_t p_te
+ * (a user's router then has dx += dlogits W_r^T, dW_r += x^T dlogits).
+ * Outputs: counts, probs [groups,E]; stats [3] f32: loss, balance, z; dlogits
+ * f32, row t at dlogits + t*ldd.  counts, probs, dlogits may be NULL.  Tokens of
+ * no group get zeros in dlogits.  Groups without tokens have counts and probs 0.
+ * A logit of -inf is a masked expert: probability and gradient 0.  A row of
+ * nothing but -inf has probabilities, gradient and lse of 0 and counts as a
+ * token.  A NaN or +inf in a row makes its gradient NaN and sets
+ * R3_DATA_NONFINITE; an id >= E is not counted and sets R3_DATA_IDX_RANGE.
+ * Of desc T, E, K, idx and idx_token_stride are used.  Rows are ld elements apart
+ * (ld, ldd >= E; they may start at any element).  dlogits may be logits itself
+ * with ldd = ld; otherwise no output, nor ws, may lie between another array's
+ * first element and its last.  T * max(ld, ldd) <= 2^48.
+ * A token's gradient is the same bits whatever the other groups' logits are.
+ * ws: device workspace of r3_balance_loss_workspace_bytes(), 256-byte aligned.
+ */
+size_t r3_balance_loss_workspace_bytes(const r3_layer_desc *desc, int nseq);
+int r3_balance_loss(const r3_layer_desc *desc, const float *logits, int64_t ld, const void *idx, const int32_t *seq_start, int nseq,
+                    float balance_coef, float z_coef, int32_t *counts, float *probs, float *stats, float *dlogits, int64_t ldd,
+                    int32_t *status_word, void *ws, size_t ws_bytes, void *stream);
+
+/*
  * Orthogonalised updates: a batch of gradients (dW_gate, dW_up, dW_down or dW_r
  * as r3_moe_backward writes them, or momenta of them) by Newton-Schulz
  * products, for optimisers whose update keeps a gradient's singular vectors and

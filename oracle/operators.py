@@ -177,3 +177,129 @@ def orthogonalize(G, steps=5, coef=QUINTIC, eps=1e-7, scale=1.0, to="f32"):
     tol = abs(scale) * (3 * np.linalg.norm(Y - X) + chain * size + half * size * 1.01 + 1e-30)
     out = scale * (X if G.shape[0] <= G.shape[1] else X.T)
     return out, tol
+
+
+def spans(starts, n):
+    """[begin, end) of each sequence; one of everything without starts."""
+    return [(0, n)] if starts is None else [(int(a), int(b)) for a, b in zip(starts, starts[1:])]
+
+
+def policy_loss(logp, adv, old=None, infer=None, ref=None, entropy=None, target=None, starts=None, ratio="token", norm="tokens", adv_seq=False,
+                clip_low=0.2, clip_high=0.2, dual_clip=0.0, weight_cap=np.inf, kl_coef=0.0, entropy_coef=0.0, scale=1.0):
+    """stats [8], dlogp, dentropy [n] and their bounds."""
+    n = len(logp)
+    lo, hi, dual, cap, beta, gamma, scale = (float(np.float32(v)) for v in (clip_low, clip_high, dual_clip, weight_cap, kl_coef, entropy_coef, scale))
+    live = np.zeros(n, dtype=bool)
+    seqs = spans(starts, n)
+    for a, b in seqs:
+        live[a:b] = True
+    if target is not None:
+        live &= target >= 0
+    groups = [np.arange(a, b)[live[a:b]] for a, b in seqs]
+    N, S = sum(len(g) for g in groups), sum(len(g) > 0 for g in groups)
+    dl, dh, tl, th = np.zeros(n), np.zeros(n), np.zeros(n), np.zeros(n)
+    parts, room, cuts, weights, wroom = np.zeros(3), np.zeros(3), 0, 0.0, 0.0
+    with np.errstate(all="ignore"):
+        borders = np.log1p(hi), np.log1p(-lo), np.log(dual) if dual else np.inf
+        for q, g in enumerate(groups):
+            m = len(g)
+            if m == 0:
+                continue
+            nu = scale / N if norm == "tokens" else scale / (S * m) if norm == "sequences" else scale
+            x = logp[g]
+            A = np.full(m, adv[q]) if adv_seq else adv[g]
+            o = x if old is None else old[g]
+            d = x - o
+            # the ratio's exponent is rounded once; exp by three roundings
+            if ratio == "sequence":
+                d = np.full(m, d.mean())
+            r = np.exp(d)
+            tr = U * (np.abs(d) + 6)
+            lw = np.zeros(m) if infer is None else o - infer[g]
+            w = np.minimum(np.exp(lw), cap) if infer is not None else np.ones(m)
+            tw = U * (np.abs(lw) + 6)
+            up, down, over = d > borders[0], d < borders[1], d > borders[2]
+            used = np.where(A > 0, np.where(up, 1 + hi, r), np.where(over, dual, np.where(down, 1 - lo, r)))
+            cut = np.where(A > 0, up, np.where(A < 0, down | over, False)).astype(bool)
+            part = np.where(cut, 0.0, -w * A * r)
+            part[A == 0] = 0.0
+            l = np.where(A == 0, 0.0, -w * A * used)
+            tpart = np.abs(part) * (tr + tw + 8 * U)
+            if ratio == "sequence":
+                part, tpart = np.full(m, part.mean()), np.full(m, tpart.mean() + 4 * U * np.abs(part).mean())
+            tl[g] = tpart
+            dl[g] = part
+            parts[0] += nu * l.sum()
+            room[0] += abs(nu) * (np.abs(l) * (tr + tw + 12 * U)).sum()
+            if ref is not None:
+                k = ref[g] - x
+                dl[g] -= beta * np.expm1(k)
+                tl[g] += abs(beta) * U * (8 * np.abs(np.expm1(k)) + np.exp(k) * np.abs(k))
+                parts[1] += nu * (np.expm1(k) - k).sum()
+                room[1] += abs(nu) * U * (12 * np.abs(np.expm1(k) - k) + 2 * np.abs(np.expm1(k) * k) + 4 * np.abs(k) * (np.abs(k) > 0.12)).sum()
+            if entropy is not None:
+                parts[2] += nu * entropy[g].sum()
+                room[2] += abs(nu) * 4 * U * np.abs(entropy[g]).sum()
+            dl[g] *= nu
+            tl[g] = abs(nu) * tl[g] + 4 * U * np.abs(dl[g])
+            dh[g] = -gamma * nu
+            th[g] = 4 * U * np.abs(dh[g])
+            cuts += cut.sum()
+            weights += w.sum()
+            wroom += (w * tw).sum()
+    one = max(N, 1)
+    inv = 1 / scale if scale else 0.0
+    stats = np.array([parts[0] + beta * parts[1] - gamma * parts[2], parts[0], parts[1] * inv, parts[2] * inv, cuts / one, weights / one, N, S])
+    tol = np.array([room[0] + abs(beta) * room[1] + abs(gamma) * room[2], room[0], room[1] * abs(inv), room[2] * abs(inv), 0.0, wroom / one, 0.0, 0.0])
+    tol += 2 * U * np.abs(stats) + 1e-37
+    return {"stats": stats, "dlogp": dl, "dentropy": dh, "tol_stats": tol, "tol_dlogp": tl + 1e-37, "tol_dentropy": th + 1e-37}
+
+
+def balance_loss(z, idx, starts=None, alpha=0.01, zeta=0.0):
+    """z [T,E], idx [T,K].  stats [3], counts, probs [groups,E], dlogits [T,E] and bounds."""
+    T, E = z.shape
+    K = idx.shape[1]
+    alpha, zeta = float(np.float32(alpha)), float(np.float32(zeta))
+    groups = spans(starts, T)
+    some, N = max(1, sum(b > a for a, b in groups)), max(1, sum(b - a for a, b in groups))
+    out = {"counts": np.zeros((len(groups), E), dtype=np.int64), "probs": np.zeros((len(groups), E)), "dlogits": np.zeros((T, E)),
+           "tol_probs": np.zeros((len(groups), E)), "tol_dlogits": np.zeros((T, E))}
+    bal = zl = tb = tz = 0.0
+    C = 16 + E / 8              # sums over a row, by 2 to 64 lanes
+    with np.errstate(all="ignore"):
+        for g, (a, b) in enumerate(groups):
+            if a >= b:
+                continue
+            n = b - a
+            ids = idx[a:b].reshape(-1)
+            c = np.bincount(ids[ids < E], minlength=E)
+            out["counts"][g] = c
+            f = c * E / (K * n)
+            m = z[a:b].max(1, keepdims=True)
+            empty = m[:, 0] == -np.inf
+            x = np.where(empty[:, None], -np.inf, z[a:b] - np.where(empty[:, None], 0.0, m))
+            e = np.exp(x)
+            S = e.sum(1, keepdims=True)
+            p = np.where(empty[:, None], 0.0, e / np.where(empty[:, None], 1.0, S))
+            ax = np.where(p > 0, -x, 0.0)
+            lse = np.where(empty, 0.0, np.where(empty, 0.0, m[:, 0]) + np.log(np.where(empty, 1.0, S[:, 0])))
+            ts = U * (C + 3 * (p * ax).sum(1, keepdims=True))       # S, relative
+            tp = p * (U * (3 * ax + 8) + ts)
+            mean = (f * p).sum(1, keepdims=True)
+            tm = (f * tp).sum(1, keepdims=True) + U * C * mean
+            tlse = ts[:, 0] + 3 * U * (np.abs(lse) + np.log(np.where(empty, 1.0, S[:, 0])))
+            ga, gz = alpha / (some * n), 2 * zeta / N
+            out["dlogits"][a:b] = ga * p * (f - mean) + gz * lse[:, None] * p
+            out["tol_dlogits"][a:b] = (tp * (abs(ga) * np.abs(f - mean) + np.abs(gz * lse)[:, None]) + p * (abs(ga) * (tm + 4 * U * (f + mean))
+                                       + np.abs(gz) * tlse[:, None] + 4 * U * np.abs(gz * lse)[:, None])) + 1e-37
+            out["probs"][g] = p.mean(0)
+            out["tol_probs"][g] = tp.mean(0) + U * (200 + T / 1000) * p.mean(0) + 1e-37
+            bal += mean.sum() / n
+            tb += tm.sum() / n
+            zl += (lse ** 2).sum()
+            tz += (2 * np.abs(lse) * tlse + tlse ** 2).sum()
+    bal, zl = bal / some, zl / N
+    out["stats"] = np.array([alpha * bal + zeta * zl, bal, zl])
+    out["tol_stats"] = np.array([abs(alpha) * tb / some + abs(zeta) * tz / N, tb / some, tz / N]) + 2 * U * (
+        np.abs(out["stats"]) + np.array([abs(alpha * bal) + abs(zeta * zl), 0, 0])) + 1e-37
+    return out

@@ -1,6 +1,7 @@
 // C ABI of the replayed MoE layer: argument checks, workspace carving and the
 // launch sequence of each call.  See include/r3.h for the contract.
 #include <atomic>
+#include <cfloat>
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
@@ -50,6 +51,15 @@ bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 bool overlap(const void *p, size_t np, const void *q, size_t nq) {
     return p && q && (uintptr_t)p < (uintptr_t)q + nq && (uintptr_t)q < (uintptr_t)p + np;
 }
+// whether an output shares bytes with another array; the first `outs` of them are outputs
+struct Span { const void *p; size_t bytes; };
+template <int N> bool any_overlap(const Span (&at)[N], int outs) {
+    for (int i = 0; i < outs; ++i)
+        for (int j = i + 1; j < N; ++j)
+            if (overlap(at[i].p, at[i].bytes, at[j].p, at[j].bytes)) return true;
+    return false;
+}
+bool finite(float v) { return v >= -FLT_MAX && v <= FLT_MAX; }
 bool force_simt() {
     const char *v = getenv("R3_FORCE_SIMT");
     return v && v[0] == '1';
@@ -552,6 +562,83 @@ int r3_token_logprobs_backward(int64_t n, int64_t V, int dtype, const void *logi
                                                  (hipStream_t)stream));
 }
 
+
+static int check_policy(const r3_policy_desc *D) {
+    if (!D || D->n < 0 || D->nseq < 0 || (D->flags & ~R3_FLAG_SEQ_ADVANTAGE)) return R3_ERR_INVALID_ARG;
+    if ((D->ratio != R3_RATIO_TOKEN && D->ratio != R3_RATIO_SEQUENCE) || D->norm < R3_MEAN_TOKENS || D->norm > R3_SUM) return R3_ERR_INVALID_ARG;
+    if (!(D->clip_low >= 0.0f && D->clip_low <= 1.0f) || !(D->clip_high >= 0.0f && finite(D->clip_high)) ||
+        !(D->dual_clip == 0.0f || (D->dual_clip > 1.0f && finite(D->dual_clip))) || !(D->weight_cap > 0.0f) || !finite(D->kl_coef) ||
+        !finite(D->entropy_coef) || !finite(D->scale))
+        return R3_ERR_INVALID_ARG;
+    if (D->n > 0x7fffffffll - 65536 || D->nseq > 0x7fffffff - 65536) return R3_ERR_UNSUPPORTED;
+    return R3_OK;
+}
+
+size_t r3_policy_loss_workspace_bytes(const r3_policy_desc *desc) {
+    return check_policy(desc) == R3_OK ? policy_loss_ws_bytes(desc->n, desc->nseq) : 0;
+}
+
+int r3_policy_loss(const r3_policy_desc *desc, const float *logp, const float *logp_old, const float *logp_infer, const float *logp_ref,
+                   const float *entropy, const float *advantage, const int32_t *target, const int32_t *seq_start, float *dlogp,
+                   float *dentropy, float *stats, int32_t *status_word, void *ws, size_t ws_bytes, void *stream) {
+    const int rc = check_policy(desc);
+    if (rc) return rc;
+    const r3_policy_desc &D = *desc;
+    if (!stats || (D.n > 0 && (!logp || !advantage)) || (seq_start && D.nseq == 0)) return R3_ERR_INVALID_ARG;
+    if (D.n > 0 && ((D.kl_coef != 0.0f && !logp_ref) || (D.entropy_coef != 0.0f && !entropy))) return R3_ERR_INVALID_ARG;
+    const void *words[] = {logp, logp_old, logp_infer, logp_ref, entropy, advantage, target, seq_start, dlogp, dentropy, stats, status_word};
+    for (const void *p : words)
+        if (!aligned(p, 4)) return R3_ERR_INVALID_ARG;
+    const size_t need = policy_loss_ws_bytes(D.n, D.nseq);
+    if (!ws || ws_bytes < need || !aligned(ws, 256)) return R3_ERR_WORKSPACE;
+    const size_t word = (size_t)D.n * 4, seqs = (size_t)(seq_start ? D.nseq : 1) * 4;
+    const Span at[] = {{dlogp, word}, {dentropy, word}, {stats, 32}, {status_word, 4}, {ws, need}, {logp, word}, {logp_old, word}, {logp_infer, word},
+                       {logp_ref, word}, {entropy, word}, {advantage, D.flags & R3_FLAG_SEQ_ADVANTAGE ? seqs : word}, {target, word}, {seq_start, seqs + 4}};
+    if (any_overlap(at, 5)) return R3_ERR_INVALID_ARG;
+    return hip_rc(launch_policy_loss(D, logp, logp_old, logp_infer, logp_ref, entropy, advantage, target, seq_start, dlogp, dentropy, stats,
+                                     status_word, ws, (hipStream_t)stream));
+}
+
+// of the descriptor, T, E, K and the record's fields
+static int check_routing_desc(const r3_layer_desc *D, Dims &m) {
+    if (!D) return R3_ERR_INVALID_ARG;
+    r3_layer_desc routing = *D;
+    routing.d = routing.F = 1;
+    routing.act = R3_F32;
+    routing.flags = 0;
+    return check_desc(&routing, m);
+}
+
+size_t r3_balance_loss_workspace_bytes(const r3_layer_desc *desc, int nseq) {
+    Dims m;
+    return check_routing_desc(desc, m) == R3_OK && nseq >= 0 && nseq <= 0x7fffffff - 65536 ? balance_loss_ws_bytes(m.T, m.E, nseq) : 0;
+}
+
+int r3_balance_loss(const r3_layer_desc *desc, const float *logits, int64_t ld, const void *idx, const int32_t *seq_start, int nseq,
+                    float balance_coef, float z_coef, int32_t *counts, float *probs, float *stats, float *dlogits, int64_t ldd,
+                    int32_t *status_word, void *ws, size_t ws_bytes, void *stream) {
+    Dims m;
+    const int rc = check_routing_desc(desc, m);
+    if (rc) return rc;
+    if (!logits || !idx || !stats || ld < m.E || (dlogits && ldd < m.E) || (seq_start ? nseq < 1 : nseq != 0) || !finite(balance_coef) || !finite(z_coef))
+        return R3_ERR_INVALID_ARG;
+    const void *words[] = {logits, seq_start, counts, probs, stats, dlogits, status_word};
+    for (const void *p : words)
+        if (!aligned(p, 4)) return R3_ERR_INVALID_ARG;
+    if (m.idx == R3_IDX_U16 && !aligned(idx, 2)) return R3_ERR_INVALID_ARG;
+    if (nseq > 0x7fffffff - 65536 || rows_too_far(m.T, ld) || (dlogits && rows_too_far(m.T, ldd)) || rows_too_far(m.T, m.stride)) return R3_ERR_UNSUPPORTED;
+    const size_t need = balance_loss_ws_bytes(m.T, m.E, nseq);
+    if (!ws || ws_bytes < need || !aligned(ws, 256)) return R3_ERR_WORKSPACE;
+    const size_t ib = m.idx == R3_IDX_U8 ? 1 : 2, groups = (size_t)(nseq > 0 ? nseq : 1) * m.E * 4;
+    const bool own_place = dlogits == logits && ldd == ld;
+    const Span at[] = {{dlogits, ((size_t)(m.T - 1) * ldd + m.E) * 4}, {counts, groups}, {probs, groups}, {stats, 12}, {status_word, 4}, {ws, need},
+                       {own_place ? nullptr : logits, ((size_t)(m.T - 1) * ld + m.E) * 4}, {idx, ((size_t)(m.T - 1) * m.stride + m.K) * ib},
+                       {seq_start, ((size_t)nseq + 1) * 4}};
+    if (any_overlap(at, 6)) return R3_ERR_INVALID_ARG;
+    return hip_rc(launch_balance_loss(m.T, m.E, m.K, logits, ld, idx, m.idx, m.stride, seq_start, nseq, balance_coef, z_coef, counts, probs, stats,
+                                      dlogits, ldd, status_word, ws, (hipStream_t)stream));
+}
+
 static const float kQuintic[3] = {3.4445f, -4.775f, 2.0315f};
 
 static bool ortho_sizes_ok(int64_t batch, int64_t rows, int64_t cols) {
@@ -567,10 +654,10 @@ int r3_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int dtype_in, co
                      const float *coef, float eps, float scale, int32_t *status_word, void *ws, size_t ws_bytes, void *stream) {
     if (batch < 0 || rows <= 0 || cols <= 0 || (dtype_in != R3_BF16 && dtype_in != R3_F32) || (dtype_out != R3_BF16 && dtype_out != R3_F32))
         return R3_ERR_INVALID_ARG;
-    if (steps < 1 || steps > R3_MAX_STEPS || !(eps >= 0.0f && eps <= 1e30f) || !(scale >= -1e30f && scale <= 1e30f)) return R3_ERR_INVALID_ARG;
+    if (steps < 1 || steps > R3_MAX_STEPS || !(eps >= 0.0f && finite(eps)) || !finite(scale)) return R3_ERR_INVALID_ARG;
     const float *q = coef ? coef : kQuintic;
     for (int i = 0; i < 3; ++i)
-        if (!(q[i] >= -1e30f && q[i] <= 1e30f)) return R3_ERR_INVALID_ARG;
+        if (!finite(q[i])) return R3_ERR_INVALID_ARG;
     const size_t ib = dtype_in == R3_BF16 ? 2 : 4, ob = dtype_out == R3_BF16 ? 2 : 4;
     if (!aligned(G, ib) || !aligned(out, ob) || !aligned(status_word, 4)) return R3_ERR_INVALID_ARG;
     if (!ortho_sizes_ok(batch, rows, cols) || !orthogonalize_in_range(steps, q)) return R3_ERR_UNSUPPORTED;
@@ -579,9 +666,8 @@ int r3_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int dtype_in, co
     const size_t need = orthogonalize_ws_bytes(batch, rows, cols, dtype_out);
     if (!ws || ws_bytes < need || !aligned(ws, 256)) return R3_ERR_WORKSPACE;
     const size_t n = (size_t)batch * rows * cols;
-    if ((!(out == G && ib == ob) && overlap(G, n * ib, out, n * ob)) || overlap(G, n * ib, ws, need) || overlap(out, n * ob, ws, need) ||
-        overlap(status_word, 4, G, n * ib) || overlap(status_word, 4, out, n * ob) || overlap(status_word, 4, ws, need))
-        return R3_ERR_INVALID_ARG;
+    const Span at[] = {{out, n * ob}, {status_word, 4}, {ws, need}, {out == G && ib == ob ? nullptr : G, n * ib}};
+    if (any_overlap(at, 3)) return R3_ERR_INVALID_ARG;
     return hip_rc(launch_orthogonalize(batch, rows, cols, dtype_in, G, dtype_out, out, steps, q, eps, scale, status_word, ws,
                                        (hipStream_t)stream));
 }

@@ -10,7 +10,8 @@ enum ProfTag {
     PROF_RECORD = 0, PROF_LOGITS, PROF_GATE, PROF_PERMUTE_INDEX, PROF_GATHER_ROWS, PROF_FFN1, PROF_FFN2,
     PROF_COMBINE, PROF_GATE_BWD, PROF_DWR, PROF_DH, PROF_WGRAD, PROF_DXP, PROF_DX_FINISH, PROF_WGRAD_PAIR,
     PROF_ROUTING_DIFF, PROF_POLICY, PROF_CACHE_APPEND, PROF_CACHE_GATHER, PROF_AGREEMENT, PROF_LOGPROBS, PROF_LOGPROBS_BWD,
-    PROF_COMBINE_BWD, PROF_PERMUTE_BWD, PROF_ORTHO, PROF_NTAGS
+    PROF_COMBINE_BWD, PROF_PERMUTE_BWD, PROF_ORTHO, PROF_POLICY_LOSS, PROF_BALANCE_LOSS,
+    PROF_NTAGS
 };
 struct ProfScope {
     int tag, slot;
@@ -79,6 +80,16 @@ hipError_t launch_combine_backward(int T, int d, int K, int act, const void *dy,
                                    void *dYp, float *dgates, float *dz, hipStream_t s);
 hipError_t launch_permute_backward(int T, int d, int K, int act, const void *dXp, const int32_t *inv_perm, const void *add, void *dx,
                                    hipStream_t s);
+
+// r3_losses.hip (nseq < 1, or no seq_start: one sequence of everything)
+size_t policy_loss_ws_bytes(int64_t n, int nseq);
+hipError_t launch_policy_loss(const r3_policy_desc &D, const float *logp, const float *old, const float *infer, const float *ref,
+                              const float *entropy, const float *adv, const int32_t *target, const int32_t *seq_start, float *dlogp,
+                              float *dentropy, float *stats, int32_t *status, void *ws, hipStream_t s);
+size_t balance_loss_ws_bytes(int64_t T, int E, int nseq);
+hipError_t launch_balance_loss(int T, int E, int K, const float *logits, int64_t ld, const void *idx, int idx_dtype, int64_t stride,
+                               const int32_t *seq_start, int nseq, float alpha, float zeta, int32_t *counts, float *probs, float *stats,
+                               float *dlogits, int64_t ldd, int32_t *status, void *ws, hipStream_t s);
 
 // r3_ortho.hip
 size_t orthogonalize_ws_bytes(int64_t batch, int64_t rows, int64_t cols, int dtype_out);

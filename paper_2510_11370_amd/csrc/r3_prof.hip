@@ -22,7 +22,7 @@ const char *kNames[PROF_NTAGS] = {"record_topk", "router_logits", "replay_gate",
                                   "router_wgrad", "ffn_dh", "ffn_wgrad_down", "ffn_dxp", "dx_finish",
                                   "ffn_wgrad_gate_up", "routing_diff", "policy_discrepancy",
                                   "mask_cache_append", "mask_cache_gather", "agreement", "token_logprobs",
-                                  "token_logprobs_backward", "combine_backward", "permute_backward", "orthogonalize"};
+                                  "token_logprobs_backward", "combine_backward", "permute_backward", "orthogonalize", "policy_loss", "balance_loss"};
 }  // namespace
 
 ProfScope::ProfScope(int tag_, hipStream_t s_) : tag(tag_), slot(-1), s(s_) {

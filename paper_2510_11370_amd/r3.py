@@ -25,15 +25,25 @@ EXPORTS = ["r3_version", "r3_workspace_bytes", "r3_record_topk", "r3_replay_gate
            "r3_profile_mfma", "r3_profile_mfma_flops", "r3_profile_gemm_mix", "r3_routing_diff", "r3_policy_discrepancy",
            "r3_policy_workspace_bytes", "r3_mask_cache_append", "r3_mask_cache_gather",
            "r3_combine_backward", "r3_permute_backward", "r3_token_logprobs_workspace_bytes", "r3_token_logprobs",
-           "r3_token_logprobs_backward", "r3_orthogonalize_workspace_bytes", "r3_orthogonalize"]
+           "r3_token_logprobs_backward", "r3_orthogonalize_workspace_bytes", "r3_orthogonalize",
+           "r3_policy_loss_workspace_bytes", "r3_policy_loss", "r3_balance_loss_workspace_bytes", "r3_balance_loss"]
 MAX_TOP = 32
 MAX_STEPS = 64
+RATIO = {"token": 0, "sequence": 1}
+NORM = {"tokens": 0, "sequences": 1, "sum": 2}
+FLAG_SEQ_ADVANTAGE = 1
 
 
 class LayerDesc(C.Structure):
     _fields_ = [("T", C.c_int32), ("d", C.c_int32), ("E", C.c_int32), ("K", C.c_int32),
                 ("F", C.c_int32), ("act", C.c_int32), ("idx", C.c_int32), ("flags", C.c_int32),
                 ("idx_token_stride", C.c_int64)]
+
+
+class PolicyDesc(C.Structure):
+    _fields_ = [("n", C.c_int64), ("nseq", C.c_int32), ("ratio", C.c_int32), ("norm", C.c_int32), ("flags", C.c_int32),
+                ("clip_low", C.c_float), ("clip_high", C.c_float), ("dual_clip", C.c_float), ("weight_cap", C.c_float),
+                ("kl_coef", C.c_float), ("entropy_coef", C.c_float), ("scale", C.c_float)]
 
 
 class R3Error(RuntimeError):
@@ -69,6 +79,12 @@ def lib():
         L.r3_orthogonalize_workspace_bytes.restype = C.c_size_t
         L.r3_orthogonalize_workspace_bytes.argtypes = [i64, i64, i64, i32]
         L.r3_orthogonalize.argtypes = [i64, i64, i64, i32, p, i32, p, i32, C.POINTER(f32), f32, f32, p, p, C.c_size_t, p]
+        L.r3_policy_loss_workspace_bytes.restype = C.c_size_t
+        L.r3_policy_loss_workspace_bytes.argtypes = [C.POINTER(PolicyDesc)]
+        L.r3_policy_loss.argtypes = [C.POINTER(PolicyDesc)] + [p] * 13 + [C.c_size_t, p]
+        L.r3_balance_loss_workspace_bytes.restype = C.c_size_t
+        L.r3_balance_loss_workspace_bytes.argtypes = [C.POINTER(LayerDesc), i32]
+        L.r3_balance_loss.argtypes = [C.POINTER(LayerDesc), p, i64, p, p, i32, f32, f32, p, p, p, p, i64, p, p, C.c_size_t, p]
         _lib = L
     return _lib
 
@@ -280,6 +296,77 @@ def token_logprobs_backward(logits, target, stats, dlogits, dlogp=None, entropy=
         _at(w, "dentropy", dentropy, dev, f, (n,)), dlogits.data_ptr(), ldd, _raw_stream(dev)), "r3_token_logprobs_backward")
 
 
+def _workspace(what, ws, dev, make):
+    if ws is None:
+        return make()
+    if ws.get_device() != dev or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        raise R3Error("%s: ws has to be a dense uint8 tensor on cuda:%d" % (what, dev))
+    return ws
+
+
+def policy_desc(n, nseq=1, ratio="token", norm="tokens", adv_seq=False, clip_low=0.2, clip_high=0.2, dual_clip=0.0,
+                weight_cap=float("inf"), kl_coef=0.0, entropy_coef=0.0, scale=1.0):
+    """ratio: "token" or "sequence"; norm: "tokens", "sequences" or "sum"; adv_seq: an advantage to a sequence, not to a token.
+    dual_clip 0: none."""
+    return PolicyDesc(n, nseq, RATIO[ratio], NORM[norm], FLAG_SEQ_ADVANTAGE if adv_seq else 0, clip_low, clip_high, dual_clip,
+                      weight_cap, kl_coef, entropy_coef, scale)
+
+
+def policy_loss_workspace(D, device="cuda"):
+    """A workspace tensor for policy_loss."""
+    return torch.empty(max(lib().r3_policy_loss_workspace_bytes(C.byref(D)), 256), dtype=torch.uint8, device=device)
+
+
+def policy_loss(D, logp, advantage, stats, logp_old=None, logp_infer=None, logp_ref=None, entropy=None, target=None, seq_start=None,
+                dlogp=None, dentropy=None, status=None, ws=None):
+    """Clipped policy loss of n tokens in packed sequences (seq_start int32 [nseq+1]; None: one): stats [8] float32 (loss, its
+    policy, KL and entropy parts, share of clipped tokens, mean weight, live tokens, live sequences), gradients dlogp and dentropy
+    [n].  A token with target (int32 [n]) -1 is left out.  advantage [n], or [nseq] with adv_seq.  ws: policy_loss_workspace(D)."""
+    w, dev, f, i, n = "policy_loss", _device("policy_loss", logp), torch.float32, torch.int32, (D.n,)
+    ws = _workspace(w, ws, dev, lambda: policy_loss_workspace(D, logp.device))
+    seqs = D.nseq if seq_start is not None else 1
+    _check(lib().r3_policy_loss(
+        C.byref(D), _at(w, "logp", logp, dev, f, n), _at(w, "logp_old", logp_old, dev, f, n), _at(w, "logp_infer", logp_infer, dev, f, n),
+        _at(w, "logp_ref", logp_ref, dev, f, n), _at(w, "entropy", entropy, dev, f, n),
+        _at(w, "advantage", advantage, dev, f, (seqs,) if D.flags & FLAG_SEQ_ADVANTAGE else n), _at(w, "target", target, dev, i, n),
+        _at(w, "seq_start", seq_start, dev, i, (seqs + 1,)), _at(w, "dlogp", dlogp, dev, f, n), _at(w, "dentropy", dentropy, dev, f, n),
+        _at(w, "stats", stats, dev, f, (8,)), _at(w, "status", status, dev, i, (1,)), ws.data_ptr(), ws.numel(), _raw_stream(dev)),
+        "r3_policy_loss")
+
+
+def balance_loss_workspace(D, nseq=0, device="cuda"):
+    """A workspace tensor for balance_loss; nseq: sequences in seq_start, 0 without it."""
+    return torch.empty(max(lib().r3_balance_loss_workspace_bytes(C.byref(D), nseq), 256), dtype=torch.uint8, device=device)
+
+
+def _rows(what, name, t, dev, T, E):
+    """Address and row stride of [T, E] float32 rows, each of them dense"""
+    if t is None:
+        return 0, E
+    if t.dtype is not torch.float32 or t.get_device() != dev or t.shape != (T, E) or (E > 1 and t.stride(1) != 1):
+        raise R3Error("%s: %s has to be float32 rows of shape %s on cuda:%d" % (what, name, (T, E), dev))
+    return t.data_ptr(), t.stride(0) if T > 1 else max(E, t.stride(0))
+
+
+def balance_loss(D, logits, idx, stats, counts=None, probs=None, dlogits=None, seq_start=None, balance_coef=0.01, z_coef=0.0, status=None,
+                 ws=None):
+    """Load-balance loss of the record idx (as replay_gate takes it) and z-loss of the router's logits [T,E] (rows may be strided):
+    stats [3] float32 (loss, balance, z), counts (int32) and probs [groups,E], dlogits [T,E], which may be logits.  Groups: the
+    sequences of seq_start (int32 [nseq+1]), or the whole batch.  ws: balance_loss_workspace(D, nseq)."""
+    w, dev, f, i = "balance_loss", _device("balance_loss", logits), torch.float32, torch.int32
+    nseq = 0 if seq_start is None else seq_start.numel() - 1
+    groups = (max(nseq, 1), D.E)
+    ws = _workspace(w, ws, dev, lambda: balance_loss_workspace(D, nseq, logits.device))
+    at, ld = _rows(w, "logits", logits, dev, D.T, D.E)
+    dat, ldd = _rows(w, "dlogits", dlogits, dev, D.T, D.E)
+    if idx.get_device() != dev or idx.dtype is not idx_torch_dtype(D) or idx.numel() < D.T * D.K:
+        raise R3Error("%s: idx has to be the record of desc's type on cuda:%d" % (w, dev))
+    _check(lib().r3_balance_loss(
+        C.byref(D), at, ld, idx.data_ptr(), _at(w, "seq_start", seq_start, dev, i, (nseq + 1,)), nseq, balance_coef, z_coef,
+        _at(w, "counts", counts, dev, i, groups), _at(w, "probs", probs, dev, f, groups), _at(w, "stats", stats, dev, f, (3,)), dat, ldd,
+        _at(w, "status", status, dev, i, (1,)), ws.data_ptr(), ws.numel(), _raw_stream(dev)), "r3_balance_loss")
+
+
 _FLOATS = {torch.bfloat16: BF16, torch.float32: F32}
 
 
@@ -304,10 +391,7 @@ def orthogonalize(G, out, steps=5, coef=None, eps=1e-7, scale=1.0, status=None, 
     w = "orthogonalize"
     b, r, c, src, to = _matrices(w, G, out)
     dev = _device(w, G)
-    if ws is None:
-        ws = orthogonalize_workspace(G, out)
-    elif ws.get_device() != dev or ws.dtype is not torch.uint8 or not ws.is_contiguous():
-        raise R3Error("%s: ws has to be a dense uint8 tensor on cuda:%d" % (w, dev))
+    ws = _workspace(w, ws, dev, lambda: orthogonalize_workspace(G, out))
     _check(lib().r3_orthogonalize(
         b, r, c, src, _at(w, "G", G, dev, G.dtype, G.shape), to, _at(w, "out", out, dev, out.dtype, G.shape), steps,
         None if coef is None else (C.c_float * 3)(*coef), eps, scale, _at(w, "status", status, dev, torch.int32, (1,)),

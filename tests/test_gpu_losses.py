@@ -1,0 +1,303 @@
+"""r3_policy_loss and r3_balance_loss against oracle/operators.py (64 bits)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as ref
+from paper_2510_11370_amd import r3
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _near(got, want, tol, what):
+    got = got.cpu().double().numpy()
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (what, np.argwhere(bad)[:3].tolist(), got[bad][:3], want[bad][:3], np.broadcast_to(tol, got.shape)[bad][:3])
+
+
+def _starts(kind, n, seed=0):
+    rng = np.random.default_rng(seed + n)
+    if kind == "none":
+        return None
+    if kind == "one":
+        return np.array([0, n])
+    if kind == "singles":
+        return np.arange(n + 1)
+    if kind == "inside":          # tokens before the first and behind the last
+        return np.array([n // 5, n // 5, n // 2, n - n // 4])
+    if kind == "empty":
+        return np.array([0, 0, 0, n // 3, n // 3, n, n])
+    if kind == "nothing":
+        return np.array([n // 2, n // 2])
+    cuts = np.sort(rng.integers(0, n + 1, {"few": 3, "many": max(1, n // 9)}[kind]))
+    return np.concatenate([[0], cuts, [n]])
+
+
+def _policy(n, starts, seed=0, adv_seq=False, skip=0.3):
+    rng = np.random.default_rng(seed + 7 * n)
+    nseq = 1 if starts is None else len(starts) - 1
+    f = lambda v: v.astype(np.float32)  # noqa: E731
+    logp = f(-np.abs(rng.normal(0, 2, n)))
+    old = f(logp + rng.normal(0, 0.3, n))
+    a = {"logp": logp, "old": old, "infer": f(old + rng.normal(0, 0.3, n)), "ref": f(logp + rng.normal(0, 0.4, n)),
+         "entropy": f(np.abs(rng.normal(0, 1, n))), "adv": f(rng.normal(0, 1, nseq if adv_seq else n)),
+         "target": np.where(rng.random(n) < skip, -1, rng.integers(0, 1000, n)).astype(np.int32)}
+    a["adv"][::7] = 0.0
+    # some tokens far from the others, on each side
+    a["old"][::11] -= np.float32(2.0)
+    a["old"][::13] += np.float32(2.0)
+    a["ref"][::5] = a["logp"][::5] + f(rng.normal(0, 1e-3, len(a["ref"][::5])))
+    return a
+
+
+def _run_policy(a, starts, gradients=True, **kw):
+    D = r3.policy_desc(len(a["logp"]), 1 if starts is None else len(starts) - 1, **kw)
+    t = {k: None if v is None else torch.tensor(v, device=DEV) for k, v in a.items()}
+    n = D.n
+    stats, status = torch.full((9,), 77.0, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    dl, dh = (torch.full((n + 3,), 77.0, device=DEV) for _ in range(2))
+    r3.policy_loss(D, t["logp"], t["adv"], stats[:8], logp_old=t["old"], logp_infer=t["infer"], logp_ref=t["ref"], entropy=t["entropy"],
+                   target=t["target"], seq_start=None if starts is None else torch.tensor(starts, dtype=torch.int32, device=DEV),
+                   dlogp=dl[:n] if gradients else None, dentropy=dh[:n] if gradients else None, status=status)
+    assert stats[8] == 77 and (dl[n if gradients else 0:] == 77).all() and (dh[n if gradients else 0:] == 77).all()
+    return {"stats": stats[:8], "dlogp": dl[:n], "dentropy": dh[:n]}, status.item()
+
+
+def _check_policy(a, starts, **kw):
+    got, status = _run_policy(a, starts, **kw)
+    c = {k: None if v is None else (v if v.dtype.kind == "i" else v.astype(np.float64)) for k, v in a.items()}
+    want = ref.policy_loss(c["logp"], c["adv"], c["old"], c["infer"], c["ref"], c["entropy"], c["target"], starts, **kw)
+    for k in got:
+        _near(got[k], want[k], want["tol_" + k], k)
+    assert status == 0
+    return got
+
+
+ALL = dict(kl_coef=0.05, entropy_coef=0.01, weight_cap=1.3, clip_high=0.28)
+
+
+@pytest.mark.parametrize("ratio", ["token", "sequence"])
+@pytest.mark.parametrize("norm", ["tokens", "sequences", "sum"])
+@pytest.mark.parametrize("kind", ["none", "one", "singles", "inside", "empty", "nothing", "few", "many"])
+@pytest.mark.parametrize("n", [1, 2, 63, 500, 513, 2500])
+def test_policy_loss(n, kind, norm, ratio):
+    starts = _starts(kind, n)
+    for adv_seq in (False, True):
+        a = _policy(n, starts, adv_seq=adv_seq)
+        got = _check_policy(a, starts, ratio=ratio, norm=norm, adv_seq=adv_seq, dual_clip=3.0 if adv_seq else 0.0, scale=0.7, **ALL)
+        alone, _ = _run_policy(a, starts, gradients=False, ratio=ratio, norm=norm, adv_seq=adv_seq, dual_clip=3.0 if adv_seq else 0.0, scale=0.7, **ALL)
+        assert torch.equal(alone["stats"], got["stats"])
+
+
+@pytest.mark.parametrize("ratio", ["token", "sequence"])
+@pytest.mark.parametrize("kind,n", [("one", 70001), ("few", 300007), ("many", 20011), ("singles", 9000), ("inside", 1100003)])
+def test_policy_loss_over_many_pieces(kind, n, ratio):
+    starts = _starts(kind, n)
+    a = _policy(n, starts)
+    one = _check_policy(a, starts, ratio=ratio, norm="sequences", **ALL)
+    again, _ = _run_policy(a, starts, ratio=ratio, norm="sequences", **ALL)
+    for k in one:
+        assert torch.equal(one[k], again[k]), k
+
+
+@pytest.mark.parametrize("without", ["old", "infer", "ref", "entropy", "target"])
+def test_arrays_that_are_not_given(without):
+    a = _policy(700, None)
+    a[without] = None
+    kw = dict(ALL)
+    if without == "ref":
+        kw["kl_coef"] = 0.0
+    if without == "entropy":
+        kw["entropy_coef"] = 0.0
+    _check_policy(a, None, **kw)
+    _check_policy(a, None, ratio="sequence", **kw)
+
+
+def test_nothing_is_live():
+    a = _policy(300, None)
+    a["target"][:] = -1
+    got = _check_policy(a, None, **ALL)
+    assert all((v == 0).all() for v in got.values())
+    stats = torch.full((8,), 7.0, device=DEV)
+    none = torch.empty(0, device=DEV)
+    r3.policy_loss(r3.policy_desc(0), none, none, stats, seq_start=torch.zeros(2, dtype=torch.int32, device=DEV))
+    assert (stats == 0).all()
+
+
+@pytest.mark.parametrize("ratio", ["token", "sequence"])
+def test_what_left_out_tokens_hold_does_not_matter(ratio):
+    starts = np.array([40, 300, 320, 900])
+    a = _policy(1000, starts)
+    b = {k: v.copy() for k, v in a.items()}
+    dead = a["target"] < 0
+    dead[:40] = dead[900:] = True
+    for k in ("logp", "old", "infer", "ref", "entropy", "adv"):
+        b[k][dead] = np.where(np.arange(dead.sum()) % 2, np.nan, np.inf)
+    x, _ = _run_policy(a, starts, ratio=ratio, **ALL)
+    y, status = _run_policy(b, starts, ratio=ratio, **ALL)
+    assert status == 0
+    for k in x:
+        assert torch.equal(x[k], y[k]), k
+
+
+@pytest.mark.parametrize("which", ["logp", "old", "infer", "ref", "entropy", "adv"])
+def test_a_value_that_is_not_a_number_is_told(which):
+    a = _policy(600, None, skip=0.0)
+    a[which][333] = np.nan
+    for ratio in ("token", "sequence"):
+        got, status = _run_policy(a, None, ratio=ratio, **ALL)
+        assert status == r3.DATA_NONFINITE and torch.isnan(got["stats"][0])
+        if ratio == "token":
+            bad = torch.isnan(got["dlogp"]).nonzero().view(-1).tolist()
+            assert bad == ([] if which == "entropy" else [333]) or (which in ("logp", "old", "infer", "adv") and set(bad) <= {333}), bad
+
+
+def test_masked_tokens_have_no_ratio():
+    """A token that the policy has masked since (log-probability -inf): ratio 0, no policy gradient for A > 0."""
+    a = _policy(64, None, skip=0.0)
+    a["logp"][5] = -np.inf
+    a["adv"][5] = 1.0
+    a["ref"] = None
+    got, status = _run_policy(a, None, entropy_coef=0.01)
+    assert status == 0 and got["dlogp"][5] == 0 and torch.isfinite(got["stats"]).all()
+
+
+def test_on_the_policy_the_gradient_is_the_advantage():
+    a = _policy(400, None)
+    for k in ("old", "infer", "ref", "entropy"):
+        a[k] = None
+    got, _ = _run_policy(a, None, norm="sum")
+    live = torch.tensor(a["target"] >= 0)
+    assert torch.equal(got["dlogp"].cpu(), torch.where(live, -torch.tensor(a["adv"]), torch.zeros(400)))
+    assert got["stats"][4] == 0 and got["stats"][5] == 1
+
+
+def test_the_gradient_against_differences():
+    n, h = 40, 2.0 ** -7
+    starts = np.array([0, 15, 15, 40])
+    a = _policy(n, starts)
+    for ratio in ("token", "sequence"):
+        got, _ = _run_policy(a, starts, ratio=ratio, norm="sequences", clip_low=1.0, clip_high=1e6, kl_coef=0.3, entropy_coef=0.0, weight_cap=2.0)
+        for i in np.flatnonzero(a["target"] >= 0)[:6]:
+            v = []
+            for s in (h, -h):
+                b = {k: x.copy() for k, x in a.items()}
+                b["logp"][i] += np.float32(s)
+                v.append(_run_policy(b, starts, ratio=ratio, norm="sequences", clip_low=1.0, clip_high=1e6, kl_coef=0.3, entropy_coef=0.0,
+                                     weight_cap=2.0)[0]["stats"][0].double().item())
+            # the third derivative's h^2 / 6 times terms of a few units, and roundings of the loss over 2 h
+            big = max(1.0, float(np.exp(np.abs(a["logp"] - a["old"]).max())))
+            assert abs((v[0] - v[1]) / (2 * h) - got["dlogp"][i].item()) < h * h * big + 64 * 2.0 ** -24 * max(1, abs(v[0])) / h, (ratio, i)
+
+
+# ---- balance ----
+
+def _routing(T, E, K, seed=0, dtype=None):
+    rng = np.random.default_rng(seed + T + E)
+    z = rng.normal(0, 1.5, (T, E)).astype(np.float32)
+    idx = np.argsort(-z - rng.gumbel(0, 0.3, (T, E)), 1)[:, :K]
+    return z, np.sort(idx, 1)
+
+
+def _run_balance(z, idx, starts, pad=0, dpad=0, stride=0, u16=False, keep=("counts", "probs", "dlogits"), **kw):
+    T, E = z.shape
+    K = idx.shape[1]
+    idt = torch.uint16 if u16 or E > 256 else torch.uint8
+    rec = np.full((T, max(stride, K)), 255 if idt is torch.uint8 else 65535)
+    rec[:, :K] = idx
+    D = r3.desc(T, 16, E, K, 16, idx_dtype=idt, idx_token_stride=stride)
+    full = torch.full((T, E + pad), 77.0, device=DEV)
+    full[:, :E] = torch.tensor(z)
+    groups = 1 if starts is None else len(starts) - 1
+    dfull = torch.full((T, E + dpad), 77.0, device=DEV)
+    out = {"counts": torch.full((groups, E), -7, dtype=torch.int32, device=DEV), "probs": torch.full((groups, E), 77.0, device=DEV), "dlogits": dfull[:, :E]}
+    stats, status = torch.full((3,), 77.0, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    rec_t = torch.tensor(rec.astype(np.uint8)) if idt is torch.uint8 else torch.tensor(rec.astype(np.int32)).to(torch.uint16)
+    r3.balance_loss(D, full[:, :E], rec_t.to(DEV), stats, **{k: out[k] for k in keep}, status=status,
+                    seq_start=None if starts is None else torch.tensor(starts, dtype=torch.int32, device=DEV), **kw)
+    assert (dfull[:, E:] == 77).all()
+    out["stats"] = stats
+    return out, status.item()
+
+
+def _check_balance(z, idx, starts, got, alpha, zeta):
+    want = ref.balance_loss(z.astype(np.float64), idx, starts, alpha, zeta)
+    assert np.array_equal(got["counts"].cpu().numpy(), want["counts"])
+    for k in ("stats", "probs", "dlogits"):
+        _near(got[k], want[k], want["tol_" + k], k)
+
+
+@pytest.mark.parametrize("T,E,K", [(1, 1, 1), (1, 8, 2), (5, 3, 2), (256, 8, 2), (300, 16, 1), (77, 60, 5), (200, 64, 6), (1025, 128, 8), (130, 256, 8),
+                                   (33, 257, 3), (65, 384, 6), (20, 513, 4), (9, 1030, 3), (5, 2100, 64), (3, 4096, 8), (4100, 31, 4)])
+@pytest.mark.parametrize("kind", ["none", "one", "inside", "empty", "many"])
+def test_balance_loss(T, E, K, kind):
+    starts = _starts(kind, T)
+    z, idx = _routing(T, E, K)
+    got, status = _run_balance(z, idx, starts, pad=T % 3, dpad=T % 2, stride=K + 2 if T % 2 else 0, balance_coef=0.3, z_coef=0.02)
+    assert status == 0
+    _check_balance(z, idx, starts, got, 0.3, 0.02)
+    for k in ("counts", "probs", "dlogits", None):
+        alone, _ = _run_balance(z, idx, starts, keep=() if k is None else (k,), balance_coef=0.3, z_coef=0.02)
+        assert torch.equal(alone["stats"], got["stats"]) and (k is None or torch.equal(alone[k], got[k])), k
+
+
+@pytest.mark.parametrize("kind,T", [("none", 70001), ("few", 30007), ("singles", 5000), ("many", 9001)])
+def test_balance_loss_over_many_pieces(kind, T):
+    starts = _starts(kind, T)
+    z, idx = _routing(T, 40, 3)
+    got, _ = _run_balance(z, idx, starts, balance_coef=1.0, z_coef=0.0)
+    _check_balance(z, idx, starts, got, 1.0, 0.0)
+    again, _ = _run_balance(z, idx, starts, balance_coef=1.0, z_coef=0.0)
+    for k in got:
+        assert torch.equal(got[k], again[k]), k
+
+
+def test_two_byte_records_and_the_logits_own_place():
+    z, idx = _routing(500, 128, 8)
+    a, _ = _run_balance(z, idx, None, balance_coef=0.1, z_coef=0.1)
+    b, _ = _run_balance(z, idx, None, u16=True, balance_coef=0.1, z_coef=0.1)
+    for k in a:
+        assert torch.equal(a[k], b[k]), k
+    t = torch.tensor(z, device=DEV)
+    r3.balance_loss(r3.desc(500, 16, 128, 8, 16), t, torch.tensor(idx.astype(np.uint8), device=DEV), torch.empty(3, device=DEV), dlogits=t,
+                    balance_coef=0.1, z_coef=0.1)
+    assert torch.equal(t, a["dlogits"])
+
+
+def test_masked_experts_empty_rows_and_values_that_are_not_finite():
+    z, idx = _routing(300, 24, 3)
+    z[:, 4] = -np.inf
+    z[10] = -np.inf
+    z[20, 1:] = -np.inf
+    z[30] = np.finfo(np.float32).min
+    z[31, ::2] = np.finfo(np.float32).min
+    z[32] = 3e38
+    got, status = _run_balance(z, idx, None, balance_coef=0.3, z_coef=0.0)
+    assert status == 0
+    with np.errstate(all="ignore"):
+        want = ref.balance_loss(z.astype(np.float64), idx, None, 0.3, 0.0)
+    _near(got["dlogits"], want["dlogits"], want["tol_dlogits"], "dlogits")
+    _near(got["probs"], want["probs"], want["tol_probs"], "probs")
+    _near(got["stats"][1], want["stats"][1], want["tol_stats"][1], "balance")
+    assert (got["dlogits"].cpu().numpy()[np.isinf(z)] == 0).all()
+    for bad in (np.nan, np.inf):
+        w = np.where(np.isinf(z), np.float32(-9.0), z)
+        w[30:33] = 0.0
+        clean, _ = _run_balance(w, idx, None, balance_coef=0.3, z_coef=0.1)
+        w[7, 23] = bad
+        got, status = _run_balance(w, idx, None, balance_coef=0.3, z_coef=0.1)
+        assert status == r3.DATA_NONFINITE and torch.isnan(got["dlogits"][7]).all() and torch.isnan(got["stats"][0])
+        rest = torch.arange(300, device=DEV) != 7
+        assert torch.equal(got["dlogits"][rest], clean["dlogits"][rest])
+        w[7] = -np.inf
+        w[7, 2] = np.nan
+        assert _run_balance(w, idx, None)[1] == r3.DATA_NONFINITE
+
+
+def test_ids_out_of_range_are_not_counted():
+    z, idx = _routing(90, 20, 4)
+    idx[5, 1], idx[6, 0] = 20, 255
+    got, status = _run_balance(z, idx, None, balance_coef=0.3, z_coef=0.02)
+    assert status == r3.DATA_IDX_RANGE
+    _check_balance(z, idx, None, got, 0.3, 0.02)
