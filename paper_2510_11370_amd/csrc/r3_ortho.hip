@@ -15,6 +15,7 @@
 
 #include "r3_kernels.h"
 #include "r3_mfma2.h"
+#include "r3_vec.h"
 
 namespace r3 {
 namespace {
@@ -26,10 +27,9 @@ typedef f16_t f16x8_t __attribute__((ext_vector_type(8)));
 constexpr int kSide = 128;                 // a work-group's tile
 constexpr int kWin = kSide * kBK3 * 2;     // 16 KB: 64 k of an operand
 constexpr float kUnit = 4096.0f;           // what is stored is times this
-constexpr int kPitch = kSide + 8;          // of a tile of results in LDS (f16)
-constexpr int kPitchF = kSide + 4;         // (f32)
-constexpr int kLdsBytes = 2 * kSide * kPitch * 2;   // 68 KB: four windows of operands, or two tiles of f16, or one of f32
-static_assert(kLdsBytes >= 4 * kWin && kLdsBytes >= kSide * kPitchF * 4, "");
+constexpr int kPitchF = kSide + 4;         // of a tile of results in LDS
+constexpr int kLdsBytes = kSide * kPitchF * 4;   // 66 KB: four windows of operands, or a tile of results
+static_assert(kLdsBytes >= 4 * kWin, "");
 
 enum { kGram = 0, kPoly = 1, kStep = 2, kLast = 3 };
 
@@ -134,13 +134,28 @@ __device__ __forceinline__ void multiply(Acc &acc, int nw, const PL &pl, const c
 __device__ __forceinline__ f16_t part_hi(float v) { return (f16_t)v; }
 __device__ __forceinline__ f16_t part_lo(float v, f16_t hi) { return (f16_t)(v - (float)hi); }
 
-// a tile in LDS to its place, a row of 128 f16 to 16 lanes
-__device__ __forceinline__ void put_tile(const f16_t *t, f16_t *dst, int64_t ld) {
+// A tile of results in LDS, row q at q kPitchF with its columns' fours exchanged by q / 8, so that eight rows' values of a column, 16 x 4
+// of them to a wave, meet at most two at a time in a bank; col is a multiple of 8 (read_down: row).
+__device__ __forceinline__ int sums_at(int q, int p) { return q * kPitchF + (p ^ (((q >> 3) & 7) << 2)); }
+__device__ __forceinline__ void read_along(const float *sums, int row, int col, float *v) {
+    *(f32x4_t *)v = *(const f32x4_t *)(sums + sums_at(row, col));
+    *(f32x4_t *)(v + 4) = *(const f32x4_t *)(sums + sums_at(row, col + 4));
+}
+__device__ __forceinline__ void read_down(const float *sums, int row, int col, float *v) {
+    const float *at = sums + sums_at(row, col);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int c = threadIdx.x + 256 * i, r = c >> 4, o = (c & 15) * 8;
-        *(f16x8_t *)(dst + (int64_t)r * ld + o) = *(const f16x8_t *)(t + r * kPitch + o);
+    for (int u = 0; u < 8; ++u) v[u] = at[u * kPitchF];
+}
+// eight values to their place, and what their rounding leaves
+template <bool LO> __device__ __forceinline__ void put8(const Pair &dst, int64_t e, const float *v) {
+    f16x8_t h, lo;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        h[u] = part_hi(v[u]);
+        lo[u] = part_lo(v[u], h[u]);
     }
+    *(f16x8_t *)(dst.hi + e) = h;
+    if constexpr (LO) *(f16x8_t *)(dst.lo + e) = lo;
 }
 
 // where a work-group's number takes it: the groups of an XCD (every eighth) have neighbouring tiles, and so the same matrices in its L2
@@ -194,96 +209,87 @@ __global__ void __launch_bounds__(256, 2) ortho_tile_kernel(Ortho o) {
         multiply<PARTS>(acc, o.sp / kBK3, pl, (const char *)(o.X.hi + xo), (const char *)(o.X.lo + xo), TrLoad::advance(2 * o.lp), ql,
                         (const char *)(o.B.hi + bo), (const char *)(o.B.lo + bo), KcLoad::advance(0), lds);
     }
-    // A lane's results: rows q0 + 16 j + (lane & 15), columns p0 + 16 i + 4 (lane >> 4) .. + 3.
-    const int qr = q0 + (lane & 15), pc = p0 + 4 * (lane >> 4);
-    const int64_t ld = MODE == kStep || MODE == kLast ? o.lp : o.sp;
-    const int64_t tile = m * (MODE == kStep || MODE == kLast ? xs : as) + (int64_t)ti * kSide * ld + (int64_t)tj * kSide;
-    f16_t *t0 = (f16_t *)lds, *t1 = t0 + kSide * kPitch;
-    // what a lane's four results are, times kUnit
-    auto value = [&](int i, int j, float (&v)[4]) {
-        const int64_t e = tile + (int64_t)(qr + 16 * j) * ld + pc + 16 * i;
-        float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    // The sums through LDS, so that whole lines of X or A are read and written.  A lane's: rows q0 + 16 j + (lane & 15), columns
+    // p0 + 16 i + 4 (lane >> 4) .. + 3.
+    float *sums = (float *)lds;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            *(f32x4_t *)(sums + sums_at(q0 + 16 * j + (lane & 15), p0 + 16 * i + 4 * (lane >> 4))) = acc[i][j] * (1.0f / kUnit);
+    __syncthreads();
+    constexpr bool kMirror = MODE == kGram || MODE == kPoly;
+    const int64_t ld = kMirror ? o.sp : o.lp;
+    const int64_t tile = m * (kMirror ? as : xs) + (int64_t)ti * kSide * ld + (int64_t)tj * kSide;
+    const Pair dst = MODE == kGram ? o.A : MODE == kPoly ? o.B : o.Y;
+    // eight columns of a row to a thread at a time (times kUnit: both operands are)
+#pragma unroll 2
+    for (int k = 0; k < kSide * kSide / 8 / 256; ++k) {
+        const int c = threadIdx.x + 256 * k, r = c >> 4, col = (c & 15) * 8;
+        const int64_t e = tile + (int64_t)r * ld + col;
+        float v[8], x[8];
         if constexpr (MODE != kGram) {
             const Pair in = MODE == kPoly ? o.A : o.X;
-            const f16x4_t h = *(const f16x4_t *)(in.hi + e);
+            const f16x8_t h = *(const f16x8_t *)(in.hi + e);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) x[u] = (float)h[u];
+            for (int u = 0; u < 8; ++u) x[u] = (float)h[u];
             if (MODE != kPoly || SPLIT) {
-                const f16x4_t lo = *(const f16x4_t *)(in.lo + e);
+                const f16x8_t lo = *(const f16x8_t *)(in.lo + e);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) x[u] += (float)lo[u];
+                for (int u = 0; u < 8; ++u) x[u] += (float)lo[u];
             }
         }
+        read_along(sums, r, col, v);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const float r = acc[i][j][u] * (1.0f / kUnit);   // (both operands are times kUnit)
-            if constexpr (MODE == kGram) v[u] = r;
-            else if constexpr (MODE == kPoly) {
-                v[u] = fmaf(o.c, r, o.b * x[u]);
-                const int row = ti * kSide + qr + 16 * j;
-                if (row == tj * kSide + pc + 16 * i + u && row < o.s) v[u] += o.a * kUnit;
-            } else v[u] = fmaf(o.a, x[u], r);
+        for (int u = 0; u < 8; ++u) {
+            if constexpr (MODE == kPoly) {
+                v[u] = fmaf(o.c, v[u], o.b * x[u]);
+                const int row = ti * kSide + r;
+                if (row == tj * kSide + col + u && row < o.s) v[u] += o.a * kUnit;
+            } else if constexpr (MODE == kStep || MODE == kLast) {
+                v[u] = fmaf(o.a, x[u], v[u]);
+                if constexpr (MODE == kLast) v[u] *= o.out;
+            }
         }
-    };
+        if constexpr (MODE == kPoly || MODE == kLast) {
+#pragma unroll
+            for (int u = 0; u < 8; u += 4) *(f32x4_t *)(sums + sums_at(r, col + u)) = *(const f32x4_t *)(v + u);
+        }
+        if constexpr (MODE != kLast) put8<MODE == kStep || SPLIT>(dst, e, v);
+    }
     if constexpr (MODE == kLast) {
-        float *tf = (float *)lds;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float v[4];
-                value(i, j, v);
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int q = qr + 16 * j, p = pc + 16 * i + u;
-                    tf[o.transposed ? p * kPitchF + q : q * kPitchF + p] = v[u] * o.out;
-                }
-            }
         __syncthreads();
         const int rows = o.transposed ? o.l : o.s, cols = o.transposed ? o.s : o.l;
         const int r0 = (o.transposed ? tj : ti) * kSide, c0 = (o.transposed ? ti : tj) * kSide;
-        OUT *dst = (OUT *)o.O + m * rows * cols;
-        for (int k = threadIdx.x; k < kSide * kSide; k += 256) {
-            const int r = k >> 7, c = k & 127;
-            if (r0 + r < rows && c0 + c < cols) Elem<OUT>::st(dst + (int64_t)(r0 + r) * cols + c0 + c, tf[r * kPitchF + c]);
-        }
-    } else {
-        // hi and lo of a step's result, or the tile and its mirror image
-        constexpr bool kMirror = MODE == kGram || MODE == kPoly;
-        const Pair dst = MODE == kGram ? o.A : MODE == kPoly ? o.B : o.Y;
-        const int64_t mirrored = m * as + (int64_t)tj * kSide * ld + (int64_t)ti * kSide;
+        OUT *out = (OUT *)o.O + m * rows * cols;
+        for (int k = 0; k < kSide * kSide / 8 / 256; ++k) {
+            const int e = threadIdx.x + 256 * k, r = e >> 4, c = (e & 15) * 8;
+            if (r0 + r >= rows || c0 + c >= cols) continue;
+            float v[8];
+            if (o.transposed) read_down(sums, c, r, v);
+            else read_along(sums, r, c, v);
+            OUT *at = out + (int64_t)(r0 + r) * cols + c0 + c;
+            if (c0 + c + 8 <= cols) {
 #pragma unroll
-        for (int pass = 0; pass < (kMirror && SPLIT ? 2 : 1); ++pass) {
-            if (pass) __syncthreads();
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float v[4];
-                    value(i, j, v);
-                    f16x4_t h, lo;
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        h[u] = part_hi(v[u]);
-                        lo[u] = part_lo(v[u], h[u]);
-                    }
-                    const int q = qr + 16 * j, p = pc + 16 * i;
-                    const f16x4_t w = pass ? lo : h;
-                    *(f16x4_t *)(t0 + q * kPitch + p) = w;
-                    if constexpr (kMirror) {
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) t1[(p + u) * kPitch + q] = w[u];
-                    } else {
-                        *(f16x4_t *)(t1 + q * kPitch + p) = lo;
-                    }
-                }
-            __syncthreads();
-            put_tile(t0, (pass ? dst.lo : dst.hi) + tile, ld);
-            if constexpr (kMirror) {
-                if (ti != tj) put_tile(t1, (pass ? dst.lo : dst.hi) + mirrored, ld);
+                for (int u = 0; u < 8; u += Row<OUT>::kVec) Row<OUT>::store(at + u, v + u);
             } else {
-                put_tile(t1, dst.lo + tile, ld);
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (c0 + c + u < cols) Elem<OUT>::st(at + u, v[u]);
             }
+        }
+    }
+    if constexpr (kMirror) {
+        if (ti == tj) return;
+        __syncthreads();
+        // the mirror image: eight rows' values of one column to a thread
+        const int64_t mirrored = m * as + (int64_t)tj * kSide * ld + (int64_t)ti * kSide;
+#pragma unroll 2
+        for (int k = 0; k < kSide * kSide / 8 / 256; ++k) {
+            const int c = threadIdx.x + 256 * k, r = c >> 4, col = (c & 15) * 8;
+            float v[8];
+            read_down(sums, col, r, v);
+            put8<SPLIT>(dst, mirrored + (int64_t)r * ld + col, v);
         }
     }
 }
@@ -319,15 +325,16 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(const T *__restrict__ G
     if (threadIdx.x == 0) part[blockIdx.x] = (ws[0] + ws[1]) + (ws[2] + ws[3]);
 }
 
-// a 64 x 64 tile of X; a tall G's through LDS
+// A 128 x 128 tile of X, a tall G's through LDS.  Rows of G are read in vectors of 16 bytes, at any element's address.
 template <typename T>
 __global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ G, Ortho o, int parts, const double *__restrict__ part, double eps,
                                                           int32_t *__restrict__ status) {
-    __shared__ float tile[64][65];
+    extern __shared__ __align__(1024) char lds[];
     __shared__ double inv_s;
-    const int nj = o.lp / 64, per = o.sp / 64 * nj;
+    float *tile = (float *)lds;
+    const int nj = o.lp / kSide, per = o.sp / kSide * nj;
     const int64_t m = blockIdx.x / per;
-    const int t = (int)(blockIdx.x - m * per), i0 = t / nj * 64, j0 = t % nj * 64;
+    const int t = (int)(blockIdx.x - m * per), i0 = t / nj * kSide, j0 = t % nj * kSide;
     if (threadIdx.x < kWave) {
         const double s = wave_sum((int)threadIdx.x < parts ? part[m * parts + threadIdx.x] : 0.0);
         if (threadIdx.x == 0) {
@@ -336,33 +343,43 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ 
             if (!isfinite(s) && t == 0 && status) atomicOr(status, R3_DATA_NONFINITE);
         }
     }
-    __syncthreads();
-    const double inv = inv_s;
     const T *g = G + m * (int64_t)o.s * o.l;
-    const int c = threadIdx.x & 63, r = threadIdx.x >> 6;
     const int r0 = o.transposed ? j0 : i0, c0 = o.transposed ? i0 : j0, rows = o.transposed ? o.l : o.s, cols = o.transposed ? o.s : o.l;
-#pragma unroll 4
-    for (int k = r; k < 64; k += 4) {
-        const bool in = r0 + k < rows && c0 + c < cols;
-        const float v = in ? (float)((double)Elem<T>::ld(g + (int64_t)(r0 + k) * cols + c0 + c) * inv) : 0.0f;
-        if (o.transposed) tile[c][k] = v;
-        else tile[k][c] = v;
+    constexpr int N = Row<T>::kVec, kEach = kSide * kSide / N / 256, kRow = kSide / N;
+    float x[kEach][N];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int e = threadIdx.x + 256 * k, r = e / kRow, c = e % kRow * N;
+        const T *at = g + (int64_t)(r0 + r) * cols + c0 + c;
+        const bool row = r0 + r < rows;
+        if (row && c0 + c + N <= cols) Row<T>::unpack(Row<T>::load(at), x[k]);
+        else {
+#pragma unroll
+            for (int u = 0; u < N; ++u) x[k][u] = row && c0 + c + u < cols ? Elem<T>::ld(at + u) : 0.0f;
+        }
     }
     __syncthreads();
-    const int64_t base = m * (int64_t)o.sp * o.lp;
+    const double inv = inv_s;
+    // (in 64 bits: 1 / |G| may be beyond f32's range)  Beyond G's rows and columns X is 0 whatever the norm is.
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int e = threadIdx.x + 256 * k, row = e >> 3, col = (e & 7) * 8;
-        f16x8_t h, lo;
+    for (int k = 0; k < kEach; ++k) {
+        const int e = threadIdx.x + 256 * k, r = e / kRow, c = e % kRow * N;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const float v = tile[row][col + u];
-            h[u] = part_hi(v);
-            lo[u] = part_lo(v, h[u]);
+        for (int u = 0; u < N; ++u) {
+            x[k][u] = r0 + r < rows && c0 + c + u < cols ? (float)((double)x[k][u] * inv) : 0.0f;
         }
-        const int64_t at = base + (int64_t)(i0 + row) * o.lp + j0 + col;
-        *(f16x8_t *)(o.X.hi + at) = h;
-        *(f16x8_t *)(o.X.lo + at) = lo;
+#pragma unroll
+        for (int u = 0; u < N; u += 4) *(f32x4_t *)(tile + sums_at(r, c + u)) = f32x4_t{x[k][u], x[k][u + 1], x[k][u + 2], x[k][u + 3]};
+    }
+    __syncthreads();
+    const int64_t base = m * (int64_t)o.sp * o.lp + (int64_t)i0 * o.lp + j0;
+#pragma unroll 2
+    for (int k = 0; k < kSide * kSide / 8 / 256; ++k) {
+        const int e = threadIdx.x + 256 * k, r = e >> 4, c = (e & 15) * 8;
+        float v[8];
+        if (o.transposed) read_down(tile, c, r, v);
+        else read_along(tile, r, c, v);
+        put8<true>(o.X, base + (int64_t)r * o.lp + c, v);
     }
 }
 
@@ -473,11 +490,12 @@ hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int d
         o.X = pair(p.X, xs); o.Y = pair(p.Y, xs); o.A = pair(p.A, as); o.B = pair(p.B, as);
         o.O = (char *)out + (size_t)m0 * elems * ob;
         const char *g = (const char *)G + (size_t)m0 * elems * eb;
-        const unsigned tiles64 = (unsigned)(nm * (p.sp / 64) * (p.lp / 64));
+        const unsigned ntiles = (unsigned)(nm * (p.sp / kSide) * (p.lp / kSide));
         auto start = [&](auto type) {
             typedef decltype(type) T;
             ortho_norm_kernel<T><<<(unsigned)(nm * p.parts), 256, 0, s>>>((const T *)g, elems, p.parts, part);
-            ortho_start_kernel<T><<<tiles64, 256, 0, s>>>((const T *)g, o, p.parts, part, (double)eps, status);
+            (void)hipFuncSetAttribute((const void *)ortho_start_kernel<T>, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+            ortho_start_kernel<T><<<ntiles, 256, kLdsBytes, s>>>((const T *)g, o, p.parts, part, (double)eps, status);
         };
         if (dtype_in == R3_BF16) start(bf16_t{});
         else start(float{});
