@@ -12,6 +12,7 @@
 // it is 1e-2 ... 4e-2.  For f32 results all of X, A, B are such pairs and products are the three of their parts that count
 // (hi lo, lo hi, hi hi): 22 bits, 3e-7 ... 8e-7 where f32 products give 2e-7 ... 5e-7.
 #include <cmath>
+#include <utility>
 
 #include "r3_kernels.h"
 #include "r3_mfma2.h"
@@ -28,24 +29,27 @@ constexpr int kSide = 128;                 // a work-group's tile
 constexpr int kWin = kSide * kBK3 * 2;     // 16 KB: 64 k of an operand
 constexpr float kUnit = 4096.0f;           // what is stored is times this
 constexpr int kPitchF = kSide + 4;         // of a tile of results in LDS
-constexpr int kLdsBytes = kSide * kPitchF * 4;   // 66 KB: four windows of operands, or a tile of results
-static_assert(kLdsBytes >= 4 * kWin, "");
-
-enum { kGram = 0, kPoly = 1, kStep = 2, kLast = 3 };
+constexpr int kLdsGram = kSide * kPitchF * 4;   // 66 KB: four windows of operands, or a tile of results
+constexpr int kLdsProduct = 3 * 24 * 1024;      // 72 KB: three stages of operands, or a tile of results
+static_assert(kLdsGram >= 4 * kWin && kLdsProduct >= kLdsGram, "");
 
 struct Pair { f16_t *hi, *lo; };   // lo may be null
-struct Ortho {
-    int s, l, sp, lp;              // X is s x l in sp x lp, zeros beyond
+
+// A launch's product D[q][p] = sum_k Q[q][k] P[p][k] per matrix and what is made of it, all in units of 1 / kUnit:
+//   result = D + c1 E1 + c2 E2 + diag I
+// kSquare: q, p < s, symmetric, lower half and its mirror image; kStep: p < l; kLast: p < l, times `out`, to the caller's array.
+enum { kGram = 0, kSquare = 1, kStep = 2, kLast = 3 };
+struct Product {
+    int s, l, sp, lp;              // X is s x l in sp x lp, A and the like s x s in sp x sp, zeros beyond
     int ntiles;                    // of a matrix
-    Pair X, Y, A, B;
-    float a, b, c, out;            // X' = a X + B X (kStep, kLast: times out); B = a I + b A + c A A (kPoly)
+    Pair Q, P, E1, E2, dst;
+    float cd, c1, c2, diag, out;
     void *O;
     bool transposed;
 };
 
-// one operand's window of 64 k, rows or k-rows of ld bytes; all of them exist
+// Operands with k along their rows (X in X X^T): windows of 64 k, 128 rows.  All rows exist.
 struct KcLoad {
-    static constexpr bool kTr = false;
     int voff, step;
     KcFrag16 fr;
     __device__ __forceinline__ void init(int ld, int wave_base) {
@@ -54,57 +58,44 @@ struct KcLoad {
         step = 32 * ld;
         fr.init(wave_base, lane);
     }
-    __device__ __forceinline__ static uint32_t advance(int) { return kBK3 * 2; }   // from window to window
-    __device__ __forceinline__ void issue(const Src &src, int J, uint32_t win) const {
-        const rsrc_t r = src_rsrc_inside(src, J);
+    __device__ __forceinline__ void issue(const char *base, int J, uint32_t win) const {
+        const rsrc_t r = src_rsrc_inside(Src{base, 0, kBK3 * 2}, J);
         const int w = threadIdx.x >> 6;
 #pragma unroll
         for (int i = 0; i < 4; ++i) lds_load16_soff(r, win + 1024 * (w + 4 * i), voff, i * step);
     }
     __device__ __forceinline__ f16x8_t frag(const char *win, int t, int u) const { return __builtin_bit_cast(f16x8_t, fr.read(win, t, u)); }
 };
-struct TrLoad {
-    static constexpr bool kTr = true;
-    int ld;
-    DmaTR<128> dma;
-    TrFrag16<128> fr;
-    __device__ __forceinline__ void init(int ld_, int wave_base) {
-        ld = ld_;
-        dma.init(ld, 0);
-        fr.init(wave_base);
-    }
-    __device__ __forceinline__ static uint32_t advance(int ld) { return 32u * ld; }   // from half to half
-    __device__ __forceinline__ void issue(const Src &src, int J, uint32_t win) const {
-        dma.issue(src_rsrc_inside(src, 2 * J), win);
-        dma.issue(src_rsrc_inside(src, 2 * J + 1), win + kWin / 2);
-    }
-    __device__ __forceinline__ f16x8_t frag(const char *win, int t, int u) const {
-        return __builtin_bit_cast(f16x8_t, fr.read(win + u * (kWin / 2), t));
-    }
-};
 
-typedef f32x4_t Acc[4][4];
-
-// All loads of a window have landed and everybody has left the one before, whose place the next loads take.
-__device__ __forceinline__ void meet() {
+// All but LOADS of this wave's loads have landed and everybody has left the stage before, whose place the next loads take.
+template <int LOADS = 0> __device__ __forceinline__ void meet() {
     asm volatile("" ::: "memory");
-    window_barrier<0>();
+    window_barrier<LOADS>();
     asm volatile("" ::: "memory");
 }
 
-// acc[i][j] += sum over k of P's row p and Q's row q; 4 waves of 64 x 64, as 4 x 4 of 16 x 16.  `parts` 1: hi hi; 3: lo hi, hi lo, hi hi.
-template <int PARTS, class PL, class QL>
-__device__ __forceinline__ void multiply(Acc &acc, int nw, const PL &pl, const char *phi, const char *plo, uint32_t padv, const QL &ql,
-                                         const char *qhi, const char *qlo, uint32_t qadv, char *lds) {
+// Which parts of the operands a pass multiplies: 1: hi hi; 3: lo hi, hi lo, hi hi.
+template <int PARTS> struct Passes {
+    const char *hi, *lo;
+    int low;     // the pass that takes lo
+    __device__ __forceinline__ const char *of(int pass) const { return PARTS == 3 && pass == low ? lo : hi; }
+};
+
+// 128 x 128 from rows with k along them; 4 waves of 64 x 64, as 4 x 4 of 16 x 16
+template <int PARTS>
+__device__ __forceinline__ void multiply_rows(f32x4_t (&acc)[4][4], int nw, int ld, const Passes<PARTS> &P, const Passes<PARTS> &Q, int p0, int q0,
+                                              char *lds) {
+    KcLoad pl, ql;
+    pl.init(ld, p0);
+    ql.init(ld, q0);
     const uint32_t at = lds_addr(lds);
-    int part = 0, J = 0;      // of the next window to load
+    int pass = 0, J = 0;      // of the next window to load
     auto issue = [&](int buf) {
-        const bool plow = PARTS == 3 && part == 0, qlow = PARTS == 3 && part == 1;
-        pl.issue(Src{plow ? plo : phi, 0, padv}, J, at + buf * 2 * kWin);
-        ql.issue(Src{qlow ? qlo : qhi, 0, qadv}, J, at + buf * 2 * kWin + kWin);
+        pl.issue(P.of(pass), J, at + buf * 2 * kWin);
+        ql.issue(Q.of(pass), J, at + buf * 2 * kWin + kWin);
         if (++J == nw) {
             J = 0;
-            ++part;
+            ++pass;
         }
     };
     issue(0);
@@ -127,6 +118,64 @@ __device__ __forceinline__ void multiply(Acc &acc, int nw, const PL &pl, const c
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], q[j], acc[i][j], 0, 0, 0);
                 }
         }
+    }
+    meet();
+}
+
+// 256 (P) x 128 (Q) from k-rows (X, and symmetric matrices, whose k-rows are their rows); 4 waves of 128 x 64, as 8 x 4 of 16 x 16; a ring
+// of three stages of 32 k.  Two work-groups to a compute unit: one multiplies while the other is in its epilogue.  P's columns past its
+// row's end are the next row's: finite or not, they stay in results that nobody stores.
+constexpr int kStageP = 32 * 256 * 2, kStageQ = 32 * kSide * 2, kStage = kStageP + kStageQ;   // 24 KB
+constexpr int kLoads = kStage / 4096;     // 16-byte loads of a wave to a stage
+template <int PARTS>
+__device__ __forceinline__ void multiply_columns(f32x4_t (&acc)[8][4], int nk, int ldp, int ldq, const Passes<PARTS> &P, const Passes<PARTS> &Q, int p0,
+                                                 int q0, bool live, char *lds) {
+    DmaTR<256> pd;
+    DmaTR<kSide> qd;
+    TrFrag16<256> pf;
+    TrFrag16<kSide> qf;
+    pd.init(ldp, 0);
+    qd.init(ldq, 0);
+    pf.init(p0);
+    qf.init(q0);
+    const uint32_t at = lds_addr(lds);
+    int pass = 0, J = 0, to = 0;      // of the next stage to load, and where it goes
+    auto issue = [&]() {
+        pd.issue(src_rsrc_inside(Src{P.of(pass), 0, 32u * ldp}, J), at + to);
+        qd.issue(src_rsrc_inside(Src{Q.of(pass), 0, 32u * ldq}, J), at + to + kStageP);
+        to = to == 2 * kStage ? 0 : to + kStage;
+        if (++J == nk) {
+            J = 0;
+            ++pass;
+        }
+    };
+    const int n = PARTS * nk;
+    issue();
+    if (n > 1) issue();
+    const char *st = lds;
+    for (int kt = 0; kt < n; ++kt) {
+        if (kt + 1 < n) meet<kLoads>();
+        else meet();
+        if (kt + 2 < n) issue();
+        if (live) {
+            f16x8_t q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] = __builtin_bit_cast(f16x8_t, qf.read(st + kStageP, j));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                f16x8_t p[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[i] = __builtin_bit_cast(f16x8_t, pf.read(st, 4 * h + i));
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int ii = 0; ii < 4; ++ii) {
+                        const int i = (j & 1) ? 3 - ii : ii;
+                        acc[4 * h + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], q[j], acc[4 * h + i][j], 0, 0, 0);
+                    }
+            }
+        }
+        st = st == lds + 2 * kStage ? lds : st + kStage;
     }
     meet();
 }
@@ -157,105 +206,50 @@ template <bool LO> __device__ __forceinline__ void put8(const Pair &dst, int64_t
     *(f16x8_t *)(dst.hi + e) = h;
     if constexpr (LO) *(f16x8_t *)(dst.lo + e) = lo;
 }
-
-// where a work-group's number takes it: the groups of an XCD (every eighth) have neighbouring tiles, and so the same matrices in its L2
-__device__ __forceinline__ int64_t xcd_share(int64_t id, int64_t n) {
-    const int64_t x = id & 7, q = n >> 3, r = n & 7;
-    return x * q + (x < r ? x : r) + (id >> 3);
+// v += c times eight values
+template <bool LO> __device__ __forceinline__ void add8(const Pair &src, int64_t e, float c, float *v) {
+    const f16x8_t h = *(const f16x8_t *)(src.hi + e);
+    f16x8_t lo;
+    if constexpr (LO) lo = *(const f16x8_t *)(src.lo + e);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = fmaf(c, LO ? (float)h[u] + (float)lo[u] : (float)h[u], v[u]);
 }
 
+// What is made of a 128 x 128 tile of sums: rows of block ti, columns of block tj.  Through LDS, so that whole lines are read and written.
 template <int MODE, bool SPLIT, typename OUT>
-__global__ void __launch_bounds__(256, 2) ortho_tile_kernel(Ortho o) {
-    extern __shared__ __align__(1024) char lds[];
-    const int64_t at = xcd_share(blockIdx.x, gridDim.x), m = at / o.ntiles;
-    const int t = (int)(at - m * o.ntiles);
-    int ti, tj;       // tile row and column
-    if constexpr (MODE == kGram || MODE == kPoly) {
-        ti = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
-        while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
-        while (ti * (ti + 1) / 2 > t) --ti;
-        tj = t - ti * (ti + 1) / 2;
-    } else {
-        const int nj = o.lp / kSide;
-        ti = t / nj;
-        tj = t - ti * nj;
-    }
-    ti = __builtin_amdgcn_readfirstlane(ti);
-    tj = __builtin_amdgcn_readfirstlane(tj);
-    const int64_t xs = (int64_t)o.sp * o.lp, as = (int64_t)o.sp * o.sp;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
-    const int p0 = 64 * (wave & 1), q0 = 64 * (wave >> 1);
-    Acc acc;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int PARTS = SPLIT ? 3 : 1;
-    KcLoad ql;
-    if constexpr (MODE == kGram || MODE == kPoly) {
-        const Pair in = MODE == kGram ? o.X : o.A;
-        const int ldk = MODE == kGram ? o.lp : o.sp;
-        const int64_t base = m * (MODE == kGram ? xs : as), ro = base + (int64_t)ti * kSide * ldk, co = base + (int64_t)tj * kSide * ldk;
-        KcLoad pl;
-        pl.init(2 * ldk, p0);
-        ql.init(2 * ldk, q0);
-        multiply<PARTS>(acc, ldk / kBK3, pl, (const char *)(in.hi + co), (const char *)(in.lo + co), KcLoad::advance(0), ql,
-                        (const char *)(in.hi + ro), (const char *)(in.lo + ro), KcLoad::advance(0), lds);
-    } else {
-        TrLoad pl;
-        pl.init(2 * o.lp, p0);
-        ql.init(2 * o.sp, q0);
-        const int64_t xo = m * xs + (int64_t)tj * kSide, bo = m * as + (int64_t)ti * kSide * o.sp;
-        multiply<PARTS>(acc, o.sp / kBK3, pl, (const char *)(o.X.hi + xo), (const char *)(o.X.lo + xo), TrLoad::advance(2 * o.lp), ql,
-                        (const char *)(o.B.hi + bo), (const char *)(o.B.lo + bo), KcLoad::advance(0), lds);
-    }
-    // The sums through LDS, so that whole lines of X or A are read and written.  A lane's: rows q0 + 16 j + (lane & 15), columns
-    // p0 + 16 i + 4 (lane >> 4) .. + 3.
-    float *sums = (float *)lds;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            *(f32x4_t *)(sums + sums_at(q0 + 16 * j + (lane & 15), p0 + 16 * i + 4 * (lane >> 4))) = acc[i][j] * (1.0f / kUnit);
-    __syncthreads();
-    constexpr bool kMirror = MODE == kGram || MODE == kPoly;
-    const int64_t ld = kMirror ? o.sp : o.lp;
+__device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti, int tj, float *sums) {
+    constexpr bool kMirror = MODE == kGram || MODE == kSquare;
+    const int64_t xs = (int64_t)o.sp * o.lp, as = (int64_t)o.sp * o.sp, ld = kMirror ? o.sp : o.lp;
     const int64_t tile = m * (kMirror ? as : xs) + (int64_t)ti * kSide * ld + (int64_t)tj * kSide;
-    const Pair dst = MODE == kGram ? o.A : MODE == kPoly ? o.B : o.Y;
-    // eight columns of a row to a thread at a time (times kUnit: both operands are)
+    const bool mirror = kMirror && ti != tj;
+    // eight columns of a row to a thread at a time
 #pragma unroll 2
     for (int k = 0; k < kSide * kSide / 8 / 256; ++k) {
         const int c = threadIdx.x + 256 * k, r = c >> 4, col = (c & 15) * 8;
         const int64_t e = tile + (int64_t)r * ld + col;
-        float v[8], x[8];
-        if constexpr (MODE != kGram) {
-            const Pair in = MODE == kPoly ? o.A : o.X;
-            const f16x8_t h = *(const f16x8_t *)(in.hi + e);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = (float)h[u];
-            if (MODE != kPoly || SPLIT) {
-                const f16x8_t lo = *(const f16x8_t *)(in.lo + e);
-#pragma unroll
-                for (int u = 0; u < 8; ++u) x[u] += (float)lo[u];
-            }
-        }
+        float v[8];
         read_along(sums, r, col, v);
+        if constexpr (MODE == kSquare) {
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            if constexpr (MODE == kPoly) {
-                v[u] = fmaf(o.c, v[u], o.b * x[u]);
-                const int row = ti * kSide + r;
-                if (row == tj * kSide + col + u && row < o.s) v[u] += o.a * kUnit;
-            } else if constexpr (MODE == kStep || MODE == kLast) {
-                v[u] = fmaf(o.a, x[u], v[u]);
-                if constexpr (MODE == kLast) v[u] *= o.out;
+            for (int u = 0; u < 8; ++u) v[u] *= o.cd;
+            add8<SPLIT>(o.E1, e, o.c1, v);
+            if (o.E2.hi) add8<SPLIT>(o.E2, e, o.c2, v);
+            const int row = ti * kSide + r;
+            if (ti == tj && row < o.s) {
+#pragma unroll
+                for (int u = 0; u < 8; ++u) v[u] += row == tj * kSide + col + u ? o.diag : 0.0f;
             }
         }
-        if constexpr (MODE == kPoly || MODE == kLast) {
+        if constexpr (MODE == kStep || MODE == kLast) add8<true>(o.E1, e, o.c1, v);
+        if constexpr (MODE == kLast) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] *= o.out;
+        }
+        if (MODE == kLast || (MODE == kSquare && mirror)) {
 #pragma unroll
             for (int u = 0; u < 8; u += 4) *(f32x4_t *)(sums + sums_at(r, col + u)) = *(const f32x4_t *)(v + u);
         }
-        if constexpr (MODE != kLast) put8<MODE == kStep || SPLIT>(dst, e, v);
+        if constexpr (MODE != kLast) put8<MODE == kStep || SPLIT>(o.dst, e, v);
     }
     if constexpr (MODE == kLast) {
         __syncthreads();
@@ -280,7 +274,7 @@ __global__ void __launch_bounds__(256, 2) ortho_tile_kernel(Ortho o) {
         }
     }
     if constexpr (kMirror) {
-        if (ti == tj) return;
+        if (!mirror) return;
         __syncthreads();
         // the mirror image: eight rows' values of one column to a thread
         const int64_t mirrored = m * as + (int64_t)tj * kSide * ld + (int64_t)ti * kSide;
@@ -289,8 +283,87 @@ __global__ void __launch_bounds__(256, 2) ortho_tile_kernel(Ortho o) {
             const int c = threadIdx.x + 256 * k, r = c >> 4, col = (c & 15) * 8;
             float v[8];
             read_down(sums, col, r, v);
-            put8<SPLIT>(dst, mirrored + (int64_t)r * ld + col, v);
+            put8<SPLIT>(o.dst, mirrored + (int64_t)r * ld + col, v);
         }
+    }
+}
+
+// where a work-group's number takes it: the groups of an XCD (every eighth) have neighbouring tiles, and so the same matrices in its L2
+__device__ __forceinline__ int64_t xcd_share(int64_t id, int64_t n) {
+    const int64_t x = id & 7, q = n >> 3, r = n & 7;
+    return x * q + (x < r ? x : r) + (id >> 3);
+}
+
+// A lane's sums of a 64 x 64 or 128 x 64 block: rows q0 + 16 j + (lane & 15), columns p0 + 16 i + 4 (lane >> 4) .. + 3.
+template <int NI>
+__device__ __forceinline__ void put_sums(const f32x4_t (&acc)[NI][4], int p0, int q0, float *sums) {
+    const int lane = lane_id();
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)   // (both operands are times kUnit)
+            *(f32x4_t *)(sums + sums_at(q0 + 16 * j + (lane & 15), p0 + 16 * i + 4 * (lane >> 4))) = acc[i][j] * (1.0f / kUnit);
+}
+
+template <bool SPLIT> __global__ void __launch_bounds__(256, 2) ortho_gram_kernel(Product o) {
+    extern __shared__ __align__(1024) char lds[];
+    const int64_t at = xcd_share(blockIdx.x, gridDim.x), m = at / o.ntiles;
+    const int t = (int)(at - m * o.ntiles);
+    int ti = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+    while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
+    while (ti * (ti + 1) / 2 > t) --ti;
+    ti = __builtin_amdgcn_readfirstlane(ti);
+    const int tj = __builtin_amdgcn_readfirstlane(t - ti * (ti + 1) / 2);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p0 = 64 * (wave & 1), q0 = 64 * (wave >> 1);
+    f32x4_t acc[4][4] = {};
+    constexpr int PARTS = SPLIT ? 3 : 1;
+    const int64_t base = m * o.sp * (int64_t)o.lp, ro = base + (int64_t)ti * kSide * o.lp, co = base + (int64_t)tj * kSide * o.lp;
+    multiply_rows<PARTS>(acc, o.lp / kBK3, 2 * o.lp, Passes<PARTS>{(const char *)(o.P.hi + co), (const char *)(o.P.lo + co), 0},
+                         Passes<PARTS>{(const char *)(o.P.hi + ro), (const char *)(o.P.lo + ro), 1}, p0, q0, lds);
+    put_sums(acc, p0, q0, (float *)lds);
+    __syncthreads();
+    finish_tile<kGram, SPLIT, float>(o, m, ti, tj, (float *)lds);
+}
+
+template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(256, 2) ortho_product_kernel(Product o) {
+    extern __shared__ __align__(1024) char lds[];
+    const int64_t at = xcd_share(blockIdx.x, gridDim.x), m = at / o.ntiles;
+    const int t = (int)(at - m * o.ntiles);
+    // tj: of 256 columns.  Of symmetric results rows ti have the tiles 0 .. ti / 2; else a column of tiles after the other
+    int ti, tj;
+    if constexpr (MODE == kSquare) {
+        // rows 2 r and 2 r + 1 begin at r (r + 1) and (r + 1) (r + 1)
+        int r = (int)(sqrtf((float)t + 0.25f) - 0.5f);
+        while ((r + 1) * (r + 2) <= t) ++r;
+        while (r * (r + 1) > t) --r;
+        const int in = t - r * (r + 1);
+        ti = 2 * r + (in > r);
+        tj = in > r ? in - r - 1 : in;
+    } else {
+        const int ni = o.sp / kSide;
+        tj = t / ni;
+        ti = t - tj * ni;
+    }
+    ti = __builtin_amdgcn_readfirstlane(ti);
+    tj = __builtin_amdgcn_readfirstlane(tj);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = wave & 1, q0 = 64 * (wave >> 1);
+    const int64_t xs = (int64_t)o.sp * o.lp, as = (int64_t)o.sp * o.sp;
+    const int ldp = MODE == kSquare ? o.sp : o.lp, blocks = ldp / kSide;
+    // whether a half of the tile's columns is wanted
+    auto wanted = [&](int h) { return 2 * tj + h < blocks && (MODE != kSquare || 2 * tj + h <= ti); };
+    f32x4_t acc[8][4] = {};
+    constexpr int PARTS = SPLIT ? 3 : 1;
+    const int64_t po = m * (MODE == kSquare ? as : xs) + (int64_t)tj * 2 * kSide, qo = m * as + (int64_t)ti * kSide;
+    multiply_columns<PARTS>(acc, o.sp / 32, 2 * ldp, 2 * o.sp, Passes<PARTS>{(const char *)(o.P.hi + po), (const char *)(o.P.lo + po), 0},
+                            Passes<PARTS>{(const char *)(o.Q.hi + qo), (const char *)(o.Q.lo + qo), 1}, 2 * 64 * half, q0, wanted(half), lds);
+    float *sums = (float *)lds;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (!wanted(h)) break;
+        if (h) __syncthreads();
+        if (half == h) put_sums(acc, 0, q0, sums);
+        __syncthreads();
+        finish_tile<MODE, SPLIT, OUT>(o, m, ti, 2 * tj + h, sums);
     }
 }
 
@@ -327,7 +400,7 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(const T *__restrict__ G
 
 // A 128 x 128 tile of X, a tall G's through LDS.  Rows of G are read in vectors of 16 bytes, at any element's address.
 template <typename T>
-__global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ G, Ortho o, int parts, const double *__restrict__ part, double eps,
+__global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ G, Product o, int parts, const double *__restrict__ part, double eps,
                                                           int32_t *__restrict__ status) {
     extern __shared__ __align__(1024) char lds[];
     __shared__ double inv_s;
@@ -379,14 +452,18 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ 
         float v[8];
         if (o.transposed) read_down(tile, c, r, v);
         else read_along(tile, r, c, v);
-        put8<true>(o.X, base + (int64_t)r * o.lp + c, v);
+        put8<true>(o.dst, base + (int64_t)r * o.lp + c, v);
     }
 }
+
+// Small matrices are a few tiles whose products cost next to nothing, and few directions in which an error could be lost (3 x 5, f16
+// operands: 6e-3 of the norm at worst).
+bool split_products(int64_t s, int dtype_out) { return dtype_out == R3_F32 || s <= kSide; }
 
 struct Plan {
     int s, l, sp, lp, parts;
     int64_t chunk;             // matrices at a time
-    size_t norm, X, Y, A, B, total;
+    size_t norm, X, Y, A, B, C, total;
     bool split;
 };
 
@@ -396,80 +473,126 @@ Plan plan(int64_t batch, int64_t rows, int64_t cols, int dtype_out) {
     p.l = (int)(rows < cols ? cols : rows);
     p.sp = (p.s + kSide - 1) / kSide * kSide;
     p.lp = (p.l + kSide - 1) / kSide * kSide;
-    p.split = dtype_out == R3_F32;
+    p.split = split_products(p.s, dtype_out);
     const int64_t elems = rows * cols;
     p.parts = (int)((elems + kNormElems - 1) / kNormElems);
     if (p.parts > kNormParts) p.parts = kNormParts;
-    const size_t x = (size_t)p.sp * p.lp * 4, a = (size_t)p.sp * p.sp * (p.split ? 4 : 2);   // of a matrix: X or Y, A or B
+    const size_t x = (size_t)p.sp * p.lp * 4, a = (size_t)p.sp * p.sp * (p.split ? 4 : 2);   // of a matrix: X or Y, A, B or C
     const size_t most = (size_t)4 << 30;
-    const int64_t fit = (int64_t)(most / (2 * (x + a)));
+    const int64_t fit = (int64_t)(most / (2 * x + 3 * a));
     p.chunk = fit < 1 ? 1 : fit < batch ? fit : batch;
     size_t o = 0;
-    auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes, 256); return at; };
+    // (a tile of 256 columns may read 128 columns past a matrix's last)
+    auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes + 2 * kSide, 256); return at; };
     p.norm = take((size_t)batch * p.parts * sizeof(double));
     p.X = take(x * p.chunk);
     p.Y = take(x * p.chunk);
     p.A = take(a * p.chunk);
     p.B = take(a * p.chunk);
+    p.C = take(a * p.chunk);
     p.total = o;
     return p;
 }
 
-template <int MODE, bool SPLIT, typename OUT> hipError_t tiles(const Ortho &o, int64_t matrices, hipStream_t s) {
-    auto k = ortho_tile_kernel<MODE, SPLIT, OUT>;
-    (void)hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
-    k<<<(unsigned)(matrices * o.ntiles), 256, kLdsBytes, s>>>(o);
+// Steps taken together: X'' = Q X with Q = (a + b A' + c A' A') (a + b A + c A A) and A' = (a + b A + c A A)^2 A, without X' between them:
+// five products of s x s instead of one, and a product with X and an X X^T less.  For f32 results wherever two steps are left; for bf16
+// ones at the start alone, where it costs no exactness: later a rounding of X enters the second product times a^2.  (Relative error beside
+// the result's rounding, five steps, random 256 x 768 / falling singular values / rank 3: apart 1.0e-3 / 7e-4 / 2.5e-3, the first two
+// together 1.0e-3 / 7e-4 / 2.5e-3, the first two pairs 1.2e-3 / 1.6e-3 / 9e-3.)
+bool two_together(int step, int steps, bool split) { return split ? steps - step >= 2 : step == 0 && steps >= 3; }
+// what of step k's polynomial is taken out of the matrix and applied to X itself
+double apart(int k, int steps, const float *q) { return k >= steps - 2 ? (double)q[0] + q[1] + q[2] : (double)q[0]; }
+
+// Whether every element stays in (-15, 15), so that times kUnit it is an f16: a matrix's are at most its largest singular value, that of X
+// at most 1 at the start and then what the quintic makes of it.
+bool in_range(int steps, const float *q, bool split) {
+    const double a = q[0], b = q[1], c = q[2], room = 1.01;    // for roundings and what lies between the points
+    double r = 1.0;
+    for (int k = 0; k < steps;) {
+        const bool two = two_together(k, steps, split);
+        double most = 0.0, next = 0.0;
+        for (int i = 0; i <= 1024; ++i) {
+            const double x = r * i / 1024, y = x * x, P = a + y * (b + y * c);
+            double all[6] = {x, y, P - a, 0.0, 0.0, 0.0}, to = x * P;
+            if (two) {
+                const double y1 = to * to, P1 = a + y1 * (b + y1 * c);
+                all[3] = P * y;
+                all[4] = y1;
+                all[5] = P1 - a;
+                all[2] = std::fmax(std::fabs(all[2]), std::fabs(P * P1 - apart(k, steps, q) * apart(k + 1, steps, q)));
+                to *= P1;
+            } else all[2] = P - apart(k, steps, q);
+            for (double v : all) most = std::fmax(most, std::fabs(v));
+            next = std::fmax(next, std::fabs(to));
+        }
+        if (!(most * room < 15.0 && next * room < 15.0)) return false;
+        r = next * 1.001;
+        k += two ? 2 : 1;
+    }
+    return true;
+}
+
+template <class K> hipError_t launch(K k, unsigned grid, int lds, const Product &o, hipStream_t s) {
+    (void)hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    k<<<grid, 256, lds, s>>>(o);
     return hipGetLastError();
 }
 
-template <bool SPLIT, typename OUT> hipError_t iterate(Ortho o, int64_t matrices, int steps, const float *coef, float scale, hipStream_t s) {
-    const int ns = o.sp / kSide, half = ns * (ns + 1) / 2, full = ns * (o.lp / kSide);
+template <bool SPLIT, typename OUT>
+hipError_t iterate(Product o, Pair X, Pair Y, Pair A, Pair B, Pair C, int64_t matrices, int steps, const float *coef, float scale, hipStream_t s) {
+    const int ns = o.sp / kSide, half = ns * (ns + 1) / 2, wide = (o.lp + 2 * kSide - 1) / (2 * kSide);
     const float a = coef[0], b = coef[1], c = coef[2];
-    for (int k = 0; k < steps; ++k) {
-        // what is taken out of the polynomial and applied to X itself
-        const float apart = k >= steps - 2 ? a + b + c : a;
+    hipError_t e = hipSuccess;
+    auto gram = [&](Pair to) {
         o.ntiles = half;
-        hipError_t e = tiles<kGram, SPLIT, float>(o, matrices, s);
-        if (e != hipSuccess) return e;
-        o.a = a - apart;
-        o.b = b;
-        o.c = c;
-        e = tiles<kPoly, SPLIT, float>(o, matrices, s);
-        if (e != hipSuccess) return e;
-        o.ntiles = full;
-        o.a = apart;
+        o.P = X; o.dst = to;
+        if (e == hipSuccess) e = launch(ortho_gram_kernel<SPLIT>, (unsigned)(matrices * half), kLdsGram, o, s);
+    };
+    const int r = ns / 2;       // tiles of symmetric results: 1, 1, 2, 2, ...
+    const int square_tiles = r * (r + 1) + (ns & 1 ? r + 1 : 0);
+    auto square = [&](Pair to, float cd, Pair q, Pair p, float c1, Pair e1, float c2, Pair e2, double diag) {
+        o.ntiles = square_tiles;
+        o.Q = q; o.P = p; o.E1 = e1; o.E2 = e2; o.dst = to;
+        o.cd = cd; o.c1 = c1; o.c2 = c2; o.diag = (float)(diag * kUnit);
+        if (e == hipSuccess) e = launch(ortho_product_kernel<kSquare, SPLIT, float>, (unsigned)(matrices * square_tiles), kLdsProduct, o, s);
+    };
+    const Pair none = {nullptr, nullptr};
+    for (int k = 0; k < steps;) {
+        const bool two = two_together(k, steps, SPLIT);
+        double out_of = apart(k, steps, coef);
+        Pair q = B;
+        gram(A);
+        if (two) {
+            out_of *= apart(k + 1, steps, coef);
+            square(B, c, A, A, b, A, 0.0f, none, 0.0);                                      // B = b A + c A A
+            square(C, 1.0f, B, A, a, A, 0.0f, none, 0.0);                                   // C = (a + B) A
+            square(A, 1.0f, C, B, a, C, 0.0f, none, 0.0);                                   // A' = C (a + B)
+            square(C, c, A, A, b, A, 0.0f, none, 0.0);                                      // B' = b A' + c A' A'
+            square(A, 1.0f, C, B, a, B, a, C, (double)a * a - out_of);                      // Q = (a + B') (a + B)
+            q = A;
+        } else {
+            square(B, c, A, A, b, A, 0.0f, none, (double)a - out_of);
+        }
+        k += two ? 2 : 1;
+        o.ntiles = ns * wide;
+        o.Q = q; o.P = X; o.E1 = X; o.dst = Y;
+        o.c1 = (float)out_of;
         o.out = scale / kUnit;
-        e = k + 1 < steps ? tiles<kStep, SPLIT, float>(o, matrices, s) : tiles<kLast, SPLIT, OUT>(o, matrices, s);
-        if (e != hipSuccess) return e;
-        const Pair t = o.X;
-        o.X = o.Y;
-        o.Y = t;
+        const unsigned grid = (unsigned)(matrices * o.ntiles);
+        if (e == hipSuccess)
+            e = k < steps ? launch(ortho_product_kernel<kStep, SPLIT, float>, grid, kLdsProduct, o, s)
+                          : launch(ortho_product_kernel<kLast, SPLIT, OUT>, grid, kLdsProduct, o, s);
+        std::swap(X, Y);
     }
-    return hipSuccess;
+    return e;
 }
 
 }  // namespace
 
 size_t orthogonalize_ws_bytes(int64_t batch, int64_t rows, int64_t cols, int dtype_out) { return plan(batch, rows, cols, dtype_out).total; }
 
-// Whether every element stays in (-15, 15): a matrix's are at most its largest singular value, which is at most 1 at the start and then
-// what the quintic makes of it.
-bool orthogonalize_in_range(int steps, const float *coef) {
-    const double a = coef[0], b = coef[1], c = coef[2];
-    double r = 1.0;
-    for (int k = 0; k < steps; ++k) {
-        const double apart = k >= steps - 2 ? a + b + c : a;
-        double x_most = 0.0, b_most = 0.0;
-        for (int i = 0; i <= 1024; ++i) {
-            const double x = r * i / 1024, y = x * x;
-            x_most = std::fmax(x_most, std::fabs(x * (a + y * (b + y * c))));
-            b_most = std::fmax(b_most, std::fabs(a - apart + y * (b + y * c)));
-        }
-        const double room = 1.01;    // for roundings and what lies between the points
-        if (!(r * r * room < 15.0 && b_most * room < 15.0 && x_most * room < 15.0)) return false;
-        r = x_most * 1.001;
-    }
-    return true;
+bool orthogonalize_in_range(int64_t rows, int64_t cols, int dtype_out, int steps, const float *coef) {
+    return in_range(steps, coef, split_products(rows < cols ? rows : cols, dtype_out));
 }
 
 hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int dtype_in, const void *G, int dtype_out, void *out, int steps,
@@ -483,25 +606,27 @@ hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int d
     for (int64_t m0 = 0; m0 < batch; m0 += p.chunk) {
         const int64_t nm = batch - m0 < p.chunk ? batch - m0 : p.chunk;
         const int64_t xs = (int64_t)p.sp * p.lp * p.chunk, as = (int64_t)p.sp * p.sp * p.chunk;
-        Ortho o = {};
+        Product o = {};
         o.s = p.s; o.l = p.l; o.sp = p.sp; o.lp = p.lp;
         o.transposed = rows > cols;
         auto pair = [&](size_t at, int64_t n) { return Pair{(f16_t *)(base + at), (f16_t *)(base + at) + n}; };
-        o.X = pair(p.X, xs); o.Y = pair(p.Y, xs); o.A = pair(p.A, as); o.B = pair(p.B, as);
+        const Pair X = pair(p.X, xs), Y = pair(p.Y, xs), A = pair(p.A, as), B = pair(p.B, as), C = pair(p.C, as);
         o.O = (char *)out + (size_t)m0 * elems * ob;
+        o.dst = X;
         const char *g = (const char *)G + (size_t)m0 * elems * eb;
         const unsigned ntiles = (unsigned)(nm * (p.sp / kSide) * (p.lp / kSide));
         auto start = [&](auto type) {
             typedef decltype(type) T;
             ortho_norm_kernel<T><<<(unsigned)(nm * p.parts), 256, 0, s>>>((const T *)g, elems, p.parts, part);
-            (void)hipFuncSetAttribute((const void *)ortho_start_kernel<T>, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
-            ortho_start_kernel<T><<<ntiles, 256, kLdsBytes, s>>>((const T *)g, o, p.parts, part, (double)eps, status);
+            (void)hipFuncSetAttribute((const void *)ortho_start_kernel<T>, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsGram);
+            ortho_start_kernel<T><<<ntiles, 256, kLdsGram, s>>>((const T *)g, o, p.parts, part, (double)eps, status);
         };
         if (dtype_in == R3_BF16) start(bf16_t{});
         else start(float{});
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        e = p.split ? iterate<true, float>(o, nm, steps, coef, scale, s) : iterate<false, bf16_t>(o, nm, steps, coef, scale, s);
+        auto run = !p.split ? iterate<false, bf16_t> : dtype_out == R3_F32 ? iterate<true, float> : iterate<true, bf16_t>;
+        e = run(o, X, Y, A, B, C, nm, steps, coef, scale, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
