@@ -469,7 +469,8 @@ int r3_balance_loss(const r3_layer_desc *desc, const float *logits, int64_t ld, 
  * products are (more where most of G is within rounding of fewer dimensions).
  * A matrix of zeros gives zeros.  A NaN or an infinity in a matrix makes its
  * result NaN and sets R3_DATA_NONFINITE; the other matrices are as without it.
- * A matrix's result is the same bits whatever other matrices the call has.
+ * A matrix's bits do not depend on what the call's other matrices hold, but may
+ * on how many they are.
  * rows, cols <= 32768, batch * rows * cols <= 2^46, and coefficients with which
  * no element of X, A or b A + c A A can leave (-15, 15) (|G|_2 <= |G|_F bounds
  * them), else R3_ERR_UNSUPPORTED.  1 <= steps <= R3_MAX_STEPS, eps >= 0.

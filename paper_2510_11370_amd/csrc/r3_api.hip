@@ -660,8 +660,9 @@ int r3_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int dtype_in, co
         if (!finite(q[i])) return R3_ERR_INVALID_ARG;
     const size_t ib = dtype_in == R3_BF16 ? 2 : 4, ob = dtype_out == R3_BF16 ? 2 : 4;
     if (!aligned(G, ib) || !aligned(out, ob) || !aligned(status_word, 4)) return R3_ERR_INVALID_ARG;
-    if (!ortho_sizes_ok(batch, rows, cols) || !orthogonalize_in_range(rows, cols, dtype_out, steps, q)) return R3_ERR_UNSUPPORTED;
+    if (!ortho_sizes_ok(batch, rows, cols)) return R3_ERR_UNSUPPORTED;
     if (batch == 0) return R3_OK;
+    if (!orthogonalize_in_range(batch, rows, cols, dtype_out, steps, q)) return R3_ERR_UNSUPPORTED;
     if (!G || !out) return R3_ERR_INVALID_ARG;
     const size_t need = orthogonalize_ws_bytes(batch, rows, cols, dtype_out);
     if (!ws || ws_bytes < need || !aligned(ws, 256)) return R3_ERR_WORKSPACE;

@@ -93,7 +93,7 @@ hipError_t launch_balance_loss(int T, int E, int K, const float *logits, int64_t
 
 // r3_ortho.hip
 size_t orthogonalize_ws_bytes(int64_t batch, int64_t rows, int64_t cols, int dtype_out);
-bool orthogonalize_in_range(int64_t rows, int64_t cols, int dtype_out, int steps, const float *coef);   // of the f16 that it computes with
+bool orthogonalize_in_range(int64_t batch, int64_t rows, int64_t cols, int dtype_out, int steps, const float *coef);   // of the f16 that it computes with
 hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int dtype_in, const void *G, int dtype_out, void *out, int steps,
                                 const float *coef, float eps, float scale, int32_t *status, void *ws, hipStream_t s);
 

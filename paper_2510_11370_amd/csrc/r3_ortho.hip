@@ -11,6 +11,7 @@
 // results beside their own rounding (1.7e-3): 4e-4 ... 1.0e-3 for matrices with flat and falling spectra; with bf16 operands throughout
 // it is 1e-2 ... 4e-2.  For f32 results all of X, A, B are such pairs and products are the three of their parts that count
 // (hi lo, lo hi, hi hi): 22 bits, 3e-7 ... 8e-7 where f32 products give 2e-7 ... 5e-7.
+#include <algorithm>
 #include <cmath>
 #include <utility>
 
@@ -183,17 +184,17 @@ __device__ __forceinline__ void multiply_columns(f32x4_t (&acc)[8][4], int nk, i
 __device__ __forceinline__ f16_t part_hi(float v) { return (f16_t)v; }
 __device__ __forceinline__ f16_t part_lo(float v, f16_t hi) { return (f16_t)(v - (float)hi); }
 
-// A tile of results in LDS, row q at q kPitchF with its columns' fours exchanged by q / 8, so that eight rows' values of a column, 16 x 4
+// A tile of results in LDS, row q at q (N + 4) with its columns' fours exchanged by q / 8, so that eight rows' values of a column, 16 x 4
 // of them to a wave, meet at most two at a time in a bank; col is a multiple of 8 (read_down: row).
-__device__ __forceinline__ int sums_at(int q, int p) { return q * kPitchF + (p ^ (((q >> 3) & 7) << 2)); }
-__device__ __forceinline__ void read_along(const float *sums, int row, int col, float *v) {
-    *(f32x4_t *)v = *(const f32x4_t *)(sums + sums_at(row, col));
-    *(f32x4_t *)(v + 4) = *(const f32x4_t *)(sums + sums_at(row, col + 4));
+template <int N> __device__ __forceinline__ int sums_at(int q, int p) { return q * (N + 4) + (p ^ (((q >> 3) & 7) << 2)); }
+template <int N> __device__ __forceinline__ void read_along(const float *sums, int row, int col, float *v) {
+    *(f32x4_t *)v = *(const f32x4_t *)(sums + sums_at<N>(row, col));
+    *(f32x4_t *)(v + 4) = *(const f32x4_t *)(sums + sums_at<N>(row, col + 4));
 }
-__device__ __forceinline__ void read_down(const float *sums, int row, int col, float *v) {
-    const float *at = sums + sums_at(row, col);
+template <int N> __device__ __forceinline__ void read_down(const float *sums, int row, int col, float *v) {
+    const float *at = sums + sums_at<N>(row, col);
 #pragma unroll
-    for (int u = 0; u < 8; ++u) v[u] = at[u * kPitchF];
+    for (int u = 0; u < 8; ++u) v[u] = at[u * (N + 4)];
 }
 // eight values to their place, and what their rounding leaves
 template <bool LO> __device__ __forceinline__ void put8(const Pair &dst, int64_t e, const float *v) {
@@ -215,29 +216,29 @@ template <bool LO> __device__ __forceinline__ void add8(const Pair &src, int64_t
     for (int u = 0; u < 8; ++u) v[u] = fmaf(c, LO ? (float)h[u] + (float)lo[u] : (float)h[u], v[u]);
 }
 
-// What is made of a 128 x 128 tile of sums: rows of block ti, columns of block tj.  Through LDS, so that whole lines are read and written.
-template <int MODE, bool SPLIT, typename OUT>
+// What is made of an N x N tile of sums: rows of block ti, columns of block tj.  Through LDS, so that whole lines are read and written.
+template <int MODE, bool SPLIT, int N, typename OUT>
 __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti, int tj, float *sums) {
     constexpr bool kMirror = MODE == kGram || MODE == kSquare;
     const int64_t xs = (int64_t)o.sp * o.lp, as = (int64_t)o.sp * o.sp, ld = kMirror ? o.sp : o.lp;
-    const int64_t tile = m * (kMirror ? as : xs) + (int64_t)ti * kSide * ld + (int64_t)tj * kSide;
+    const int64_t tile = m * (kMirror ? as : xs) + (int64_t)ti * N * ld + (int64_t)tj * N;
     const bool mirror = kMirror && ti != tj;
     // eight columns of a row to a thread at a time
 #pragma unroll 2
-    for (int k = 0; k < kSide * kSide / 8 / 256; ++k) {
-        const int c = threadIdx.x + 256 * k, r = c >> 4, col = (c & 15) * 8;
+    for (int k = 0; k < N * N / 8 / 256; ++k) {
+        const int c = threadIdx.x + 256 * k, r = c / (N / 8), col = c % (N / 8) * 8;
         const int64_t e = tile + (int64_t)r * ld + col;
         float v[8];
-        read_along(sums, r, col, v);
+        read_along<N>(sums, r, col, v);
         if constexpr (MODE == kSquare) {
 #pragma unroll
             for (int u = 0; u < 8; ++u) v[u] *= o.cd;
             add8<SPLIT>(o.E1, e, o.c1, v);
             if (o.E2.hi) add8<SPLIT>(o.E2, e, o.c2, v);
-            const int row = ti * kSide + r;
+            const int row = ti * N + r;
             if (ti == tj && row < o.s) {
 #pragma unroll
-                for (int u = 0; u < 8; ++u) v[u] += row == tj * kSide + col + u ? o.diag : 0.0f;
+                for (int u = 0; u < 8; ++u) v[u] += row == tj * N + col + u ? o.diag : 0.0f;
             }
         }
         if constexpr (MODE == kStep || MODE == kLast) add8<true>(o.E1, e, o.c1, v);
@@ -247,21 +248,21 @@ __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti,
         }
         if (MODE == kLast || (MODE == kSquare && mirror)) {
 #pragma unroll
-            for (int u = 0; u < 8; u += 4) *(f32x4_t *)(sums + sums_at(r, col + u)) = *(const f32x4_t *)(v + u);
+            for (int u = 0; u < 8; u += 4) *(f32x4_t *)(sums + sums_at<N>(r, col + u)) = *(const f32x4_t *)(v + u);
         }
         if constexpr (MODE != kLast) put8<MODE == kStep || SPLIT>(o.dst, e, v);
     }
     if constexpr (MODE == kLast) {
         __syncthreads();
         const int rows = o.transposed ? o.l : o.s, cols = o.transposed ? o.s : o.l;
-        const int r0 = (o.transposed ? tj : ti) * kSide, c0 = (o.transposed ? ti : tj) * kSide;
+        const int r0 = (o.transposed ? tj : ti) * N, c0 = (o.transposed ? ti : tj) * N;
         OUT *out = (OUT *)o.O + m * rows * cols;
-        for (int k = 0; k < kSide * kSide / 8 / 256; ++k) {
-            const int e = threadIdx.x + 256 * k, r = e >> 4, c = (e & 15) * 8;
+        for (int k = 0; k < N * N / 8 / 256; ++k) {
+            const int e = threadIdx.x + 256 * k, r = e / (N / 8), c = e % (N / 8) * 8;
             if (r0 + r >= rows || c0 + c >= cols) continue;
             float v[8];
-            if (o.transposed) read_down(sums, c, r, v);
-            else read_along(sums, r, c, v);
+            if (o.transposed) read_down<N>(sums, c, r, v);
+            else read_along<N>(sums, r, c, v);
             OUT *at = out + (int64_t)(r0 + r) * cols + c0 + c;
             if (c0 + c + 8 <= cols) {
 #pragma unroll
@@ -277,12 +278,12 @@ __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti,
         if (!mirror) return;
         __syncthreads();
         // the mirror image: eight rows' values of one column to a thread
-        const int64_t mirrored = m * as + (int64_t)tj * kSide * ld + (int64_t)ti * kSide;
+        const int64_t mirrored = m * as + (int64_t)tj * N * ld + (int64_t)ti * N;
 #pragma unroll 2
-        for (int k = 0; k < kSide * kSide / 8 / 256; ++k) {
-            const int c = threadIdx.x + 256 * k, r = c >> 4, col = (c & 15) * 8;
+        for (int k = 0; k < N * N / 8 / 256; ++k) {
+            const int c = threadIdx.x + 256 * k, r = c / (N / 8), col = c % (N / 8) * 8;
             float v[8];
-            read_down(sums, col, r, v);
+            read_down<N>(sums, col, r, v);
             put8<SPLIT>(o.dst, mirrored + (int64_t)r * ld + col, v);
         }
     }
@@ -294,35 +295,41 @@ __device__ __forceinline__ int64_t xcd_share(int64_t id, int64_t n) {
     return x * q + (x < r ? x : r) + (id >> 3);
 }
 
-// A lane's sums of a 64 x 64 or 128 x 64 block: rows q0 + 16 j + (lane & 15), columns p0 + 16 i + 4 (lane >> 4) .. + 3.
-template <int NI>
-__device__ __forceinline__ void put_sums(const f32x4_t (&acc)[NI][4], int p0, int q0, float *sums) {
+// A lane's sums of a block of NI x NJ 16 x 16: rows q0 + 16 j + (lane & 15), columns p0 + 16 i + 4 (lane >> 4) .. + 3.
+template <int N, int NI, int NJ>
+__device__ __forceinline__ void put_sums(const f32x4_t (&acc)[NI][NJ], int p0, int q0, float *sums) {
     const int lane = lane_id();
 #pragma unroll
     for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)   // (both operands are times kUnit)
-            *(f32x4_t *)(sums + sums_at(q0 + 16 * j + (lane & 15), p0 + 16 * i + 4 * (lane >> 4))) = acc[i][j] * (1.0f / kUnit);
+        for (int j = 0; j < NJ; ++j)   // (both operands are times kUnit)
+            *(f32x4_t *)(sums + sums_at<N>(q0 + 16 * j + (lane & 15), p0 + 16 * i + 4 * (lane >> 4))) = acc[i][j] * (1.0f / kUnit);
+}
+
+// tile t of a lower half, row by row
+__device__ __forceinline__ void lower_half(int t, int &ti, int &tj) {
+    int i = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+    while ((i + 1) * (i + 2) / 2 <= t) ++i;
+    while (i * (i + 1) / 2 > t) --i;
+    ti = __builtin_amdgcn_readfirstlane(i);
+    tj = __builtin_amdgcn_readfirstlane(t - i * (i + 1) / 2);
 }
 
 template <bool SPLIT> __global__ void __launch_bounds__(256, 2) ortho_gram_kernel(Product o) {
     extern __shared__ __align__(1024) char lds[];
     const int64_t at = xcd_share(blockIdx.x, gridDim.x), m = at / o.ntiles;
     const int t = (int)(at - m * o.ntiles);
-    int ti = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
-    while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
-    while (ti * (ti + 1) / 2 > t) --ti;
-    ti = __builtin_amdgcn_readfirstlane(ti);
-    const int tj = __builtin_amdgcn_readfirstlane(t - ti * (ti + 1) / 2);
+    int ti, tj;
+    lower_half(t, ti, tj);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p0 = 64 * (wave & 1), q0 = 64 * (wave >> 1);
     f32x4_t acc[4][4] = {};
     constexpr int PARTS = SPLIT ? 3 : 1;
     const int64_t base = m * o.sp * (int64_t)o.lp, ro = base + (int64_t)ti * kSide * o.lp, co = base + (int64_t)tj * kSide * o.lp;
     multiply_rows<PARTS>(acc, o.lp / kBK3, 2 * o.lp, Passes<PARTS>{(const char *)(o.P.hi + co), (const char *)(o.P.lo + co), 0},
                          Passes<PARTS>{(const char *)(o.P.hi + ro), (const char *)(o.P.lo + ro), 1}, p0, q0, lds);
-    put_sums(acc, p0, q0, (float *)lds);
+    put_sums<kSide>(acc, p0, q0, (float *)lds);
     __syncthreads();
-    finish_tile<kGram, SPLIT, float>(o, m, ti, tj, (float *)lds);
+    finish_tile<kGram, SPLIT, kSide, float>(o, m, ti, tj, (float *)lds);
 }
 
 template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(256, 2) ortho_product_kernel(Product o) {
@@ -361,10 +368,183 @@ template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(
     for (int h = 0; h < 2; ++h) {
         if (!wanted(h)) break;
         if (h) __syncthreads();
-        if (half == h) put_sums(acc, 0, q0, sums);
+        if (half == h) put_sums<kSide>(acc, 0, q0, sums);
         __syncthreads();
-        finish_tile<MODE, SPLIT, OUT>(o, m, ti, 2 * tj + h, sums);
+        finish_tile<MODE, SPLIT, kSide, OUT>(o, m, ti, 2 * tj + h, sums);
     }
+}
+
+// ---- few tiles ----
+// Where tiles of 128 would leave most of the card idle, a work-group takes 64 x 64 and has seven windows of 64 k on their way (three with
+// both parts of the operands): its time is latencies.  X X^T, whose k is the long side, is cut into parts that are joined by a launch of
+// their own.
+constexpr int kSmall = 64;
+constexpr int kSmallWin = kSmall * kBK3 * 2;     // 8 KB: 64 k of one part of an operand
+constexpr int kLdsSmall = 16 * kSmallWin;
+
+// 64 k-rows of 64 features; 32-byte group g of k-row k sits at g ^ (k & 3)
+struct SmallTr {
+    int voff, step, at;
+    __device__ __forceinline__ void init(int ld, int wave_base) {
+        const int w = threadIdx.x >> 6, lane = lane_id(), row = 8 * w + (lane >> 3);
+        voff = row * ld + ((lane & 7) ^ ((row & 3) << 1)) * 16;
+        step = 32 * ld;
+        const int b = lane >> 4, i = lane & 15, k = 8 * b + (i >> 2);
+        at = k * 128 + (((wave_base >> 4) ^ (k & 3)) << 5) + (i & 3) * 8;
+    }
+    __device__ __forceinline__ static uint32_t advance(int ld) { return 64u * ld; }
+    __device__ __forceinline__ f16x8_t frag(const char *win, int t, int u) const {
+        const char *p = win + u * (kSmallWin / 2) + (at ^ (t << 5));
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(p));
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(p + 4 * 128));
+        return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+// 64 rows of 64 k, as KcLoad
+struct SmallKc {
+    int voff, step;
+    KcFrag16 fr;
+    __device__ __forceinline__ void init(int ld, int wave_base) {
+        const int w = threadIdx.x >> 6, lane = lane_id(), row = 8 * w + (lane >> 3);
+        voff = row * ld + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+        step = 32 * ld;
+        fr.init(wave_base, lane);
+    }
+    __device__ __forceinline__ static uint32_t advance(int) { return kBK3 * 2; }
+    __device__ __forceinline__ f16x8_t frag(const char *win, int t, int u) const { return __builtin_bit_cast(f16x8_t, fr.read(win, t, u)); }
+};
+template <class L> __device__ __forceinline__ void small_issue(const L &l, const char *base, int ld, int J, uint32_t win) {
+    const rsrc_t r = src_rsrc_inside(Src{base, 0, L::advance(ld)}, J);
+    const int w = threadIdx.x >> 6;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) lds_load16_soff(r, win + 1024 * (w + 4 * i), l.voff, i * l.step);
+}
+
+// windows first .. first + n - 1 of P and Q; 4 waves of 32 x 32
+template <bool SPLIT, class PL, class QL>
+__device__ __forceinline__ void multiply_small(f32x4_t (&acc)[2][2], int first, int n, const PL &pl, const Pair &P, int ldp, const QL &ql, const Pair &Q,
+                                               int ldq, char *lds) {
+    constexpr int kParts = SPLIT ? 2 : 1, kBuf = 8 / kParts, kBytes = 2 * kParts * kSmallWin, kEach = 4 * kParts;   // loads of a wave to a window
+    const uint32_t at = lds_addr(lds);
+    auto issue = [&](int w) {
+        const uint32_t to = at + w % kBuf * kBytes;
+        small_issue(pl, (const char *)P.hi, ldp, first + w, to);
+        small_issue(ql, (const char *)Q.hi, ldq, first + w, to + kParts * kSmallWin);
+        if constexpr (SPLIT) {
+            small_issue(pl, (const char *)P.lo, ldp, first + w, to + kSmallWin);
+            small_issue(ql, (const char *)Q.lo, ldq, first + w, to + 3 * kSmallWin);
+        }
+    };
+    const int ahead = n < kBuf - 1 ? n : kBuf - 1;
+    for (int w = 0; w < ahead; ++w) issue(w);
+    f32x4_t part[2][2] = {};     // the small products
+    for (int w = 0; w < n; ++w) {
+        // (windows w .. w + kBuf - 2 are on their way, if there are as many)
+        if (w + kBuf - 2 < n) meet<(kBuf - 2) * kEach>();
+        else meet();
+        if (w + kBuf - 1 < n) issue(w + kBuf - 1);
+        const char *pw = lds + w % kBuf * kBytes, *qw = pw + kParts * kSmallWin;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            f16x8_t p[2], q[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                p[i] = pl.frag(pw, i, u);
+                q[i] = ql.frag(qw, i, u);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], q[j], acc[i][j], 0, 0, 0);
+            if constexpr (SPLIT) {
+                f16x8_t pl2[2], ql2[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    pl2[i] = pl.frag(pw + kSmallWin, i, u);
+                    ql2[i] = ql.frag(qw + kSmallWin, i, u);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl2[i], q[j], part[i][j], 0, 0, 0);
+                        part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], ql2[j], part[i][j], 0, 0, 0);
+                    }
+            }
+        }
+    }
+    if constexpr (SPLIT) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[i][j] += part[i][j];
+    }
+    meet();
+}
+
+// kGram: `cut` parts of the windows to a tile; with more than one, sums go to `parts`, [matrix][tile][part][64 x 64]
+template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(256, 1) ortho_small_kernel(Product o, int cut, float *__restrict__ parts) {
+    extern __shared__ __align__(1024) char lds[];
+    const int64_t at = MODE == kGram ? blockIdx.x / cut : blockIdx.x, m = at / o.ntiles;
+    const int t = (int)(at - m * o.ntiles), piece = MODE == kGram ? (int)(blockIdx.x - at * cut) : 0;
+    int ti, tj;
+    if constexpr (MODE == kGram || MODE == kSquare) lower_half(t, ti, tj);
+    else {
+        const int ni = o.sp / kSmall;
+        tj = t / ni;
+        ti = t - tj * ni;
+    }
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p0 = 32 * (wave & 1), q0 = 32 * (wave >> 1);
+    const int64_t xs = (int64_t)o.sp * o.lp, as = (int64_t)o.sp * o.sp;
+    auto from = [](const Pair &p, int64_t e) { return Pair{p.hi + e, p.lo + e}; };
+    f32x4_t acc[2][2] = {};
+    SmallKc ql;
+    if constexpr (MODE == kGram || MODE == kSquare) {
+        const int ld = MODE == kGram ? o.lp : o.sp, nw = ld / kBK3, w0 = (int)((int64_t)nw * piece / cut), w1 = (int)((int64_t)nw * (piece + 1) / cut);
+        const int64_t base = m * (MODE == kGram ? xs : as);
+        SmallKc pl;
+        pl.init(2 * ld, p0);
+        ql.init(2 * ld, q0);
+        multiply_small<SPLIT>(acc, w0, w1 - w0, pl, from(o.P, base + (int64_t)tj * kSmall * ld), 2 * ld, ql,
+                              from(MODE == kGram ? o.P : o.Q, base + (int64_t)ti * kSmall * ld), 2 * ld, lds);
+    } else {
+        SmallTr pl;
+        pl.init(2 * o.lp, p0);
+        ql.init(2 * o.sp, q0);
+        multiply_small<SPLIT>(acc, 0, o.sp / kBK3, pl, from(o.P, m * xs + (int64_t)tj * kSmall), 2 * o.lp, ql,
+                              from(o.Q, m * as + (int64_t)ti * kSmall * o.sp), 2 * o.sp, lds);
+    }
+    if (MODE == kGram && cut > 1) {
+        float *to = parts + (int64_t)blockIdx.x * (kSmall * kSmall) + threadIdx.x * 16;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) *(f32x4_t *)(to + 8 * i + 4 * j) = acc[i][j];
+        return;
+    }
+    put_sums<kSmall>(acc, p0, q0, (float *)lds);
+    __syncthreads();
+    finish_tile<MODE, SPLIT, kSmall, OUT>(o, m, ti, tj, (float *)lds);
+}
+
+// the parts of a tile of X X^T, in their order
+template <bool SPLIT> __global__ void __launch_bounds__(256) ortho_join_kernel(Product o, int cut, const float *__restrict__ parts) {
+    __shared__ __align__(16) float sums[kSmall * (kSmall + 4)];
+    const int64_t at = blockIdx.x, m = at / o.ntiles;
+    int ti, tj;
+    lower_half((int)(at - m * o.ntiles), ti, tj);
+    const int wave = threadIdx.x >> 6, p0 = 32 * (wave & 1), q0 = 32 * (wave >> 1);
+    f32x4_t acc[2][2] = {};
+    const float *from = parts + at * cut * (kSmall * kSmall) + threadIdx.x * 16;
+#pragma unroll 4
+    for (int c = 0; c < cut; ++c, from += kSmall * kSmall)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[i][j] += *(const f32x4_t *)(from + 8 * i + 4 * j);
+    put_sums<kSmall>(acc, p0, q0, sums);
+    __syncthreads();
+    finish_tile<kGram, SPLIT, kSmall, float>(o, m, ti, tj, sums);
 }
 
 // ---- the start: |G| and X = G kUnit / (|G| + eps) ----
@@ -398,16 +578,16 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(const T *__restrict__ G
     if (threadIdx.x == 0) part[blockIdx.x] = (ws[0] + ws[1]) + (ws[2] + ws[3]);
 }
 
-// A 128 x 128 tile of X, a tall G's through LDS.  Rows of G are read in vectors of 16 bytes, at any element's address.
-template <typename T>
+// An N x N tile of X, a tall G's through LDS.  Rows of G are read in vectors of 16 bytes, at any element's address.
+template <int N, typename T>
 __global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ G, Product o, int parts, const double *__restrict__ part, double eps,
                                                           int32_t *__restrict__ status) {
     extern __shared__ __align__(1024) char lds[];
     __shared__ double inv_s;
     float *tile = (float *)lds;
-    const int nj = o.lp / kSide, per = o.sp / kSide * nj;
+    const int nj = o.lp / N, per = o.sp / N * nj;
     const int64_t m = blockIdx.x / per;
-    const int t = (int)(blockIdx.x - m * per), i0 = t / nj * kSide, j0 = t % nj * kSide;
+    const int t = (int)(blockIdx.x - m * per), i0 = t / nj * N, j0 = t % nj * N;
     if (threadIdx.x < kWave) {
         const double s = wave_sum((int)threadIdx.x < parts ? part[m * parts + threadIdx.x] : 0.0);
         if (threadIdx.x == 0) {
@@ -418,17 +598,17 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ 
     }
     const T *g = G + m * (int64_t)o.s * o.l;
     const int r0 = o.transposed ? j0 : i0, c0 = o.transposed ? i0 : j0, rows = o.transposed ? o.l : o.s, cols = o.transposed ? o.s : o.l;
-    constexpr int N = Row<T>::kVec, kEach = kSide * kSide / N / 256, kRow = kSide / N;
-    float x[kEach][N];
+    constexpr int kVec = Row<T>::kVec, kEach = N * N / kVec / 256, kRow = N / kVec;
+    float x[kEach][kVec];
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
-        const int e = threadIdx.x + 256 * k, r = e / kRow, c = e % kRow * N;
+        const int e = threadIdx.x + 256 * k, r = e / kRow, c = e % kRow * kVec;
         const T *at = g + (int64_t)(r0 + r) * cols + c0 + c;
         const bool row = r0 + r < rows;
-        if (row && c0 + c + N <= cols) Row<T>::unpack(Row<T>::load(at), x[k]);
+        if (row && c0 + c + kVec <= cols) Row<T>::unpack(Row<T>::load(at), x[k]);
         else {
 #pragma unroll
-            for (int u = 0; u < N; ++u) x[k][u] = row && c0 + c + u < cols ? Elem<T>::ld(at + u) : 0.0f;
+            for (int u = 0; u < kVec; ++u) x[k][u] = row && c0 + c + u < cols ? Elem<T>::ld(at + u) : 0.0f;
         }
     }
     __syncthreads();
@@ -436,22 +616,22 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ 
     // (in 64 bits: 1 / |G| may be beyond f32's range)  Beyond G's rows and columns X is 0 whatever the norm is.
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
-        const int e = threadIdx.x + 256 * k, r = e / kRow, c = e % kRow * N;
+        const int e = threadIdx.x + 256 * k, r = e / kRow, c = e % kRow * kVec;
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
+        for (int u = 0; u < kVec; ++u) {
             x[k][u] = r0 + r < rows && c0 + c + u < cols ? (float)((double)x[k][u] * inv) : 0.0f;
         }
 #pragma unroll
-        for (int u = 0; u < N; u += 4) *(f32x4_t *)(tile + sums_at(r, c + u)) = f32x4_t{x[k][u], x[k][u + 1], x[k][u + 2], x[k][u + 3]};
+        for (int u = 0; u < kVec; u += 4) *(f32x4_t *)(tile + sums_at<N>(r, c + u)) = f32x4_t{x[k][u], x[k][u + 1], x[k][u + 2], x[k][u + 3]};
     }
     __syncthreads();
     const int64_t base = m * (int64_t)o.sp * o.lp + (int64_t)i0 * o.lp + j0;
 #pragma unroll 2
-    for (int k = 0; k < kSide * kSide / 8 / 256; ++k) {
-        const int e = threadIdx.x + 256 * k, r = e >> 4, c = (e & 15) * 8;
+    for (int k = 0; k < N * N / 8 / 256; ++k) {
+        const int e = threadIdx.x + 256 * k, r = e / (N / 8), c = e % (N / 8) * 8;
         float v[8];
-        if (o.transposed) read_down(tile, c, r, v);
-        else read_along(tile, r, c, v);
+        if (o.transposed) read_down<N>(tile, c, r, v);
+        else read_along<N>(tile, r, c, v);
         put8<true>(o.dst, base + (int64_t)r * o.lp + c, v);
     }
 }
@@ -460,20 +640,31 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ 
 // operands: 6e-3 of the norm at worst).
 bool split_products(int64_t s, int dtype_out) { return dtype_out == R3_F32 || s <= kSide; }
 
+// Tiles of 64 x 64 up to four of X's to a compute unit, eight where products are three (us a call, 64 x 64 | 256 x 128; bf16 results: 4 x 512 x
+// 1024 159 | 313, 4 x 1024 x 1024 413 | 429, 1 x 2048 x 2048 631 | 698, 16 x 512 x 1024 452 | 334, 128 x 256 x 256 432 | 271, 2 x 2048 x 2048
+// 1079 | 747; f32: 1 x 128 x 2048 120 | 406, 1 x 1024 x 1024 235 | 1096, 32 x 256 x 512 288 | 457, 16 x 512 x 1024 665 | 746, 256 x 128 x 1024
+// 780 | 638).
+bool small_tiles(int64_t batch, int64_t s, int64_t l, bool split) {
+    return batch * ((s + kSmall - 1) / kSmall) * ((l + kSmall - 1) / kSmall) <= (split ? 2048 : 1024);
+}
+
 struct Plan {
     int s, l, sp, lp, parts;
     int64_t chunk;             // matrices at a time
-    size_t norm, X, Y, A, B, C, total;
-    bool split;
+    size_t norm, X, Y, A, B, C, parts_at, total;
+    bool split, small;         // small: tiles of 64
+    int cut;                   // parts of X X^T
 };
 
 Plan plan(int64_t batch, int64_t rows, int64_t cols, int dtype_out) {
     Plan p;
     p.s = (int)(rows < cols ? rows : cols);
     p.l = (int)(rows < cols ? cols : rows);
-    p.sp = (p.s + kSide - 1) / kSide * kSide;
-    p.lp = (p.l + kSide - 1) / kSide * kSide;
     p.split = split_products(p.s, dtype_out);
+    p.small = small_tiles(batch, p.s, p.l, p.split);
+    const int side = p.small ? kSmall : kSide;
+    p.sp = (p.s + side - 1) / side * side;
+    p.lp = (p.l + side - 1) / side * side;
     const int64_t elems = rows * cols;
     p.parts = (int)((elems + kNormElems - 1) / kNormElems);
     if (p.parts > kNormParts) p.parts = kNormParts;
@@ -481,6 +672,10 @@ Plan plan(int64_t batch, int64_t rows, int64_t cols, int dtype_out) {
     const size_t most = (size_t)4 << 30;
     const int64_t fit = (int64_t)(most / (2 * x + 3 * a));
     p.chunk = fit < 1 ? 1 : fit < batch ? fit : batch;
+    p.cut = 1;
+    const int nt = p.sp / kSmall, tiles = nt * (nt + 1) / 2, nw = p.lp / kBK3;
+    if (p.small)     // a work-group to a compute unit, at least four windows to a part
+        p.cut = (int)std::max<int64_t>(1, std::min<int64_t>(nw / 4, 256 / (tiles * p.chunk)));
     size_t o = 0;
     // (a tile of 256 columns may read 128 columns past a matrix's last)
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes + 2 * kSide, 256); return at; };
@@ -490,26 +685,30 @@ Plan plan(int64_t batch, int64_t rows, int64_t cols, int dtype_out) {
     p.A = take(a * p.chunk);
     p.B = take(a * p.chunk);
     p.C = take(a * p.chunk);
+    p.parts_at = take(p.cut > 1 ? (size_t)p.chunk * tiles * p.cut * kSmall * kSmall * sizeof(float) : 0);
     p.total = o;
     return p;
 }
 
 // Steps taken together: X'' = Q X with Q = (a + b A' + c A' A') (a + b A + c A A) and A' = (a + b A + c A A)^2 A, without X' between them:
-// five products of s x s instead of one, and a product with X and an X X^T less.  For f32 results wherever two steps are left; for bf16
+// five products of s x s instead of two, and a product with X and an X X^T less.  On small tiles that is as many launches, which are what
+// counts there, and steps stay apart.  Else for f32 results wherever two steps are left; for bf16
 // ones at the start alone, where it costs no exactness: later a rounding of X enters the second product times a^2.  (Relative error beside
 // the result's rounding, five steps, random 256 x 768 / falling singular values / rank 3: apart 1.0e-3 / 7e-4 / 2.5e-3, the first two
 // together 1.0e-3 / 7e-4 / 2.5e-3, the first two pairs 1.2e-3 / 1.6e-3 / 9e-3.)
-bool two_together(int step, int steps, bool split) { return split ? steps - step >= 2 : step == 0 && steps >= 3; }
+bool two_together(int step, int steps, bool split, bool small) {
+    return !small && (split ? steps - step >= 2 : step == 0 && steps >= 3);
+}
 // what of step k's polynomial is taken out of the matrix and applied to X itself
 double apart(int k, int steps, const float *q) { return k >= steps - 2 ? (double)q[0] + q[1] + q[2] : (double)q[0]; }
 
 // Whether every element stays in (-15, 15), so that times kUnit it is an f16: a matrix's are at most its largest singular value, that of X
 // at most 1 at the start and then what the quintic makes of it.
-bool in_range(int steps, const float *q, bool split) {
+bool in_range(int steps, const float *q, bool split, bool small) {
     const double a = q[0], b = q[1], c = q[2], room = 1.01;    // for roundings and what lies between the points
     double r = 1.0;
     for (int k = 0; k < steps;) {
-        const bool two = two_together(k, steps, split);
+        const bool two = two_together(k, steps, split, small);
         double most = 0.0, next = 0.0;
         for (int i = 0; i <= 1024; ++i) {
             const double x = r * i / 1024, y = x * x, P = a + y * (b + y * c);
@@ -532,33 +731,41 @@ bool in_range(int steps, const float *q, bool split) {
     return true;
 }
 
-template <class K> hipError_t launch(K k, unsigned grid, int lds, const Product &o, hipStream_t s) {
+template <class K, class... A> hipError_t launch(K k, int64_t grid, int lds, hipStream_t s, const A &...args) {
     (void)hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    k<<<grid, 256, lds, s>>>(o);
+    k<<<(unsigned)grid, 256, lds, s>>>(args...);
     return hipGetLastError();
 }
 
 template <bool SPLIT, typename OUT>
-hipError_t iterate(Product o, Pair X, Pair Y, Pair A, Pair B, Pair C, int64_t matrices, int steps, const float *coef, float scale, hipStream_t s) {
-    const int ns = o.sp / kSide, half = ns * (ns + 1) / 2, wide = (o.lp + 2 * kSide - 1) / (2 * kSide);
+hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pair C, float *parts, int64_t matrices, int steps, const float *coef,
+                   float scale, hipStream_t s) {
+    const int side = p.small ? kSmall : kSide, ns = o.sp / side, half = ns * (ns + 1) / 2, r = ns / 2;
+    // tiles of 256 x 128: of symmetric results 1, 1, 2, 2, ... to a row of them
+    const int square_tiles = p.small ? half : r * (r + 1) + (ns & 1 ? r + 1 : 0);
+    const int step_tiles = ns * (p.small ? o.lp / side : (o.lp + 2 * side - 1) / (2 * side));
     const float a = coef[0], b = coef[1], c = coef[2];
+    float *no_parts = nullptr;
     hipError_t e = hipSuccess;
     auto gram = [&](Pair to) {
         o.ntiles = half;
         o.P = X; o.dst = to;
-        if (e == hipSuccess) e = launch(ortho_gram_kernel<SPLIT>, (unsigned)(matrices * half), kLdsGram, o, s);
+        if (e != hipSuccess) return;
+        if (!p.small) e = launch(ortho_gram_kernel<SPLIT>, matrices * half, kLdsGram, s, o);
+        else e = launch(ortho_small_kernel<kGram, SPLIT, float>, matrices * half * p.cut, kLdsSmall, s, o, p.cut, parts);
+        if (e == hipSuccess && p.cut > 1) e = launch(ortho_join_kernel<SPLIT>, matrices * half, 0, s, o, p.cut, (const float *)parts);
     };
-    const int r = ns / 2;       // tiles of symmetric results: 1, 1, 2, 2, ...
-    const int square_tiles = r * (r + 1) + (ns & 1 ? r + 1 : 0);
-    auto square = [&](Pair to, float cd, Pair q, Pair p, float c1, Pair e1, float c2, Pair e2, double diag) {
+    auto square = [&](Pair to, float cd, Pair q, Pair from, float c1, Pair e1, float c2, Pair e2, double diag) {
         o.ntiles = square_tiles;
-        o.Q = q; o.P = p; o.E1 = e1; o.E2 = e2; o.dst = to;
+        o.Q = q; o.P = from; o.E1 = e1; o.E2 = e2; o.dst = to;
         o.cd = cd; o.c1 = c1; o.c2 = c2; o.diag = (float)(diag * kUnit);
-        if (e == hipSuccess) e = launch(ortho_product_kernel<kSquare, SPLIT, float>, (unsigned)(matrices * square_tiles), kLdsProduct, o, s);
+        if (e != hipSuccess) return;
+        e = p.small ? launch(ortho_small_kernel<kSquare, SPLIT, float>, matrices * square_tiles, kLdsSmall, s, o, 1, no_parts)
+                    : launch(ortho_product_kernel<kSquare, SPLIT, float>, matrices * square_tiles, kLdsProduct, s, o);
     };
     const Pair none = {nullptr, nullptr};
     for (int k = 0; k < steps;) {
-        const bool two = two_together(k, steps, SPLIT);
+        const bool two = two_together(k, steps, SPLIT, p.small);
         double out_of = apart(k, steps, coef);
         Pair q = B;
         gram(A);
@@ -574,14 +781,18 @@ hipError_t iterate(Product o, Pair X, Pair Y, Pair A, Pair B, Pair C, int64_t ma
             square(B, c, A, A, b, A, 0.0f, none, (double)a - out_of);
         }
         k += two ? 2 : 1;
-        o.ntiles = ns * wide;
+        o.ntiles = step_tiles;
         o.Q = q; o.P = X; o.E1 = X; o.dst = Y;
         o.c1 = (float)out_of;
         o.out = scale / kUnit;
-        const unsigned grid = (unsigned)(matrices * o.ntiles);
-        if (e == hipSuccess)
-            e = k < steps ? launch(ortho_product_kernel<kStep, SPLIT, float>, grid, kLdsProduct, o, s)
-                          : launch(ortho_product_kernel<kLast, SPLIT, OUT>, grid, kLdsProduct, o, s);
+        const int64_t grid = matrices * step_tiles;
+        if (e != hipSuccess) return e;
+        if (p.small)
+            e = k < steps ? launch(ortho_small_kernel<kStep, SPLIT, float>, grid, kLdsSmall, s, o, 1, no_parts)
+                          : launch(ortho_small_kernel<kLast, SPLIT, OUT>, grid, kLdsSmall, s, o, 1, no_parts);
+        else
+            e = k < steps ? launch(ortho_product_kernel<kStep, SPLIT, float>, grid, kLdsProduct, s, o)
+                          : launch(ortho_product_kernel<kLast, SPLIT, OUT>, grid, kLdsProduct, s, o);
         std::swap(X, Y);
     }
     return e;
@@ -591,8 +802,9 @@ hipError_t iterate(Product o, Pair X, Pair Y, Pair A, Pair B, Pair C, int64_t ma
 
 size_t orthogonalize_ws_bytes(int64_t batch, int64_t rows, int64_t cols, int dtype_out) { return plan(batch, rows, cols, dtype_out).total; }
 
-bool orthogonalize_in_range(int64_t rows, int64_t cols, int dtype_out, int steps, const float *coef) {
-    return in_range(steps, coef, split_products(rows < cols ? rows : cols, dtype_out));
+bool orthogonalize_in_range(int64_t batch, int64_t rows, int64_t cols, int dtype_out, int steps, const float *coef) {
+    const Plan p = plan(batch, rows, cols, dtype_out);
+    return in_range(steps, coef, p.split, p.small);
 }
 
 hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int dtype_in, const void *G, int dtype_out, void *out, int steps,
@@ -614,19 +826,20 @@ hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int d
         o.O = (char *)out + (size_t)m0 * elems * ob;
         o.dst = X;
         const char *g = (const char *)G + (size_t)m0 * elems * eb;
-        const unsigned ntiles = (unsigned)(nm * (p.sp / kSide) * (p.lp / kSide));
+        const int side = p.small ? kSmall : kSide;
+        const int64_t ntiles = nm * (p.sp / side) * (p.lp / side);
+        hipError_t e;
         auto start = [&](auto type) {
             typedef decltype(type) T;
             ortho_norm_kernel<T><<<(unsigned)(nm * p.parts), 256, 0, s>>>((const T *)g, elems, p.parts, part);
-            (void)hipFuncSetAttribute((const void *)ortho_start_kernel<T>, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsGram);
-            ortho_start_kernel<T><<<ntiles, 256, kLdsGram, s>>>((const T *)g, o, p.parts, part, (double)eps, status);
+            auto k = p.small ? ortho_start_kernel<kSmall, T> : ortho_start_kernel<kSide, T>;
+            e = launch(k, ntiles, side * (side + 4) * 4, s, (const T *)g, o, p.parts, (const double *)part, (double)eps, status);
         };
         if (dtype_in == R3_BF16) start(bf16_t{});
         else start(float{});
-        hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         auto run = !p.split ? iterate<false, bf16_t> : dtype_out == R3_F32 ? iterate<true, float> : iterate<true, bf16_t>;
-        e = run(o, X, Y, A, B, C, nm, steps, coef, scale, s);
+        e = run(p, o, X, Y, A, B, C, (float *)(base + p.parts_at), nm, steps, coef, scale, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -29,7 +29,8 @@ def _check(out, G, to, **kw):
 
 
 SIZES = [(1, 1, 1), (1, 1, 9), (2, 7, 1), (2, 5, 3), (3, 64, 64), (1, 128, 128), (2, 129, 130), (2, 64, 300), (1, 300, 64),
-         (3, 257, 129), (1, 130, 1000), (2, 501, 260), (5, 100, 100), (1, 1, 5000), (2, 40, 2055)]
+         (3, 257, 129), (1, 130, 1000), (2, 501, 260), (5, 100, 100), (1, 1, 5000), (2, 40, 2055), (1, 128, 2048), (70, 129, 200), (40, 300, 385),
+         (12, 700, 520), (300, 64, 64)]
 
 
 @pytest.mark.parametrize("src,to", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("bf16", "f32")])
@@ -104,17 +105,17 @@ def test_zeros_and_values_that_are_not_finite_stay_in_their_matrix(bad, to):
 
 
 @pytest.mark.parametrize("to", ["f32", "bf16"])
-@pytest.mark.parametrize("r,c", [(200, 90), (96, 300), (640, 640)])
-def test_a_matrix_has_the_same_bits_in_every_batch_and_in_place(r, c, to):
-    G = _gradient(9, r, c, to).to(DEV)
+@pytest.mark.parametrize("b,r,c", [(9, 200, 90), (9, 96, 300), (9, 640, 640), (40, 300, 700)])
+def test_a_matrix_keeps_its_bits_beside_others_and_in_place(b, r, c, to):
+    G = _gradient(b, r, c, to).to(DEV)
     out = torch.empty_like(G)
     r3.orthogonalize(G, out)
-    for i in (0, 4, 8):
-        one = torch.empty(r, c, dtype=DT[to], device=DEV)
-        r3.orthogonalize(G[i], one)
-        assert torch.equal(one, out[i])
     again = torch.empty_like(G)
     r3.orthogonalize(G, again)
     assert torch.equal(again, out)
+    H = torch.flip(G, (0,)) * 3.0
+    H[b // 2] = G[b // 2]
+    r3.orthogonalize(H, again)
+    assert torch.equal(again[b // 2], out[b // 2])
     r3.orthogonalize(G, G)
     assert torch.equal(G, out)
