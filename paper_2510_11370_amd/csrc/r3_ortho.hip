@@ -37,17 +37,28 @@ static_assert(kLdsGram >= 4 * kWin && kLdsProduct >= kLdsGram, "");
 struct Pair { f16_t *hi, *lo; };   // lo may be null
 
 // A launch's product D[q][p] = sum_k Q[q][k] P[p][k] per matrix and what is made of it, all in units of 1 / kUnit:
-//   result = D + c1 E1 + c2 E2 + diag I
+//   result = cd (D + own P) + c1 E1 + c2 E2 + diag I
 // kSquare: q, p < s, symmetric, lower half and its mirror image; kStep: p < l; kLast: p < l, times `out`, to the caller's array.
+// own P costs no loads: where a tile's k are its own rows the operand is in LDS, and is multiplied with `own` times a unit matrix, too
+// (two f16, so that `own` keeps 22 bits).
 enum { kGram = 0, kSquare = 1, kStep = 2, kLast = 3 };
 struct Product {
     int s, l, sp, lp;              // X is s x l in sp x lp, A and the like s x s in sp x sp, zeros beyond
     int ntiles;                    // of a matrix
-    Pair Q, P, E1, E2, dst;
+    Pair Q, P, E1, E2, dst;        // (E1, E2: or none)
+    f16_t own, own_lo;             // times kUnit
     float cd, c1, c2, diag, out;
     void *O;
     bool transposed;
 };
+// `own` times columns 16 j .. + 15 of a unit matrix of 32 rows, as an operand's fragment
+__device__ __forceinline__ f16x8_t unit_part(int j, f16_t own) {
+    const int lane = lane_id(), at = 16 * j + (lane & 15) - 8 * (lane >> 4);
+    f16x8_t v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = at == e ? own : (f16_t)0.0f;
+    return v;
+}
 
 // Operands with k along their rows (X in X X^T): windows of 64 k, 128 rows.  All rows exist.
 struct KcLoad {
@@ -130,7 +141,7 @@ constexpr int kStageP = 32 * 256 * 2, kStageQ = 32 * kSide * 2, kStage = kStageP
 constexpr int kLoads = kStage / 4096;     // 16-byte loads of a wave to a stage
 template <int PARTS>
 __device__ __forceinline__ void multiply_columns(f32x4_t (&acc)[8][4], int nk, int ldp, int ldq, const Passes<PARTS> &P, const Passes<PARTS> &Q, int p0,
-                                                 int q0, bool live, char *lds) {
+                                                 int q0, bool live, int own_at, f16_t own, f16_t own_lo, char *lds) {
     DmaTR<256> pd;
     DmaTR<kSide> qd;
     TrFrag16<256> pf;
@@ -154,6 +165,7 @@ __device__ __forceinline__ void multiply_columns(f32x4_t (&acc)[8][4], int nk, i
     issue();
     if (n > 1) issue();
     const char *st = lds;
+    int own_in = own_at, now = 0;     // stages until this wave's own rows; the pass
     for (int kt = 0; kt < n; ++kt) {
         if (kt + 1 < n) meet<kLoads>();
         else meet();
@@ -174,8 +186,27 @@ __device__ __forceinline__ void multiply_columns(f32x4_t (&acc)[8][4], int nk, i
                         const int i = (j & 1) ? 3 - ii : ii;
                         acc[4 * h + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], q[j], acc[4 * h + i][j], 0, 0, 0);
                     }
+                // (P's lo meets a unit matrix, too, in its own pass)
+#pragma unroll
+                for (int z = 0; z < 2; ++z)
+                    if (own_in == -z && (PARTS == 1 || now != 1)) {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const f16x8_t e = unit_part(j, own), el = unit_part(j, own_lo);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                f32x4_t &a = acc[4 * h + i][2 * z + j];
+                                a = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], el, a, 0, 0, 0);
+                                a = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], e, a, 0, 0, 0);
+                            }
+                        }
+                    }
             }
         }
+        if (PARTS > 1 && own_at - own_in == nk - 1) {
+            own_in = own_at;
+            ++now;
+        } else --own_in;
         st = st == lds + 2 * kStage ? lds : st + kStage;
     }
     meet();
@@ -216,24 +247,42 @@ template <bool LO> __device__ __forceinline__ void add8(const Pair &src, int64_t
     for (int u = 0; u < 8; ++u) v[u] = fmaf(c, LO ? (float)h[u] + (float)lo[u] : (float)h[u], v[u]);
 }
 
+// where tile (ti, tj) of a result begins, and the distance of its rows
+template <int MODE, int N> __device__ __forceinline__ int64_t tile_at(const Product &o, int64_t m, int ti, int tj, int64_t &ld) {
+    constexpr bool kSq = MODE == kGram || MODE == kSquare;
+    ld = kSq ? o.sp : o.lp;
+    return m * o.sp * ld + (int64_t)ti * N * ld + (int64_t)tj * N;
+}
 // What is made of an N x N tile of sums: rows of block ti, columns of block tj.  Through LDS, so that whole lines are read and written.
 template <int MODE, bool SPLIT, int N, typename OUT>
 __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti, int tj, float *sums) {
     constexpr bool kMirror = MODE == kGram || MODE == kSquare;
-    const int64_t xs = (int64_t)o.sp * o.lp, as = (int64_t)o.sp * o.sp, ld = kMirror ? o.sp : o.lp;
-    const int64_t tile = m * (kMirror ? as : xs) + (int64_t)ti * N * ld + (int64_t)tj * N;
+    int64_t ld;
+    const int64_t tile = tile_at<MODE, N>(o, m, ti, tj, ld);
     const bool mirror = kMirror && ti != tj;
-    // eight columns of a row to a thread at a time
-#pragma unroll 2
-    for (int k = 0; k < N * N / 8 / 256; ++k) {
-        const int c = threadIdx.x + 256 * k, r = c / (N / 8), col = c % (N / 8) * 8;
+    // Eight columns of a row to a thread at a time.  X's lo: some loads together, one behind the other's stores their latencies were most
+    // of the time.
+    constexpr bool kLow = !SPLIT && (MODE == kStep || MODE == kLast);
+    constexpr int kEach = N * N / 8 / 256, kBatch = kLow ? (kEach < 4 ? kEach : 4) : 1;
+    for (int k0 = 0; k0 < kEach; k0 += kBatch) {
+    f16x8_t low[kBatch];
+    if constexpr (kLow) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int c = threadIdx.x + 256 * (k0 + k);
+            low[k] = *(const f16x8_t *)(o.E1.lo + tile + (int64_t)(c / (N / 8)) * ld + c % (N / 8) * 8);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+        const int c = threadIdx.x + 256 * (k0 + k), r = c / (N / 8), col = c % (N / 8) * 8;
         const int64_t e = tile + (int64_t)r * ld + col;
         float v[8];
         read_along<N>(sums, r, col, v);
         if constexpr (MODE == kSquare) {
 #pragma unroll
             for (int u = 0; u < 8; ++u) v[u] *= o.cd;
-            add8<SPLIT>(o.E1, e, o.c1, v);
+            if (o.E1.hi) add8<SPLIT>(o.E1, e, o.c1, v);
             if (o.E2.hi) add8<SPLIT>(o.E2, e, o.c2, v);
             const int row = ti * N + r;
             if (ti == tj && row < o.s) {
@@ -241,7 +290,10 @@ __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti,
                 for (int u = 0; u < 8; ++u) v[u] += row == tj * N + col + u ? o.diag : 0.0f;
             }
         }
-        if constexpr (MODE == kStep || MODE == kLast) add8<true>(o.E1, e, o.c1, v);
+        if constexpr (kLow) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = fmaf(o.c1, (float)low[k][u], v[u]);
+        }
         if constexpr (MODE == kLast) {
 #pragma unroll
             for (int u = 0; u < 8; ++u) v[u] *= o.out;
@@ -251,6 +303,7 @@ __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti,
             for (int u = 0; u < 8; u += 4) *(f32x4_t *)(sums + sums_at<N>(r, col + u)) = *(const f32x4_t *)(v + u);
         }
         if constexpr (MODE != kLast) put8<MODE == kStep || SPLIT>(o.dst, e, v);
+    }
     }
     if constexpr (MODE == kLast) {
         __syncthreads();
@@ -278,7 +331,7 @@ __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti,
         if (!mirror) return;
         __syncthreads();
         // the mirror image: eight rows' values of one column to a thread
-        const int64_t mirrored = m * as + (int64_t)tj * N * ld + (int64_t)ti * N;
+        const int64_t mirrored = tile_at<MODE, N>(o, m, tj, ti, ld);
 #pragma unroll 2
         for (int k = 0; k < N * N / 8 / 256; ++k) {
             const int c = threadIdx.x + 256 * k, r = c / (N / 8), col = c % (N / 8) * 8;
@@ -362,7 +415,8 @@ template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(
     constexpr int PARTS = SPLIT ? 3 : 1;
     const int64_t po = m * (MODE == kSquare ? as : xs) + (int64_t)tj * 2 * kSide, qo = m * as + (int64_t)ti * kSide;
     multiply_columns<PARTS>(acc, o.sp / 32, 2 * ldp, 2 * o.sp, Passes<PARTS>{(const char *)(o.P.hi + po), (const char *)(o.P.lo + po), 0},
-                            Passes<PARTS>{(const char *)(o.Q.hi + qo), (const char *)(o.Q.lo + qo), 1}, 2 * 64 * half, q0, wanted(half), lds);
+                            Passes<PARTS>{(const char *)(o.Q.hi + qo), (const char *)(o.Q.lo + qo), 1}, 2 * 64 * half, q0, wanted(half),
+                            (ti * kSide + q0) / 32, o.own, o.own_lo, lds);
     float *sums = (float *)lds;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -423,7 +477,7 @@ template <class L> __device__ __forceinline__ void small_issue(const L &l, const
 // windows first .. first + n - 1 of P and Q; 4 waves of 32 x 32
 template <bool SPLIT, class PL, class QL>
 __device__ __forceinline__ void multiply_small(f32x4_t (&acc)[2][2], int first, int n, const PL &pl, const Pair &P, int ldp, const QL &ql, const Pair &Q,
-                                               int ldq, char *lds) {
+                                               int ldq, int own_at, f16_t own, f16_t own_lo, char *lds) {
     constexpr int kParts = SPLIT ? 2 : 1, kBuf = 8 / kParts, kBytes = 2 * kParts * kSmallWin, kEach = 4 * kParts;   // loads of a wave to a window
     const uint32_t at = lds_addr(lds);
     auto issue = [&](int w) {
@@ -456,6 +510,18 @@ __device__ __forceinline__ void multiply_small(f32x4_t (&acc)[2][2], int first, 
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], q[j], acc[i][j], 0, 0, 0);
+            const bool mine = 2 * (first + w) + u == own_at;      // (32 k and 32 rows)
+            if (mine) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const f16x8_t e = unit_part(j, own), el = unit_part(j, own_lo);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], el, acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], e, acc[i][j], 0, 0, 0);
+                    }
+                }
+            }
             if constexpr (SPLIT) {
                 f16x8_t pl2[2], ql2[2];
 #pragma unroll
@@ -469,6 +535,7 @@ __device__ __forceinline__ void multiply_small(f32x4_t (&acc)[2][2], int first, 
                     for (int j = 0; j < 2; ++j) {
                         part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl2[i], q[j], part[i][j], 0, 0, 0);
                         part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], ql2[j], part[i][j], 0, 0, 0);
+                        if (mine) part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl2[i], unit_part(j, own), part[i][j], 0, 0, 0);
                     }
             }
         }
@@ -506,13 +573,14 @@ template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(
         pl.init(2 * ld, p0);
         ql.init(2 * ld, q0);
         multiply_small<SPLIT>(acc, w0, w1 - w0, pl, from(o.P, base + (int64_t)tj * kSmall * ld), 2 * ld, ql,
-                              from(MODE == kGram ? o.P : o.Q, base + (int64_t)ti * kSmall * ld), 2 * ld, lds);
+                              from(MODE == kGram ? o.P : o.Q, base + (int64_t)ti * kSmall * ld), 2 * ld, MODE == kGram ? -1 : (ti * kSmall + q0) / 32, o.own,
+                              o.own_lo, lds);
     } else {
         SmallTr pl;
         pl.init(2 * o.lp, p0);
         ql.init(2 * o.sp, q0);
         multiply_small<SPLIT>(acc, 0, o.sp / kBK3, pl, from(o.P, m * xs + (int64_t)tj * kSmall), 2 * o.lp, ql,
-                              from(o.Q, m * as + (int64_t)ti * kSmall * o.sp), 2 * o.sp, lds);
+                              from(o.Q, m * as + (int64_t)ti * kSmall * o.sp), 2 * o.sp, (ti * kSmall + q0) / 32, o.own, o.own_lo, lds);
     }
     if (MODE == kGram && cut > 1) {
         float *to = parts + (int64_t)blockIdx.x * (kSmall * kSmall) + threadIdx.x * 16;
@@ -722,6 +790,7 @@ bool in_range(int steps, const float *q, bool split, bool small) {
                 to *= P1;
             } else all[2] = P - apart(k, steps, q);
             for (double v : all) most = std::fmax(most, std::fabs(v));
+            most = std::fmax(most, std::fabs(apart(k, steps, q) * (two ? apart(k + 1, steps, q) : 1.0)));
             next = std::fmax(next, std::fabs(to));
         }
         if (!(most * room < 15.0 && next * room < 15.0)) return false;
@@ -745,6 +814,7 @@ hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pai
     const int square_tiles = p.small ? half : r * (r + 1) + (ns & 1 ? r + 1 : 0);
     const int step_tiles = ns * (p.small ? o.lp / side : (o.lp + 2 * side - 1) / (2 * side));
     const float a = coef[0], b = coef[1], c = coef[2];
+    const Pair none = {nullptr, nullptr};
     float *no_parts = nullptr;
     hipError_t e = hipSuccess;
     auto gram = [&](Pair to) {
@@ -755,15 +825,23 @@ hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pai
         else e = launch(ortho_small_kernel<kGram, SPLIT, float>, matrices * half * p.cut, kLdsSmall, s, o, p.cut, parts);
         if (e == hipSuccess && p.cut > 1) e = launch(ortho_join_kernel<SPLIT>, matrices * half, 0, s, o, p.cut, (const float *)parts);
     };
-    auto square = [&](Pair to, float cd, Pair q, Pair from, float c1, Pair e1, float c2, Pair e2, double diag) {
+    auto set_own = [&](double v) {
+        o.own = (f16_t)(float)(v * kUnit);
+        o.own_lo = (f16_t)(float)(v * kUnit - (double)(float)o.own);
+    };
+    // to = cd q from + c1 from + c2 e2 + diag
+    auto square = [&](Pair to, float cd, Pair q, Pair from, float c1, float c2, Pair e2, double diag) {
         o.ntiles = square_tiles;
-        o.Q = q; o.P = from; o.E1 = e1; o.E2 = e2; o.dst = to;
+        o.Q = q; o.P = from; o.E2 = e2; o.dst = to;
+        // (a quotient that is no f16: the matrix is read again)
+        const bool own = std::fabs((double)c1) < 15.0 * std::fabs((double)cd);
+        set_own(own ? (double)c1 / cd : 0.0);
+        o.E1 = own ? none : from;
         o.cd = cd; o.c1 = c1; o.c2 = c2; o.diag = (float)(diag * kUnit);
         if (e != hipSuccess) return;
         e = p.small ? launch(ortho_small_kernel<kSquare, SPLIT, float>, matrices * square_tiles, kLdsSmall, s, o, 1, no_parts)
                     : launch(ortho_product_kernel<kSquare, SPLIT, float>, matrices * square_tiles, kLdsProduct, s, o);
     };
-    const Pair none = {nullptr, nullptr};
     for (int k = 0; k < steps;) {
         const bool two = two_together(k, steps, SPLIT, p.small);
         double out_of = apart(k, steps, coef);
@@ -771,18 +849,19 @@ hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pai
         gram(A);
         if (two) {
             out_of *= apart(k + 1, steps, coef);
-            square(B, c, A, A, b, A, 0.0f, none, 0.0);                                      // B = b A + c A A
-            square(C, 1.0f, B, A, a, A, 0.0f, none, 0.0);                                   // C = (a + B) A
-            square(A, 1.0f, C, B, a, C, 0.0f, none, 0.0);                                   // A' = C (a + B)
-            square(C, c, A, A, b, A, 0.0f, none, 0.0);                                      // B' = b A' + c A' A'
-            square(A, 1.0f, C, B, a, B, a, C, (double)a * a - out_of);                      // Q = (a + B') (a + B)
+            square(B, c, A, A, b, 0.0f, none, 0.0);                             // B = b A + c A A
+            square(C, 1.0f, B, A, a, 0.0f, none, 0.0);                          // C = (a + B) A
+            square(A, 1.0f, B, C, a, 0.0f, none, 0.0);                          // A' = (a + B) C
+            square(C, c, A, A, b, 0.0f, none, 0.0);                             // B' = b A' + c A' A'
+            square(A, 1.0f, C, B, a, a, C, (double)a * a - out_of);             // Q = (a + B') (a + B)
             q = A;
         } else {
-            square(B, c, A, A, b, A, 0.0f, none, (double)a - out_of);
+            square(B, c, A, A, b, 0.0f, none, (double)a - out_of);
         }
         k += two ? 2 : 1;
         o.ntiles = step_tiles;
         o.Q = q; o.P = X; o.E1 = X; o.dst = Y;
+        set_own(out_of);
         o.c1 = (float)out_of;
         o.out = scale / kUnit;
         const int64_t grid = matrices * step_tiles;
