@@ -34,6 +34,8 @@
 // later stages to warm L2 was tried and measured slower: the extra requests cost more in the
 // vector memory path than the shorter load latency gave back.)
 #pragma once
+#include <type_traits>
+
 #include "r3_mfma.h"
 
 namespace r3 {
@@ -357,14 +359,29 @@ struct Frags {
     }
 };
 
+// The instruction: bf16, or f16 for an operand that says so (`typedef MfmaF16 Mfma`; its fragments travel as bf16x8_t, too).
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+struct MfmaBf16 {
+    static __device__ __forceinline__ f32x4_t run(const bf16x8_t &a, const bf16x8_t &b, const f32x4_t &c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+struct MfmaF16 {
+    static __device__ __forceinline__ f32x4_t run(const bf16x8_t &a, const bf16x8_t &b, const f32x4_t &c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+    }
+};
+template <class Op, class = void> struct MfmaOf { typedef MfmaBf16 T; };
+template <class Op> struct MfmaOf<Op, std::void_t<typename Op::Mfma>> { typedef typename Op::Mfma T; };
+
 // four MFMAs: half H of the wave's P tiles with Q tile j.  The P index runs back and forth, so that neighbouring MFMAs share
 // an operand.
-template <int H>
+template <int H, class M = MfmaBf16>
 __device__ __forceinline__ void mfma_col(Acc2 &acc, const bf16x8_t (&a)[kHalfP], const bf16x8_t &b, int j) {
 #pragma unroll
     for (int ii = 0; ii < kHalfP; ++ii) {
         const int i = (j & 1) ? kHalfP - 1 - ii : ii;
-        acc[H * kHalfP + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b, acc[H * kHalfP + i][j], 0, 0, 0);
+        acc[H * kHalfP + i][j] = M::run(a[i], b, acc[H * kHalfP + i][j]);
     }
 }
 // One MFMA, some of the READS LDS reads, one MFMA, ...: the first MFMA goes out at once (right after a barrier the matrix
@@ -387,38 +404,39 @@ __device__ __forceinline__ void thread_reads() {
 // registers in all next to the 128 accumulators (with a second set for Q, 16 more, the kernels spill).  Left alone the
 // compiler sinks the reads below the MFMAs and every sub-step starts by waiting on LDS: hence the fixed order.
 // fp(i), fq(j): the step's fragments of P tile i and Q tile j.
-template <int PREADS, int QREADS, class FP, class FQ>
+template <int PREADS, int QREADS, class M = MfmaBf16, class FP, class FQ>
 __device__ __forceinline__ void step_first(Acc2 &acc, Frags &f, FP fp, FQ fq) {
 #pragma unroll
     for (int i = 0; i < kHalfP; ++i) f.y[i] = fp(i);
-    mfma_col<1>(acc, f.x, f.q[0], 0);
+    mfma_col<1, M>(acc, f.x, f.q[0], 0);
     thread_reads<kHalfP * PREADS>();
 #pragma unroll
     for (int j = 1; j < kTQ2; ++j) {
         f.q[j - 1] = fq(j - 1);
-        mfma_col<1>(acc, f.x, f.q[j], j);
+        mfma_col<1, M>(acc, f.x, f.q[j], j);
         thread_reads<QREADS>();
     }
 }
-template <int PREADS, int QREADS, class FP, class FQ>
+template <int PREADS, int QREADS, class M = MfmaBf16, class FP, class FQ>
 __device__ __forceinline__ void step_second(Acc2 &acc, Frags &f, FP fp, FQ fq) {
     f.q[kTQ2 - 1] = fq(kTQ2 - 1);
     f.x[0] = fp(kHalfP);
     f.x[1] = fp(kHalfP + 1);
-    mfma_col<0>(acc, f.y, f.q[0], 0);
+    mfma_col<0, M>(acc, f.y, f.q[0], 0);
     thread_reads<2 * PREADS + QREADS>();
     f.x[2] = fp(kHalfP + 2);
     f.x[3] = fp(kHalfP + 3);
-    mfma_col<0>(acc, f.y, f.q[1], 1);
+    mfma_col<0, M>(acc, f.y, f.q[1], 1);
     thread_reads<2 * PREADS>();
-    mfma_col<0>(acc, f.y, f.q[2], 2);
-    mfma_col<0>(acc, f.y, f.q[3], 3);
+    mfma_col<0, M>(acc, f.y, f.q[2], 2);
+    mfma_col<0, M>(acc, f.y, f.q[3], 3);
     __builtin_amdgcn_sched_barrier(0);
 }
 // the last second half
+template <class M = MfmaBf16>
 __device__ __forceinline__ void step_last(Acc2 &acc, const Frags &f) {
 #pragma unroll
-    for (int j = 0; j < kTQ2; ++j) mfma_col<1>(acc, f.x, f.q[j], j);
+    for (int j = 0; j < kTQ2; ++j) mfma_col<1, M>(acc, f.x, f.q[j], j);
 }
 
 // The same two sub-steps for the ring of stages, whose operands are both transposed tiles.  Such a fragment is two LDS reads, a stage's 24 of
@@ -764,10 +782,10 @@ __device__ __forceinline__ void window_compute(Acc2 &acc, Frags &f, const POp &P
     for (int u = 0; u < 2; ++u) {
         auto fp = [&](int i) { return win_frag(P, pwin, i, u); };
         auto fq = [&](int j) { return win_frag(Q, qwin, j, u); };
-        step_first<POp::kReads, QOp::kReads>(acc, f, fp, fq);
+        step_first<POp::kReads, QOp::kReads, typename MfmaOf<POp>::T>(acc, f, fp, fq);
         if (u == 0 && load_q) win_issue(Q, Jnext, qnext, qrows);
         __builtin_amdgcn_sched_barrier(0);
-        step_second<POp::kReads, QOp::kReads>(acc, f, fp, fq);
+        step_second<POp::kReads, QOp::kReads, typename MfmaOf<POp>::T>(acc, f, fp, fq);
     }
 }
 
@@ -830,7 +848,7 @@ __device__ __forceinline__ void mfma_mainloop3(Acc2 &acc, int nw, const POp &P, 
             window_barrier();
         }
     }
-    step_last(acc, f);
+    step_last<typename MfmaOf<POp>::T>(acc, f);
 }
 
 // ---------------------------------------------------------------------------

@@ -24,15 +24,13 @@ namespace {
 
 typedef _Float16 f16_t;
 typedef f16_t f16x4_t __attribute__((ext_vector_type(4)));
-typedef f16_t f16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kSide = 128;                 // a work-group's tile
-constexpr int kWin = kSide * kBK3 * 2;     // 16 KB: 64 k of an operand
 constexpr float kUnit = 4096.0f;           // what is stored is times this
 constexpr int kPitchF = kSide + 4;         // of a tile of results in LDS
-constexpr int kLdsGram = kSide * kPitchF * 4;   // 66 KB: four windows of operands, or a tile of results
+constexpr int kLdsGram = kSide * kPitchF * 4;   // 66 KB: a tile of results (X X^T: two, where the windows of operands were)
 constexpr int kLdsProduct = 3 * 24 * 1024;      // 72 KB: three stages of operands, or a tile of results
-static_assert(kLdsGram >= 4 * kWin && kLdsProduct >= kLdsGram, "");
+static_assert(2 * kLdsGram >= 2 * kSuperBytes && kLdsProduct >= kLdsGram, "");
 
 struct Pair { f16_t *hi, *lo; };   // lo may be null
 
@@ -60,25 +58,6 @@ __device__ __forceinline__ f16x8_t unit_part(int j, f16_t own) {
     return v;
 }
 
-// Operands with k along their rows (X in X X^T): windows of 64 k, 128 rows.  All rows exist.
-struct KcLoad {
-    int voff, step;
-    KcFrag16 fr;
-    __device__ __forceinline__ void init(int ld, int wave_base) {
-        const int w = threadIdx.x >> 6, lane = lane_id(), row = 8 * w + (lane >> 3);
-        voff = row * ld + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
-        step = 32 * ld;
-        fr.init(wave_base, lane);
-    }
-    __device__ __forceinline__ void issue(const char *base, int J, uint32_t win) const {
-        const rsrc_t r = src_rsrc_inside(Src{base, 0, kBK3 * 2}, J);
-        const int w = threadIdx.x >> 6;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) lds_load16_soff(r, win + 1024 * (w + 4 * i), voff, i * step);
-    }
-    __device__ __forceinline__ f16x8_t frag(const char *win, int t, int u) const { return __builtin_bit_cast(f16x8_t, fr.read(win, t, u)); }
-};
-
 // All but LOADS of this wave's loads have landed and everybody has left the stage before, whose place the next loads take.
 template <int LOADS = 0> __device__ __forceinline__ void meet() {
     asm volatile("" ::: "memory");
@@ -93,46 +72,39 @@ template <int PARTS> struct Passes {
     __device__ __forceinline__ const char *of(int pass) const { return PARTS == 3 && pass == low ? lo : hi; }
 };
 
-// 128 x 128 from rows with k along them; 4 waves of 64 x 64, as 4 x 4 of 16 x 16
-template <int PARTS>
-__device__ __forceinline__ void multiply_rows(f32x4_t (&acc)[4][4], int nw, int ld, const Passes<PARTS> &P, const Passes<PARTS> &Q, int p0, int q0,
-                                              char *lds) {
-    KcLoad pl, ql;
-    pl.init(ld, p0);
-    ql.init(ld, q0);
-    const uint32_t at = lds_addr(lds);
-    int pass = 0, J = 0;      // of the next window to load
-    auto issue = [&](int buf) {
-        pl.issue(P.of(pass), J, at + buf * 2 * kWin);
-        ql.issue(Q.of(pass), J, at + buf * 2 * kWin + kWin);
-        if (++J == nw) {
-            J = 0;
-            ++pass;
-        }
-    };
-    issue(0);
-    for (int w = 0; w < PARTS * nw; ++w) {
-        meet();
-        if (w + 1 < PARTS * nw) issue((w + 1) & 1);
-        const char *pw = lds + (w & 1) * 2 * kWin, *qw = pw + kWin;
+// Operands with k along their rows (X in X X^T) for the tile loop of r3_mfma2.h: windows of 64 k of 256 rows, a pass behind the other.
+// Rows past the last matrix's last read zeros, those past another's are the next one's, in results that nobody stores.
+template <int PARTS> struct RowsOp {
+    static constexpr bool kIndexed = false, kWindowed = true;
+    static constexpr int kReads = 1;
+    typedef MfmaF16 Mfma;
+    rsrc_t hi, lo;
+    int nw, low, voff, step;
+    KcFrag16 fr;
+    // `bytes`: from the tile's first row to the end of all matrices
+    __device__ __forceinline__ void init(const f16_t *h, const f16_t *l, uint64_t bytes, int ld, int nw_, int low_, int wave_base) {
+        hi = src_rsrc(Src{(const char *)h, bytes, 0u}, 0);
+        if constexpr (PARTS == 3) lo = src_rsrc(Src{(const char *)l, bytes, 0u}, 0);
+        nw = nw_;
+        low = low_;
+        const int w = threadIdx.x >> 6, lane = lane_id(), row = 8 * (w & 3) + (lane >> 3);
+        voff = row * ld + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+        step = __builtin_amdgcn_readfirstlane(32 * ld);
+        fr.init(wave_base, lane);
+    }
+    __device__ __forceinline__ void issue_window(int J, uint32_t win, int = kTile) const {
+        const int pass = PARTS == 3 ? (J >= nw) + (J >= 2 * nw) : 0;
+        const rsrc_t r = PARTS == 3 && pass == low ? lo : hi;
+        const int adv = (J - pass * nw) * (kBK3 * 2), w = threadIdx.x >> 6;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            f16x8_t p[4], q[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = pl.frag(pw, i, u);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) q[j] = ql.frag(qw, j, u);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int ii = 0; ii < 4; ++ii) {
-                    const int i = (j & 1) ? 3 - ii : ii;
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], q[j], acc[i][j], 0, 0, 0);
-                }
+        for (int i = 0; i < 8; ++i) {
+            int sum = adv + i * step;
+            asm("" : "+s"(sum));
+            lds_load16(r, win + 1024 * ((w & 3) + kLoaderWaves * i), voff + sum);
         }
     }
-    meet();
-}
+    __device__ __forceinline__ bf16x8_t frag_window(const char *win, int t, int u) const { return fr.read(win, t, u); }
+};
 
 // 256 (P) x 128 (Q) from k-rows (X, and symmetric matrices, whose k-rows are their rows); 4 waves of 128 x 64, as 8 x 4 of 16 x 16; a ring
 // of three stages of 32 k.  Two work-groups to a compute unit: one multiplies while the other is in its epilogue.  P's columns past its
@@ -255,7 +227,7 @@ template <int MODE, int N> __device__ __forceinline__ int64_t tile_at(const Prod
 }
 // What is made of an N x N tile of sums: rows of block ti, columns of block tj.  Through LDS, so that whole lines are read and written.
 template <int MODE, bool SPLIT, int N, typename OUT>
-__device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti, int tj, float *sums) {
+__device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti, int tj, float *sums, int tid) {
     constexpr bool kMirror = MODE == kGram || MODE == kSquare;
     int64_t ld;
     const int64_t tile = tile_at<MODE, N>(o, m, ti, tj, ld);
@@ -269,13 +241,13 @@ __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti,
     if constexpr (kLow) {
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            const int c = threadIdx.x + 256 * (k0 + k);
+            const int c = tid + 256 * (k0 + k);
             low[k] = *(const f16x8_t *)(o.E1.lo + tile + (int64_t)(c / (N / 8)) * ld + c % (N / 8) * 8);
         }
     }
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-        const int c = threadIdx.x + 256 * (k0 + k), r = c / (N / 8), col = c % (N / 8) * 8;
+        const int c = tid + 256 * (k0 + k), r = c / (N / 8), col = c % (N / 8) * 8;
         const int64_t e = tile + (int64_t)r * ld + col;
         float v[8];
         read_along<N>(sums, r, col, v);
@@ -311,7 +283,7 @@ __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti,
         const int r0 = (o.transposed ? tj : ti) * N, c0 = (o.transposed ? ti : tj) * N;
         OUT *out = (OUT *)o.O + m * rows * cols;
         for (int k = 0; k < N * N / 8 / 256; ++k) {
-            const int e = threadIdx.x + 256 * k, r = e / (N / 8), c = e % (N / 8) * 8;
+            const int e = tid + 256 * k, r = e / (N / 8), c = e % (N / 8) * 8;
             if (r0 + r >= rows || c0 + c >= cols) continue;
             float v[8];
             if (o.transposed) read_down<N>(sums, c, r, v);
@@ -329,12 +301,12 @@ __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti,
     }
     if constexpr (kMirror) {
         if (!mirror) return;
-        __syncthreads();
+        if constexpr (MODE == kSquare) __syncthreads();
         // the mirror image: eight rows' values of one column to a thread
         const int64_t mirrored = tile_at<MODE, N>(o, m, tj, ti, ld);
 #pragma unroll 2
         for (int k = 0; k < N * N / 8 / 256; ++k) {
-            const int c = threadIdx.x + 256 * k, r = c / (N / 8), col = c % (N / 8) * 8;
+            const int c = tid + 256 * k, r = c / (N / 8), col = c % (N / 8) * 8;
             float v[8];
             read_down<N>(sums, col, r, v);
             put8<SPLIT>(o.dst, mirrored + (int64_t)r * ld + col, v);
@@ -368,21 +340,33 @@ __device__ __forceinline__ void lower_half(int t, int &ti, int &tj) {
     tj = __builtin_amdgcn_readfirstlane(t - i * (i + 1) / 2);
 }
 
-template <bool SPLIT> __global__ void __launch_bounds__(256, 2) ortho_gram_kernel(Product o) {
+// X X^T: 256 x 256, the lower half of them.  Its k is the long side and its results are few: the tile loop with the fewest loads.
+template <bool SPLIT> __global__ void __launch_bounds__(kThreads2, kMinWavesPerSimd) ortho_gram_kernel(Product o, int64_t matrices) {
     extern __shared__ __align__(1024) char lds[];
     const int64_t at = xcd_share(blockIdx.x, gridDim.x), m = at / o.ntiles;
-    const int t = (int)(at - m * o.ntiles);
     int ti, tj;
-    lower_half(t, ti, tj);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p0 = 64 * (wave & 1), q0 = 64 * (wave >> 1);
-    f32x4_t acc[4][4] = {};
+    lower_half((int)(at - m * o.ntiles), ti, tj);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pw = wave & 1, qw = wave >> 1;
     constexpr int PARTS = SPLIT ? 3 : 1;
-    const int64_t base = m * o.sp * (int64_t)o.lp, ro = base + (int64_t)ti * kSide * o.lp, co = base + (int64_t)tj * kSide * o.lp;
-    multiply_rows<PARTS>(acc, o.lp / kBK3, 2 * o.lp, Passes<PARTS>{(const char *)(o.P.hi + co), (const char *)(o.P.lo + co), 0},
-                         Passes<PARTS>{(const char *)(o.P.hi + ro), (const char *)(o.P.lo + ro), 1}, p0, q0, lds);
-    put_sums<kSide>(acc, p0, q0, (float *)lds);
-    __syncthreads();
-    finish_tile<kGram, SPLIT, kSide, float>(o, m, ti, tj, (float *)lds);
+    const int64_t xs = (int64_t)o.sp * o.lp, end = matrices * xs;
+    const int64_t po = m * xs + (int64_t)tj * kTile * o.lp, qo = m * xs + (int64_t)ti * kTile * o.lp;
+    const int nw = o.lp / kBK3;
+    RowsOp<PARTS> P, Q;
+    P.init(o.P.hi + po, o.P.lo + po, (uint64_t)(end - po) * 2, 2 * o.lp, nw, 0, 128 * pw);
+    Q.init(o.P.hi + qo, o.P.lo + qo, (uint64_t)(end - qo) * 2, 2 * o.lp, nw, 1, kWaveRowsQ * qw);
+    Acc2 acc;
+    zero_acc2(acc);
+    mfma_mainloop3<true>(acc, PARTS * nw, P, Q, lds);
+    // two blocks of 128 x 128 at a time, to four waves each
+    const int blocks = o.sp / kSide;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        __syncthreads();
+        if ((qw >> 1) == h) put_sums<kSide>(acc, 0, 64 * (qw & 1), (float *)(lds + pw * kLdsGram));
+        __syncthreads();
+        const int side = wave >> 2, ci = 2 * ti + h, cj = 2 * tj + side;
+        if (ci < blocks && cj <= ci) finish_tile<kGram, SPLIT, kSide, float>(o, m, ci, cj, (float *)(lds + side * kLdsGram), threadIdx.x & 255);
+    }
 }
 
 template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(256, 2) ortho_product_kernel(Product o) {
@@ -424,7 +408,7 @@ template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(
         if (h) __syncthreads();
         if (half == h) put_sums<kSide>(acc, 0, q0, sums);
         __syncthreads();
-        finish_tile<MODE, SPLIT, kSide, OUT>(o, m, ti, 2 * tj + h, sums);
+        finish_tile<MODE, SPLIT, kSide, OUT>(o, m, ti, 2 * tj + h, sums, threadIdx.x);
     }
 }
 
@@ -592,7 +576,7 @@ template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(
     }
     put_sums<kSmall>(acc, p0, q0, (float *)lds);
     __syncthreads();
-    finish_tile<MODE, SPLIT, kSmall, OUT>(o, m, ti, tj, (float *)lds);
+    finish_tile<MODE, SPLIT, kSmall, OUT>(o, m, ti, tj, (float *)lds, threadIdx.x);
 }
 
 // the parts of a tile of X X^T, in their order
@@ -612,7 +596,7 @@ template <bool SPLIT> __global__ void __launch_bounds__(256) ortho_join_kernel(P
             for (int j = 0; j < 2; ++j) acc[i][j] += *(const f32x4_t *)(from + 8 * i + 4 * j);
     put_sums<kSmall>(acc, p0, q0, sums);
     __syncthreads();
-    finish_tile<kGram, SPLIT, kSmall, float>(o, m, ti, tj, sums);
+    finish_tile<kGram, SPLIT, kSmall, float>(o, m, ti, tj, sums, threadIdx.x);
 }
 
 // ---- the start: |G| and X = G kUnit / (|G| + eps) ----
@@ -800,9 +784,9 @@ bool in_range(int steps, const float *q, bool split, bool small) {
     return true;
 }
 
-template <class K, class... A> hipError_t launch(K k, int64_t grid, int lds, hipStream_t s, const A &...args) {
+template <int NT = 256, class K, class... A> hipError_t launch(K k, int64_t grid, int lds, hipStream_t s, const A &...args) {
     (void)hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    k<<<(unsigned)grid, 256, lds, s>>>(args...);
+    k<<<(unsigned)grid, NT, lds, s>>>(args...);
     return hipGetLastError();
 }
 
@@ -821,7 +805,11 @@ hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pai
         o.ntiles = half;
         o.P = X; o.dst = to;
         if (e != hipSuccess) return;
-        if (!p.small) e = launch(ortho_gram_kernel<SPLIT>, matrices * half, kLdsGram, s, o);
+        if (!p.small) {
+            const int nt = (o.sp + kTile - 1) / kTile;
+            o.ntiles = nt * (nt + 1) / 2;
+            e = launch<kThreads2>(ortho_gram_kernel<SPLIT>, matrices * o.ntiles, 2 * kLdsGram, s, o, matrices);
+        }
         else e = launch(ortho_small_kernel<kGram, SPLIT, float>, matrices * half * p.cut, kLdsSmall, s, o, p.cut, parts);
         if (e == hipSuccess && p.cut > 1) e = launch(ortho_join_kernel<SPLIT>, matrices * half, 0, s, o, p.cut, (const float *)parts);
     };
