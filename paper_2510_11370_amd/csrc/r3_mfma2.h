@@ -446,38 +446,38 @@ __device__ __forceinline__ void step_last(Acc2 &acc, const Frags &f) {
 // four to a column, and none with the last, before the loads and the barrier: 37.7 us (32x32x16 MFMAs 36.9); 65536 Zipf tokens of the
 // 2048 x 768 x 128-expert layer dW_down 1382 -> 1337, dW_gate/dW_up 2903 -> 2847.  On the windows, half of whose operands or more come in single
 // reads, this order is no faster (131072 tokens forward 0.4 % slower).
-template <class FP, class FQ>
+template <class M = MfmaBf16, class FP, class FQ>
 __device__ __forceinline__ void ring_first(Acc2 &acc, Frags &f, FP fp, FQ fq) {
     f.y[0] = fp(0);
     f.y[1] = fp(1);
-    mfma_col<1>(acc, f.x, f.q[0], 0);
+    mfma_col<1, M>(acc, f.x, f.q[0], 0);
     thread_reads<4>();
     f.q[0] = fq(0);
     f.y[2] = fp(2);
-    mfma_col<1>(acc, f.x, f.q[1], 1);
+    mfma_col<1, M>(acc, f.x, f.q[1], 1);
     thread_reads<4>();
     f.q[1] = fq(1);
     f.y[3] = fp(3);
-    mfma_col<1>(acc, f.x, f.q[2], 2);
+    mfma_col<1, M>(acc, f.x, f.q[2], 2);
     thread_reads<4>();
-    mfma_col<1>(acc, f.x, f.q[3], 3);
+    mfma_col<1, M>(acc, f.x, f.q[3], 3);
     __builtin_amdgcn_sched_barrier(0);
 }
-template <class FP, class FQ>
+template <class M = MfmaBf16, class FP, class FQ>
 __device__ __forceinline__ void ring_second(Acc2 &acc, Frags &f, FP fp, FQ fq) {
     f.q[2] = fq(2);
     f.x[0] = fp(kHalfP);
-    mfma_col<0>(acc, f.y, f.q[0], 0);
+    mfma_col<0, M>(acc, f.y, f.q[0], 0);
     thread_reads<4>();
     f.q[3] = fq(3);
     f.x[1] = fp(kHalfP + 1);
-    mfma_col<0>(acc, f.y, f.q[1], 1);
+    mfma_col<0, M>(acc, f.y, f.q[1], 1);
     thread_reads<4>();
     f.x[2] = fp(kHalfP + 2);
     f.x[3] = fp(kHalfP + 3);
-    mfma_col<0>(acc, f.y, f.q[2], 2);
+    mfma_col<0, M>(acc, f.y, f.q[2], 2);
     thread_reads<4>();
-    mfma_col<0>(acc, f.y, f.q[3], 3);
+    mfma_col<0, M>(acc, f.y, f.q[3], 3);
     __builtin_amdgcn_sched_barrier(0);
 }
 

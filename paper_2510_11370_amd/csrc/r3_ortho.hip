@@ -28,11 +28,10 @@ typedef f16_t f16x4_t __attribute__((ext_vector_type(4)));
 constexpr int kSide = 128;                 // a work-group's tile
 constexpr float kUnit = 4096.0f;           // what is stored is times this
 constexpr int kPitchF = kSide + 4;         // of a tile of results in LDS
-constexpr int kLdsGram = kSide * kPitchF * 4;   // 66 KB: a tile of results (X X^T: two, where the windows of operands were)
-constexpr int kLdsProduct = 3 * 24 * 1024;      // 72 KB: three stages of operands, or a tile of results
-static_assert(2 * kLdsGram >= 2 * kSuperBytes && kLdsProduct >= kLdsGram, "");
+constexpr int kLdsTile = kSide * kPitchF * 4;   // 66 KB: 128 x 128 results; two of them, where the windows or stages of operands were
+static_assert(2 * kLdsTile >= 2 * kSuperBytes && 2 * kLdsTile >= kStages2 * kStageBytes, "");
 
-struct Pair { f16_t *hi, *lo; };   // lo may be null
+struct Pair { f16_t *hi, *lo; };   // (lo: f16, or X's 8 bits where only hi is multiplied)
 
 // A launch's product D[q][p] = sum_k Q[q][k] P[p][k] per matrix and what is made of it, all in units of 1 / kUnit:
 //   result = cd (D + own P) + c1 E1 + c2 E2 + diag I
@@ -43,6 +42,7 @@ enum { kGram = 0, kSquare = 1, kStep = 2, kLast = 3 };
 struct Product {
     int s, l, sp, lp;              // X is s x l in sp x lp, A and the like s x s in sp x sp, zeros beyond
     int ntiles;                    // of a matrix
+    int passes;                    // through k: 1, or 3 for pairs (as a constant of the loop it costs registers that spill)
     Pair Q, P, E1, E2, dst;        // (E1, E2: or none)
     f16_t own, own_lo;             // times kUnit
     float cd, c1, c2, diag, out;
@@ -50,12 +50,12 @@ struct Product {
     bool transposed;
 };
 // `own` times columns 16 j .. + 15 of a unit matrix of 32 rows, as an operand's fragment
-__device__ __forceinline__ f16x8_t unit_part(int j, f16_t own) {
-    const int lane = lane_id(), at = 16 * j + (lane & 15) - 8 * (lane >> 4);
+__device__ __forceinline__ bf16x8_t unit_part(int lane, int j, f16_t own) {
+    const int at = 16 * j + (lane & 15) - 8 * (lane >> 4);
     f16x8_t v;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = at == e ? own : (f16_t)0.0f;
-    return v;
+    return __builtin_bit_cast(bf16x8_t, v);
 }
 
 // All but LOADS of this wave's loads have landed and everybody has left the stage before, whose place the next loads take.
@@ -65,12 +65,7 @@ template <int LOADS = 0> __device__ __forceinline__ void meet() {
     asm volatile("" ::: "memory");
 }
 
-// Which parts of the operands a pass multiplies: 1: hi hi; 3: lo hi, hi lo, hi hi.
-template <int PARTS> struct Passes {
-    const char *hi, *lo;
-    int low;     // the pass that takes lo
-    __device__ __forceinline__ const char *of(int pass) const { return PARTS == 3 && pass == low ? lo : hi; }
-};
+// `PARTS` of the operations below: 1: hi hi; 3: lo hi, hi lo, hi hi, one pass through k after the other (`low`: which takes an operand's lo)
 
 // Operands with k along their rows (X in X X^T) for the tile loop of r3_mfma2.h: windows of 64 k of 256 rows, a pass behind the other.
 // Rows past the last matrix's last read zeros, those past another's are the next one's, in results that nobody stores.
@@ -106,82 +101,84 @@ template <int PARTS> struct RowsOp {
     __device__ __forceinline__ bf16x8_t frag_window(const char *win, int t, int u) const { return fr.read(win, t, u); }
 };
 
-// 256 (P) x 128 (Q) from k-rows (X, and symmetric matrices, whose k-rows are their rows); 4 waves of 128 x 64, as 8 x 4 of 16 x 16; a ring
-// of three stages of 32 k.  Two work-groups to a compute unit: one multiplies while the other is in its epilogue.  P's columns past its
-// row's end are the next row's: finite or not, they stay in results that nobody stores.
-constexpr int kStageP = 32 * 256 * 2, kStageQ = 32 * kSide * 2, kStage = kStageP + kStageQ;   // 24 KB
-constexpr int kLoads = kStage / 4096;     // 16-byte loads of a wave to a stage
-template <int PARTS>
-__device__ __forceinline__ void multiply_columns(f32x4_t (&acc)[8][4], int nk, int ldp, int ldq, const Passes<PARTS> &P, const Passes<PARTS> &Q, int p0,
-                                                 int q0, bool live, int own_at, f16_t own, f16_t own_lo, char *lds) {
-    DmaTR<256> pd;
-    DmaTR<kSide> qd;
-    TrFrag16<256> pf;
-    TrFrag16<kSide> qf;
-    pd.init(ldp, 0);
-    qd.init(ldq, 0);
-    pf.init(p0);
-    qf.init(q0);
+// Operands whose k-rows are rows in memory (X, and symmetric matrices, whose rows and columns are the same): stages of 32 k of 256
+// columns.  Columns past a row's end are the next row's, in results that nobody stores; past the last matrix they are zeros.
+struct ColumnsOp {
+    const char *hi, *lo;
+    uint64_t bytes;
+    uint32_t step;
+    int nk, low;     // (low < 0: hi alone)
+    DmaTR<256> dma;
+    TrFrag16<256> fr;
+    // `bytes`: from the tile's first element to the end of all matrices
+    __device__ __forceinline__ void init(const f16_t *h, const f16_t *l, uint64_t bytes_, int ld, int nk_, int low_, int wave_base) {
+        hi = (const char *)h;
+        lo = (const char *)l;
+        bytes = bytes_;
+        step = 32u * ld;
+        nk = nk_;
+        low = low_;
+        dma.init(ld, 0);
+        fr.init(wave_base);
+    }
+    __device__ __forceinline__ void issue(int kt, uint32_t tile) const {
+        const int pass = (kt >= nk) + (kt >= 2 * nk);
+        dma.issue(src_rsrc(Src{pass == low ? lo : hi, bytes, step}, kt - pass * nk), tile);
+    }
+};
+
+// 256 x 256 in the ring of stages of r3_mfma2.h (its sub-steps, its waves' shares).  Where a stage's k are a wave's own rows, 64 of them in
+// two stages from own_at, P meets `own` times a unit matrix, too (P's lo in its own pass).
+__device__ __forceinline__ void multiply_columns(Acc2 &acc, int passes, const ColumnsOp &P, const ColumnsOp &Q, int own_at, f16_t own, f16_t own_lo,
+                                                 char *lds) {
     const uint32_t at = lds_addr(lds);
-    int pass = 0, J = 0, to = 0;      // of the next stage to load, and where it goes
-    auto issue = [&]() {
-        pd.issue(src_rsrc_inside(Src{P.of(pass), 0, 32u * ldp}, J), at + to);
-        qd.issue(src_rsrc_inside(Src{Q.of(pass), 0, 32u * ldq}, J), at + to + kStageP);
-        to = to == 2 * kStage ? 0 : to + kStage;
-        if (++J == nk) {
-            J = 0;
-            ++pass;
-        }
+    const bool loader = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) < kLoaderWaves;
+    const int nk = P.nk, n = passes * nk;
+    auto issue = [&](int kt) {
+        const uint32_t to = at + (kt & 3) * kStageBytes;
+        P.issue(kt, to);
+        Q.issue(kt, to + kOperandBytes);
     };
-    const int n = PARTS * nk;
-    issue();
-    if (n > 1) issue();
-    const char *st = lds;
+    if (loader) issue(0);
+    if (loader && n > 1) issue(1);
+    if (n > 1) stage_barrier<8>(loader);
+    else stage_barrier<0>(loader);
+    Frags f;
+    f.clear();
     int own_in = own_at, now = 0;     // stages until this wave's own rows; the pass
+#pragma nounroll
     for (int kt = 0; kt < n; ++kt) {
-        if (kt + 1 < n) meet<kLoads>();
-        else meet();
-        if (kt + 2 < n) issue();
-        if (live) {
-            f16x8_t q[4];
+        const char *st = lds + (kt & 3) * kStageBytes;
+        auto fp = [&](int i) { return P.fr.read(st, i); };
+        auto fq = [&](int j) { return Q.fr.read(st + kOperandBytes, j); };
+        ring_first<MfmaF16>(acc, f, fp, fq);
+        if (loader && kt + 2 < n) issue(kt + 2);
+        __builtin_amdgcn_sched_barrier(0);
+        ring_second<MfmaF16>(acc, f, fp, fq);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) q[j] = __builtin_bit_cast(f16x8_t, qf.read(st + kStageP, j));
+        for (int z = 0; z < 2; ++z)
+            if (own_in == -z && now != 1) {
+                int lane = lane_id();
+                asm volatile("" : "+v"(lane));     // (made here, or the fragments are kept in registers all the way)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                f16x8_t p[4];
+                for (int j = 0; j < 2; ++j) {
+                    const bf16x8_t e = unit_part(lane, j, own), el = unit_part(lane, j, own_lo);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = __builtin_bit_cast(f16x8_t, pf.read(st, 4 * h + i));
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int ii = 0; ii < 4; ++ii) {
-                        const int i = (j & 1) ? 3 - ii : ii;
-                        acc[4 * h + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], q[j], acc[4 * h + i][j], 0, 0, 0);
+                    for (int i = 0; i < kTP2; ++i) {
+                        const bf16x8_t &p = i < kHalfP ? f.y[i % kHalfP] : f.x[i % kHalfP];
+                        acc[i][2 * z + j] = MfmaF16::run(p, el, acc[i][2 * z + j]);
+                        acc[i][2 * z + j] = MfmaF16::run(p, e, acc[i][2 * z + j]);
                     }
-                // (P's lo meets a unit matrix, too, in its own pass)
-#pragma unroll
-                for (int z = 0; z < 2; ++z)
-                    if (own_in == -z && (PARTS == 1 || now != 1)) {
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const f16x8_t e = unit_part(j, own), el = unit_part(j, own_lo);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                f32x4_t &a = acc[4 * h + i][2 * z + j];
-                                a = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], el, a, 0, 0, 0);
-                                a = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], e, a, 0, 0, 0);
-                            }
-                        }
-                    }
+                }
             }
-        }
-        if (PARTS > 1 && own_at - own_in == nk - 1) {
+        if (own_at - own_in == nk - 1) {
             own_in = own_at;
             ++now;
         } else --own_in;
-        st = st == lds + 2 * kStage ? lds : st + kStage;
+        if (kt + 2 < n) stage_barrier<8>(loader);
+        else stage_barrier<0>(loader);
     }
-    meet();
+    step_last<MfmaF16>(acc, f);
 }
 
 __device__ __forceinline__ f16_t part_hi(float v) { return (f16_t)v; }
@@ -199,8 +196,28 @@ template <int N> __device__ __forceinline__ void read_down(const float *sums, in
 #pragma unroll
     for (int u = 0; u < 8; ++u) v[u] = at[u * (N + 4)];
 }
-// eight values to their place, and what their rounding leaves
-template <bool LO> __device__ __forceinline__ void put8(const Pair &dst, int64_t e, const float *v) {
+// What an f16 leaves of a value where it is not multiplied (X's, bf16 results): 8 bits with 2 of mantissa, times 2^8, which takes 1e-3 to 2^4
+// times kUnit's results to the middle of their range.  A quarter less to move than with f16 (128 of 2048 x 768: X' 476 | 414 us).
+constexpr float kLow = 256.0f;
+__device__ __forceinline__ uint2 pack_low(const float *v, const f16x8_t &h) {
+    float r[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) r[u] = (v[u] - (float)h[u]) * kLow;
+    int a = __builtin_amdgcn_cvt_pk_bf8_f32(r[0], r[1], 0, false), b = __builtin_amdgcn_cvt_pk_bf8_f32(r[4], r[5], 0, false);
+    a = __builtin_amdgcn_cvt_pk_bf8_f32(r[2], r[3], a, true);
+    b = __builtin_amdgcn_cvt_pk_bf8_f32(r[6], r[7], b, true);
+    return make_uint2((unsigned)a, (unsigned)b);
+}
+__device__ __forceinline__ void add_low(const uint2 &low, float c, float *v) {
+    typedef float f32x2_t __attribute__((ext_vector_type(2)));
+    const f32x2_t r[4] = {__builtin_amdgcn_cvt_pk_f32_bf8((int)low.x, false), __builtin_amdgcn_cvt_pk_f32_bf8((int)low.x, true),
+                          __builtin_amdgcn_cvt_pk_f32_bf8((int)low.y, false), __builtin_amdgcn_cvt_pk_f32_bf8((int)low.y, true)};
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = fmaf(c * (1.0f / kLow), r[u >> 1][u & 1], v[u]);
+}
+// eight values to their place, and what their rounding leaves: nothing of it, an f16 or 8 bits
+enum { kNoRest = 0, kRest16 = 1, kRest8 = 2 };
+template <int REST> __device__ __forceinline__ void put8(const Pair &dst, int64_t e, const float *v) {
     f16x8_t h, lo;
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
@@ -208,7 +225,8 @@ template <bool LO> __device__ __forceinline__ void put8(const Pair &dst, int64_t
         lo[u] = part_lo(v[u], h[u]);
     }
     *(f16x8_t *)(dst.hi + e) = h;
-    if constexpr (LO) *(f16x8_t *)(dst.lo + e) = lo;
+    if constexpr (REST == kRest16) *(f16x8_t *)(dst.lo + e) = lo;
+    if constexpr (REST == kRest8) *(uint2 *)((char *)dst.lo + e) = pack_low(v, h);
 }
 // v += c times eight values
 template <bool LO> __device__ __forceinline__ void add8(const Pair &src, int64_t e, float c, float *v) {
@@ -225,24 +243,25 @@ template <int MODE, int N> __device__ __forceinline__ int64_t tile_at(const Prod
     ld = kSq ? o.sp : o.lp;
     return m * o.sp * ld + (int64_t)ti * N * ld + (int64_t)tj * N;
 }
-// What is made of an N x N tile of sums: rows of block ti, columns of block tj.  Through LDS, so that whole lines are read and written.
+// What is made of an N x N tile of sums, rows of block ti and columns of block tj, by 256 threads.  Through LDS, so that whole lines are read
+// and written; everybody meets between the two.
 template <int MODE, bool SPLIT, int N, typename OUT>
-__device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti, int tj, float *sums, int tid) {
+__device__ __forceinline__ void finish_rows(const Product &o, int64_t m, int ti, int tj, float *sums, int tid) {
     constexpr bool kMirror = MODE == kGram || MODE == kSquare;
     int64_t ld;
     const int64_t tile = tile_at<MODE, N>(o, m, ti, tj, ld);
     const bool mirror = kMirror && ti != tj;
     // Eight columns of a row to a thread at a time.  X's lo: some loads together, one behind the other's stores their latencies were most
     // of the time.
-    constexpr bool kLow = !SPLIT && (MODE == kStep || MODE == kLast);
-    constexpr int kEach = N * N / 8 / 256, kBatch = kLow ? (kEach < 4 ? kEach : 4) : 1;
+    constexpr bool kAddLow = !SPLIT && (MODE == kStep || MODE == kLast);
+    constexpr int kEach = N * N / 8 / 256, kBatch = kAddLow ? (kEach < 4 ? kEach : 4) : 1;
     for (int k0 = 0; k0 < kEach; k0 += kBatch) {
-    f16x8_t low[kBatch];
-    if constexpr (kLow) {
+    uint2 low[kBatch];
+    if constexpr (kAddLow) {
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             const int c = tid + 256 * (k0 + k);
-            low[k] = *(const f16x8_t *)(o.E1.lo + tile + (int64_t)(c / (N / 8)) * ld + c % (N / 8) * 8);
+            low[k] = *(const uint2 *)((const char *)o.E1.lo + tile + (int64_t)(c / (N / 8)) * ld + c % (N / 8) * 8);
         }
     }
 #pragma unroll
@@ -262,10 +281,7 @@ __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti,
                 for (int u = 0; u < 8; ++u) v[u] += row == tj * N + col + u ? o.diag : 0.0f;
             }
         }
-        if constexpr (kLow) {
-#pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = fmaf(o.c1, (float)low[k][u], v[u]);
-        }
+        if constexpr (kAddLow) add_low(low[k], o.c1, v);
         if constexpr (MODE == kLast) {
 #pragma unroll
             for (int u = 0; u < 8; ++u) v[u] *= o.out;
@@ -274,11 +290,13 @@ __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti,
 #pragma unroll
             for (int u = 0; u < 8; u += 4) *(f32x4_t *)(sums + sums_at<N>(r, col + u)) = *(const f32x4_t *)(v + u);
         }
-        if constexpr (MODE != kLast) put8<MODE == kStep || SPLIT>(o.dst, e, v);
+        if constexpr (MODE != kLast) put8<SPLIT ? kRest16 : MODE == kStep ? kRest8 : kNoRest>(o.dst, e, v);
     }
     }
+}
+template <int MODE, bool SPLIT, int N, typename OUT>
+__device__ __forceinline__ void finish_rest(const Product &o, int64_t m, int ti, int tj, const float *sums, int tid) {
     if constexpr (MODE == kLast) {
-        __syncthreads();
         const int rows = o.transposed ? o.l : o.s, cols = o.transposed ? o.s : o.l;
         const int r0 = (o.transposed ? tj : ti) * N, c0 = (o.transposed ? ti : tj) * N;
         OUT *out = (OUT *)o.O + m * rows * cols;
@@ -299,17 +317,17 @@ __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti,
             }
         }
     }
-    if constexpr (kMirror) {
-        if (!mirror) return;
-        if constexpr (MODE == kSquare) __syncthreads();
+    if constexpr (MODE == kGram || MODE == kSquare) {
+        if (ti == tj) return;
         // the mirror image: eight rows' values of one column to a thread
+        int64_t ld;
         const int64_t mirrored = tile_at<MODE, N>(o, m, tj, ti, ld);
 #pragma unroll 2
         for (int k = 0; k < N * N / 8 / 256; ++k) {
             const int c = tid + 256 * k, r = c / (N / 8), col = c % (N / 8) * 8;
             float v[8];
             read_down<N>(sums, col, r, v);
-            put8<SPLIT>(o.dst, mirrored + (int64_t)r * ld + col, v);
+            put8<SPLIT ? kRest16 : kNoRest>(o.dst, mirrored + (int64_t)r * ld + col, v);
         }
     }
 }
@@ -329,6 +347,25 @@ __device__ __forceinline__ void put_sums(const f32x4_t (&acc)[NI][NJ], int p0, i
 #pragma unroll
         for (int j = 0; j < NJ; ++j)   // (both operands are times kUnit)
             *(f32x4_t *)(sums + sums_at<N>(q0 + 16 * j + (lane & 15), p0 + 16 * i + 4 * (lane >> 4))) = acc[i][j] * (1.0f / kUnit);
+}
+
+// What is made of a 256 x 256 tile: two blocks of 128 x 128 at a time, to four waves each, in LDS where the operands were.  `blocks`: of a
+// row of results.
+template <int MODE, bool SPLIT, typename OUT>
+__device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti, int tj, int blocks, const Acc2 &acc, char *lds) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pw = wave & 1, qw = wave >> 1, side = wave >> 2, tid = threadIdx.x & 255;
+    float *mine = (float *)(lds + side * kLdsTile);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int ci = 2 * ti + h, cj = 2 * tj + side;
+        const bool wanted = ci < o.sp / kSide && cj < blocks && (MODE == kStep || MODE == kLast || cj <= ci);
+        __syncthreads();
+        if ((qw >> 1) == h) put_sums<kSide>(acc, 0, 64 * (qw & 1), (float *)(lds + pw * kLdsTile));
+        __syncthreads();
+        if (wanted) finish_rows<MODE, SPLIT, kSide, OUT>(o, m, ci, cj, mine, tid);
+        if constexpr (MODE == kSquare || MODE == kLast) __syncthreads();
+        if (wanted) finish_rest<MODE, SPLIT, kSide, OUT>(o, m, ci, cj, mine, tid);
+    }
 }
 
 // tile t of a lower half, row by row
@@ -357,59 +394,32 @@ template <bool SPLIT> __global__ void __launch_bounds__(kThreads2, kMinWavesPerS
     Acc2 acc;
     zero_acc2(acc);
     mfma_mainloop3<true>(acc, PARTS * nw, P, Q, lds);
-    // two blocks of 128 x 128 at a time, to four waves each
-    const int blocks = o.sp / kSide;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        __syncthreads();
-        if ((qw >> 1) == h) put_sums<kSide>(acc, 0, 64 * (qw & 1), (float *)(lds + pw * kLdsGram));
-        __syncthreads();
-        const int side = wave >> 2, ci = 2 * ti + h, cj = 2 * tj + side;
-        if (ci < blocks && cj <= ci) finish_tile<kGram, SPLIT, kSide, float>(o, m, ci, cj, (float *)(lds + side * kLdsGram), threadIdx.x & 255);
-    }
+    finish_tile<kGram, SPLIT, float>(o, m, ti, tj, o.sp / kSide, acc, lds);
 }
 
-template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(256, 2) ortho_product_kernel(Product o) {
+// The other products.  Tiles of symmetric results are the lower half of them, of others a column of tiles after the other: they share X's
+// columns.
+template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(kThreads2, kMinWavesPerSimd) ortho_product_kernel(Product o, int64_t matrices) {
     extern __shared__ __align__(1024) char lds[];
     const int64_t at = xcd_share(blockIdx.x, gridDim.x), m = at / o.ntiles;
     const int t = (int)(at - m * o.ntiles);
-    // tj: of 256 columns.  Of symmetric results rows ti have the tiles 0 .. ti / 2; else a column of tiles after the other
     int ti, tj;
-    if constexpr (MODE == kSquare) {
-        // rows 2 r and 2 r + 1 begin at r (r + 1) and (r + 1) (r + 1)
-        int r = (int)(sqrtf((float)t + 0.25f) - 0.5f);
-        while ((r + 1) * (r + 2) <= t) ++r;
-        while (r * (r + 1) > t) --r;
-        const int in = t - r * (r + 1);
-        ti = 2 * r + (in > r);
-        tj = in > r ? in - r - 1 : in;
-    } else {
-        const int ni = o.sp / kSide;
-        tj = t / ni;
-        ti = t - tj * ni;
+    if constexpr (MODE == kSquare) lower_half(t, ti, tj);
+    else {
+        const int ni = (o.sp + kTile - 1) / kTile;
+        tj = __builtin_amdgcn_readfirstlane(t / ni);
+        ti = __builtin_amdgcn_readfirstlane(t - t / ni * ni);
     }
-    ti = __builtin_amdgcn_readfirstlane(ti);
-    tj = __builtin_amdgcn_readfirstlane(tj);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = wave & 1, q0 = 64 * (wave >> 1);
-    const int64_t xs = (int64_t)o.sp * o.lp, as = (int64_t)o.sp * o.sp;
-    const int ldp = MODE == kSquare ? o.sp : o.lp, blocks = ldp / kSide;
-    // whether a half of the tile's columns is wanted
-    auto wanted = [&](int h) { return 2 * tj + h < blocks && (MODE != kSquare || 2 * tj + h <= ti); };
-    f32x4_t acc[8][4] = {};
-    constexpr int PARTS = SPLIT ? 3 : 1;
-    const int64_t po = m * (MODE == kSquare ? as : xs) + (int64_t)tj * 2 * kSide, qo = m * as + (int64_t)ti * kSide;
-    multiply_columns<PARTS>(acc, o.sp / 32, 2 * ldp, 2 * o.sp, Passes<PARTS>{(const char *)(o.P.hi + po), (const char *)(o.P.lo + po), 0},
-                            Passes<PARTS>{(const char *)(o.Q.hi + qo), (const char *)(o.Q.lo + qo), 1}, 2 * 64 * half, q0, wanted(half),
-                            (ti * kSide + q0) / 32, o.own, o.own_lo, lds);
-    float *sums = (float *)lds;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        if (!wanted(h)) break;
-        if (h) __syncthreads();
-        if (half == h) put_sums<kSide>(acc, 0, q0, sums);
-        __syncthreads();
-        finish_tile<MODE, SPLIT, kSide, OUT>(o, m, ti, 2 * tj + h, sums, threadIdx.x);
-    }
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pw = wave & 1, qw = wave >> 1;
+    const int ldp = MODE == kSquare ? o.sp : o.lp;
+    const int64_t ps = (int64_t)o.sp * ldp, qs = (int64_t)o.sp * o.sp, po = m * ps + (int64_t)tj * kTile, qo = m * qs + (int64_t)ti * kTile;
+    ColumnsOp P, Q;
+    P.init(o.P.hi + po, o.P.lo + po, (uint64_t)(matrices * ps - po) * 2, 2 * ldp, o.sp / 32, SPLIT ? 0 : -1, 128 * pw);
+    Q.init(o.Q.hi + qo, o.Q.lo + qo, (uint64_t)(matrices * qs - qo) * 2, 2 * o.sp, o.sp / 32, SPLIT ? 1 : -1, kWaveRowsQ * qw);
+    Acc2 acc;
+    zero_acc2(acc);
+    multiply_columns(acc, o.passes, P, Q, (ti * kTile + kWaveRowsQ * qw) / 32, o.own, o.own_lo, lds);
+    finish_tile<MODE, SPLIT, OUT>(o, m, ti, tj, ldp / kSide, acc, lds);
 }
 
 // ---- few tiles ----
@@ -431,11 +441,11 @@ struct SmallTr {
         at = k * 128 + (((wave_base >> 4) ^ (k & 3)) << 5) + (i & 3) * 8;
     }
     __device__ __forceinline__ static uint32_t advance(int ld) { return 64u * ld; }
-    __device__ __forceinline__ f16x8_t frag(const char *win, int t, int u) const {
+    __device__ __forceinline__ bf16x8_t frag(const char *win, int t, int u) const {
         const char *p = win + u * (kSmallWin / 2) + (at ^ (t << 5));
         const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(p));
         const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(p + 4 * 128));
-        return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
 // 64 rows of 64 k, as KcLoad
@@ -449,7 +459,7 @@ struct SmallKc {
         fr.init(wave_base, lane);
     }
     __device__ __forceinline__ static uint32_t advance(int) { return kBK3 * 2; }
-    __device__ __forceinline__ f16x8_t frag(const char *win, int t, int u) const { return __builtin_bit_cast(f16x8_t, fr.read(win, t, u)); }
+    __device__ __forceinline__ bf16x8_t frag(const char *win, int t, int u) const { return fr.read(win, t, u); }
 };
 template <class L> __device__ __forceinline__ void small_issue(const L &l, const char *base, int ld, int J, uint32_t win) {
     const rsrc_t r = src_rsrc_inside(Src{base, 0, L::advance(ld)}, J);
@@ -484,7 +494,7 @@ __device__ __forceinline__ void multiply_small(f32x4_t (&acc)[2][2], int first, 
         const char *pw = lds + w % kBuf * kBytes, *qw = pw + kParts * kSmallWin;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            f16x8_t p[2], q[2];
+            bf16x8_t p[2], q[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 p[i] = pl.frag(pw, i, u);
@@ -493,21 +503,21 @@ __device__ __forceinline__ void multiply_small(f32x4_t (&acc)[2][2], int first, 
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], q[j], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < 2; ++j) acc[i][j] = MfmaF16::run(p[i], q[j], acc[i][j]);
             const bool mine = 2 * (first + w) + u == own_at;      // (32 k and 32 rows)
             if (mine) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const f16x8_t e = unit_part(j, own), el = unit_part(j, own_lo);
+                    const bf16x8_t e = unit_part(lane_id(), j, own), el = unit_part(lane_id(), j, own_lo);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], el, acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], e, acc[i][j], 0, 0, 0);
+                        acc[i][j] = MfmaF16::run(p[i], el, acc[i][j]);
+                        acc[i][j] = MfmaF16::run(p[i], e, acc[i][j]);
                     }
                 }
             }
             if constexpr (SPLIT) {
-                f16x8_t pl2[2], ql2[2];
+                bf16x8_t pl2[2], ql2[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     pl2[i] = pl.frag(pw + kSmallWin, i, u);
@@ -517,9 +527,9 @@ __device__ __forceinline__ void multiply_small(f32x4_t (&acc)[2][2], int first, 
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl2[i], q[j], part[i][j], 0, 0, 0);
-                        part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], ql2[j], part[i][j], 0, 0, 0);
-                        if (mine) part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl2[i], unit_part(j, own), part[i][j], 0, 0, 0);
+                        part[i][j] = MfmaF16::run(pl2[i], q[j], part[i][j]);
+                        part[i][j] = MfmaF16::run(p[i], ql2[j], part[i][j]);
+                        if (mine) part[i][j] = MfmaF16::run(pl2[i], unit_part(lane_id(), j, own), part[i][j]);
                     }
             }
         }
@@ -576,7 +586,9 @@ template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(
     }
     put_sums<kSmall>(acc, p0, q0, (float *)lds);
     __syncthreads();
-    finish_tile<MODE, SPLIT, kSmall, OUT>(o, m, ti, tj, (float *)lds, threadIdx.x);
+    finish_rows<MODE, SPLIT, kSmall, OUT>(o, m, ti, tj, (float *)lds, threadIdx.x);
+    __syncthreads();
+    finish_rest<MODE, SPLIT, kSmall, OUT>(o, m, ti, tj, (float *)lds, threadIdx.x);
 }
 
 // the parts of a tile of X X^T, in their order
@@ -596,7 +608,8 @@ template <bool SPLIT> __global__ void __launch_bounds__(256) ortho_join_kernel(P
             for (int j = 0; j < 2; ++j) acc[i][j] += *(const f32x4_t *)(from + 8 * i + 4 * j);
     put_sums<kSmall>(acc, p0, q0, sums);
     __syncthreads();
-    finish_tile<kGram, SPLIT, kSmall, float>(o, m, ti, tj, sums, threadIdx.x);
+    finish_rows<kGram, SPLIT, kSmall, float>(o, m, ti, tj, sums, threadIdx.x);
+    finish_rest<kGram, SPLIT, kSmall, float>(o, m, ti, tj, sums, threadIdx.x);
 }
 
 // ---- the start: |G| and X = G kUnit / (|G| + eps) ----
@@ -633,7 +646,7 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(const T *__restrict__ G
 // An N x N tile of X, a tall G's through LDS.  Rows of G are read in vectors of 16 bytes, at any element's address.
 template <int N, typename T>
 __global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ G, Product o, int parts, const double *__restrict__ part, double eps,
-                                                          int32_t *__restrict__ status) {
+                                                          bool split, int32_t *__restrict__ status) {
     extern __shared__ __align__(1024) char lds[];
     __shared__ double inv_s;
     float *tile = (float *)lds;
@@ -684,7 +697,8 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ 
         float v[8];
         if (o.transposed) read_down<N>(tile, c, r, v);
         else read_along<N>(tile, r, c, v);
-        put8<true>(o.dst, base + (int64_t)r * o.lp + c, v);
+        if (split) put8<kRest16>(o.dst, base + (int64_t)r * o.lp + c, v);
+        else put8<kRest8>(o.dst, base + (int64_t)r * o.lp + c, v);
     }
 }
 
@@ -720,7 +734,7 @@ Plan plan(int64_t batch, int64_t rows, int64_t cols, int dtype_out) {
     const int64_t elems = rows * cols;
     p.parts = (int)((elems + kNormElems - 1) / kNormElems);
     if (p.parts > kNormParts) p.parts = kNormParts;
-    const size_t x = (size_t)p.sp * p.lp * 4, a = (size_t)p.sp * p.sp * (p.split ? 4 : 2);   // of a matrix: X or Y, A, B or C
+    const size_t x = (size_t)p.sp * p.lp * (p.split ? 4 : 3), a = (size_t)p.sp * p.sp * (p.split ? 4 : 2);   // of a matrix: X or Y, A, B or C
     const size_t most = (size_t)4 << 30;
     const int64_t fit = (int64_t)(most / (2 * x + 3 * a));
     p.chunk = fit < 1 ? 1 : fit < batch ? fit : batch;
@@ -793,23 +807,17 @@ template <int NT = 256, class K, class... A> hipError_t launch(K k, int64_t grid
 template <bool SPLIT, typename OUT>
 hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pair C, float *parts, int64_t matrices, int steps, const float *coef,
                    float scale, hipStream_t s) {
-    const int side = p.small ? kSmall : kSide, ns = o.sp / side, half = ns * (ns + 1) / 2, r = ns / 2;
-    // tiles of 256 x 128: of symmetric results 1, 1, 2, 2, ... to a row of them
-    const int square_tiles = p.small ? half : r * (r + 1) + (ns & 1 ? r + 1 : 0);
-    const int step_tiles = ns * (p.small ? o.lp / side : (o.lp + 2 * side - 1) / (2 * side));
+    const int side = p.small ? kSmall : kTile, ns = (o.sp + side - 1) / side, half = ns * (ns + 1) / 2, step_tiles = ns * ((o.lp + side - 1) / side);
     const float a = coef[0], b = coef[1], c = coef[2];
     const Pair none = {nullptr, nullptr};
     float *no_parts = nullptr;
+    o.passes = SPLIT ? 3 : 1;
     hipError_t e = hipSuccess;
     auto gram = [&](Pair to) {
         o.ntiles = half;
         o.P = X; o.dst = to;
         if (e != hipSuccess) return;
-        if (!p.small) {
-            const int nt = (o.sp + kTile - 1) / kTile;
-            o.ntiles = nt * (nt + 1) / 2;
-            e = launch<kThreads2>(ortho_gram_kernel<SPLIT>, matrices * o.ntiles, 2 * kLdsGram, s, o, matrices);
-        }
+        if (!p.small) e = launch<kThreads2>(ortho_gram_kernel<SPLIT>, matrices * half, 2 * kLdsTile, s, o, matrices);
         else e = launch(ortho_small_kernel<kGram, SPLIT, float>, matrices * half * p.cut, kLdsSmall, s, o, p.cut, parts);
         if (e == hipSuccess && p.cut > 1) e = launch(ortho_join_kernel<SPLIT>, matrices * half, 0, s, o, p.cut, (const float *)parts);
     };
@@ -819,7 +827,7 @@ hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pai
     };
     // to = cd q from + c1 from + c2 e2 + diag
     auto square = [&](Pair to, float cd, Pair q, Pair from, float c1, float c2, Pair e2, double diag) {
-        o.ntiles = square_tiles;
+        o.ntiles = half;
         o.Q = q; o.P = from; o.E2 = e2; o.dst = to;
         // (a quotient that is no f16: the matrix is read again)
         const bool own = std::fabs((double)c1) < 15.0 * std::fabs((double)cd);
@@ -827,8 +835,8 @@ hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pai
         o.E1 = own ? none : from;
         o.cd = cd; o.c1 = c1; o.c2 = c2; o.diag = (float)(diag * kUnit);
         if (e != hipSuccess) return;
-        e = p.small ? launch(ortho_small_kernel<kSquare, SPLIT, float>, matrices * square_tiles, kLdsSmall, s, o, 1, no_parts)
-                    : launch(ortho_product_kernel<kSquare, SPLIT, float>, matrices * square_tiles, kLdsProduct, s, o);
+        e = p.small ? launch(ortho_small_kernel<kSquare, SPLIT, float>, matrices * half, kLdsSmall, s, o, 1, no_parts)
+                    : launch<kThreads2>(ortho_product_kernel<kSquare, SPLIT, float>, matrices * half, 2 * kLdsTile, s, o, matrices);
     };
     for (int k = 0; k < steps;) {
         const bool two = two_together(k, steps, SPLIT, p.small);
@@ -858,8 +866,8 @@ hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pai
             e = k < steps ? launch(ortho_small_kernel<kStep, SPLIT, float>, grid, kLdsSmall, s, o, 1, no_parts)
                           : launch(ortho_small_kernel<kLast, SPLIT, OUT>, grid, kLdsSmall, s, o, 1, no_parts);
         else
-            e = k < steps ? launch(ortho_product_kernel<kStep, SPLIT, float>, grid, kLdsProduct, s, o)
-                          : launch(ortho_product_kernel<kLast, SPLIT, OUT>, grid, kLdsProduct, s, o);
+            e = k < steps ? launch<kThreads2>(ortho_product_kernel<kStep, SPLIT, float>, grid, 2 * kLdsTile, s, o, matrices)
+                          : launch<kThreads2>(ortho_product_kernel<kLast, SPLIT, OUT>, grid, 2 * kLdsTile, s, o, matrices);
         std::swap(X, Y);
     }
     return e;
@@ -900,7 +908,7 @@ hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int d
             typedef decltype(type) T;
             ortho_norm_kernel<T><<<(unsigned)(nm * p.parts), 256, 0, s>>>((const T *)g, elems, p.parts, part);
             auto k = p.small ? ortho_start_kernel<kSmall, T> : ortho_start_kernel<kSide, T>;
-            e = launch(k, ntiles, side * (side + 4) * 4, s, (const T *)g, o, p.parts, (const double *)part, (double)eps, status);
+            e = launch(k, ntiles, side * (side + 4) * 4, s, (const T *)g, o, p.parts, (const double *)part, (double)eps, p.split, status);
         };
         if (dtype_in == R3_BF16) start(bf16_t{});
         else start(float{});
