@@ -35,10 +35,11 @@ struct Pair { f16_t *hi, *lo; };   // (lo: f16, or X's 8 bits where only hi is m
 
 // A launch's product D[q][p] = sum_k Q[q][k] P[p][k] per matrix and what is made of it, all in units of 1 / kUnit:
 //   result = cd (D + own P) + c1 E1 + c2 E2 + diag I
-// kSquare: q, p < s, symmetric, lower half and its mirror image; kStep: p < l; kLast: p < l, times `out`, to the caller's array.
+// kSquare: q, p < s, symmetric, lower half and its mirror image; kStep: p < l; kStepLow: the same with c1 times the 8 bits of E1 (if there
+// are any) and 8 bits of its own (if dst has a place for them); kLast: as kStepLow, times `out`, to the caller's array.
 // own P costs no loads: where a tile's k are its own rows the operand is in LDS, and is multiplied with `own` times a unit matrix, too
 // (two f16, so that `own` keeps 22 bits).
-enum { kGram = 0, kSquare = 1, kStep = 2, kLast = 3 };
+enum { kGram = 0, kSquare = 1, kStep = 2, kStepLow = 3, kLast = 4 };
 struct Product {
     int s, l, sp, lp;              // X is s x l in sp x lp, A and the like s x s in sp x sp, zeros beyond
     int ntiles;                    // of a matrix
@@ -253,11 +254,11 @@ __device__ __forceinline__ void finish_rows(const Product &o, int64_t m, int ti,
     const bool mirror = kMirror && ti != tj;
     // Eight columns of a row to a thread at a time.  X's lo: some loads together, one behind the other's stores their latencies were most
     // of the time.
-    constexpr bool kAddLow = !SPLIT && (MODE == kStep || MODE == kLast);
+    constexpr bool kAddLow = !SPLIT && (MODE == kStepLow || MODE == kLast);
     constexpr int kEach = N * N / 8 / 256, kBatch = kAddLow ? (kEach < 4 ? kEach : 4) : 1;
     for (int k0 = 0; k0 < kEach; k0 += kBatch) {
     uint2 low[kBatch];
-    if constexpr (kAddLow) {
+    if (kAddLow && o.E1.lo) {
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             const int c = tid + 256 * (k0 + k);
@@ -281,7 +282,7 @@ __device__ __forceinline__ void finish_rows(const Product &o, int64_t m, int ti,
                 for (int u = 0; u < 8; ++u) v[u] += row == tj * N + col + u ? o.diag : 0.0f;
             }
         }
-        if constexpr (kAddLow) add_low(low[k], o.c1, v);
+        if (kAddLow && o.E1.lo) add_low(low[k], o.c1, v);
         if constexpr (MODE == kLast) {
 #pragma unroll
             for (int u = 0; u < 8; ++u) v[u] *= o.out;
@@ -290,7 +291,10 @@ __device__ __forceinline__ void finish_rows(const Product &o, int64_t m, int ti,
 #pragma unroll
             for (int u = 0; u < 8; u += 4) *(f32x4_t *)(sums + sums_at<N>(r, col + u)) = *(const f32x4_t *)(v + u);
         }
-        if constexpr (MODE != kLast) put8<SPLIT ? kRest16 : MODE == kStep ? kRest8 : kNoRest>(o.dst, e, v);
+        if constexpr (MODE == kStepLow) {
+            if (o.dst.lo) put8<kRest8>(o.dst, e, v);
+            else put8<kNoRest>(o.dst, e, v);
+        } else if constexpr (MODE != kLast) put8<SPLIT ? kRest16 : kNoRest>(o.dst, e, v);
     }
     }
 }
@@ -349,8 +353,88 @@ __device__ __forceinline__ void put_sums(const f32x4_t (&acc)[NI][NJ], int p0, i
             *(f32x4_t *)(sums + sums_at<N>(q0 + 16 * j + (lane & 15), p0 + 16 * i + 4 * (lane >> 4))) = acc[i][j] * (1.0f / kUnit);
 }
 
-// What is made of a 256 x 256 tile: two blocks of 128 x 128 at a time, to four waves each, in LDS where the operands were.  `blocks`: of a
-// row of results.
+// ---- the ends of 256 x 256 tiles ----
+// Where a result needs nothing but its sums it is rounded in registers, and the whole tile is f16 in LDS, where the operands were (pairs:
+// hi, then lo): one round trip, and whole lines to memory.  With f32 sums in LDS, two blocks of 128 x 128 at a time (below), a product
+// of 128 times 768 x 768 took 115 us instead of 9x.
+constexpr int kPitch16 = kTile + 8;
+static_assert(kTile * kPitch16 * 2 <= 2 * kLdsTile, "");
+
+template <int MODE, bool SPLIT>
+__device__ __forceinline__ void finish_rounded(const Product &o, int64_t m, int ti, int tj, int blocks, const Acc2 &acc, char *lds) {
+    constexpr bool kSq = MODE == kGram || MODE == kSquare;
+    f16_t *t = (f16_t *)lds;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), pw = wave & 1, qw = wave >> 1;
+    const int r = lane & 15, c = 4 * (lane >> 4);
+    int64_t ld;
+    const int64_t tile = tile_at<MODE, kTile>(o, m, ti, tj, ld);
+    const float unit = MODE == kSquare ? o.cd * (1.0f / kUnit) : 1.0f / kUnit;   // (both operands are times kUnit)
+    // (blocks of 128 x 128: h down, g along)
+    auto wanted = [&](int h, int g) { return 2 * ti + h < o.sp / kSide && 2 * tj + g < blocks && (!kSq || 2 * tj + g <= 2 * ti + h); };
+    const bool mine = wanted(qw >> 1, pw);
+#pragma unroll
+    for (int part = 0; part < (SPLIT ? 2 : 1); ++part) {
+        __syncthreads();
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < kTP2; ++i)
+#pragma unroll
+                for (int j = 0; j < kTQ2; ++j) {
+                    const int q = kWaveRowsQ * qw + 16 * j + r, p = 128 * pw + 16 * i + c;
+                    f32x4_t v = acc[i][j] * unit;
+                    if constexpr (MODE == kSquare) {
+                        // (an operand's multiple that is no f16, or the second of two steps')
+                        auto plus = [&](const Pair &from, float by) {
+                            const int64_t e = tile + (int64_t)q * ld + p;
+                            const f16x4_t h = *(const f16x4_t *)(from.hi + e);
+                            f16x4_t lo = {};
+                            if constexpr (SPLIT) lo = *(const f16x4_t *)(from.lo + e);
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) v[u] = fmaf(by, (float)h[u] + (float)lo[u], v[u]);
+                        };
+                        if (o.E1.hi) plus(o.E1, o.c1);
+                        if (o.E2.hi) plus(o.E2, o.c2);
+                        if (ti == tj && kWaveRowsQ * qw + 16 * j == 128 * pw + 16 * i) {
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) v[u] += r == c + u && ti * kTile + q < o.s ? o.diag : 0.0f;
+                        }
+                    }
+                    f16x4_t w;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) w[u] = part ? part_lo(v[u], part_hi(v[u])) : part_hi(v[u]);
+                    *(f16x4_t *)(t + q * kPitch16 + p) = w;
+                }
+        }
+        __syncthreads();
+        f16_t *dst = part ? o.dst.lo : o.dst.hi;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int h = b >> 1, g = b & 1;
+            if (!wanted(h, g)) continue;
+            const f16_t *from = t + kSide * (h * kPitch16 + g);
+            f16_t *to = dst + tile + (int64_t)h * kSide * ld + g * kSide;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int e = threadIdx.x + kThreads2 * k, row = e >> 4, col = (e & 15) * 8;
+                *(f16x8_t *)(to + (int64_t)row * ld + col) = *(const f16x8_t *)(from + row * kPitch16 + col);
+            }
+            // the mirror image through the transposing reads: of 16 columns, 32 rows of a wave's at a time
+            if (!kSq || 2 * tj + g == 2 * ti + h) continue;
+            f16_t *mirror = dst + tile_at<MODE, kSide>(o, m, 2 * tj + g, 2 * ti + h, ld) + (int64_t)(16 * wave + r) * ld;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int q = 32 * k + 2 * c;
+                const f16_t *at = from + (q + (r >> 2)) * kPitch16 + 16 * wave + (r & 3) * 4;
+                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at));
+                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at + 4 * kPitch16));
+                *(s16x8_t *)(mirror + q) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            }
+        }
+    }
+}
+
+// The others (X's 8 bits, the caller's array): two blocks of 128 x 128 at a time, to four waves each, f32 in LDS.  `blocks`: of a row of
+// results.
 template <int MODE, bool SPLIT, typename OUT>
 __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti, int tj, int blocks, const Acc2 &acc, char *lds) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pw = wave & 1, qw = wave >> 1, side = wave >> 2, tid = threadIdx.x & 255;
@@ -358,12 +442,12 @@ __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti,
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int ci = 2 * ti + h, cj = 2 * tj + side;
-        const bool wanted = ci < o.sp / kSide && cj < blocks && (MODE == kStep || MODE == kLast || cj <= ci);
+        const bool wanted = ci < o.sp / kSide && cj < blocks;
         __syncthreads();
         if ((qw >> 1) == h) put_sums<kSide>(acc, 0, 64 * (qw & 1), (float *)(lds + pw * kLdsTile));
         __syncthreads();
         if (wanted) finish_rows<MODE, SPLIT, kSide, OUT>(o, m, ci, cj, mine, tid);
-        if constexpr (MODE == kSquare || MODE == kLast) __syncthreads();
+        if constexpr (MODE == kLast) __syncthreads();
         if (wanted) finish_rest<MODE, SPLIT, kSide, OUT>(o, m, ci, cj, mine, tid);
     }
 }
@@ -394,7 +478,7 @@ template <bool SPLIT> __global__ void __launch_bounds__(kThreads2, kMinWavesPerS
     Acc2 acc;
     zero_acc2(acc);
     mfma_mainloop3<true>(acc, PARTS * nw, P, Q, lds);
-    finish_tile<kGram, SPLIT, float>(o, m, ti, tj, o.sp / kSide, acc, lds);
+    finish_rounded<kGram, SPLIT>(o, m, ti, tj, o.sp / kSide, acc, lds);
 }
 
 // The other products.  Tiles of symmetric results are the lower half of them, of others a column of tiles after the other: they share X's
@@ -419,7 +503,8 @@ template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(
     Acc2 acc;
     zero_acc2(acc);
     multiply_columns(acc, o.passes, P, Q, (ti * kTile + kWaveRowsQ * qw) / 32, o.own, o.own_lo, lds);
-    finish_tile<MODE, SPLIT, OUT>(o, m, ti, tj, ldp / kSide, acc, lds);
+    if constexpr (MODE == kSquare || MODE == kStep) finish_rounded<MODE, SPLIT>(o, m, ti, tj, ldp / kSide, acc, lds);
+    else finish_tile<MODE, SPLIT, OUT>(o, m, ti, tj, ldp / kSide, acc, lds);
 }
 
 // ---- few tiles ----
@@ -856,18 +941,27 @@ hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pai
         }
         k += two ? 2 : 1;
         o.ntiles = step_tiles;
-        o.Q = q; o.P = X; o.E1 = X; o.dst = Y;
+        // (pairs have X's lo in their products; else 8 bits of it count while three steps and more are left)
+        const bool had = !SPLIT && steps - (k - (two ? 2 : 1)) > 2, keeps = !SPLIT && steps - k > 2;
+        o.Q = q; o.P = X; o.E1 = had ? X : none; o.dst = SPLIT || keeps ? Y : Pair{Y.hi, nullptr};
         set_own(out_of);
         o.c1 = (float)out_of;
         o.out = scale / kUnit;
         const int64_t grid = matrices * step_tiles;
         if (e != hipSuccess) return e;
-        if (p.small)
-            e = k < steps ? launch(ortho_small_kernel<kStep, SPLIT, float>, grid, kLdsSmall, s, o, 1, no_parts)
-                          : launch(ortho_small_kernel<kLast, SPLIT, OUT>, grid, kLdsSmall, s, o, 1, no_parts);
-        else
-            e = k < steps ? launch<kThreads2>(ortho_product_kernel<kStep, SPLIT, float>, grid, 2 * kLdsTile, s, o, matrices)
-                          : launch<kThreads2>(ortho_product_kernel<kLast, SPLIT, OUT>, grid, 2 * kLdsTile, s, o, matrices);
+        auto step = [&](auto mode) {
+            constexpr int MODE = decltype(mode)::value;
+            return p.small ? launch(ortho_small_kernel<MODE, SPLIT, float>, grid, kLdsSmall, s, o, 1, no_parts)
+                           : launch<kThreads2>(ortho_product_kernel<MODE, SPLIT, float>, grid, 2 * kLdsTile, s, o, matrices);
+        };
+        if (k == steps) {
+            e = p.small ? launch(ortho_small_kernel<kLast, SPLIT, OUT>, grid, kLdsSmall, s, o, 1, no_parts)
+                        : launch<kThreads2>(ortho_product_kernel<kLast, SPLIT, OUT>, grid, 2 * kLdsTile, s, o, matrices);
+        } else if constexpr (SPLIT) {
+            e = step(std::integral_constant<int, kStep>{});
+        } else {
+            e = had || keeps ? step(std::integral_constant<int, kStepLow>{}) : step(std::integral_constant<int, kStep>{});
+        }
         std::swap(X, Y);
     }
     return e;
