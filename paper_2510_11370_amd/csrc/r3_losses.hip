@@ -29,16 +29,33 @@ struct Seqs {
         const int64_t v = start[q];
         return v < 0 ? 0 : v > n ? n : v;
     }
-    // the sequence that holds position t: the last that starts at or before it; -1 before the first, nseq behind the last
-    __device__ __forceinline__ int of(int64_t t) const {
-        if (!start) return 0;
-        int lo = -1, hi = nseq + 1;   // start[lo] <= t < start[hi]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (start[mid] <= t) lo = mid;
-            else hi = mid;
+    // The sequences that hold positions t0 and t1, the same in all lanes: the last that starts at or before each; -1 before the first,
+    // nseq behind the last.  64 starts are looked at together, so that a search of 4096 takes two trips to memory.
+    __device__ __forceinline__ void of(int64_t t0, int64_t t1, int &q0, int &q1) const {
+        q0 = q1 = 0;
+        if (!start) return;
+        const int lane = threadIdx.x & (kWave - 1);
+        int lo0 = -1, hi0 = nseq + 1, lo1 = -1, hi1 = nseq + 1;   // start[lo] <= t < start[hi]
+        while (hi0 - lo0 > 1 || hi1 - lo1 > 1) {
+            const int d0 = (hi0 - lo0 - 1 + kWave - 1) / kWave, d1 = (hi1 - lo1 - 1 + kWave - 1) / kWave;
+            const int64_t i0 = lo0 + (int64_t)d0 * (lane + 1), i1 = lo1 + (int64_t)d1 * (lane + 1);
+            const bool in0 = i0 < hi0, in1 = i1 < hi1;
+            const int32_t s0 = start[in0 ? i0 : 0], s1 = start[in1 ? i1 : 0];
+            // (starts ascend: the lanes that hold are the first ones)
+            const int n0 = __popcll(__ballot(in0 && s0 <= t0)), n1 = __popcll(__ballot(in1 && s1 <= t1));
+            if (hi0 - lo0 > 1) {
+                const int64_t up = lo0 + (int64_t)d0 * (n0 + 1);
+                lo0 += d0 * n0;
+                hi0 = up < hi0 ? (int)up : hi0;
+            }
+            if (hi1 - lo1 > 1) {
+                const int64_t up = lo1 + (int64_t)d1 * (n1 + 1);
+                lo1 += d1 * n1;
+                hi1 = up < hi1 ? (int)up : hi1;
+            }
         }
-        return lo;
+        q0 = lo0;
+        q1 = lo1;
     }
 };
 
@@ -71,13 +88,12 @@ struct SegSum {      // of a segment
 };
 struct SeqOut {      // of a sequence
     double live;
-    float nu;        // a token's weight
     float up, down;  // what the ratio counts as for A > 0 and A < 0 (sequence ratios)
     float grad;      // and the policy's part of a token's gradient
     int cut;         // bit 0: cut for A > 0, bit 1: for A < 0
 };
 enum { kPolicySums = 5 };   // policy, kl, entropy, cut, weights
-struct PolicyTotals { double live, seqs; };
+struct PolicyTotals { double live, seqs; };   // of some of the sequences
 
 struct Policy {
     Seqs q;
@@ -93,142 +109,223 @@ struct Policy {
     SegSum *seg;
     SeqOut *seq;
     PolicyTotals *tot;
+    int ntot;
     double *part;    // [npieces][kPolicySums]
 };
 
-__device__ __forceinline__ double log_ratio(const Policy &a, int64_t t) { return a.old ? (double)a.logp[t] - (double)a.old[t] : 0.0; }
-__device__ __forceinline__ float weight(const Policy &a, int64_t t) {
-    if (!a.infer) return 1.0f;
-    return __builtin_elementwise_minimum(expf((a.old ? a.old[t] : a.logp[t]) - a.infer[t]), a.cap);   // (a NaN stays one)
-}
-
-__device__ __forceinline__ void seg_add(const Policy &a, int q, int64_t t, SegSum &s) {
-    if (a.target && a.target[t] < 0) return;
-    ++s.live;
-    if (!a.seq_ratio) return;
-    s.d += log_ratio(a, t);
-    const float A = a.adv[a.adv_seq ? q : t], wA = weight(a, t) * A;
-    if (A > 0.0f) s.pos += wA;
-    else if (A < 0.0f) s.neg += wA;
-    else s.pos += wA * 0.0f;   // (a NaN stays one)
-}
-
-template <int NT> __device__ void policy_segments(const Policy &a, int p) {
-    __shared__ double room[NT / kWave];
-    __shared__ int64_t iroom[NT / kWave];
-    const int64_t lo = (int64_t)p * a.piece, hi = lesser(lo + a.piece, a.q.n);
-    if (lo >= hi) return;
-    int q0 = a.q.of(lo), q1 = a.q.of(hi - 1);
-    q0 = q0 < 0 ? 0 : q0;
-    q1 = q1 >= a.q.nseq ? a.q.nseq - 1 : q1;
-    // few segments: all threads to each; many: a wave to each
-    if (q1 - q0 < 4) {
-        for (int q = q0; q <= q1; ++q) {
-            const int64_t b = larger(lo, a.q.first(q)), e = lesser(hi, a.q.first(q + 1));
-            SegSum s = {0.0, 0.0, 0.0, 0};
-            for (int64_t t = b + threadIdx.x; t < e; t += NT) seg_add(a, q, t, s);
-            s.live = block_sum<NT>(s.live, iroom);
-            if (a.seq_ratio) {
-                s.d = block_sum<NT>(s.d, room);
-                s.pos = block_sum<NT>(s.pos, room);
-                s.neg = block_sum<NT>(s.neg, room);
-            }
-            if (threadIdx.x == 0 && b < e) a.seg[p + q] = s;
-        }
-        return;
-    }
-    for (int q = q0 + (int)threadIdx.x / kWave; q <= q1; q += NT / kWave) {
-        const int64_t b = larger(lo, a.q.first(q)), e = lesser(hi, a.q.first(q + 1));
-        SegSum s = {0.0, 0.0, 0.0, 0};
-        for (int64_t t = b + lane_id(); t < e; t += kWave) seg_add(a, q, t, s);
-        s.live = wave_sum(s.live);
-        if (a.seq_ratio) {
-            s.d = wave_sum(s.d);
-            s.pos = wave_sum(s.pos);
-            s.neg = wave_sum(s.neg);
-        }
-        if (lane_id() == 0 && b < e) a.seg[p + q] = s;
-    }
-}
-
-// One work-group: sequences' sums, what follows from them, and the numbers of live tokens and sequences.
-template <int NT> __device__ void policy_sequences(const Policy &a) {
-    __shared__ double room[NT / kWave];
-    const int lane = lane_id();
-    double live = 0.0, seqs = 0.0;
-    for (int base = 0; base < a.q.nseq; base += NT) {
-        const int q = base + threadIdx.x;
-        int64_t b = 0, e = 0;
-        if (q < a.q.nseq) {
-            b = a.q.first(q);
-            e = a.q.first(q + 1);
-        }
-        const int s0 = b < e ? (int)(b / a.piece) : 0, ns = b < e ? (int)((e - 1) / a.piece) - s0 + 1 : 0;
-        SegSum s = {0.0, 0.0, 0.0, 0};
-        constexpr int kFew = 8;
-        auto add = [](SegSum &x, const SegSum &y) {
-            x.d += y.d;
-            x.pos += y.pos;
-            x.neg += y.neg;
-            x.live += y.live;
-        };
-        if (ns <= kFew)
-            for (int i = 0; i < ns; ++i) add(s, a.seg[s0 + q + i]);
-        // a long sequence's segments to a wave
-        for (uint64_t many = __ballot(ns > kFew); many; many &= many - 1) {
-            const int who = __builtin_ctzll(many), f = __shfl(s0 + q, who), n = __shfl(ns, who);
-            SegSum w = {0.0, 0.0, 0.0, 0};
-            for (int i = lane; i < n; i += kWave) add(w, a.seg[f + i]);
-            w.d = wave_sum(w.d);
-            w.pos = wave_sum(w.pos);
-            w.neg = wave_sum(w.neg);
-            w.live = wave_sum(w.live);
-            if (lane == who) s = w;
-        }
-        if (q < a.q.nseq) {
-            SeqOut o = {(double)s.live, 0.0f, 0.0f, 0.0f, 0.0f, 0};
-            if (a.seq_ratio && s.live > 0) {
-                const double d = s.d / (double)s.live;
-                const float r = expf((float)d);
-                const bool up = d > a.log_up, down = d < a.log_down, over = d > a.log_dual;
-                o.up = up ? a.up : r;
-                o.down = over ? a.dual : down ? a.down : r;
-                o.cut = (up ? 1 : 0) | (down || over ? 2 : 0);
-                o.grad = (float)(-(double)r * ((up ? 0.0 : s.pos) + (down || over ? 0.0 : s.neg)) / (double)s.live);
-            }
-            a.seq[q] = o;
-            live += (double)s.live;
-            seqs += s.live > 0;
-        }
-    }
-    live = block_sum<NT>(live, room);
-    seqs = block_sum<NT>(seqs, room);
-    for (int q = threadIdx.x; q < a.q.nseq; q += NT) {
-        const double n = a.seq[q].live;
-        a.seq[q].nu = n == 0.0 ? 0.0f : (float)(a.norm == R3_MEAN_TOKENS ? a.scale / live : a.norm == R3_MEAN_SEQUENCES ? a.scale / (seqs * n) : a.scale);
-    }
-    if (threadIdx.x == 0) *a.tot = {live, seqs};
-}
-
-struct PolicyIn {
-    float logp, old, infer, ref, entropy, adv;
+// A token's values.  All of them are on their way before the first is used, kAhead tokens of a thread at a time: nothing else keeps the
+// card busy here.
+constexpr int kAhead = 4;
+struct Token {
+    float x, old, infer, A, ref, H;
     bool live;
 };
+template <bool ALL> __device__ __forceinline__ Token token(const Policy &a, int q, int64_t t, int64_t end) {
+    Token k = {};
+    k.live = t < end;
+    const int64_t i = k.live ? t : end - 1;
+    if (a.target) k.live &= a.target[i] >= 0;
+    if (!ALL && !a.seq_ratio) return k;
+    k.x = a.logp[i];
+    k.old = a.old ? a.old[i] : k.x;
+    k.A = a.adv[a.adv_seq ? q : i];
+    if (a.infer) k.infer = a.infer[i];
+    if (ALL && a.ref) k.ref = a.ref[i];
+    if (ALL && a.entropy) k.H = a.entropy[i];
+    return k;
+}
+__device__ __forceinline__ float weight(const Policy &a, const Token &k) {
+    return a.infer ? __builtin_elementwise_minimum(expf(k.old - k.infer), a.cap) : 1.0f;   // (a NaN stays one)
+}
 
-template <int NT> __device__ void policy_tokens(const Policy &a, int p) {
-    __shared__ double room[NT / kWave];
+// f(q, begin, end, all) for every segment of [lo, hi) of sequences q0 .. q1: all NT threads to each of a few, a wave to each of many
+template <int NT, class F> __device__ __forceinline__ void for_segments(const Seqs &s, int64_t lo, int64_t hi, int q0, int q1, F f) {
+    const bool few = q1 - q0 < 4;
+    for (int q = few ? q0 : q0 + (int)threadIdx.x / kWave; q <= q1; q += few ? 1 : NT / kWave)
+        f(q, larger(lo, s.first(q)), lesser(hi, s.first(q + 1)), few);
+}
+// sequences of a piece
+__device__ __forceinline__ void of_piece(const Seqs &s, int64_t lo, int64_t hi, int &q0, int &q1) {
+    s.of(lo, hi - 1, q0, q1);
+    q0 = q0 < 0 ? 0 : q0;
+    q1 = q1 >= s.nseq ? s.nseq - 1 : q1;
+}
+
+// this thread's part of the sums over tokens b + first, + step, ... < e of sequence q
+__device__ __forceinline__ SegSum segment_part(const Policy &a, int q, int64_t b, int64_t e, int first, int step) {
+    SegSum s = {0.0, 0.0, 0.0, 0};
+    if (!a.target && !a.seq_ratio) {      // (nothing to read)
+        if (first == 0 && b < e) s.live = e - b;
+        return s;
+    }
+    for (int64_t t = b + first; t < e; t += kAhead * step) {
+        Token k[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) k[u] = token<false>(a, q, t + u * step, e);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (!k[u].live) continue;
+            ++s.live;
+            if (!a.seq_ratio) continue;
+            s.d += (double)k[u].x - (double)k[u].old;
+            const float wA = weight(a, k[u]) * k[u].A;
+            if (k[u].A > 0.0f) s.pos += wA;
+            else if (k[u].A < 0.0f) s.neg += wA;
+            else s.pos += wA * 0.0f;   // (a NaN stays one)
+        }
+    }
+    return s;
+}
+__device__ __forceinline__ void over_wave_sums(const Policy &a, SegSum &x) {
+    x.live = wave_sum((int)x.live);     // (at most 2^31 tokens)
+    if (!a.seq_ratio) return;
+    x.d = wave_sum(x.d);
+    x.pos = wave_sum(x.pos);
+    x.neg = wave_sum(x.neg);
+}
+__device__ __forceinline__ void add_sums(SegSum &x, const SegSum &y) {
+    x.d += y.d;
+    x.pos += y.pos;
+    x.neg += y.neg;
+    x.live += y.live;
+}
+// over a work-group, in thread 0; `room`: as many as it has waves
+template <int NT> __device__ __forceinline__ void over_block_sums(const Policy &a, SegSum &x, SegSum *room) {
+    over_wave_sums(a, x);
+    __syncthreads();
+    if (lane_id() == 0) room[threadIdx.x / kWave] = x;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int w = 1; w < NT / kWave; ++w) add_sums(x, room[w]);
+}
+// what follows from a sequence's sums
+__device__ __forceinline__ SeqOut sequence_result(const Policy &a, const SegSum &s) {
+    SeqOut o = {(double)s.live, 0.0f, 0.0f, 0.0f, 0};
+    if (a.seq_ratio && s.live > 0) {
+        const double d = s.d / (double)s.live;
+        const float r = expf((float)d);
+        const bool up = d > a.log_up, down = d < a.log_down, much = d > a.log_dual;
+        o.up = up ? a.up : r;
+        o.down = much ? a.dual : down ? a.down : r;
+        o.cut = (up ? 1 : 0) | (down || much ? 2 : 0);
+        o.grad = (float)(-(double)r * ((up ? 0.0 : s.pos) + (down || much ? 0.0 : s.neg)) / (double)s.live);
+    }
+    return o;
+}
+// a token's weight in the loss; all: live tokens, and sequences that hold them
+__device__ __forceinline__ float token_weight(const Policy &a, double live_in_seq, const PolicyTotals &all) {
+    if (live_in_seq == 0.0) return 0.0f;
+    return (float)(a.norm == R3_MEAN_TOKENS ? a.scale / all.live : a.norm == R3_MEAN_SEQUENCES ? a.scale / (all.seqs * live_in_seq) : a.scale);
+}
+
+__global__ void __launch_bounds__(kThreads) policy_segments_kernel(Policy a) {
+    __shared__ SegSum room[kThreads / kWave];
+    const int p = blockIdx.x;
     const int64_t lo = (int64_t)p * a.piece, hi = lesser(lo + a.piece, a.q.n);
-    const int64_t begin = a.q.first(0), end = a.q.first(a.q.nseq);
+    int q0, q1;
+    of_piece(a.q, lo, hi, q0, q1);
+    for_segments<kThreads>(a.q, lo, hi, q0, q1, [&](int q, int64_t b, int64_t e, bool all) {
+        SegSum s = segment_part(a, q, b, e, all ? (int)threadIdx.x : lane_id(), all ? kThreads : kWave);
+        if (all) over_block_sums<kThreads>(a, s, room);
+        else over_wave_sums(a, s);
+        if ((all ? (int)threadIdx.x : lane_id()) == 0 && b < e) a.seg[p + q] = s;
+    });
+}
+
+// Sequences' sums from their segments', to a wave each or (many) a thread each and a wave to those of many segments.
+template <bool MANY> __global__ void __launch_bounds__(kThreads) policy_sequences_kernel(Policy a) {
+    __shared__ PolicyTotals room[kThreads / kWave];
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    // where sequence q's segments are, and how many
+    auto segments = [&](int q, int &at, int &n) {
+        const int64_t b = a.q.first(q), e = a.q.first(q + 1);
+        at = b < e ? (int)(b / a.piece) + q : 0;
+        n = b < e ? (int)((e - 1) / a.piece) + q - at + 1 : 0;
+    };
+    PolicyTotals t = {0.0, 0.0};
+    auto done = [&](int q, const SegSum &s) {
+        a.seq[q] = sequence_result(a, s);
+        t.live += (double)s.live;
+        t.seqs += s.live > 0;
+    };
+    int at = 0, n = 0;
+    SegSum s = {0.0, 0.0, 0.0, 0};
+    if constexpr (!MANY) {
+        const int q = blockIdx.x * (kThreads / kWave) + wave;
+        if (q < a.q.nseq) {
+            segments(q, at, n);
+            for (int i = lane; i < n; i += kWave) add_sums(s, a.seg[at + i]);
+            over_wave_sums(a, s);
+            if (lane == 0) done(q, s);
+        }
+    } else {
+        constexpr int kFew = 4;
+        const int q = blockIdx.x * kThreads + threadIdx.x;
+        if (q < a.q.nseq) segments(q, at, n);
+        if (n <= kFew)
+            for (int i = 0; i < n; ++i) add_sums(s, a.seg[at + i]);
+        for (uint64_t many = __ballot(n > kFew); many; many &= many - 1) {
+            const int who = __builtin_ctzll(many), f = __shfl(at, who), m = __shfl(n, who);
+            SegSum w = {0.0, 0.0, 0.0, 0};
+            for (int i = lane; i < m; i += kWave) add_sums(w, a.seg[f + i]);
+            over_wave_sums(a, w);
+            if (lane == who) s = w;
+        }
+        if (q < a.q.nseq) done(q, s);
+    }
+    t.live = wave_sum(t.live);
+    t.seqs = wave_sum(t.seqs);
+    if (lane == 0) room[wave] = t;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kThreads / kWave; ++w) {
+            t.live += room[w].live;
+            t.seqs += room[w].seqs;
+        }
+        a.tot[blockIdx.x] = t;
+    }
+}
+
+// Both at once, a work-group to a sequence, where even one that holds all tokens is gone through soon enough.
+__global__ void __launch_bounds__(1024) policy_whole_kernel(Policy a) {
+    __shared__ SegSum room[1024 / kWave];
+    const int q = blockIdx.x;
+    SegSum s = segment_part(a, q, a.q.first(q), a.q.first(q + 1), threadIdx.x, 1024);
+    over_block_sums<1024>(a, s, room);
+    if (threadIdx.x == 0) {
+        a.seq[q] = sequence_result(a, s);
+        a.tot[q] = {(double)s.live, s.live > 0 ? 1.0 : 0.0};
+    }
+}
+
+// All live tokens and sequences, in every thread.
+template <int NT> __device__ PolicyTotals policy_totals(const Policy &a, PolicyTotals *room) {
+    PolicyTotals t = {0.0, 0.0};
+    for (int i = threadIdx.x; i < a.ntot; i += NT) {
+        t.live += a.tot[i].live;
+        t.seqs += a.tot[i].seqs;
+    }
+    t.live = wave_sum(t.live);
+    t.seqs = wave_sum(t.seqs);
+    if (lane_id() == 0) room[threadIdx.x / kWave] = t;
+    __syncthreads();
+    t = room[0];
+    for (int w = 1; w < NT / kWave; ++w) {
+        t.live += room[w].live;
+        t.seqs += room[w].seqs;
+    }
+    return t;
+}
+
+// A thread's part of the loss.
+struct PolicyPart {
     double sum[kPolicySums] = {};
     bool bad = false;
-    const int qa = lo < hi ? a.q.of(lo) : 0, qb = lo < hi ? a.q.of(hi - 1) : 0;
-    for (int64_t t = lo + threadIdx.x; t < hi; t += NT) {
-        const bool live = t >= begin && t < end && !(a.target && a.target[t] < 0);
-        const int q = qa == qb ? qa : a.q.of(t);
-        float g = 0.0f, gh = 0.0f;
-        if (live && q >= 0 && q < a.q.nseq) {
-            const SeqOut s = a.seq[q];
-            const float A = a.adv[a.adv_seq ? q : t], w = weight(a, t), wA = w * A, x = a.logp[t];
+    // live or not: token t, of a sequence with result s, weighing nu
+    __device__ __forceinline__ void take(const Policy &a, int64_t t, const Token &k, const SeqOut &s, float nu) {
+        float g = 0.0f;
+        if (k.live) {
+            const float A = k.A, w = weight(a, k), wA = w * A;
             float used;
             bool cut;
             if (a.seq_ratio) {
@@ -236,90 +333,217 @@ template <int NT> __device__ void policy_tokens(const Policy &a, int p) {
                 cut = A > 0.0f ? s.cut & 1 : A < 0.0f ? s.cut & 2 : false;
                 g = s.grad;
             } else {
-                const double d = log_ratio(a, t);
+                const double d = (double)k.x - (double)k.old;
                 const float r = expf((float)d);
                 const bool up = d > a.log_up, down = d < a.log_down, over = d > a.log_dual;
                 used = A > 0.0f ? (up ? a.up : r) : over ? a.dual : down ? a.down : r;
                 cut = A > 0.0f ? up : A < 0.0f ? down || over : false;
-                g = cut ? 0.0f : -wA * r;
+                g = cut || A == 0.0f ? 0.0f : -wA * r;
             }
-            const float l = A == 0.0f ? 0.0f : -wA * used;
-            if (A == 0.0f && !a.seq_ratio) g = 0.0f;
-            float all = l;
-            sum[0] += (double)s.nu * l;
+            float l = A == 0.0f ? 0.0f : -wA * used;
+            sum[0] += (double)nu * l;
             if (a.ref) {
-                const float k = a.ref[t] - x, e = expm1f(k);
-                // e^q - 1 - q: its leading terms where they cancel
-                const double k3 = fabsf(k) < 0.125f ? (double)k * k * (0.5 + (double)k * (1.0 / 6 + (double)k * (1.0 / 24 + (double)k * (1.0 / 120 + (double)k * (1.0 / 720 + (double)k * (1.0 / 5040)))))) : (double)e - k;
-                sum[1] += (double)s.nu * k3;
-                g = fmaf(-a.kl, e, g);
-                all += a.kl * (float)k3;
+                const float x = k.ref - k.x, ex = expm1f(x);
+                // e^x - 1 - x: its leading terms where they cancel (the next is 2e-10 of them)
+                const double y = x;
+                const double k3 = fabsf(x) < 0.125f ? y * y * (1.0 / 2 + y * (1.0 / 6 + y * (1.0 / 24 + y * (1.0 / 120 + y * (1.0 / 720 + y * (1.0 / 5040))))))
+                                                    : (double)ex - y;
+                sum[1] += (double)nu * k3;
+                g = fmaf(-a.kl, ex, g);
+                l += a.kl * (float)k3;
             }
             if (a.entropy) {
-                const float H = a.entropy[t];
-                sum[2] += (double)s.nu * H;
-                all -= a.ent * H;
+                sum[2] += (double)nu * k.H;
+                l -= a.ent * k.H;
             }
             sum[3] += cut;
             sum[4] += w;
-            g *= s.nu;
-            gh = -a.ent * s.nu;
-            bad |= !isfinite(all) || !isfinite(g);
+            g *= nu;
+            bad |= !isfinite(l) || !isfinite(g);
         }
         if (a.dlogp) a.dlogp[t] = g;
-        if (a.dentropy) a.dentropy[t] = gh;
+        if (a.dentropy) a.dentropy[t] = k.live ? -a.ent * nu : 0.0f;
     }
+};
+// Sequences of a piece that fit into LDS: a piece of as many or fewer is gone through once, whatever its borders are.
+constexpr int kLocal = 128;
+struct Local {
+    SeqOut seq[kLocal];
+    float nu[kLocal];
+    int border[kLocal + 1];      // where they begin, from the piece's first token
+};
+// tokens lo .. hi - 1 of n sequences from q0 on, those outside [begin, end) of none
+template <int NT>
+__device__ __forceinline__ void policy_pass(const Policy &a, const Local &local, int q0, int n, int64_t lo, int64_t hi, int64_t begin, int64_t end, PolicyPart &part) {
+    for (int64_t t = lo + threadIdx.x; t < hi; t += kAhead * NT) {
+        Token k[kAhead];
+        int at[kAhead];
 #pragma unroll
-    for (int i = 0; i < kPolicySums; ++i) {
-        const double v = block_sum<NT>(sum[i], room);
-        if (threadIdx.x == 0) a.part[(int64_t)p * kPolicySums + i] = v;
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t i = lesser(t + u * NT, hi - 1);
+            int x = 0, y = n;      // border[x] <= i - lo < border[y]
+            while (y - x > 1) {
+                const int m = (x + y) >> 1;
+                if (local.border[m] <= (int)(i - lo)) x = m;
+                else y = m;
+            }
+            at[u] = x;
+            k[u] = {};
+            if (i >= begin && i < end) k[u] = token<true>(a, q0 + x, i, hi);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (t + u * NT < hi) part.take(a, t + u * NT, k[u], local.seq[at[u]], local.nu[at[u]]);
     }
-    if (a.status && __any(bad) && lane_id() == 0) atomicOr(a.status, R3_DATA_NONFINITE);
+}
+// the parts over a work-group, in the first kPolicySums threads
+template <int NT> __device__ __forceinline__ double policy_sum(PolicyPart &part, double (*room)[kPolicySums]) {
+#pragma unroll
+    for (int i = 0; i < kPolicySums; ++i) part.sum[i] = wave_sum(part.sum[i]);
+    if (lane_id() == 0)
+#pragma unroll
+        for (int i = 0; i < kPolicySums; ++i) room[threadIdx.x / kWave][i] = part.sum[i];
+    __syncthreads();
+    double v = 0.0;
+    if (threadIdx.x < kPolicySums)
+        for (int i = 0; i < NT / kWave; ++i) v += room[i][threadIdx.x];
+    return v;
+}
+__device__ __forceinline__ void policy_report(const Policy &a, const PolicyPart &part) {
+    if (a.status && __any(part.bad) && lane_id() == 0) atomicOr(a.status, R3_DATA_NONFINITE);
 }
 
-// One work-group: the loss and its parts.
-template <int NT> __device__ void policy_finish(const Policy &a) {
-    __shared__ double room[NT / kWave];
+__global__ void __launch_bounds__(kThreads) policy_tokens_kernel(Policy a) {
+    __shared__ double room[kThreads / kWave][kPolicySums];
+    __shared__ PolicyTotals troom[kThreads / kWave];
+    __shared__ Local local;
+    const int64_t lo = (int64_t)blockIdx.x * a.piece, hi = lesser(lo + a.piece, a.q.n);
+    int q0, q1;
+    of_piece(a.q, lo, hi, q0, q1);
+    const int n = q1 - q0 + 1;      // (0 where all tokens are of no sequence)
+    const int64_t begin = a.q.first(0), end = a.q.first(a.q.nseq);
+    const PolicyTotals all = policy_totals<kThreads>(a, troom);
+    PolicyPart part;
+    if (n <= kLocal) {
+        for (int i = threadIdx.x; i <= n; i += kThreads) {
+            local.border[i] = (int)(larger(lo, lesser(hi, a.q.first(q0 + i))) - lo);
+            if (i < n) {
+                local.seq[i] = a.seq[q0 + i];
+                local.nu[i] = token_weight(a, local.seq[i].live, all);
+            }
+        }
+        __syncthreads();
+        policy_pass<kThreads>(a, local, q0, n, lo, hi, begin, end, part);
+    } else {
+        for (int64_t t = lo + threadIdx.x; t < hi; t += kThreads)
+            if (t < begin || t >= end) part.take(a, t, Token{}, SeqOut{}, 0.0f);
+        for_segments<kThreads>(a.q, lo, hi, q0, q1, [&](int q, int64_t b, int64_t e, bool) {
+            if (b >= e) return;
+            const SeqOut s = a.seq[q];
+            const float nu = token_weight(a, s.live, all);
+            for (int64_t t = b + lane_id(); t < e; t += kWave) part.take(a, t, token<true>(a, q, t, e), s, nu);
+        });
+    }
+    const double v = policy_sum<kThreads>(part, room);
+    if (threadIdx.x < kPolicySums) a.part[(int64_t)blockIdx.x * kPolicySums + threadIdx.x] = v;
+    policy_report(a, part);
+}
+
+// the loss and its parts, from the sums
+__device__ __forceinline__ void policy_stats(const Policy &a, const double (&v)[kPolicySums], const PolicyTotals &all) {
+    const double some = all.live > 0.0 ? all.live : 1.0, unit = a.scale != 0.0f ? 1.0 / a.scale : 0.0;
+    a.stats[0] = (float)(v[0] + (double)a.kl * v[1] - (double)a.ent * v[2]);
+    a.stats[1] = (float)v[0];
+    a.stats[2] = (float)(v[1] * unit);
+    a.stats[3] = (float)(v[2] * unit);
+    a.stats[4] = (float)(v[3] / some);
+    a.stats[5] = (float)(v[4] / some);
+    a.stats[6] = (float)all.live;
+    a.stats[7] = (float)all.seqs;
+}
+__global__ void __launch_bounds__(kThreads) policy_finish_kernel(Policy a) {
+    __shared__ double room[kThreads / kWave][kPolicySums], total[kPolicySums];
+    __shared__ PolicyTotals troom[kThreads / kWave];
+    PolicyPart part;
+    for (int p = threadIdx.x; p < a.npieces; p += kThreads)
+#pragma unroll
+        for (int i = 0; i < kPolicySums; ++i) part.sum[i] += a.part[(int64_t)p * kPolicySums + i];
+    const double s = policy_sum<kThreads>(part, room);
+    if (threadIdx.x < kPolicySums) total[threadIdx.x] = s;
+    const PolicyTotals all = policy_totals<kThreads>(a, troom);
+    __syncthreads();
+    if (threadIdx.x > 0) return;
     double v[kPolicySums];
-#pragma unroll
-    for (int i = 0; i < kPolicySums; ++i) {
-        double s = 0.0;
-        for (int p = threadIdx.x; p < a.npieces; p += NT) s += a.part[(int64_t)p * kPolicySums + i];
-        v[i] = block_sum<NT>(s, room);
-    }
-    if (threadIdx.x == 0) {
-        const double live = a.tot->live, some = live > 0.0 ? live : 1.0, unit = a.scale != 0.0f ? 1.0 / a.scale : 0.0;
-        a.stats[0] = (float)(v[0] + (double)a.kl * v[1] - (double)a.ent * v[2]);
-        a.stats[1] = (float)v[0];
-        a.stats[2] = (float)(v[1] * unit);
-        a.stats[3] = (float)(v[2] * unit);
-        a.stats[4] = (float)(v[3] / some);
-        a.stats[5] = (float)(v[4] / some);
-        a.stats[6] = (float)live;
-        a.stats[7] = (float)a.tot->seqs;
-    }
+    for (int i = 0; i < kPolicySums; ++i) v[i] = total[i];
+    policy_stats(a, v, all);
 }
 
-__global__ void __launch_bounds__(kThreads) policy_segments_kernel(Policy a) { policy_segments<kThreads>(a, blockIdx.x); }
-__global__ void __launch_bounds__(1024) policy_sequences_kernel(Policy a) { policy_sequences<1024>(a); }
-__global__ void __launch_bounds__(kThreads) policy_tokens_kernel(Policy a) { policy_tokens<kThreads>(a, blockIdx.x); }
-__global__ void __launch_bounds__(kThreads) policy_finish_kernel(Policy a) { policy_finish<kThreads>(a); }
+// One work-group does it all, with the sequences in LDS.
+constexpr int kSmallThreads = 512;
+constexpr int64_t kPolicySmall = 4096;
+__global__ void __launch_bounds__(kSmallThreads) policy_small_kernel(Policy a) {
+    __shared__ double room[kSmallThreads / kWave][kPolicySums], total[kPolicySums];
+    __shared__ SegSum sroom[kSmallThreads / kWave];
+    __shared__ Local local;
+    const int n = a.q.nseq;
+    const int64_t begin = a.q.first(0), end = a.q.first(n);
+    for (int i = threadIdx.x; i <= n; i += kSmallThreads) local.border[i] = (int)a.q.first(i);
+    __syncthreads();
+    if (n <= 2) {
+        for (int q = 0; q < n; ++q) {
+            SegSum s = segment_part(a, q, local.border[q], local.border[q + 1], threadIdx.x, kSmallThreads);
+            over_block_sums<kSmallThreads>(a, s, sroom);
+            if (threadIdx.x == 0) local.seq[q] = sequence_result(a, s);
+        }
+    } else {
+        for (int q = threadIdx.x / kWave; q < n; q += kSmallThreads / kWave) {
+            SegSum s = segment_part(a, q, local.border[q], local.border[q + 1], lane_id(), kWave);
+            over_wave_sums(a, s);
+            if (lane_id() == 0) local.seq[q] = sequence_result(a, s);
+        }
+    }
+    __syncthreads();
+    PolicyTotals all = {0.0, 0.0};
+    for (int q = 0; q < n; ++q) {
+        all.live += local.seq[q].live;
+        all.seqs += local.seq[q].live > 0.0;
+    }
+    for (int q = threadIdx.x; q < n; q += kSmallThreads) local.nu[q] = token_weight(a, local.seq[q].live, all);
+    __syncthreads();
+    PolicyPart part;
+    policy_pass<kSmallThreads>(a, local, 0, n, 0, a.q.n, begin, end, part);
+    const double s = policy_sum<kSmallThreads>(part, room);
+    if (threadIdx.x < kPolicySums) total[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double v[kPolicySums];
+        for (int i = 0; i < kPolicySums; ++i) v[i] = total[i];
+        policy_stats(a, v, all);
+    }
+    policy_report(a, part);
+}
 
 struct PolicyPlan {
-    int piece, npieces;
+    int piece, npieces, ntot;
+    bool small, whole, many;
     size_t seg, seq, tot, part, total;
 };
 PolicyPlan policy_plan(int64_t n, int nseq) {
     PolicyPlan p;
+    p.small = n <= kPolicySmall && nseq <= kLocal;
+    // a work-group to a sequence: 128 tokens to a thread if one has them all
+    p.whole = n <= 131072 && nseq >= 8 && nseq <= 4096;
+    p.many = nseq > 4096;
+    p.ntot = p.whole ? nseq : p.many ? (nseq + kThreads - 1) / kThreads : (nseq + kThreads / kWave - 1) / (kThreads / kWave);
     // at least two tokens to a thread, and at most 1024 work-groups until a piece has 8192
-    int64_t piece = align_up((size_t)((n + 1023) / 1024), kThreads);
+    const int64_t piece = align_up((size_t)((n + 1023) / 1024), kThreads);
     p.piece = (int)std::min<int64_t>(std::max<int64_t>(piece, 2 * kThreads), 8192);
     p.npieces = (int)((n + p.piece - 1) / p.piece);
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes, 256); return at; };
-    p.seg = take((size_t)(p.npieces + nseq) * sizeof(SegSum));
+    p.seg = take(p.whole ? 0 : (size_t)(p.npieces + nseq) * sizeof(SegSum));
     p.seq = take((size_t)nseq * sizeof(SeqOut));
-    p.tot = take(sizeof(PolicyTotals));
+    p.tot = take((size_t)p.ntot * sizeof(PolicyTotals));
     p.part = take((size_t)p.npieces * kPolicySums * sizeof(double));
     p.total = o;
     return p;
@@ -348,8 +572,16 @@ hipError_t launch_policy_loss(const r3_policy_desc &D, const float *logp, const 
     a.log_dual = D.dual_clip > 0.0f ? std::log((double)D.dual_clip) : INFINITY;
     a.cap = D.weight_cap; a.kl = D.kl_coef; a.ent = D.entropy_coef; a.scale = D.scale;
     a.seg = (SegSum *)(base + p.seg); a.seq = (SeqOut *)(base + p.seq); a.tot = (PolicyTotals *)(base + p.tot); a.part = (double *)(base + p.part);
-    if (p.npieces) policy_segments_kernel<<<p.npieces, kThreads, 0, s>>>(a);
-    policy_sequences_kernel<<<1, 1024, 0, s>>>(a);
+    a.ntot = p.ntot;
+    if (p.small) {
+        policy_small_kernel<<<1, kSmallThreads, 0, s>>>(a);
+        return hipGetLastError();
+    }
+    if (p.whole) policy_whole_kernel<<<nseq, 1024, 0, s>>>(a);
+    else {
+        if (p.npieces) policy_segments_kernel<<<p.npieces, kThreads, 0, s>>>(a);
+        (p.many ? policy_sequences_kernel<true> : policy_sequences_kernel<false>)<<<p.ntot, kThreads, 0, s>>>(a);
+    }
     if (p.npieces) policy_tokens_kernel<<<p.npieces, kThreads, 0, s>>>(a);
     policy_finish_kernel<<<1, kThreads, 0, s>>>(a);
     return hipGetLastError();
@@ -370,101 +602,145 @@ struct Balance {
     int T, E, K;
     int piece0, npieces0;      // of the counts
     int piece, npieces;        // of the logits
+    bool once;                 // dlogits is more than the caches may hold for who reads it (131072 x 128 marked | not 28.6 | 32.3 us, 65536 16.3 | 16.6)
     const void *idx;
     int64_t stride;            // of a token's record
     const float *logits;
     int64_t ld, ldd;
     float alpha, zeta;
     int32_t *counts;           // [groups, E]
-    float *probs, *stats, *dlogits;
+    float *probs, *stats, *dlogits;   // (probs, dlogits: or none)
     int32_t *status;
     int32_t *hist;             // [segments of pieces0, E]
     float *psum;               // [segments, E]
-    double *lsum;              // [segments][2]: sums of f p and lse^2
+    double *lsum;              // [pieces][2]: sums of f p, each over its group's tokens, and of lse^2
     double *tot;               // groups that hold tokens, tokens
 };
 
-template <typename IdxT> __device__ void balance_counts(const Balance &a, int p, int *hist) {
+// The record's counts in each segment of piece p.  Ids that lie one behind the other are read 16 bytes at a time.
+template <int NT, typename IdxT> __device__ void balance_counts(const Balance &a, int p, int *hist) {
     const int64_t lo = (int64_t)p * a.piece0, hi = lesser(lo + a.piece0, a.T);
-    if (lo >= hi) return;
-    int q0 = a.q.of(lo), q1 = a.q.of(hi - 1);
-    q0 = q0 < 0 ? 0 : q0;
-    q1 = q1 >= a.q.nseq ? a.q.nseq - 1 : q1;
     bool bad = false;
-    for (int q = q0; q <= q1; ++q) {
-        const int64_t b = larger(lo, a.q.first(q)), e = lesser(hi, a.q.first(q + 1));
-        if (b >= e) continue;
-        for (int i = threadIdx.x; i < a.E; i += blockDim.x) hist[i] = 0;
-        __syncthreads();
-        const IdxT *idx = (const IdxT *)a.idx + b * a.stride;
-        const int n = (int)(e - b) * a.K;
-        for (int i = threadIdx.x; i < n; i += blockDim.x) {
-            const int t = i / a.K, id = idx[(int64_t)t * a.stride + (i - t * a.K)];
-            if (id < a.E) atomicAdd(&hist[id], 1);
-            else bad = true;
+    if (lo < hi) {
+        int q0, q1;
+        of_piece(a.q, lo, hi, q0, q1);
+        for (int q = q0; q <= q1; ++q) {
+            const int64_t b = larger(lo, a.q.first(q)), e = lesser(hi, a.q.first(q + 1));
+            if (b >= e) continue;
+            for (int i = threadIdx.x; i < a.E; i += NT) hist[i] = 0;
+            __syncthreads();
+            const IdxT *idx = (const IdxT *)a.idx + b * a.stride;
+            const int n = (int)(e - b) * a.K;
+            auto one = [&](int id) {
+                if (id < a.E) atomicAdd(&hist[id], 1);
+                else bad = true;
+            };
+            if (a.stride == a.K) {
+                constexpr int kVec = 16 / (int)sizeof(IdxT);
+                const int head = (int)lesser(n, ((16 - (int)((uintptr_t)idx & 15)) & 15) / (int)sizeof(IdxT)), vecs = (n - head) / kVec;
+                for (int i = threadIdx.x; i < vecs; i += NT) {
+                    const uint4 v = ((const uint4 *)(idx + head))[i];
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int u = 0; u < kVec; ++u) one((int)((w[u * (int)sizeof(IdxT) / 4] >> (8 * (int)sizeof(IdxT) * u % 32)) & ((1u << 8 * sizeof(IdxT)) - 1)));
+                }
+                const int rest = n - vecs * kVec;     // in front and behind
+                for (int i = threadIdx.x; i < rest; i += NT) one(idx[i < head ? i : i + vecs * kVec]);
+            } else {
+                for (int i = threadIdx.x; i < n; i += NT) {
+                    const int t = i / a.K;
+                    one(idx[(int64_t)t * a.stride + (i - t * a.K)]);
+                }
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < a.E; i += NT) a.hist[(int64_t)(p + q) * a.E + i] = hist[i];
+            __syncthreads();
         }
-        __syncthreads();
-        for (int i = threadIdx.x; i < a.E; i += blockDim.x) a.hist[(int64_t)(p + q) * a.E + i] = hist[i];
-        __syncthreads();
     }
     if (a.status && bad) atomicOr(a.status, R3_DATA_IDX_RANGE);
+}
+// groups and tokens, by one work-group
+template <int NT> __device__ void balance_totals(const Balance &a, double *room) {
+    double some = 0.0;
+    for (int q = threadIdx.x; q < a.q.nseq; q += NT) some += a.q.first(q) < a.q.first(q + 1);
+    some = block_sum<NT>(some, room);
+    if (threadIdx.x == 0) {
+        a.tot[0] = some;
+        a.tot[1] = (double)(a.q.first(a.q.nseq) - a.q.first(0));
+    }
 }
 
 template <typename IdxT> __global__ void __launch_bounds__(1024) balance_counts_kernel(Balance a) {
     __shared__ int hist[kMaxE];
-    balance_counts<IdxT>(a, blockIdx.x, hist);
+    __shared__ double room[1024 / kWave];
+    balance_counts<1024, IdxT>(a, blockIdx.x, hist);
+    if (blockIdx.x == 0) balance_totals<1024>(a, room);
 }
 
-// counts over a group's segments, a thread to a count; the first work-group also counts groups and tokens
+// A group's counts of 16 experts, 16 threads to each, segments in turn and then the 16 sums in their order
+constexpr int kColumns = 16;
+template <int NT> __device__ void balance_join(const Balance &a, int64_t item, int (*sums)[kColumns]) {
+    constexpr int kRows = NT / kColumns;
+    const int per = (a.E + kColumns - 1) / kColumns, q = (int)(item / per), l = threadIdx.x % kColumns, w = threadIdx.x / kColumns;
+    const int c = (int)(item - (int64_t)q * per) * kColumns + l;
+    const int64_t b = a.q.first(q), e = a.q.first(q + 1);
+    int n = 0;
+    if (b < e && c < a.E) {
+        const int p0 = (int)(b / a.piece0), p1 = (int)((e - 1) / a.piece0);
+#pragma unroll 4
+        for (int p = p0 + w; p <= p1; p += kRows) n += a.hist[(int64_t)(p + q) * a.E + c];
+    }
+    __syncthreads();
+    sums[w][l] = n;
+    __syncthreads();
+    if (w > 0 || c >= a.E) return;
+    n = 0;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) n += sums[i][l];
+    a.counts[(int64_t)q * a.E + c] = n;
+}
+__device__ __forceinline__ int64_t balance_items(const Balance &a) { return (int64_t)a.q.nseq * ((a.E + kColumns - 1) / kColumns); }
 __global__ void __launch_bounds__(kThreads) balance_join_kernel(Balance a) {
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i < (int64_t)a.q.nseq * a.E) {
-        const int q = (int)(i / a.E), e = (int)(i - (int64_t)q * a.E);
-        const int64_t b = a.q.first(q), end = a.q.first(q + 1);
-        int c = 0;
-        if (b < end) {
-            const int p0 = (int)(b / a.piece0), p1 = (int)((end - 1) / a.piece0);
-            const int32_t *h = a.hist + (int64_t)(p0 + q) * a.E + e;
-            int p = p0;
-            for (; p + 7 <= p1; p += 8, h += 8 * (int64_t)a.E) {
-                int v[8];
-#pragma unroll
-                for (int u = 0; u < 8; ++u) v[u] = h[u * (int64_t)a.E];
-#pragma unroll
-                for (int u = 0; u < 8; ++u) c += v[u];
-            }
-            for (; p <= p1; ++p, h += a.E) c += *h;
-        }
-        a.counts[i] = c;
-    }
-    if (blockIdx.x == 0) {
-        __shared__ double room[kThreads / kWave];
-        double some = 0.0;
-        for (int q = threadIdx.x; q < a.q.nseq; q += kThreads) some += a.q.first(q) < a.q.first(q + 1);
-        some = block_sum<kThreads>(some, room);
-        if (threadIdx.x == 0) {
-            a.tot[0] = some;
-            a.tot[1] = (double)(a.q.first(a.q.nseq) - a.q.first(0));
-        }
-    }
+    __shared__ int sums[kThreads / kColumns][kColumns];
+    for (int64_t i = blockIdx.x, n = balance_items(a); i < n; i += gridDim.x) balance_join<kThreads>(a, i, sums);
 }
 
-template <int L, class F> __device__ __forceinline__ float over_lanes(float v, F f) {   // L neighbouring lanes
-#pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, kWave));
+// A value over L neighbouring lanes, in all of them: within 16 by moves in the vector pipe (pairs, pairs of pairs, mirrored halves of 8 and 16)
+template <int L, class F> __device__ __forceinline__ float over_lanes(float v, F f) {
+    if constexpr (L >= 2) v = f(v, lane_move<0xb1, 0xf>(v, v));
+    if constexpr (L >= 4) v = f(v, lane_move<0x4e, 0xf>(v, v));
+    if constexpr (L >= 8) v = f(v, lane_move<0x141, 0xf>(v, v));
+    if constexpr (L >= 16) v = f(v, lane_move<0x140, 0xf>(v, v));
+    if constexpr (L >= 32) v = f(v, __shfl_xor(v, 16, kWave));
+    if constexpr (L >= 64) v = f(v, __shfl_xor(v, 32, kWave));
     return v;
 }
 
-// A token to L lanes, V vectors of four logits to a lane.  Lane l of them has columns 4 (l + L v) .. + 3.
-template <int L, int V> __global__ void __launch_bounds__(kThreads) balance_tokens_kernel(Balance a) {
-    constexpr int kTok = kThreads / L;       // tokens at a time
+// A token to L lanes, V vectors of four logits to a lane: lane l of them has columns 4 (l + L v) .. + 3.  The next token's logits are on
+// their way while one is worked on.
+template <int NT, int L, int V> __device__ void balance_tokens(const Balance &a, int p) {
+    constexpr int kTok = NT / L;       // tokens at a time
     __shared__ float sums[kTok][L * 4];
-    __shared__ double room[kThreads / kWave];
-    const int64_t lo = (int64_t)blockIdx.x * a.piece, hi = lesser(lo + a.piece, a.T);
+    __shared__ double room[NT / kWave];
+    const int64_t lo = (int64_t)p * a.piece, hi = lesser(lo + a.piece, a.T);
     const int l = threadIdx.x % L, w = threadIdx.x / L;
-    const int qa = a.q.of(lo), qb = a.q.of(hi - 1);
+    int qa, qb;
+    a.q.of(lo, hi - 1, qa, qb);
+    double tf = 0.0, tz = 0.0;       // this piece's part of the loss
     bool bad = false;
     auto columns = [&](int v) { const int c = 4 * (l + L * v); return c + 4 <= a.E ? 4 : a.E - c; };   // (none: 0 or less)
+    auto load = [&](int64_t t, float (&x)[V][4]) {
+        const float *z = a.logits + t * a.ld;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int n = columns(v), c = 4 * (l + L * v);
+            if (n == 4) Row<float>::unpack(Row<float>::load(z + c), x[v]);
+            else {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) x[v][u] = u < n ? z[c + u] : -INFINITY;
+            }
+        }
+    };
     for (int q = qa; q <= qb; ++q) {
         const bool none = q < 0 || q >= a.q.nseq;    // tokens of no sequence
         const int64_t b = q < 0 ? lo : larger(lo, a.q.first(q)), e = q < 0 ? lesser(hi, a.q.first(0)) : q >= a.q.nseq ? hi : lesser(hi, a.q.first(q + 1));
@@ -477,6 +753,8 @@ template <int L, int V> __global__ void __launch_bounds__(kThreads) balance_toke
         }
         const double len = (double)(a.q.first(q + 1) - a.q.first(q));
         const float share = (float)((double)a.E / (a.K * len)), ga = (float)(a.alpha / (a.tot[0] * len)), gz = (float)(2.0 * a.zeta / a.tot[1]);
+        float x[V][4];
+        if (b + w < e) load(b + w, x);
         float f[V][4], acc[V][4];
 #pragma unroll
         for (int v = 0; v < V; ++v)
@@ -485,23 +763,16 @@ template <int L, int V> __global__ void __launch_bounds__(kThreads) balance_toke
                 f[v][u] = u < columns(v) ? (float)a.counts[(int64_t)q * a.E + 4 * (l + L * v) + u] * share : 0.0f;
                 acc[v][u] = 0.0f;
             }
-        double sf = 0.0, sz = 0.0;
+        double sf = 0.0;
         for (int64_t t = b + w; t < e; t += kTok) {
-            const float *z = a.logits + t * a.ld;
-            float x[V][4];
+            float next[V][4];
+            if (t + kTok < e) load(t + kTok, next);
             float m = -INFINITY;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int n = columns(v), c = 4 * (l + L * v);
-                if (n == 4) Row<float>::unpack(Row<float>::load(z + c), x[v]);
-                else {
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) x[v][u] = u < n ? z[c + u] : -INFINITY;
-                }
+            for (int v = 0; v < V; ++v)
 #pragma unroll
                 for (int u = 0; u < 4; ++u) m = __builtin_elementwise_maximum(m, x[v][u]);
-            }
-            m = over_lanes<L>(m, [](float p, float r) { return __builtin_elementwise_maximum(p, r); });
+            m = over_lanes<L>(m, [](float i, float j) { return __builtin_elementwise_maximum(i, j); });
             const bool empty = m == -INFINITY;    // nothing but masked experts
             float S = 0.0f, dot = 0.0f;
 #pragma unroll
@@ -512,13 +783,15 @@ template <int L, int V> __global__ void __launch_bounds__(kThreads) balance_toke
                     S += x[v][u];
                     dot = fmaf(f[v][u], x[v][u], dot);
                 }
-            S = over_lanes<L>(S, [](float p, float r) { return p + r; });
-            dot = over_lanes<L>(dot, [](float p, float r) { return p + r; });
-            const float inv = empty ? 0.0f : 1.0f / S, mean = dot * inv, lse = empty ? 0.0f : m + logf(S), zg = gz * lse;
-            bad |= !isfinite(mean) || !isfinite(lse);
+            S = over_lanes<L>(S, [](float i, float j) { return i + j; });
+            dot = over_lanes<L>(dot, [](float i, float j) { return i + j; });
+            // (1 <= S <= E; the hardware's reciprocal and logarithm are off by one unit in the last place)
+            const float inv = empty ? 0.0f : __builtin_amdgcn_rcpf(S), mean = dot * inv;
+            const float lse = empty ? 0.0f : fmaf(__builtin_amdgcn_logf(S), 0.693147180559945f, m), zg = gz * lse;
+            bad |= !isfinite(mean + lse);
             if (l == 0) {
                 sf += mean;
-                sz += (double)lse * lse;
+                tz += (double)lse * lse;
             }
             float *g = a.dlogits + t * a.ldd;
 #pragma unroll
@@ -532,81 +805,60 @@ template <int L, int V> __global__ void __launch_bounds__(kThreads) balance_toke
                     d[u] = pr * fmaf(ga, f[v][u] - mean, zg);
                 }
                 if (a.dlogits) {
-                    if (n == 4) Row<float>::store(g + c, d);
-                    else
+                    if (n == 4) {
+                        if (a.once) Row<float>::store_once(g + c, d);
+                        else Row<float>::store(g + c, d);
+                    } else
 #pragma unroll
                         for (int u = 0; u < 4; ++u)
                             if (u < n) g[c + u] = d[u];
                 }
             }
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) x[v][u] = next[v][u];
         }
-        const int64_t seg = (int64_t)blockIdx.x + q;
-        sf = block_sum<kThreads>(sf, room);
-        sz = block_sum<kThreads>(sz, room);
-        if (threadIdx.x == 0) {
-            a.lsum[2 * seg] = sf;
-            a.lsum[2 * seg + 1] = sz;
-        }
+        tf += sf / len;
         if (a.probs) {
+            const int64_t seg = (int64_t)p + q;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
+                __syncthreads();
 #pragma unroll
                 for (int u = 0; u < 4; ++u) sums[w][4 * l + u] = acc[v][u];
                 __syncthreads();
                 const int c = threadIdx.x, at = 4 * L * v + c;
                 if (c < 4 * L && at < a.E) {
                     float s = 0.0f;
+#pragma unroll 8
                     for (int i = 0; i < kTok; ++i) s += sums[i][c];
                     a.psum[seg * a.E + at] = s;
                 }
-                __syncthreads();
             }
         }
+    }
+    tf = block_sum<NT>(tf, room);
+    tz = block_sum<NT>(tz, room);
+    if (threadIdx.x == 0) {
+        a.lsum[2 * (int64_t)p] = tf;
+        a.lsum[2 * (int64_t)p + 1] = tz;
     }
     if (a.status && __any(bad) && lane_id() == 0) atomicOr(a.status, R3_DATA_NONFINITE);
 }
 
-// the first work-group: the loss; the others: mean probabilities, a thread to one
-__global__ void __launch_bounds__(kThreads) balance_finish_kernel(Balance a) {
-    if (blockIdx.x > 0) {
-        const int64_t i = (int64_t)(blockIdx.x - 1) * kThreads + threadIdx.x;
-        if (i >= (int64_t)a.q.nseq * a.E) return;
-        const int q = (int)(i / a.E), c = (int)(i - (int64_t)q * a.E);
-        const int64_t b = a.q.first(q), e = a.q.first(q + 1);
-        double s = 0.0;
-        if (b < e) {
-            const int p0 = (int)(b / a.piece), p1 = (int)((e - 1) / a.piece);
-            const float *at = a.psum + (int64_t)(p0 + q) * a.E + c;
-            int p = p0;
-            for (; p + 7 <= p1; p += 8, at += 8 * (int64_t)a.E) {
-                float v[8];
-#pragma unroll
-                for (int u = 0; u < 8; ++u) v[u] = at[u * (int64_t)a.E];
-#pragma unroll
-                for (int u = 0; u < 8; ++u) s += v[u];
-            }
-            for (; p <= p1; ++p, at += a.E) s += *at;
-            s /= (double)(e - b);
-        }
-        a.probs[i] = (float)s;
-        return;
-    }
-    __shared__ double room[kThreads / kWave];
+template <int L, int V> __global__ void __launch_bounds__(kThreads) balance_tokens_kernel(Balance a) { balance_tokens<kThreads, L, V>(a, blockIdx.x); }
+
+// The loss, by one work-group.
+template <int NT> __device__ void balance_loss(const Balance &a, double *room) {
     double bal = 0.0, z = 0.0;
-    // a wave to a group
-    for (int q = threadIdx.x / kWave; q < a.q.nseq; q += kThreads / kWave) {
-        const int64_t b = a.q.first(q), e = a.q.first(q + 1);
-        if (b >= e) continue;
-        const int p0 = (int)(b / a.piece), p1 = (int)((e - 1) / a.piece);
-        double s = 0.0;
-        for (int p = p0 + lane_id(); p <= p1; p += kWave) {
-            s += a.lsum[2 * (int64_t)(p + q)];
-            z += a.lsum[2 * (int64_t)(p + q) + 1];
-        }
-        bal += s / (double)(e - b);
+#pragma unroll 4
+    for (int p = threadIdx.x; p < a.npieces; p += NT) {
+        bal += a.lsum[2 * (int64_t)p];
+        z += a.lsum[2 * (int64_t)p + 1];
     }
-    bal = block_sum<kThreads>(bal, room);
-    z = block_sum<kThreads>(z, room);
+    bal = block_sum<NT>(bal, room);
+    z = block_sum<NT>(z, room);
     if (threadIdx.x == 0) {
         const double some = a.tot[0] > 0.0 ? a.tot[0] : 1.0, n = a.tot[1] > 0.0 ? a.tot[1] : 1.0;
         a.stats[0] = (float)((double)a.alpha * bal / some + (double)a.zeta * z / n);
@@ -615,23 +867,75 @@ __global__ void __launch_bounds__(kThreads) balance_finish_kernel(Balance a) {
     }
 }
 
+// Mean probabilities of 16 experts of a group, as balance_join
+template <int NT> __device__ void balance_probs(const Balance &a, int64_t item, double (*sums)[kColumns]) {
+    constexpr int kRows = NT / kColumns;
+    const int per = (a.E + kColumns - 1) / kColumns, q = (int)(item / per), l = threadIdx.x % kColumns, w = threadIdx.x / kColumns;
+    const int c = (int)(item - (int64_t)q * per) * kColumns + l;
+    const int64_t b = a.q.first(q), e = a.q.first(q + 1);
+    double s = 0.0;
+    if (b < e && c < a.E) {
+        const int p0 = (int)(b / a.piece), p1 = (int)((e - 1) / a.piece);
+#pragma unroll 8
+        for (int p = p0 + w; p <= p1; p += kRows) s += a.psum[(int64_t)(p + q) * a.E + c];
+    }
+    __syncthreads();
+    sums[w][l] = s;
+    __syncthreads();
+    if (w > 0 || c >= a.E) return;
+    s = 0.0;
+#pragma unroll 8
+    for (int i = 0; i < kRows; ++i) s += sums[i][l];
+    a.probs[(int64_t)q * a.E + c] = b < e ? (float)(s / (double)(e - b)) : 0.0f;
+}
+
+// the first work-group: the loss
+template <int NT> __global__ void __launch_bounds__(NT) balance_finish_kernel(Balance a) {
+    __shared__ double room[NT / kWave], sums[NT / kColumns][kColumns];
+    if (blockIdx.x == 0) balance_loss<NT>(a, room);
+    else
+        for (int64_t i = blockIdx.x - 1, n = balance_items(a); i < n; i += gridDim.x - 1) balance_probs<NT>(a, i, sums);
+}
+
+// one work-group does it all, a step behind the other
+constexpr int kSmallE = 256;
+template <typename IdxT, int L> __global__ void __launch_bounds__(kThreads) balance_small_kernel(Balance a) {
+    __shared__ int hist[kSmallE];
+    __shared__ double room[kThreads / kWave], dsum[kThreads / kColumns][kColumns];
+    __shared__ int isum[kThreads / kColumns][kColumns];
+    balance_counts<kThreads, IdxT>(a, 0, hist);
+    balance_totals<kThreads>(a, room);
+    __syncthreads();
+    for (int64_t i = 0, n = balance_items(a); i < n; ++i) balance_join<kThreads>(a, i, isum);
+    __syncthreads();
+    balance_tokens<kThreads, L, 1>(a, 0);
+    __syncthreads();
+    balance_loss<kThreads>(a, room);
+    if (a.probs)
+        for (int64_t i = 0, n = balance_items(a); i < n; ++i) balance_probs<kThreads>(a, i, dsum);
+}
+
+// One work-group up to 16 K logits of few groups.
+bool balance_small(int64_t T, int E, int nseq) { return E <= kSmallE && T * E <= 16384 && T <= 512 && nseq * E <= 1024; }
+
 struct BalancePlan {
     int piece0, npieces0, piece, npieces;
     size_t hist, psum, lsum, tot, counts, total;
 };
 BalancePlan balance_plan(int64_t T, int E, int nseq) {
     BalancePlan p;
-    // counts: at most 64 work-groups of 1024 threads, so that few parts are added up
-    p.piece0 = (int)std::max<int64_t>((T + 63) / 64, 128);
+    // counts: at most 128 work-groups of 1024 threads, so that few parts are added up
+    p.piece0 = (int)std::max<int64_t>((T + 127) / 128, 128);
+    // logits: 16 KB and more to a work-group, at most 1024 of them (65536 x 128: 16.6 us; 2048 of them, whose beginnings and ends count, 20.3)
+    p.piece = (int)std::max<int64_t>((T + 1023) / 1024, std::max<int64_t>(4, 4096 / E));
+    if (balance_small(T, E, nseq)) p.piece0 = p.piece = (int)T;
     p.npieces0 = (int)((T + p.piece0 - 1) / p.piece0);
-    const int64_t least = std::max<int64_t>(4, 8192 / E);     // 32 KB of logits
-    p.piece = (int)std::max<int64_t>((T + 2047) / 2048, least);
     p.npieces = (int)((T + p.piece - 1) / p.piece);
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes, 256); return at; };
     p.hist = take((size_t)(p.npieces0 + nseq) * E * sizeof(int32_t));
     p.psum = take((size_t)(p.npieces + nseq) * E * sizeof(float));
-    p.lsum = take((size_t)(p.npieces + nseq) * 2 * sizeof(double));
+    p.lsum = take((size_t)p.npieces * 2 * sizeof(double));
     p.tot = take(2 * sizeof(double));
     p.counts = take((size_t)nseq * E * sizeof(int32_t));
     p.total = o;
@@ -652,29 +956,47 @@ hipError_t launch_balance_loss(int T, int E, int K, const float *logits, int64_t
     Balance a = {};
     a.q = {seq_start, nseq, T};
     a.T = T; a.E = E; a.K = K;
+    a.once = (int64_t)T * E * (int64_t)sizeof(float) > 48 << 20;
     a.piece0 = p.piece0; a.npieces0 = p.npieces0; a.piece = p.piece; a.npieces = p.npieces;
     a.idx = idx; a.stride = stride; a.logits = logits; a.ld = ld; a.ldd = ldd; a.alpha = alpha; a.zeta = zeta;
-    a.counts = counts ? counts : (int32_t *)(base + p.counts);
-    a.probs = probs; a.stats = stats; a.dlogits = dlogits; a.status = status;
+    a.counts = counts ? counts : (int32_t *)(base + p.counts); a.probs = probs; a.stats = stats; a.dlogits = dlogits; a.status = status;
     a.hist = (int32_t *)(base + p.hist); a.psum = (float *)(base + p.psum); a.lsum = (double *)(base + p.lsum); a.tot = (double *)(base + p.tot);
-    if (idx_dtype == R3_IDX_U8) balance_counts_kernel<uint8_t><<<p.npieces0, 1024, 0, s>>>(a);
-    else balance_counts_kernel<uint16_t><<<p.npieces0, 1024, 0, s>>>(a);
-    const unsigned each = (unsigned)(((int64_t)nseq * E + kThreads - 1) / kThreads);
-    balance_join_kernel<<<each, kThreads, 0, s>>>(a);
     const int vecs = (E + 3) / 4;
-    auto go = [&](auto lanes, auto v) { balance_tokens_kernel<decltype(lanes)::value, decltype(v)::value><<<p.npieces, kThreads, 0, s>>>(a); };
-    typedef std::integral_constant<int, 1> one;
-    if (vecs <= 2) go(std::integral_constant<int, 2>{}, one{});
-    else if (vecs <= 4) go(std::integral_constant<int, 4>{}, one{});
-    else if (vecs <= 8) go(std::integral_constant<int, 8>{}, one{});
-    else if (vecs <= 16) go(std::integral_constant<int, 16>{}, one{});
-    else if (vecs <= 32) go(std::integral_constant<int, 32>{}, one{});
-    else if (vecs <= 64) go(std::integral_constant<int, 64>{}, one{});
-    else if (vecs <= 128) go(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
-    else if (vecs <= 256) go(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
-    else if (vecs <= 512) go(std::integral_constant<int, 64>{}, std::integral_constant<int, 8>{});
-    else go(std::integral_constant<int, 64>{}, std::integral_constant<int, 16>{});
-    balance_finish_kernel<<<1 + (probs ? each : 0), kThreads, 0, s>>>(a);
+    const bool u8 = idx_dtype == R3_IDX_U8;
+    auto lanes = [&](auto go) {     // of a token
+        if (vecs <= 2) go(std::integral_constant<int, 2>{});
+        else if (vecs <= 4) go(std::integral_constant<int, 4>{});
+        else if (vecs <= 8) go(std::integral_constant<int, 8>{});
+        else go(std::integral_constant<int, 16>{});
+    };
+    if (balance_small(T, E, nseq)) {
+        auto go = [&](auto l) {
+            constexpr int L = decltype(l)::value;
+            if (u8) balance_small_kernel<uint8_t, L><<<1, kThreads, 0, s>>>(a);
+            else balance_small_kernel<uint16_t, L><<<1, kThreads, 0, s>>>(a);
+        };
+        if (vecs <= 16) lanes(go);
+        else if (vecs <= 32) go(std::integral_constant<int, 32>{});
+        else go(std::integral_constant<int, 64>{});
+        return hipGetLastError();
+    }
+    if (u8) balance_counts_kernel<uint8_t><<<p.npieces0, 1024, 0, s>>>(a);
+    else balance_counts_kernel<uint16_t><<<p.npieces0, 1024, 0, s>>>(a);
+    const int64_t items = (int64_t)nseq * ((E + kColumns - 1) / kColumns), most = 1 << 20;
+    balance_join_kernel<<<(unsigned)std::min(items, most), kThreads, 0, s>>>(a);
+    auto go = [&](auto l, auto v) { balance_tokens_kernel<decltype(l)::value, decltype(v)::value><<<p.npieces, kThreads, 0, s>>>(a); };
+    typedef std::integral_constant<int, 64> wave;
+    if (vecs <= 16) lanes([&](auto l) { go(l, std::integral_constant<int, 1>{}); });
+    else if (vecs <= 32) go(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
+    else if (vecs <= 64) go(std::integral_constant<int, 32>{}, std::integral_constant<int, 2>{});
+    else if (vecs <= 128) go(std::integral_constant<int, 32>{}, std::integral_constant<int, 4>{});
+    else if (vecs <= 256) go(wave{}, std::integral_constant<int, 4>{});
+    else if (vecs <= 512) go(wave{}, std::integral_constant<int, 8>{});
+    else go(wave{}, std::integral_constant<int, 16>{});
+    // (of one group's many pieces each column is a long sum)
+    const unsigned grid = (unsigned)(1 + (probs ? std::min(items, most) : 0));
+    if (p.npieces / nseq > 256) balance_finish_kernel<1024><<<grid, 1024, 0, s>>>(a);
+    else balance_finish_kernel<kThreads><<<grid, kThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 

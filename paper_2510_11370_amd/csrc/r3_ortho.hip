@@ -791,12 +791,12 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ 
 // operands: 6e-3 of the norm at worst).
 bool split_products(int64_t s, int dtype_out) { return dtype_out == R3_F32 || s <= kSide; }
 
-// Tiles of 64 x 64 up to four of X's to a compute unit, eight where products are three (us a call, 64 x 64 | 256 x 128; bf16 results: 4 x 512 x
-// 1024 159 | 313, 4 x 1024 x 1024 413 | 429, 1 x 2048 x 2048 631 | 698, 16 x 512 x 1024 452 | 334, 128 x 256 x 256 432 | 271, 2 x 2048 x 2048
-// 1079 | 747; f32: 1 x 128 x 2048 120 | 406, 1 x 1024 x 1024 235 | 1096, 32 x 256 x 512 288 | 457, 16 x 512 x 1024 665 | 746, 256 x 128 x 1024
-// 780 | 638).
+// Tiles of 64 x 64 up to some six of X's to a compute unit, twelve where products are three (us a call, 64 x 64 | 256 x 256; bf16 results: 16 x
+// 256 x 512 132 | 266, 8 x 512 x 1024 297 | 397, 4 x 768 x 2048 463 | 532, 30 x 300 x 700 347 | 340, 16 x 512 x 1024 486 | 412, 64 x 256 x 512
+// 360 | 288, 2 x 2048 x 2048 1297 | 865; f32: 2 x 1024 x 1024 423 | 1409, 64 x 256 x 512 490 | 638, 16 x 512 x 1024 715 | 1004, 256 x 128 x 1024
+// 1001 | 905).
 bool small_tiles(int64_t batch, int64_t s, int64_t l, bool split) {
-    return batch * ((s + kSmall - 1) / kSmall) * ((l + kSmall - 1) / kSmall) <= (split ? 2048 : 1024);
+    return batch * ((s + kSmall - 1) / kSmall) * ((l + kSmall - 1) / kSmall) <= (split ? 3000 : 1600);
 }
 
 struct Plan {

@@ -91,7 +91,8 @@ def test_policy_loss(n, kind, norm, ratio):
 
 
 @pytest.mark.parametrize("ratio", ["token", "sequence"])
-@pytest.mark.parametrize("kind,n", [("one", 70001), ("few", 300007), ("many", 20011), ("singles", 9000), ("inside", 1100003)])
+@pytest.mark.parametrize("kind,n", [("one", 70001), ("few", 300007), ("many", 20011), ("singles", 9000), ("inside", 1100003), ("few", 4096),
+                                    ("one", 4097), ("singles", 129), ("singles", 128), ("singles", 3000), ("nothing", 140000), ("many", 140003)])
 def test_policy_loss_over_many_pieces(kind, n, ratio):
     starts = _starts(kind, n)
     a = _policy(n, starts)
@@ -121,8 +122,10 @@ def test_nothing_is_live():
     assert all((v == 0).all() for v in got.values())
     stats = torch.full((8,), 7.0, device=DEV)
     none = torch.empty(0, device=DEV)
-    r3.policy_loss(r3.policy_desc(0), none, none, stats, seq_start=torch.zeros(2, dtype=torch.int32, device=DEV))
-    assert (stats == 0).all()
+    for nseq in (1, 200, 5000):
+        stats[:] = 7.0
+        r3.policy_loss(r3.policy_desc(0, nseq), none, none, stats, seq_start=torch.zeros(nseq + 1, dtype=torch.int32, device=DEV))
+        assert (stats == 0).all()
 
 
 @pytest.mark.parametrize("ratio", ["token", "sequence"])
