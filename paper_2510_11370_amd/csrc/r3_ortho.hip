@@ -570,7 +570,8 @@ __device__ __forceinline__ void multiply_small(f32x4_t (&acc)[2][2], int first, 
     };
     const int ahead = n < kBuf - 1 ? n : kBuf - 1;
     for (int w = 0; w < ahead; ++w) issue(w);
-    f32x4_t part[2][2] = {};     // the small products
+    // the small products, and the operand's own multiple, which is the most of the result: what is added to it is rounded to its last place
+    f32x4_t part[2][2] = {}, large[2][2] = {};
     for (int w = 0; w < n; ++w) {
         // (windows w .. w + kBuf - 2 are on their way, if there are as many)
         if (w + kBuf - 2 < n) meet<(kBuf - 2) * kEach>();
@@ -596,8 +597,8 @@ __device__ __forceinline__ void multiply_small(f32x4_t (&acc)[2][2], int first, 
                     const bf16x8_t e = unit_part(lane_id(), j, own), el = unit_part(lane_id(), j, own_lo);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        acc[i][j] = MfmaF16::run(p[i], el, acc[i][j]);
-                        acc[i][j] = MfmaF16::run(p[i], e, acc[i][j]);
+                        part[i][j] = MfmaF16::run(p[i], el, part[i][j]);
+                        large[i][j] = MfmaF16::run(p[i], e, large[i][j]);
                     }
                 }
             }
@@ -619,12 +620,10 @@ __device__ __forceinline__ void multiply_small(f32x4_t (&acc)[2][2], int first, 
             }
         }
     }
-    if constexpr (SPLIT) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] += part[i][j];
-    }
+        for (int j = 0; j < 2; ++j) acc[i][j] = large[i][j] + (acc[i][j] + part[i][j]);
     meet();
 }
 
