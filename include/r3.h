@@ -460,8 +460,8 @@ int r3_balance_loss(const r3_layer_desc *desc, const float *logits, int64_t ld, 
  * which takes every singular value s of G to scale f(f(... s / (|G|_F + eps))),
  * f(x) = a x + b x^3 + c x^5 (a tall matrix is worked on transposed; the result
  * is the same).  coef: HOST pointer to {a, b, c}, or NULL for
- * {3.4445, -4.775, 2.0315}, with which singular values of 0.005 and more come
- * to lie in [0.68, 1.14] after five steps.
+ * {3.4445, -4.775, 2.0315}, with which singular values of 0.002 and more come
+ * to lie in [0.68, 1.21] after five steps.
  * G and out: dense [batch, rows, cols], dtype R3_BF16 or R3_F32 each.  The
  * products' operands are f16 numbers with f32 sums; for dtype_out R3_F32 they
  * are sums of two such, 22 bits.  Relative to each matrix (2-norm) a bf16 result

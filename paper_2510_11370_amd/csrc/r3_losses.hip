@@ -144,11 +144,11 @@ template <int NT, class F> __device__ __forceinline__ void for_segments(const Se
     for (int q = few ? q0 : q0 + (int)threadIdx.x / kWave; q <= q1; q += few ? 1 : NT / kWave)
         f(q, larger(lo, s.first(q)), lesser(hi, s.first(q + 1)), few);
 }
-// sequences of a piece
+// sequences of a piece, one at least (that may hold none of its tokens)
 __device__ __forceinline__ void of_piece(const Seqs &s, int64_t lo, int64_t hi, int &q0, int &q1) {
     s.of(lo, hi - 1, q0, q1);
-    q0 = q0 < 0 ? 0 : q0;
-    q1 = q1 >= s.nseq ? s.nseq - 1 : q1;
+    q0 = q0 < 0 ? 0 : q0 < s.nseq ? q0 : s.nseq - 1;
+    q1 = q1 < q0 ? q0 : q1 < s.nseq ? q1 : s.nseq - 1;
 }
 
 // this thread's part of the sums over tokens b + first, + step, ... < e of sequence q
@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(kThreads) policy_tokens_kernel(Policy a) {
     const int64_t lo = (int64_t)blockIdx.x * a.piece, hi = lesser(lo + a.piece, a.q.n);
     int q0, q1;
     of_piece(a.q, lo, hi, q0, q1);
-    const int n = q1 - q0 + 1;      // (0 where all tokens are of no sequence)
+    const int n = q1 - q0 + 1;
     const int64_t begin = a.q.first(0), end = a.q.first(a.q.nseq);
     const PolicyTotals all = policy_totals<kThreads>(a, troom);
     PolicyPart part;

@@ -22,7 +22,8 @@ def _gradient(b, r, c, src, seed=0, kind="falling"):
 
 
 def _check(out, G, to, **kw):
-    for i in range(G.shape[0]):
+    n = G.shape[0]
+    for i in range(n) if n < 8 else (0, 1, n // 2, n - 2, n - 1):
         want, tol = ref.orthogonalize(G[i].double().numpy(), to=to, **kw)
         off = np.linalg.norm(out[i].double().cpu().numpy() - want)
         assert off <= tol, (i, off, tol, np.linalg.norm(want))
@@ -43,12 +44,45 @@ def test_orthogonalize(b, r, c, src, to):
     _check(big[:b], G, to, scale=1.5)
 
 
+# enough of them for the large tiles, whose last ones hang over the matrices
+MANY = [(110, 130, 640), (70, 300, 700), (50, 700, 400), (40, 385, 900), (64, 257, 1000), (60, 512, 512), (300, 200, 260), (9, 1100, 1300)]
+
+
+@pytest.mark.parametrize("src,to", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16")])
+@pytest.mark.parametrize("b,r,c", MANY)
+def test_many_matrices(b, r, c, src, to):
+    G = _gradient(b, r, c, src, seed=1)
+    big = torch.full((b + 1, r, c), 77.0, dtype=DT[to], device=DEV)
+    r3.orthogonalize(G.to(DEV), big[:b], scale=1.5)
+    assert (big[b:] == 77).all()
+    _check(big[:b], G, to, scale=1.5)
+    clean = big[:b].clone()
+    G[b // 3, r - 1, c - 1] = float("nan")
+    G[0] = 0.0
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    r3.orthogonalize(G.to(DEV), big[:b], scale=1.5, status=status)
+    assert status.item() == r3.DATA_NONFINITE and torch.isnan(big[b // 3]).all() and (big[0] == 0).all()
+    rest = [i for i in range(1, b) if i != b // 3]
+    assert torch.equal(big[rest], clean[rest])
+
+
+@pytest.mark.parametrize("to", ["f32", "bf16"])
+def test_many_matrices_of_low_rank(to):
+    g = torch.Generator().manual_seed(2)
+    G = (torch.randn(64, 300, 3, generator=g) * torch.tensor([1.0, 0.6, 0.1])) @ torch.randn(64, 3, 700, generator=g)
+    G[5] = torch.outer(torch.arange(300.0), torch.ones(700))
+    out = torch.empty(64, 300, 700, dtype=DT[to], device=DEV)
+    r3.orthogonalize(G.to(DEV), out)
+    _check(out[4:11], G[4:11], to)
+
+
 @pytest.mark.parametrize("steps", [1, 2, 3, 6, 9])
 @pytest.mark.parametrize("to", ["f32", "bf16"])
-def test_steps_and_coefficients(steps, to):
-    G = _gradient(2, 70, 140, "f32", seed=steps, kind="flat")
+@pytest.mark.parametrize("b,r,c", [(2, 70, 140), (70, 300, 700)])
+def test_steps_and_coefficients(b, r, c, steps, to):
+    G = _gradient(b, r, c, "f32", seed=steps, kind="flat")
     for coef in (ref.QUINTIC, (1.5, -0.5, 0.0), (15 / 8, -10 / 8, 3 / 8)):
-        out = torch.empty(2, 70, 140, dtype=DT[to], device=DEV)
+        out = torch.empty(b, r, c, dtype=DT[to], device=DEV)
         r3.orthogonalize(G.to(DEV), out, steps=steps, coef=coef, scale=-0.25, eps=0.0)
         _check(out, G, to, steps=steps, coef=coef, scale=-0.25, eps=0.0)
     a, b = torch.empty_like(out), torch.empty_like(out)
