@@ -662,7 +662,7 @@ int r3_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int dtype_in, co
     if (!aligned(G, ib) || !aligned(out, ob) || !aligned(status_word, 4)) return R3_ERR_INVALID_ARG;
     if (!ortho_sizes_ok(batch, rows, cols)) return R3_ERR_UNSUPPORTED;
     if (batch == 0) return R3_OK;
-    if (!orthogonalize_in_range(batch, rows, cols, dtype_out, steps, q)) return R3_ERR_UNSUPPORTED;
+    if (!orthogonalize_in_range(steps, q)) return R3_ERR_UNSUPPORTED;
     if (!G || !out) return R3_ERR_INVALID_ARG;
     const size_t need = orthogonalize_ws_bytes(batch, rows, cols, dtype_out);
     if (!ws || ws_bytes < need || !aligned(ws, 256)) return R3_ERR_WORKSPACE;

@@ -93,9 +93,27 @@ hipError_t launch_balance_loss(int T, int E, int K, const float *logits, int64_t
 
 // r3_ortho.hip
 size_t orthogonalize_ws_bytes(int64_t batch, int64_t rows, int64_t cols, int dtype_out);
-bool orthogonalize_in_range(int64_t batch, int64_t rows, int64_t cols, int dtype_out, int steps, const float *coef);   // of the f16 that it computes with
+bool orthogonalize_in_range(int steps, const float *coef);   // of the f16 that it computes with
 hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int dtype_in, const void *G, int dtype_out, void *out, int steps,
                                 const float *coef, float eps, float scale, int32_t *status, void *ws, hipStream_t s);
+
+// r3_ortho_narrow.hip: s <= 128.  ws: ortho_narrow_ws_bytes; norm: `norms` (at most 64) parts of each matrix's sum of squares
+struct NarrowCall {
+    int64_t batch;
+    int s, l, steps, norms;
+    bool transposed;
+    const void *G;
+    void *O, *ws;
+    const double *norm;
+    const float *coef;
+    float eps, scale;
+    int32_t *status;
+};
+constexpr int kNarrowSide = 128;
+size_t ortho_narrow_ws_bytes(int64_t batch, int64_t s, int64_t l);
+hipError_t launch_ortho_narrow(const NarrowCall &c, int dtype_in, int dtype_out, hipStream_t s);
+// what of step k's polynomial a + b A + c A A is taken out of the matrix and applied to X itself
+inline double ortho_apart(int k, int steps, const float *q) { return k >= steps - 2 ? (double)q[0] + q[1] + q[2] : (double)q[0]; }
 
 // r3_cache.hip
 hipError_t launch_cache_append(int idx_bytes, int L, int K, int P, void *pages, int64_t num_pages,

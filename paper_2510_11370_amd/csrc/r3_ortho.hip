@@ -257,45 +257,45 @@ __device__ __forceinline__ void finish_rows(const Product &o, int64_t m, int ti,
     constexpr bool kAddLow = !SPLIT && (MODE == kStepLow || MODE == kLast);
     constexpr int kEach = N * N / 8 / 256, kBatch = kAddLow ? (kEach < 4 ? kEach : 4) : 1;
     for (int k0 = 0; k0 < kEach; k0 += kBatch) {
-    uint2 low[kBatch];
-    if (kAddLow && o.E1.lo) {
+        uint2 low[kBatch];
+        if (kAddLow && o.E1.lo) {
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-            const int c = tid + 256 * (k0 + k);
-            low[k] = *(const uint2 *)((const char *)o.E1.lo + tile + (int64_t)(c / (N / 8)) * ld + c % (N / 8) * 8);
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-        const int c = tid + 256 * (k0 + k), r = c / (N / 8), col = c % (N / 8) * 8;
-        const int64_t e = tile + (int64_t)r * ld + col;
-        float v[8];
-        read_along<N>(sums, r, col, v);
-        if constexpr (MODE == kSquare) {
-#pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] *= o.cd;
-            if (o.E1.hi) add8<SPLIT>(o.E1, e, o.c1, v);
-            if (o.E2.hi) add8<SPLIT>(o.E2, e, o.c2, v);
-            const int row = ti * N + r;
-            if (ti == tj && row < o.s) {
-#pragma unroll
-                for (int u = 0; u < 8; ++u) v[u] += row == tj * N + col + u ? o.diag : 0.0f;
+            for (int k = 0; k < kBatch; ++k) {
+                const int c = tid + 256 * (k0 + k);
+                low[k] = *(const uint2 *)((const char *)o.E1.lo + tile + (int64_t)(c / (N / 8)) * ld + c % (N / 8) * 8);
             }
         }
-        if (kAddLow && o.E1.lo) add_low(low[k], o.c1, v);
-        if constexpr (MODE == kLast) {
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] *= o.out;
-        }
-        if (MODE == kLast || (MODE == kSquare && mirror)) {
+        for (int k = 0; k < kBatch; ++k) {
+            const int c = tid + 256 * (k0 + k), r = c / (N / 8), col = c % (N / 8) * 8;
+            const int64_t e = tile + (int64_t)r * ld + col;
+            float v[8];
+            read_along<N>(sums, r, col, v);
+            if constexpr (MODE == kSquare) {
 #pragma unroll
-            for (int u = 0; u < 8; u += 4) *(f32x4_t *)(sums + sums_at<N>(r, col + u)) = *(const f32x4_t *)(v + u);
+                for (int u = 0; u < 8; ++u) v[u] *= o.cd;
+                if (o.E1.hi) add8<SPLIT>(o.E1, e, o.c1, v);
+                if (o.E2.hi) add8<SPLIT>(o.E2, e, o.c2, v);
+                const int row = ti * N + r;
+                if (ti == tj && row < o.s) {
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) v[u] += row == tj * N + col + u ? o.diag : 0.0f;
+                }
+            }
+            if (kAddLow && o.E1.lo) add_low(low[k], o.c1, v);
+            if constexpr (MODE == kLast) {
+#pragma unroll
+                for (int u = 0; u < 8; ++u) v[u] *= o.out;
+            }
+            if (MODE == kLast || (MODE == kSquare && mirror)) {
+#pragma unroll
+                for (int u = 0; u < 8; u += 4) *(f32x4_t *)(sums + sums_at<N>(r, col + u)) = *(const f32x4_t *)(v + u);
+            }
+            if constexpr (MODE == kStepLow) {
+                if (o.dst.lo) put8<kRest8>(o.dst, e, v);
+                else put8<kNoRest>(o.dst, e, v);
+            } else if constexpr (MODE != kLast) put8<SPLIT ? kRest16 : kNoRest>(o.dst, e, v);
         }
-        if constexpr (MODE == kStepLow) {
-            if (o.dst.lo) put8<kRest8>(o.dst, e, v);
-            else put8<kNoRest>(o.dst, e, v);
-        } else if constexpr (MODE != kLast) put8<SPLIT ? kRest16 : kNoRest>(o.dst, e, v);
-    }
     }
 }
 template <int MODE, bool SPLIT, int N, typename OUT>
@@ -786,10 +786,6 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ 
     }
 }
 
-// Small matrices are a few tiles whose products cost next to nothing, and few directions in which an error could be lost (3 x 5, f16
-// operands: 6e-3 of the norm at worst).
-bool split_products(int64_t s, int dtype_out) { return dtype_out == R3_F32 || s <= kSide; }
-
 // Tiles of 64 x 64 up to some six of X's to a compute unit, twelve where products are three (us a call, 64 x 64 | 256 x 256; bf16 results: 16 x
 // 256 x 512 132 | 266, 8 x 512 x 1024 297 | 397, 4 x 768 x 2048 463 | 532, 30 x 300 x 700 347 | 340, 16 x 512 x 1024 486 | 412, 64 x 256 x 512
 // 360 | 288, 2 x 2048 x 2048 1297 | 865; f32: 2 x 1024 x 1024 423 | 1409, 64 x 256 x 512 490 | 638, 16 x 512 x 1024 715 | 1004, 256 x 128 x 1024
@@ -802,7 +798,8 @@ struct Plan {
     int s, l, sp, lp, parts;
     int64_t chunk;             // matrices at a time
     size_t norm, X, Y, A, B, C, parts_at, total;
-    bool split, small;         // small: tiles of 64
+    bool narrow;               // r3_ortho_narrow.hip's, with X's place for all of its workspace
+    bool split, small;         // split: products of pairs; small: tiles of 64
     int cut;                   // parts of X X^T
 };
 
@@ -810,8 +807,9 @@ Plan plan(int64_t batch, int64_t rows, int64_t cols, int dtype_out) {
     Plan p;
     p.s = (int)(rows < cols ? rows : cols);
     p.l = (int)(rows < cols ? cols : rows);
-    p.split = split_products(p.s, dtype_out);
-    p.small = small_tiles(batch, p.s, p.l, p.split);
+    p.narrow = p.s <= kNarrowSide;
+    p.split = dtype_out == R3_F32;
+    p.small = !p.narrow && small_tiles(batch, p.s, p.l, p.split);
     const int side = p.small ? kSmall : kSide;
     p.sp = (p.s + side - 1) / side * side;
     p.lp = (p.l + side - 1) / side * side;
@@ -830,6 +828,11 @@ Plan plan(int64_t batch, int64_t rows, int64_t cols, int dtype_out) {
     // (a tile of 256 columns may read 128 columns past a matrix's last)
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes + 2 * kSide, 256); return at; };
     p.norm = take((size_t)batch * p.parts * sizeof(double));
+    if (p.narrow) {
+        p.X = take(ortho_narrow_ws_bytes(batch, p.s, p.l));
+        p.total = o;
+        return p;
+    }
     p.X = take(x * p.chunk);
     p.Y = take(x * p.chunk);
     p.A = take(a * p.chunk);
@@ -842,41 +845,41 @@ Plan plan(int64_t batch, int64_t rows, int64_t cols, int dtype_out) {
 
 // Steps taken together: X'' = Q X with Q = (a + b A' + c A' A') (a + b A + c A A) and A' = (a + b A + c A A)^2 A, without X' between them:
 // five products of s x s instead of two, and a product with X and an X X^T less.  On small tiles that is as many launches, which are what
-// counts there, and steps stay apart.  Else for f32 results wherever two steps are left; for bf16
-// ones at the start alone, where it costs no exactness: later a rounding of X enters the second product times a^2.  (Relative error beside
-// the result's rounding, five steps, random 256 x 768 / falling singular values / rank 3: apart 1.0e-3 / 7e-4 / 2.5e-3, the first two
-// together 1.0e-3 / 7e-4 / 2.5e-3, the first two pairs 1.2e-3 / 1.6e-3 / 9e-3.)
-bool two_together(int step, int steps, bool split, bool small) {
-    return !small && (split ? steps - step >= 2 : step == 0 && steps >= 3);
+// counts there, and steps stay apart.  Else for f32 results wherever two steps are left; for bf16 ones at the start alone, where it costs
+// no exactness: later a rounding of X enters the second product times a^2.  (Relative error beside the result's rounding, five steps,
+// random 256 x 768 / falling singular values / rank 3: apart 1.0e-3 / 7e-4 / 2.5e-3, the first two together the same, the first two pairs
+// 1.2e-3 / 1.6e-3 / 9e-3.)
+bool two_together(int step, int steps, bool split, bool pairs) {
+    return pairs && (split ? steps - step >= 2 : step == 0 && steps >= 3);
 }
-// what of step k's polynomial is taken out of the matrix and applied to X itself
-double apart(int k, int steps, const float *q) { return k >= steps - 2 ? (double)q[0] + q[1] + q[2] : (double)q[0]; }
 
 // Whether every element stays in (-15, 15), so that times kUnit it is an f16: a matrix's are at most its largest singular value, that of X
-// at most 1 at the start and then what the quintic makes of it.
-bool in_range(int steps, const float *q, bool split, bool small) {
-    const double a = q[0], b = q[1], c = q[2], room = 1.01;    // for roundings and what lies between the points
+// at most 1 at the start and then what the quintic makes of it.  At equidistant points: between two of 2 n over (-r, r) a polynomial of degree d
+// is at most d^2 (d^2 - 1) / 24 n^2 of its maximum beyond them, 0.1 % at degree 6 and 256 points, 1.4 % at degree 24 (two steps) and 1024.
+bool in_range(int steps, const float *q, bool split, bool pairs) {
+    const double a = q[0], b = q[1], c = q[2], room = pairs ? 1.03 : 1.01;    // for roundings and what lies between the points
+    const int points = pairs ? 1024 : 256;
     double r = 1.0;
     for (int k = 0; k < steps;) {
-        const bool two = two_together(k, steps, split, small);
+        const bool two = two_together(k, steps, split, pairs);
         double most = 0.0, next = 0.0;
-        for (int i = 0; i <= 1024; ++i) {
-            const double x = r * i / 1024, y = x * x, P = a + y * (b + y * c);
+        for (int i = 0; i <= points; ++i) {
+            const double x = r * i / points, y = x * x, P = a + y * (b + y * c);
             double all[6] = {x, y, P - a, 0.0, 0.0, 0.0}, to = x * P;
             if (two) {
                 const double y1 = to * to, P1 = a + y1 * (b + y1 * c);
                 all[3] = P * y;
                 all[4] = y1;
                 all[5] = P1 - a;
-                all[2] = std::fmax(std::fabs(all[2]), std::fabs(P * P1 - apart(k, steps, q) * apart(k + 1, steps, q)));
+                all[2] = std::fmax(std::fabs(all[2]), std::fabs(P * P1 - ortho_apart(k, steps, q) * ortho_apart(k + 1, steps, q)));
                 to *= P1;
-            } else all[2] = P - apart(k, steps, q);
+            } else all[2] = P - ortho_apart(k, steps, q);
             for (double v : all) most = std::fmax(most, std::fabs(v));
-            most = std::fmax(most, std::fabs(apart(k, steps, q) * (two ? apart(k + 1, steps, q) : 1.0)));
+            most = std::fmax(most, std::fabs(ortho_apart(k, steps, q) * (two ? ortho_apart(k + 1, steps, q) : 1.0)));
             next = std::fmax(next, std::fabs(to));
         }
         if (!(most * room < 15.0 && next * room < 15.0)) return false;
-        r = next * 1.001;
+        r = next * (pairs ? 1.015 : 1.001);
         k += two ? 2 : 1;
     }
     return true;
@@ -888,9 +891,11 @@ template <int NT = 256, class K, class... A> hipError_t launch(K k, int64_t grid
     return hipGetLastError();
 }
 
-template <bool SPLIT, typename OUT>
+// bf16 results: hi hi; f32 ones: pairs.
+template <bool SPLIT>
 hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pair C, float *parts, int64_t matrices, int steps, const float *coef,
-                   float scale, hipStream_t s) {
+                   float scale, bool pairs, hipStream_t s) {
+    typedef typename std::conditional<SPLIT, float, bf16_t>::type OUT;
     const int side = p.small ? kSmall : kTile, ns = (o.sp + side - 1) / side, half = ns * (ns + 1) / 2, step_tiles = ns * ((o.lp + side - 1) / side);
     const float a = coef[0], b = coef[1], c = coef[2];
     const Pair none = {nullptr, nullptr};
@@ -923,12 +928,12 @@ hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pai
                     : launch<kThreads2>(ortho_product_kernel<kSquare, SPLIT, float>, matrices * half, 2 * kLdsTile, s, o, matrices);
     };
     for (int k = 0; k < steps;) {
-        const bool two = two_together(k, steps, SPLIT, p.small);
-        double out_of = apart(k, steps, coef);
+        const bool two = two_together(k, steps, SPLIT, pairs);
+        double out_of = ortho_apart(k, steps, coef);
         Pair q = B;
         gram(A);
         if (two) {
-            out_of *= apart(k + 1, steps, coef);
+            out_of *= ortho_apart(k + 1, steps, coef);
             square(B, c, A, A, b, 0.0f, none, 0.0);                             // B = b A + c A A
             square(C, 1.0f, B, A, a, 0.0f, none, 0.0);                          // C = (a + B) A
             square(A, 1.0f, B, C, a, 0.0f, none, 0.0);                          // A' = (a + B) C
@@ -970,10 +975,7 @@ hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pai
 
 size_t orthogonalize_ws_bytes(int64_t batch, int64_t rows, int64_t cols, int dtype_out) { return plan(batch, rows, cols, dtype_out).total; }
 
-bool orthogonalize_in_range(int64_t batch, int64_t rows, int64_t cols, int dtype_out, int steps, const float *coef) {
-    const Plan p = plan(batch, rows, cols, dtype_out);
-    return in_range(steps, coef, p.split, p.small);
-}
+bool orthogonalize_in_range(int steps, const float *coef) { return in_range(steps, coef, false, false); }
 
 hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int dtype_in, const void *G, int dtype_out, void *out, int steps,
                                 const float *coef, float eps, float scale, int32_t *status, void *ws, hipStream_t s) {
@@ -983,6 +985,26 @@ hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int d
     double *part = (double *)(base + p.norm);
     const int64_t elems = rows * cols;
     const size_t eb = dtype_in == R3_BF16 ? 2 : 4, ob = dtype_out == R3_BF16 ? 2 : 4;
+    auto norms = [&](const char *g, int64_t nm) {
+        if (dtype_in == R3_BF16) ortho_norm_kernel<bf16_t><<<(unsigned)(nm * p.parts), 256, 0, s>>>((const bf16_t *)g, elems, p.parts, part);
+        else ortho_norm_kernel<float><<<(unsigned)(nm * p.parts), 256, 0, s>>>((const float *)g, elems, p.parts, part);
+        return hipGetLastError();
+    };
+    if (p.narrow) {
+        const hipError_t e = norms((const char *)G, batch);
+        if (e != hipSuccess) return e;
+        NarrowCall c = {};
+        c.batch = batch; c.s = p.s; c.l = p.l; c.steps = steps; c.norms = p.parts;
+        c.transposed = rows > cols;
+        c.G = G; c.O = out; c.ws = base + p.X;
+        c.norm = part;
+        c.coef = coef;
+        c.eps = eps; c.scale = scale;
+        c.status = status;
+        return launch_ortho_narrow(c, dtype_in, dtype_out, s);
+    }
+    // (the matrices between two steps have larger elements than those of one: other coefficients may have room for single ones alone)
+    const bool pairs = !p.small && in_range(steps, coef, p.split, true);
     for (int64_t m0 = 0; m0 < batch; m0 += p.chunk) {
         const int64_t nm = batch - m0 < p.chunk ? batch - m0 : p.chunk;
         const int64_t xs = (int64_t)p.sp * p.lp * p.chunk, as = (int64_t)p.sp * p.sp * p.chunk;
@@ -996,18 +1018,18 @@ hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int d
         const char *g = (const char *)G + (size_t)m0 * elems * eb;
         const int side = p.small ? kSmall : kSide;
         const int64_t ntiles = nm * (p.sp / side) * (p.lp / side);
-        hipError_t e;
+        hipError_t e = norms(g, nm);
+        if (e != hipSuccess) return e;
         auto start = [&](auto type) {
             typedef decltype(type) T;
-            ortho_norm_kernel<T><<<(unsigned)(nm * p.parts), 256, 0, s>>>((const T *)g, elems, p.parts, part);
             auto k = p.small ? ortho_start_kernel<kSmall, T> : ortho_start_kernel<kSide, T>;
             e = launch(k, ntiles, side * (side + 4) * 4, s, (const T *)g, o, p.parts, (const double *)part, (double)eps, p.split, status);
         };
         if (dtype_in == R3_BF16) start(bf16_t{});
         else start(float{});
         if (e != hipSuccess) return e;
-        auto run = !p.split ? iterate<false, bf16_t> : dtype_out == R3_F32 ? iterate<true, float> : iterate<true, bf16_t>;
-        e = run(p, o, X, Y, A, B, C, (float *)(base + p.parts_at), nm, steps, coef, scale, s);
+        auto run = p.split ? iterate<true> : iterate<false>;
+        e = run(p, o, X, Y, A, B, C, (float *)(base + p.parts_at), nm, steps, coef, scale, pairs, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

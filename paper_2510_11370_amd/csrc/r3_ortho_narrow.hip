@@ -1,0 +1,437 @@
+// Newton-Schulz orthogonalisation (r3_ortho.hip has the mathematics and the numbers' scale) of matrices with a short side of at most 128: such a matrix's A = X X^T fits into
+// a compute unit's LDS as a pair of f16, and its X goes by in slabs of 64 columns.
+//
+// A work-group has a run of a matrix's slabs.  A step of it: A, B = b A + c A A + .. into LDS; of each slab X' = a X + B X, and at once X' X'^T added to its part of the next
+// step's A, in registers.  So a step is one launch that reads and writes X once, and another that joins the parts where there are more than a
+// few; as products over tiles it was five launches, each of which waited for the one before (1 x 2048 x 128: 27 launches, NNN us | 12, NNN us).  Where
+// a work-group has one matrix and all its slabs, B is the smaller part of its work; where a matrix is shared, each of its work-groups makes B for itself, which costs
+// as much as a slab.
+//
+// X, A and B are pairs of f16 times 2^12 for results of either type: products are hi hi, hi lo, lo hi.  These matrices have few directions in which an error could be lost (3 x 5, f16 operands:
+// 6e-3 of the norm at worst), and the two products more are hidden behind latencies.
+#include <algorithm>
+
+#include "r3_kernels.h"
+#include "r3_mfma2.h"
+#include "r3_vec.h"
+
+namespace r3 {
+namespace {
+
+typedef _Float16 f16_t;
+typedef f16_t f16x4_t __attribute__((ext_vector_type(4)));
+
+constexpr float kUnit = 4096.0f;      // what is stored is times this
+constexpr int kSlab = 64;             // columns
+constexpr int kFew = 2;               // parts of A that a step joins by itself
+
+enum { kStart = 0, kStep = 1, kLast = 2 };
+struct Narrow {
+    int s, l, slabs, pieces, parts;      // pieces: work-groups of a matrix; parts: of A as it is read
+    bool transposed;
+    const void *G;
+    void *O;
+    char *X;                             // [matrix][slab]: SP rows of hi, SP rows of lo, as they are in LDS
+    const float *A;                      // [matrix][part]: sums as the threads have them
+    float *A_to;
+    int norms;                           // of a matrix: parts of |G|^2
+    const double *norm;
+    double eps;
+    float apart, rest, b, c, out;        // X' = apart X + (rest I + b A + c A A) X
+    int32_t *status;
+};
+
+template <int SP> struct Shape {
+    static constexpr int kWaves = SP == 128 ? 8 : 4, kThreads = 64 * kWaves;
+    static constexpr int kPlane = SP * kSlab * 2, kBytes = 2 * kPlane;           // hi or lo of a slab, both
+    static constexpr int kPitch = SP * 2 + 16;                                   // bytes of a row of A or B
+    static constexpr int kMatrix = SP * kPitch;                                  // hi or lo of it
+    static constexpr int kLds = 2 * kMatrix + 2 * kBytes;
+    static constexpr int kGP = SP == 128 ? 4 : 2, kGQ = 2;                       // 16 x 16 tiles of a wave, of A: 64 x 32 or 32 x 32
+    static constexpr int64_t kSums = SP * SP;
+};
+static_assert(Shape<128>::kLds <= 160 * 1024, "");
+
+// A slab in LDS: rows of 128 bytes, the 16-byte chunk c of row r at c ^ ((r >> 1) & 7), so that both ways of reading it (KcFrag16's along rows,
+// and down columns) meet few banks twice.
+__device__ __forceinline__ int slab_at(int row, int col) { return row * 128 + ((((col >> 3) ^ (row >> 1)) & 7) << 4) + (col & 7) * 2; }
+// 32 rows from row 32 kk on of 16 columns, as an operand whose k are rows: two transposing reads of 4 k each
+struct DownFrag {
+    int at;
+    __device__ __forceinline__ void init(int col0) {
+        const int lane = lane_id(), i = lane & 15, k = 8 * (lane >> 4) + (i >> 2);
+        at = slab_at(k, col0 + 4 * (i & 3));
+    }
+    __device__ __forceinline__ bf16x8_t read(const char *plane, int kk) const {
+        // (rows 32 on have the same swizzle, rows 4 on the other one in bit 1)
+        const char *p = plane + kk * (32 * 128) + at, *q = plane + kk * (32 * 128) + ((at + 4 * 128) ^ 32);
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(p));
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(q));
+        return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+// 32 k (64 bytes) from k = 32 kk on of 16 rows of A or B
+template <int PITCH> __device__ __forceinline__ bf16x8_t row_frag(const char *m, int row0, int kk) {
+    const int lane = lane_id();
+    return *(const bf16x8_t *)(m + (row0 + (lane & 15)) * PITCH + kk * 64 + (lane >> 4) * 16);
+}
+// acc += P Q for pairs, the small products apart
+__device__ __forceinline__ void pair_mfma(f32x4_t &large, f32x4_t &small, const bf16x8_t (&p)[2], const bf16x8_t (&q)[2]) {
+    small = MfmaF16::run(p[1], q[0], small);
+    small = MfmaF16::run(p[0], q[1], small);
+    large = MfmaF16::run(p[0], q[0], large);
+}
+// four values as a pair, `lo_off` bytes apart
+__device__ __forceinline__ void put_pair(char *at, int lo_off, const float *v) {
+    f16x4_t h, lo;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        h[u] = (f16_t)v[u];
+        lo[u] = (f16_t)(v[u] - (float)h[u]);
+    }
+    *(f16x4_t *)at = h;
+    *(f16x4_t *)(at + lo_off) = lo;
+}
+
+template <int SP, int MODE, typename T> __global__ void __launch_bounds__(Shape<SP>::kThreads, 1) ortho_narrow_kernel(Narrow o) {
+    typedef Shape<SP> H;
+    constexpr int NT = H::kThreads, kP = H::kGP, kQ = H::kGQ;
+    extern __shared__ __align__(1024) char lds[];
+    char *const M = lds, *const S = lds + 2 * H::kMatrix;     // A or B; two slabs
+    const int64_t m = blockIdx.x / o.pieces, elems = (int64_t)o.s * o.l;
+    const int piece = (int)(blockIdx.x - m * o.pieces);
+    const int j0 = (int)((int64_t)o.slabs * piece / o.pieces), j1 = (int)((int64_t)o.slabs * (piece + 1) / o.pieces);
+    char *X = o.X + m * o.slabs * (int64_t)H::kBytes;
+    const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, c4 = 4 * (lane >> 4);
+    // of A: waves 2 along (p), the others down; of a slab: 2 along by 32 columns, the others down by 32 rows
+    const int gp = (wave & 1) * 16 * kP, gq = (wave >> 1) * 16 * kQ, xp = (wave & 1) * 32, xq = (wave >> 1) * 32;
+
+    f32x4_t A[kP][kQ], As[kP][kQ];      // large and small products
+    auto clear = [&]() {
+#pragma unroll
+        for (int i = 0; i < kP; ++i)
+#pragma unroll
+            for (int j = 0; j < kQ; ++j) A[i][j] = As[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    };
+    // += slab slab^T
+    KcFrag16 fp, fq;
+    fp.init(gp, lane);
+    fq.init(gq, lane);
+    auto gram = [&](const char *slab) {
+#pragma unroll
+        for (int u = 0; u < kSlab / 32; ++u) {
+            bf16x8_t p[kP][2], q[kQ][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int i = 0; i < kP; ++i) p[i][h] = fp.read(slab + h * H::kPlane, i, u);
+#pragma unroll
+                for (int j = 0; j < kQ; ++j) q[j][h] = fq.read(slab + h * H::kPlane, j, u);
+            }
+#pragma unroll
+            for (int j = 0; j < kQ; ++j)
+#pragma unroll
+                for (int i = 0; i < kP; ++i) pair_mfma(A[i][j], As[i][j], p[i], q[j]);
+        }
+    };
+    constexpr int kChunks = H::kBytes / 16 / NT;      // 16-byte pieces of a slab to a thread
+    auto load = [&](int j, char *slab) {
+        const rsrc_t d = src_rsrc_inside(Src{X + (int64_t)j * H::kBytes, 0, 0}, 0);
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) lds_load16(d, lds_addr(slab) + 1024 * (wave + H::kWaves * i), (wave + H::kWaves * i) * 1024 + lane * 16);
+    };
+    auto store = [&](int j, const char *slab) {
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int at = (tid + NT * i) * 16;
+            *(uint4 *)(X + (int64_t)j * H::kBytes + at) = *(const uint4 *)(slab + at);
+        }
+    };
+    auto sums_of = [&](int64_t part, int i, int j) { return part * H::kSums + (((int64_t)i * kQ + j) * NT + tid) * 4; };
+
+    if constexpr (MODE == kStart) {
+        // X = G / (|G| + eps)
+        const T *G = (const T *)o.G + m * elems;
+        const double sum = wave_sum(lane < o.norms ? o.norm[m * o.norms + lane] : 0.0), n = sqrt(sum) + o.eps;
+        // (in 64 bits: 1 / |G| may be beyond f32's range)
+        const double inv = n == 0.0 ? 0.0 : isfinite(sum) ? (double)kUnit / n : (double)NAN;
+        if (tid == 0 && piece == 0 && !isfinite(sum) && o.status) atomicOr(o.status, R3_DATA_NONFINITE);
+        clear();
+        for (int j = j0; j < j1; ++j) {
+            char *slab = S + (j & 1) * H::kBytes;
+            constexpr int kEach = SP * kSlab / NT;
+            float v[kEach];
+            // (in G's order, so that a wave's loads lie together; beyond its rows and columns X is 0 whatever the norm is)
+            auto place = [&](int k, int &row, int &col) {
+                const int e = tid + NT * k;
+                row = o.transposed ? e % SP : e / kSlab;
+                col = o.transposed ? e / SP : e % kSlab;
+            };
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) {
+                int row, col;
+                place(k, row, col);
+                const int64_t at = o.transposed ? (int64_t)(j * kSlab + col) * o.s + row : (int64_t)row * o.l + j * kSlab + col;
+                v[k] = row < o.s && j * kSlab + col < o.l ? Elem<T>::ld(G + at) : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) {
+                int row, col;
+                place(k, row, col);
+                const float x = row < o.s && j * kSlab + col < o.l ? (float)((double)v[k] * inv) : 0.0f;
+                const f16_t h = (f16_t)x;
+                char *at = slab + slab_at(row, col);
+                *(f16_t *)at = h;
+                *(f16_t *)(at + H::kPlane) = (f16_t)(x - (float)h);
+            }
+            // (two slabs: everybody has left the one before the last)
+            __syncthreads();
+            gram(slab);
+            store(j, slab);
+        }
+    } else {
+        load(j0, S + (j0 & 1) * H::kBytes);
+        // A
+#pragma unroll
+        for (int i = 0; i < kP; ++i)
+#pragma unroll
+            for (int j = 0; j < kQ; ++j) A[i][j] = *(const f32x4_t *)(o.A + sums_of(m * o.parts, i, j));
+        for (int k = 1; k < o.parts; ++k)
+#pragma unroll
+            for (int i = 0; i < kP; ++i)
+#pragma unroll
+                for (int j = 0; j < kQ; ++j) A[i][j] += *(const f32x4_t *)(o.A + sums_of(m * o.parts + k, i, j));
+#pragma unroll
+        for (int i = 0; i < kP; ++i)
+#pragma unroll
+            for (int j = 0; j < kQ; ++j) {
+                float v[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v[u] = A[i][j][u];
+                put_pair(M + (gq + 16 * j + r) * H::kPitch + (gp + 16 * i + c4) * 2, H::kMatrix, v);
+            }
+        __syncthreads();
+        // B in its place
+        f32x4_t B[kP][kQ], Bs[kP][kQ];
+#pragma unroll
+        for (int i = 0; i < kP; ++i)
+#pragma unroll
+            for (int j = 0; j < kQ; ++j) B[i][j] = Bs[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int kk = 0; kk < SP / 32; ++kk) {
+            bf16x8_t p[kP][2], q[kQ][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int i = 0; i < kP; ++i) p[i][h] = row_frag<H::kPitch>(M + h * H::kMatrix, gp + 16 * i, kk);
+#pragma unroll
+                for (int j = 0; j < kQ; ++j) q[j][h] = row_frag<H::kPitch>(M + h * H::kMatrix, gq + 16 * j, kk);
+            }
+#pragma unroll
+            for (int j = 0; j < kQ; ++j)
+#pragma unroll
+                for (int i = 0; i < kP; ++i) pair_mfma(B[i][j], Bs[i][j], p[i], q[j]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kP; ++i)
+#pragma unroll
+            for (int j = 0; j < kQ; ++j) {
+                float v[4];
+                const int row = gq + 16 * j + r;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    v[u] = fmaf(o.c, (B[i][j][u] + Bs[i][j][u]) * (1.0f / kUnit), o.b * A[i][j][u]);
+                    if (row == gp + 16 * i + c4 + u && row < o.s) v[u] += o.rest * kUnit;
+                }
+                put_pair(M + row * H::kPitch + (gp + 16 * i + c4) * 2, H::kMatrix, v);
+            }
+        if constexpr (MODE == kStep) clear();
+        DownFrag down[2];
+        down[0].init(xp);
+        down[1].init(xp + 16);
+        for (int j = j0; j < j1; ++j) {
+            char *slab = S + (j & 1) * H::kBytes;
+            asm volatile("" ::: "memory");
+            window_barrier<0>();      // the slab has come, B is there, everybody has left the slab before
+            asm volatile("" ::: "memory");
+            if (j + 1 < j1) load(j + 1, S + ((j + 1) & 1) * H::kBytes);
+            f32x4_t x[2][2], xs[2][2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) x[i][k] = xs[i][k] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int kk = 0; kk < SP / 32; ++kk) {
+                bf16x8_t p[2][2], q[2][2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        p[i][h] = down[i].read(slab + h * H::kPlane, kk);
+                        q[i][h] = row_frag<H::kPitch>(M + h * H::kMatrix, xq + 16 * i, kk);
+                    }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) pair_mfma(x[i][k], xs[i][k], p[i], q[k]);
+            }
+            // a lane's: rows xq + 16 k + r, columns xp + 16 i + c4 .. + 3
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const char *at = slab + slab_at(xq + 16 * k + r, xp + 16 * i + c4);
+                    const f16x4_t h = *(const f16x4_t *)at, lo = *(const f16x4_t *)(at + H::kPlane);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) x[i][k][u] = fmaf(o.apart, (float)h[u] + (float)lo[u], (x[i][k][u] + xs[i][k][u]) * (1.0f / kUnit));
+                }
+            if constexpr (MODE == kLast) {
+                T *O = (T *)o.O + m * elems;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int row = xq + 16 * k + r, col = j * kSlab + xp + 16 * i + c4;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            if (row < o.s && col + u < o.l)
+                                Elem<T>::st(O + (o.transposed ? (int64_t)(col + u) * o.s + row : (int64_t)row * o.l + col + u), x[i][k][u] * o.out);
+                    }
+            } else {
+                // Everybody has read the slab: X' in its place.  (Bare waits, so that the next slab's loads stay on their way.)
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        float v[4];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) v[u] = x[i][k][u];
+                        put_pair(slab + slab_at(xq + 16 * k + r, xp + 16 * i + c4), H::kPlane, v);
+                    }
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                gram(slab);
+                store(j, slab);
+            }
+        }
+    }
+    if constexpr (MODE != kLast) {
+#pragma unroll
+        for (int i = 0; i < kP; ++i)
+#pragma unroll
+            for (int j = 0; j < kQ; ++j) *(f32x4_t *)(o.A_to + sums_of(m * o.pieces + piece, i, j)) = (A[i][j] + As[i][j]) * (1.0f / kUnit);
+    }
+}
+
+// the parts of a matrix's A, in their order
+__global__ void __launch_bounds__(64) ortho_narrow_join_kernel(const float *__restrict__ parts, int pieces, int64_t sums, float *__restrict__ A) {
+    const int per = (int)(sums / 256);
+    const int64_t m = blockIdx.x / per, at = (int64_t)(blockIdx.x - m * per) * 256 + threadIdx.x * 4;
+    const float *from = parts + m * pieces * sums + at;
+    f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 16
+    for (int k = 0; k < pieces; ++k) sum += *(const f32x4_t *)(from + k * sums);
+    *(f32x4_t *)(A + m * sums + at) = sum;
+}
+
+struct Plan {
+    int slabs, pieces;
+    int64_t chunk;             // matrices at a time
+    size_t X, A, A2, total;
+};
+template <int SP> Plan plan(int64_t batch, int64_t l) {
+    typedef Shape<SP> H;
+    Plan p;
+    p.slabs = (int)((l + kSlab - 1) / kSlab);
+    const size_t x = (size_t)p.slabs * H::kBytes;
+    p.chunk = std::min<int64_t>(batch, std::max<int64_t>(1, (int64_t)(((size_t)4 << 30) / (x + 4 * H::kSums * sizeof(float)))));
+    // Work-groups to a matrix: the fewest rounds of slabs over the card, where B costs as much as one, and a launch to join A as much as some
+    p.pieces = 1;
+    double best = 0.0;
+    for (int n = 1; n <= std::min(p.slabs, 256); ++n) {
+        const int64_t rounds = (p.chunk * n + 255) / 256;
+        const double cost = (double)rounds * ((p.slabs + n - 1) / n + 1.5) + (n > kFew ? 3.0 : 0.3 * n);
+        if (n == 1 || cost < best) {
+            best = cost;
+            p.pieces = n;
+        }
+    }
+    const size_t a = (size_t)p.chunk * H::kSums * sizeof(float);
+    size_t o = 0;
+    auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes, 256); return at; };
+    p.X = take(x * p.chunk);
+    p.A = take(a * p.pieces);
+    p.A2 = take(p.pieces > kFew ? a : a * p.pieces);
+    p.total = o;
+    return p;
+}
+
+template <int SP, typename IN, typename OUT> hipError_t run(const NarrowCall &c, hipStream_t s) {
+    typedef Shape<SP> H;
+    const Plan p = plan<SP>(c.batch, c.l);
+    char *base = (char *)c.ws;
+    const int64_t elems = (int64_t)c.s * c.l;
+    Narrow o = {};
+    o.s = c.s; o.l = c.l; o.slabs = p.slabs; o.pieces = p.pieces;
+    o.transposed = c.transposed;
+    o.X = base + p.X;
+    o.norms = c.norms;
+    o.eps = c.eps;
+    o.out = c.scale / kUnit;
+    o.status = c.status;
+    const float a = c.coef[0];
+    o.b = c.coef[1];
+    o.c = c.coef[2];
+    hipError_t e = hipSuccess;
+    for (int64_t m0 = 0; m0 < c.batch; m0 += p.chunk) {
+        const int64_t nm = std::min(p.chunk, c.batch - m0);
+        o.G = (const IN *)c.G + m0 * elems;
+        o.O = (OUT *)c.O + m0 * elems;
+        o.norm = c.norm + m0 * c.norms;
+        float *now = (float *)(base + p.A), *other = (float *)(base + p.A2);
+        auto go = [&](auto kernel) {
+            if (e != hipSuccess) return;
+            (void)hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, H::kLds);
+            kernel<<<(unsigned)(nm * p.pieces), H::kThreads, H::kLds, s>>>(o);
+            e = hipGetLastError();
+        };
+        // `now`: the work-groups' sums; with many of them `other` is what they are joined into
+        o.A_to = now;
+        go(ortho_narrow_kernel<SP, kStart, IN>);
+        for (int k = 0; k < c.steps && e == hipSuccess; ++k) {
+            o.parts = p.pieces;
+            o.A = now;
+            if (p.pieces > kFew) {
+                ortho_narrow_join_kernel<<<(unsigned)(nm * (H::kSums / 256)), 64, 0, s>>>(now, p.pieces, H::kSums, other);
+                e = hipGetLastError();
+                o.parts = 1;
+                o.A = other;
+            } else std::swap(now, other);
+            o.A_to = now;
+            o.apart = (float)ortho_apart(k, c.steps, c.coef);
+            o.rest = (float)((double)a - ortho_apart(k, c.steps, c.coef));
+            if (k + 1 < c.steps) go(ortho_narrow_kernel<SP, kStep, float>);
+            else go(ortho_narrow_kernel<SP, kLast, OUT>);
+        }
+        if (e != hipSuccess) return e;
+    }
+    return e;
+}
+
+}  // namespace
+
+size_t ortho_narrow_ws_bytes(int64_t batch, int64_t s, int64_t l) { return (s <= 64 ? plan<64>(batch, l) : plan<128>(batch, l)).total; }
+
+hipError_t launch_ortho_narrow(const NarrowCall &c, int dtype_in, int dtype_out, hipStream_t s) {
+    auto by_out = [&](auto sp, auto in) {
+        constexpr int SP = decltype(sp)::value;
+        typedef decltype(in) IN;
+        return dtype_out == R3_BF16 ? run<SP, IN, bf16_t>(c, s) : run<SP, IN, float>(c, s);
+    };
+    auto by_in = [&](auto sp) { return dtype_in == R3_BF16 ? by_out(sp, bf16_t{}) : by_out(sp, float{}); };
+    return c.s <= 64 ? by_in(std::integral_constant<int, 64>{}) : by_in(std::integral_constant<int, 128>{});
+}
+
+}  // namespace r3

@@ -66,6 +66,42 @@ def test_many_matrices(b, r, c, src, to):
     assert torch.equal(big[rest], clean[rest])
 
 
+# short sides of up to 128: one work-group to a matrix, two, many, and the last of them with a few columns
+NARROW = [(1, 128, 64), (1, 128, 65), (1, 3, 193), (1, 1000, 65), (2, 40, 20000), (128, 100, 700), (300, 128, 520), (130, 1281, 33), (60, 900, 64), (700, 20, 30),
+          (257, 2, 257), (3, 128, 8192)]
+
+
+@pytest.mark.parametrize("src,to", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("b,r,c", NARROW)
+def test_short_sides(b, r, c, src, to):
+    G = _gradient(b, r, c, src, seed=3)
+    big = torch.full((b + 1, r, c), 77.0, dtype=DT[to], device=DEV)
+    for steps in (5, 1):
+        r3.orthogonalize(G.to(DEV), big[:b], scale=1.5, steps=steps)
+        assert (big[b:] == 77).all()
+        _check(big[:b], G, to, scale=1.5, steps=steps)
+    clean = big[:b].clone()
+    G[b // 3, r - 1, c - 1] = float("-inf")
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    r3.orthogonalize(G.to(DEV), big[:b], scale=1.5, steps=1, status=status)
+    assert status.item() == r3.DATA_NONFINITE and torch.isnan(big[b // 3]).all()
+    rest = [i for i in range(b) if i != b // 3]
+    assert torch.equal(big[rest], clean[rest])
+
+
+def test_what_one_step_alone_has_room_for():
+    # two of these steps in one would need a matrix beyond the range of what products are made of
+    G = _gradient(70, 300, 700, "f32", kind="flat")
+    coef = (4.2, -14.0, 10.0)
+    for to in ("f32", "bf16"):
+        out = torch.empty(70, 300, 700, dtype=DT[to], device=DEV)
+        r3.orthogonalize(G.to(DEV), out, steps=3, coef=coef)
+        _check(out, G, to, steps=3, coef=coef)
+        one = torch.empty(1, 300, 700, dtype=DT[to], device=DEV)
+        r3.orthogonalize(G[:1].to(DEV), one, steps=3, coef=coef)
+        _check(one, G[:1], to, steps=3, coef=coef)
+
+
 @pytest.mark.parametrize("to", ["f32", "bf16"])
 def test_many_matrices_of_low_rank(to):
     g = torch.Generator().manual_seed(2)
