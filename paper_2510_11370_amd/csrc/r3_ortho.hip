@@ -508,12 +508,13 @@ template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(
 }
 
 // ---- few tiles ----
-// Where tiles of 128 would leave most of the card idle, a work-group takes 64 x 64 and has seven windows of 64 k on their way (three with
-// both parts of the operands): its time is latencies.  X X^T, whose k is the long side, is cut into parts that are joined by a launch of
+// Where tiles of 256 would leave most of the card idle, a work-group takes 64 x 64, in windows of 64 k.  Its time is latencies, which other
+// work-groups on the compute unit hide better than its own windows: with two of them in 64 KB each, four windows (two with both parts of the
+// operands), one 2048 x 2048 to bf16 took 454 us and three 1000 x 501 139, with one in 128 KB 650 and 159; with four in 32 KB
+// where products have more than 256 tiles, 392 and 138.  X X^T, whose k is the long side, is cut into parts that are joined by a launch of
 // their own.
 constexpr int kSmall = 64;
 constexpr int kSmallWin = kSmall * kBK3 * 2;     // 8 KB: 64 k of one part of an operand
-constexpr int kLdsSmall = 16 * kSmallWin;
 
 // 64 k-rows of 64 features; 32-byte group g of k-row k sits at g ^ (k & 3)
 struct SmallTr {
@@ -554,10 +555,10 @@ template <class L> __device__ __forceinline__ void small_issue(const L &l, const
 }
 
 // windows first .. first + n - 1 of P and Q; 4 waves of 32 x 32
-template <bool SPLIT, class PL, class QL>
+template <bool SPLIT, int BUF, class PL, class QL>
 __device__ __forceinline__ void multiply_small(f32x4_t (&acc)[2][2], int first, int n, const PL &pl, const Pair &P, int ldp, const QL &ql, const Pair &Q,
                                                int ldq, int own_at, f16_t own, f16_t own_lo, char *lds) {
-    constexpr int kParts = SPLIT ? 2 : 1, kBuf = 8 / kParts, kBytes = 2 * kParts * kSmallWin, kEach = 4 * kParts;   // loads of a wave to a window
+    constexpr int kParts = SPLIT ? 2 : 1, kBuf = BUF / kParts, kBytes = 2 * kParts * kSmallWin, kEach = 4 * kParts;   // loads of a wave to a window
     const uint32_t at = lds_addr(lds);
     auto issue = [&](int w) {
         const uint32_t to = at + w % kBuf * kBytes;
@@ -628,7 +629,7 @@ __device__ __forceinline__ void multiply_small(f32x4_t (&acc)[2][2], int first, 
 }
 
 // kGram: `cut` parts of the windows to a tile; with more than one, sums go to `parts`, [matrix][tile][part][64 x 64]
-template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(256, 1) ortho_small_kernel(Product o, int cut, float *__restrict__ parts) {
+template <int MODE, bool SPLIT, int BUF, typename OUT> __global__ void __launch_bounds__(256, BUF == 2 ? 4 : 2) ortho_small_kernel(Product o, int cut, float *__restrict__ parts) {
     extern __shared__ __align__(1024) char lds[];
     const int64_t at = MODE == kGram ? blockIdx.x / cut : blockIdx.x, m = at / o.ntiles;
     const int t = (int)(at - m * o.ntiles), piece = MODE == kGram ? (int)(blockIdx.x - at * cut) : 0;
@@ -650,14 +651,14 @@ template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(
         SmallKc pl;
         pl.init(2 * ld, p0);
         ql.init(2 * ld, q0);
-        multiply_small<SPLIT>(acc, w0, w1 - w0, pl, from(o.P, base + (int64_t)tj * kSmall * ld), 2 * ld, ql,
+        multiply_small<SPLIT, BUF>(acc, w0, w1 - w0, pl, from(o.P, base + (int64_t)tj * kSmall * ld), 2 * ld, ql,
                               from(MODE == kGram ? o.P : o.Q, base + (int64_t)ti * kSmall * ld), 2 * ld, MODE == kGram ? -1 : (ti * kSmall + q0) / 32, o.own,
                               o.own_lo, lds);
     } else {
         SmallTr pl;
         pl.init(2 * o.lp, p0);
         ql.init(2 * o.sp, q0);
-        multiply_small<SPLIT>(acc, 0, o.sp / kBK3, pl, from(o.P, m * xs + (int64_t)tj * kSmall), 2 * o.lp, ql,
+        multiply_small<SPLIT, BUF>(acc, 0, o.sp / kBK3, pl, from(o.P, m * xs + (int64_t)tj * kSmall), 2 * o.lp, ql,
                               from(o.Q, m * as + (int64_t)ti * kSmall * o.sp), 2 * o.sp, (ti * kSmall + q0) / 32, o.own, o.own_lo, lds);
     }
     if (MODE == kGram && cut > 1) {
@@ -786,12 +787,12 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ 
     }
 }
 
-// Tiles of 64 x 64 up to some six of X's to a compute unit, twelve where products are three (us a call, 64 x 64 | 256 x 256; bf16 results: 16 x
-// 256 x 512 132 | 266, 8 x 512 x 1024 297 | 397, 4 x 768 x 2048 463 | 532, 30 x 300 x 700 347 | 340, 16 x 512 x 1024 486 | 412, 64 x 256 x 512
-// 360 | 288, 2 x 2048 x 2048 1297 | 865; f32: 2 x 1024 x 1024 423 | 1409, 64 x 256 x 512 490 | 638, 16 x 512 x 1024 715 | 1004, 256 x 128 x 1024
-// 1001 | 905).
+// Tiles of 64 x 64 up to some twelve of X's to a compute unit, sixteen where products are three (us a call, 64 x 64 | 256 x 256; bf16
+// results: 30 x 300 x 700 235 | 346, 2 x 2048 x 2048 733 | 868, 16 x 512 x 1024 317 | 412, 24 x 444 | 428, 32 x 579 | 451, 64 x 256 x 512 222 |
+// 288, 100 x 316 | 312, 128 x 388 | 335, 40 x 385 x 900 620 | 530, 1 x 4096 x 4096 2377 | 1674; f32: 1 x 2048 x 2048 840 | 2445, 24 x 512 x 1024
+// 805 | 1034, 32 x 1079 | 1060, 10 x 768 x 2048 1090 | 1411, 128 x 256 x 512 738 | 722).
 bool small_tiles(int64_t batch, int64_t s, int64_t l, bool split) {
-    return batch * ((s + kSmall - 1) / kSmall) * ((l + kSmall - 1) / kSmall) <= (split ? 3000 : 1600);
+    return batch * ((s + kSmall - 1) / kSmall) * ((l + kSmall - 1) / kSmall) <= (split ? 4000 : 3000);
 }
 
 struct Plan {
@@ -885,6 +886,8 @@ bool in_range(int steps, const float *q, bool split, bool pairs) {
     return true;
 }
 
+template <int BUF> struct Buffers { static constexpr int kBuf = BUF, kLds = 2 * BUF * kSmallWin; };
+
 template <int NT = 256, class K, class... A> hipError_t launch(K k, int64_t grid, int lds, hipStream_t s, const A &...args) {
     (void)hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     k<<<(unsigned)grid, NT, lds, s>>>(args...);
@@ -902,12 +905,25 @@ hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pai
     float *no_parts = nullptr;
     o.passes = SPLIT ? 3 : 1;
     hipError_t e = hipSuccess;
+    // 64 x 64 tiles: four windows, or two where that puts more of them on a compute unit
+    auto small = [&](auto mode, auto type, int64_t grid, int cut, float *to) {
+        constexpr int MODE = decltype(mode)::value;
+        typedef decltype(type) T;
+        auto by = [&](auto b) {
+            typedef decltype(b) W;
+            return launch(ortho_small_kernel<MODE, SPLIT, W::kBuf, T>, grid, W::kLds, s, o, cut, to);
+        };
+        if constexpr (!SPLIT) {
+            if (grid > 256) return by(Buffers<2>{});
+        }
+        return by(Buffers<4>{});
+    };
     auto gram = [&](Pair to) {
         o.ntiles = half;
         o.P = X; o.dst = to;
         if (e != hipSuccess) return;
         if (!p.small) e = launch<kThreads2>(ortho_gram_kernel<SPLIT>, matrices * half, 2 * kLdsTile, s, o, matrices);
-        else e = launch(ortho_small_kernel<kGram, SPLIT, float>, matrices * half * p.cut, kLdsSmall, s, o, p.cut, parts);
+        else e = small(std::integral_constant<int, kGram>{}, 0.0f, matrices * half * p.cut, p.cut, parts);
         if (e == hipSuccess && p.cut > 1) e = launch(ortho_join_kernel<SPLIT>, matrices * half, 0, s, o, p.cut, (const float *)parts);
     };
     auto set_own = [&](double v) {
@@ -924,7 +940,7 @@ hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pai
         o.E1 = own ? none : from;
         o.cd = cd; o.c1 = c1; o.c2 = c2; o.diag = (float)(diag * kUnit);
         if (e != hipSuccess) return;
-        e = p.small ? launch(ortho_small_kernel<kSquare, SPLIT, float>, matrices * half, kLdsSmall, s, o, 1, no_parts)
+        e = p.small ? small(std::integral_constant<int, kSquare>{}, 0.0f, matrices * half, 1, no_parts)
                     : launch<kThreads2>(ortho_product_kernel<kSquare, SPLIT, float>, matrices * half, 2 * kLdsTile, s, o, matrices);
     };
     for (int k = 0; k < steps;) {
@@ -955,11 +971,11 @@ hipError_t iterate(const Plan &p, Product o, Pair X, Pair Y, Pair A, Pair B, Pai
         if (e != hipSuccess) return e;
         auto step = [&](auto mode) {
             constexpr int MODE = decltype(mode)::value;
-            return p.small ? launch(ortho_small_kernel<MODE, SPLIT, float>, grid, kLdsSmall, s, o, 1, no_parts)
+            return p.small ? small(mode, 0.0f, grid, 1, no_parts)
                            : launch<kThreads2>(ortho_product_kernel<MODE, SPLIT, float>, grid, 2 * kLdsTile, s, o, matrices);
         };
         if (k == steps) {
-            e = p.small ? launch(ortho_small_kernel<kLast, SPLIT, OUT>, grid, kLdsSmall, s, o, 1, no_parts)
+            e = p.small ? small(std::integral_constant<int, kLast>{}, OUT{}, grid, 1, no_parts)
                         : launch<kThreads2>(ortho_product_kernel<kLast, SPLIT, OUT>, grid, 2 * kLdsTile, s, o, matrices);
         } else if constexpr (SPLIT) {
             e = step(std::integral_constant<int, kStep>{});

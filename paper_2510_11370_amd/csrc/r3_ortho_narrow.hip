@@ -81,6 +81,27 @@ __device__ __forceinline__ void pair_mfma(f32x4_t &large, f32x4_t &small, const 
     small = MfmaF16::run(p[0], q[1], small);
     large = MfmaF16::run(p[0], q[0], large);
 }
+// four elements at any address, of which `left` are there
+__device__ __forceinline__ f32x4_t load4(const float *p, int left) {
+    if (left >= 4) return Row<float>::load(p);
+    return f32x4_t{left > 0 ? p[0] : 0.0f, left > 1 ? p[1] : 0.0f, left > 2 ? p[2] : 0.0f, 0.0f};
+}
+__device__ __forceinline__ f32x4_t load4(const bf16_t *p, int left) {
+    typedef uint32_t V __attribute__((ext_vector_type(2)));
+    typedef V U __attribute__((aligned(2)));
+    if (left >= 4) {
+        const V v = *(const U *)p;
+        return f32x4_t{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xffff0000u), __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xffff0000u)};
+    }
+    auto one = [&](int u) { return left > u ? Elem<bf16_t>::ld(p + u) : 0.0f; };
+    return f32x4_t{one(0), one(1), one(2), 0.0f};
+}
+__device__ __forceinline__ void store4(float *p, const float *v) { Row<float>::store(p, v); }
+__device__ __forceinline__ void store4(bf16_t *p, const float *v) {
+    typedef uint32_t V __attribute__((ext_vector_type(2)));
+    typedef V U __attribute__((aligned(2)));
+    *(U *)p = V{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+}
 // four values as a pair, `lo_off` bytes apart
 __device__ __forceinline__ void put_pair(char *at, int lo_off, const float *v) {
     f16x4_t h, lo;
@@ -158,35 +179,30 @@ template <int SP, int MODE, typename T> __global__ void __launch_bounds__(Shape<
         const double inv = n == 0.0 ? 0.0 : isfinite(sum) ? (double)kUnit / n : (double)NAN;
         if (tid == 0 && piece == 0 && !isfinite(sum) && o.status) atomicOr(o.status, R3_DATA_NONFINITE);
         clear();
+        // A thread has a block of 4 x 4 of a slab: four loads of four elements along G's rows (a wave: whole lines of 32 x 32), and eight bytes of four
+        // rows to LDS, each bank as often as another.
+        const int row0 = 32 * (wave % (SP / 32)) + 4 * (lane & 7), col0 = 32 * (wave / (SP / 32)) + 4 * (lane >> 3);
+        f32x4_t v[4];
+        auto fetch = [&](int j) {
+            const int at = o.transposed ? j * kSlab + col0 : row0, along = o.transposed ? row0 : j * kSlab + col0;
+            const int lines = o.transposed ? o.l : o.s, width = o.transposed ? o.s : o.l;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = at + u < lines ? load4(G + (int64_t)(at + u) * width + along, width - along) : f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        };
+        fetch(j0);
         for (int j = j0; j < j1; ++j) {
             char *slab = S + (j & 1) * H::kBytes;
-            constexpr int kEach = SP * kSlab / NT;
-            float v[kEach];
-            // (in G's order, so that a wave's loads lie together; beyond its rows and columns X is 0 whatever the norm is)
-            auto place = [&](int k, int &row, int &col) {
-                const int e = tid + NT * k;
-                row = o.transposed ? e % SP : e / kSlab;
-                col = o.transposed ? e / SP : e % kSlab;
-            };
 #pragma unroll
-            for (int k = 0; k < kEach; ++k) {
-                int row, col;
-                place(k, row, col);
-                const int64_t at = o.transposed ? (int64_t)(j * kSlab + col) * o.s + row : (int64_t)row * o.l + j * kSlab + col;
-                v[k] = row < o.s && j * kSlab + col < o.l ? Elem<T>::ld(G + at) : 0.0f;
-            }
+            for (int i = 0; i < 4; ++i) {
+                float x[4];
 #pragma unroll
-            for (int k = 0; k < kEach; ++k) {
-                int row, col;
-                place(k, row, col);
-                const float x = row < o.s && j * kSlab + col < o.l ? (float)((double)v[k] * inv) : 0.0f;
-                const f16_t h = (f16_t)x;
-                char *at = slab + slab_at(row, col);
-                *(f16_t *)at = h;
-                *(f16_t *)(at + H::kPlane) = (f16_t)(x - (float)h);
+                for (int u = 0; u < 4; ++u)      // (beyond G's rows and columns X is 0 whatever the norm is)
+                    x[u] = row0 + i < o.s && j * kSlab + col0 + u < o.l ? (float)((double)(o.transposed ? v[u][i] : v[i][u]) * inv) : 0.0f;
+                put_pair(slab + slab_at(row0 + i, col0), H::kPlane, x);
             }
             // (two slabs: everybody has left the one before the last)
             __syncthreads();
+            if (j + 1 < j1) fetch(j + 1);
             gram(slab);
             store(j, slab);
         }
@@ -294,10 +310,16 @@ template <int SP, int MODE, typename T> __global__ void __launch_bounds__(Shape<
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const int row = xq + 16 * k + r, col = j * kSlab + xp + 16 * i + c4;
+                        float v[4];
 #pragma unroll
-                        for (int u = 0; u < 4; ++u)
-                            if (row < o.s && col + u < o.l)
-                                Elem<T>::st(O + (o.transposed ? (int64_t)(col + u) * o.s + row : (int64_t)row * o.l + col + u), x[i][k][u] * o.out);
+                        for (int u = 0; u < 4; ++u) v[u] = x[i][k][u] * o.out;
+                        if (row >= o.s) continue;
+                        if (!o.transposed && col + 4 <= o.l) store4(O + (int64_t)row * o.l + col, v);
+                        else {
+#pragma unroll
+                            for (int u = 0; u < 4; ++u)
+                                if (col + u < o.l) Elem<T>::st(O + (o.transposed ? (int64_t)(col + u) * o.s + row : (int64_t)row * o.l + col + u), v[u]);
+                        }
                     }
             } else {
                 // Everybody has read the slab: X' in its place.  (Bare waits, so that the next slab's loads stay on their way.)
@@ -347,12 +369,15 @@ template <int SP> Plan plan(int64_t batch, int64_t l) {
     p.slabs = (int)((l + kSlab - 1) / kSlab);
     const size_t x = (size_t)p.slabs * H::kBytes;
     p.chunk = std::min<int64_t>(batch, std::max<int64_t>(1, (int64_t)(((size_t)4 << 30) / (x + 4 * H::kSums * sizeof(float)))));
-    // Work-groups to a matrix: the fewest rounds of slabs over the card, where B costs as much as one, and a launch to join A as much as some
+    // Work-groups to a matrix: the fewest rounds of slabs over the card, where B costs as much as one and a half (3.2 us a slab of 128 rows, 1.5 us of
+    // 64), a launch that joins A as much as three, and a part of A that is written and read a share of the card's bandwidth.  (us a call, with 32 |
+    // 16 | 8 work-groups: 1 x 128 x 2048 f32 78 | 90 | 129, 8 x 141 | 119 | 142, 16 x 194 | 135 | 152; with 4 | 2 | 1: 64 x 128 x 768 154 | 166 |
+    // 242, 128 x 276 | 201 | 255, 200 x 470 | 340 | 274, 128 x 64 x 1024 130 | 126 | 180.)
     p.pieces = 1;
     double best = 0.0;
     for (int n = 1; n <= std::min(p.slabs, 256); ++n) {
         const int64_t rounds = (p.chunk * n + 255) / 256;
-        const double cost = (double)rounds * ((p.slabs + n - 1) / n + 1.5) + (n > kFew ? 3.0 : 0.3 * n);
+        const double cost = (double)rounds * ((p.slabs + n - 1) / n + 1.5) + (n > kFew ? 3.0 : 0.3 * n) + (n > 1 ? 0.012 * SP / 128 * p.chunk * n : 0.0);
         if (n == 1 || cost < best) {
             best = cost;
             p.pieces = n;

@@ -45,7 +45,8 @@ def test_orthogonalize(b, r, c, src, to):
 
 
 # enough of them for the large tiles, whose last ones hang over the matrices
-MANY = [(110, 130, 640), (70, 300, 700), (50, 700, 400), (40, 385, 900), (64, 257, 1000), (60, 512, 512), (300, 200, 260), (9, 1100, 1300)]
+MANY = [(110, 130, 640), (70, 300, 700), (50, 700, 400), (40, 385, 900), (64, 257, 1000), (60, 512, 512), (300, 200, 260), (9, 1100, 1300),
+        (130, 130, 640), (90, 300, 700), (12, 1100, 1300)]
 
 
 @pytest.mark.parametrize("src,to", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16")])
@@ -91,10 +92,10 @@ def test_short_sides(b, r, c, src, to):
 
 def test_what_one_step_alone_has_room_for():
     # two of these steps in one would need a matrix beyond the range of what products are made of
-    G = _gradient(70, 300, 700, "f32", kind="flat")
+    G = _gradient(90, 300, 700, "f32", kind="flat")
     coef = (4.2, -14.0, 10.0)
     for to in ("f32", "bf16"):
-        out = torch.empty(70, 300, 700, dtype=DT[to], device=DEV)
+        out = torch.empty(90, 300, 700, dtype=DT[to], device=DEV)
         r3.orthogonalize(G.to(DEV), out, steps=3, coef=coef)
         _check(out, G, to, steps=3, coef=coef)
         one = torch.empty(1, 300, 700, dtype=DT[to], device=DEV)
@@ -103,18 +104,19 @@ def test_what_one_step_alone_has_room_for():
 
 
 @pytest.mark.parametrize("to", ["f32", "bf16"])
-def test_many_matrices_of_low_rank(to):
+@pytest.mark.parametrize("n", [64, 90])
+def test_many_matrices_of_low_rank(n, to):
     g = torch.Generator().manual_seed(2)
-    G = (torch.randn(64, 300, 3, generator=g) * torch.tensor([1.0, 0.6, 0.1])) @ torch.randn(64, 3, 700, generator=g)
+    G = (torch.randn(n, 300, 3, generator=g) * torch.tensor([1.0, 0.6, 0.1])) @ torch.randn(n, 3, 700, generator=g)
     G[5] = torch.outer(torch.arange(300.0), torch.ones(700))
-    out = torch.empty(64, 300, 700, dtype=DT[to], device=DEV)
+    out = torch.empty(n, 300, 700, dtype=DT[to], device=DEV)
     r3.orthogonalize(G.to(DEV), out)
     _check(out[4:11], G[4:11], to)
 
 
 @pytest.mark.parametrize("steps", [1, 2, 3, 6, 9])
 @pytest.mark.parametrize("to", ["f32", "bf16"])
-@pytest.mark.parametrize("b,r,c", [(2, 70, 140), (70, 300, 700)])
+@pytest.mark.parametrize("b,r,c", [(2, 70, 140), (70, 300, 700), (90, 300, 700), (3, 300, 700)])
 def test_steps_and_coefficients(b, r, c, steps, to):
     G = _gradient(b, r, c, "f32", seed=steps, kind="flat")
     for coef in (ref.QUINTIC, (1.5, -0.5, 0.0), (15 / 8, -10 / 8, 3 / 8)):
