@@ -36,7 +36,7 @@ struct Pair { f16_t *hi, *lo; };   // (lo: f16, or X's 8 bits where only hi is m
 // A launch's product D[q][p] = sum_k Q[q][k] P[p][k] per matrix and what is made of it, all in units of 1 / kUnit:
 //   result = cd (D + own P) + c1 E1 + c2 E2 + diag I
 // kSquare: q, p < s, symmetric, lower half and its mirror image; kStep: p < l; kStepLow: the same with c1 times the 8 bits of E1 (if there
-// are any) and 8 bits of its own (if dst has a place for them); kLast: as kStepLow, times `out`, to the caller's array.
+// are any) and 8 bits of its own (if dst has a place for them); kLast: as kStep, times `out`, to the caller's array.
 // own P costs no loads: where a tile's k are its own rows the operand is in LDS, and is multiplied with `own` times a unit matrix, too
 // (two f16, so that `own` keeps 22 bits).
 enum { kGram = 0, kSquare = 1, kStep = 2, kStepLow = 3, kLast = 4 };
@@ -254,7 +254,7 @@ __device__ __forceinline__ void finish_rows(const Product &o, int64_t m, int ti,
     const bool mirror = kMirror && ti != tj;
     // Eight columns of a row to a thread at a time.  X's lo: some loads together, one behind the other's stores their latencies were most
     // of the time.
-    constexpr bool kAddLow = !SPLIT && (MODE == kStepLow || MODE == kLast);
+    constexpr bool kAddLow = MODE == kStepLow;
     constexpr int kEach = N * N / 8 / 256, kBatch = kAddLow ? (kEach < 4 ? kEach : 4) : 1;
     for (int k0 = 0; k0 < kEach; k0 += kBatch) {
         uint2 low[kBatch];
@@ -355,8 +355,8 @@ __device__ __forceinline__ void put_sums(const f32x4_t (&acc)[NI][NJ], int p0, i
 
 // ---- the ends of 256 x 256 tiles ----
 // Where a result needs nothing but its sums it is rounded in registers, and the whole tile is f16 in LDS, where the operands were (pairs:
-// hi, then lo): one round trip, and whole lines to memory.  With f32 sums in LDS, two blocks of 128 x 128 at a time (below), a product
-// of 128 times 768 x 768 took 115 us instead of 9x.
+// hi, then lo): one round trip, and whole lines to memory.  (With f32 sums in LDS, two blocks of 128 x 128 at a time (below): 128 products of 768
+// x 768 117 us instead of 112, their last products with X of 768 x 2048, to bf16 443 instead of 419.)
 constexpr int kPitch16 = kTile + 8;
 static_assert(kTile * kPitch16 * 2 <= 2 * kLdsTile, "");
 
@@ -399,10 +399,15 @@ __device__ __forceinline__ void finish_rounded(const Product &o, int64_t m, int 
                             for (int u = 0; u < 4; ++u) v[u] += r == c + u && ti * kTile + q < o.s ? o.diag : 0.0f;
                         }
                     }
-                    f16x4_t w;
+                    if constexpr (MODE == kLast) {
+                        v *= o.out;
+                        *(uint2 *)(t + q * kPitch16 + p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+                    } else {
+                        f16x4_t w;
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) w[u] = part ? part_lo(v[u], part_hi(v[u])) : part_hi(v[u]);
-                    *(f16x4_t *)(t + q * kPitch16 + p) = w;
+                        for (int u = 0; u < 4; ++u) w[u] = part ? part_lo(v[u], part_hi(v[u])) : part_hi(v[u]);
+                        *(f16x4_t *)(t + q * kPitch16 + p) = w;
+                    }
                 }
         }
         __syncthreads();
@@ -412,28 +417,60 @@ __device__ __forceinline__ void finish_rounded(const Product &o, int64_t m, int 
             const int h = b >> 1, g = b & 1;
             if (!wanted(h, g)) continue;
             const f16_t *from = t + kSide * (h * kPitch16 + g);
+            // (the mirror image, or what a tall G's update is: through the transposing reads, of 16 columns, 32 rows of a wave's at a time)
+            auto across = [&](int k, int &q) {
+                q = 32 * k + 2 * c;
+                const f16_t *at = from + (q + (r >> 2)) * kPitch16 + 16 * wave + (r & 3) * 4;
+                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at));
+                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at + 4 * kPitch16));
+                return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            };
+            if constexpr (MODE == kLast) {
+                const int q0 = (2 * ti + h) * kSide, p0 = (2 * tj + g) * kSide;
+                bf16_t *out = (bf16_t *)o.O + m * o.s * o.l;
+                // eight values of a row of `n`, from element i on
+                auto put = [&](bf16_t *row, int i, int n, const s16x8_t &w) {
+                    typedef s16x8_t any_t __attribute__((aligned(2)));
+                    if (i + 8 <= n) *(any_t *)(row + i) = w;
+                    else {
+#pragma unroll
+                        for (int u = 0; u < 8; ++u)
+                            if (i + u < n) row[i + u] = (bf16_t)w[u];
+                    }
+                };
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (o.transposed) {
+                        int q;
+                        const s16x8_t w = across(k, q);
+                        const int p = p0 + 16 * wave + r;
+                        if (p < o.l) put(out + (int64_t)p * o.s, q0 + q, o.s, w);
+                    } else {
+                        const int e = threadIdx.x + kThreads2 * k, row = e >> 4, col = (e & 15) * 8;
+                        if (q0 + row < o.s) put(out + (int64_t)(q0 + row) * o.l, p0 + col, o.l, *(const s16x8_t *)(from + row * kPitch16 + col));
+                    }
+                }
+                continue;
+            }
             f16_t *to = dst + tile + (int64_t)h * kSide * ld + g * kSide;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int e = threadIdx.x + kThreads2 * k, row = e >> 4, col = (e & 15) * 8;
                 *(f16x8_t *)(to + (int64_t)row * ld + col) = *(const f16x8_t *)(from + row * kPitch16 + col);
             }
-            // the mirror image through the transposing reads: of 16 columns, 32 rows of a wave's at a time
             if (!kSq || 2 * tj + g == 2 * ti + h) continue;
             f16_t *mirror = dst + tile_at<MODE, kSide>(o, m, 2 * tj + g, 2 * ti + h, ld) + (int64_t)(16 * wave + r) * ld;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int q = 32 * k + 2 * c;
-                const f16_t *at = from + (q + (r >> 2)) * kPitch16 + 16 * wave + (r & 3) * 4;
-                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at));
-                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at + 4 * kPitch16));
-                *(s16x8_t *)(mirror + q) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                int q;
+                const s16x8_t w = across(k, q);
+                *(s16x8_t *)(mirror + q) = w;
             }
         }
     }
 }
 
-// The others (X's 8 bits, the caller's array): two blocks of 128 x 128 at a time, to four waves each, f32 in LDS.  `blocks`: of a row of
+// The others (X's 8 bits, f32 results): two blocks of 128 x 128 at a time, to four waves each, f32 in LDS.  `blocks`: of a row of
 // results.
 template <int MODE, bool SPLIT, typename OUT>
 __device__ __forceinline__ void finish_tile(const Product &o, int64_t m, int ti, int tj, int blocks, const Acc2 &acc, char *lds) {
@@ -503,7 +540,7 @@ template <int MODE, bool SPLIT, typename OUT> __global__ void __launch_bounds__(
     Acc2 acc;
     zero_acc2(acc);
     multiply_columns(acc, o.passes, P, Q, (ti * kTile + kWaveRowsQ * qw) / 32, o.own, o.own_lo, lds);
-    if constexpr (MODE == kSquare || MODE == kStep) finish_rounded<MODE, SPLIT>(o, m, ti, tj, ldp / kSide, acc, lds);
+    if constexpr (MODE == kSquare || MODE == kStep || (MODE == kLast && !SPLIT)) finish_rounded<MODE, SPLIT>(o, m, ti, tj, ldp / kSide, acc, lds);
     else finish_tile<MODE, SPLIT, OUT>(o, m, ti, tj, ldp / kSide, acc, lds);
 }
 
@@ -823,8 +860,9 @@ Plan plan(int64_t batch, int64_t rows, int64_t cols, int dtype_out) {
     p.chunk = fit < 1 ? 1 : fit < batch ? fit : batch;
     p.cut = 1;
     const int nt = p.sp / kSmall, tiles = nt * (nt + 1) / 2, nw = p.lp / kBK3;
-    if (p.small)     // a work-group to a compute unit, at least four windows to a part
-        p.cut = (int)std::max<int64_t>(1, std::min<int64_t>(nw / 4, 256 / (tiles * p.chunk)));
+    // A work-group to a compute unit, at least four windows to a part (of pairs) or eight; up to 24 the join costs more (3 x 1000 x 501 to bf16, 16
+    // windows, 123 us uncut, 136 in two; 5 x 200 x 1500, 24, 119 | 122 in three; 1 x 512 x 2048, 32, 133 in four, 138 in two).
+    if (p.small && (p.split || nw > 24)) p.cut = (int)std::max<int64_t>(1, std::min<int64_t>(nw / (p.split ? 4 : 8), 256 / (tiles * p.chunk)));
     size_t o = 0;
     // (a tile of 256 columns may read 128 columns past a matrix's last)
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes + 2 * kSide, 256); return at; };
