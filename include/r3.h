@@ -463,17 +463,19 @@ int r3_balance_loss(const r3_layer_desc *desc, const float *logits, int64_t ld, 
  * {3.4445, -4.775, 2.0315}, with which singular values of 0.002 and more come
  * to lie in [0.68, 1.21] after five steps.
  * G and out: dense [batch, rows, cols], dtype R3_BF16 or R3_F32 each.  The
- * products' operands are f16 numbers with f32 sums; for dtype_out R3_F32 they
- * are sums of two such, 22 bits.  Relative to each matrix (2-norm) a bf16 result
- * is off by about 1e-3 beside its own rounding, an f32 one by 1e-6, as f32
- * products are (more where most of G is within rounding of fewer dimensions).
+ * products' operands are f16 numbers with f32 sums; for dtype_out R3_F32, and
+ * where rows or cols are at most 128, they are sums of two such, 22 bits.
+ * Relative to each matrix (2-norm) a bf16 result is off by about 1e-3 beside its
+ * own rounding, an f32 one by 1e-6, as f32 products are (three times as much
+ * where most of G is within rounding of a few dimensions).
  * A matrix of zeros gives zeros.  A NaN or an infinity in a matrix makes its
  * result NaN and sets R3_DATA_NONFINITE; the other matrices are as without it.
  * A matrix's bits do not depend on what the call's other matrices hold, but may
  * on how many they are.
  * rows, cols <= 32768, batch * rows * cols <= 2^46, and coefficients with which
- * no element of X, A or b A + c A A can leave (-15, 15) (|G|_2 <= |G|_F bounds
- * them), else R3_ERR_UNSUPPORTED.  1 <= steps <= R3_MAX_STEPS, eps >= 0.
+ * no element of X, A or b A + c A A (|G|_2 <= |G|_F bounds them), nor a or
+ * a + b + c, can leave (-15, 15), else R3_ERR_UNSUPPORTED.
+ * 1 <= steps <= R3_MAX_STEPS, eps >= 0.
  * out may be G itself if the types are the same; otherwise no output, nor ws,
  * may share bytes with another array.  batch = 0 is a no-op.
  * ws: device workspace of r3_orthogonalize_workspace_bytes(), 256-byte aligned.

@@ -78,8 +78,10 @@ template <int NT, typename T> __device__ __forceinline__ T block_sum(T v, T *roo
 //   dl/dlogp = -w A r where used = r, else 0, + kl (1 - e^q).  A sequence's ratio: the sum of the first part over its tokens, divided by
 //   their number, to each of them.
 // Which side of a border a token lies on is decided on d in 64 bits, where the difference of two floats is exact.  Two passes (the first
-// reads only `target` unless ratios are a sequence's): tokens' weights need the numbers of live tokens.  Nothing but loads: the card
-// is never busy, launches and their latencies are the time up to some 100 K tokens.
+// reads only `target` unless ratios are a sequence's): tokens' weights need the numbers of live tokens.  Nothing but loads: the card is
+// never busy, launches and their latencies are the time up to some 100 K tokens (us: one work-group's 1531 tokens 10, 64 K in 64 sequences
+// 5 + 8.5 + 3, 1 M in 2048 with all terms 12.5 + 4 + 17 + 4, where the 17 move 38 MB at 2.2 TB/s).  The sums' last launch as the end of the
+// tokens' (the last work-group to come adds all up): no faster at 64 K, 27 us instead of 21 at 1 M, as many counters' turns.
 // ---------------------------------------------------------------------------------------------------------------------------------
 
 struct SegSum {      // of a segment
@@ -594,7 +596,8 @@ namespace {
 // p_t = softmax of token t's logits; loss = alpha mean_g mean_t sum_e f_e p_te + zeta mean_t lse_t^2.
 //   ds_te = alpha / (groups N) p_te (f_e - sum_i f_i p_ti) + 2 zeta / tokens lse_t p_te
 // The counts come from the record alone, a byte or two to a slot, so they are made first and the logits are read once: a token's
-// probabilities give its part of the loss and its gradient at once.  HBM-bound.
+// probabilities give its part of the loss and its gradient at once.  HBM-bound where it counts: 65536 x 128 counts 4, join 3, tokens 16 us
+// (67 MB at 4.2 TB/s), finish 4; 131072 x 128 in 64 sequences 8 + 4 + 31 + 4; 3001 x 384 in 7 6 + 3 + 14 + 4, latencies.
 // ---------------------------------------------------------------------------------------------------------------------------------
 
 struct Balance {
@@ -705,7 +708,8 @@ __global__ void __launch_bounds__(kThreads) balance_join_kernel(Balance a) {
     for (int64_t i = blockIdx.x, n = balance_items(a); i < n; i += gridDim.x) balance_join<kThreads>(a, i, sums);
 }
 
-// A value over L neighbouring lanes, in all of them: within 16 by moves in the vector pipe (pairs, pairs of pairs, mirrored halves of 8 and 16)
+// A value over L neighbouring lanes, in all of them: within 16 by moves in the vector pipe (pairs, pairs of pairs, mirrored halves of 8 and
+// 16)
 template <int L, class F> __device__ __forceinline__ float over_lanes(float v, F f) {
     if constexpr (L >= 2) v = f(v, lane_move<0xb1, 0xf>(v, v));
     if constexpr (L >= 4) v = f(v, lane_move<0x4e, 0xf>(v, v));
@@ -926,7 +930,8 @@ BalancePlan balance_plan(int64_t T, int E, int nseq) {
     BalancePlan p;
     // counts: at most 128 work-groups of 1024 threads, so that few parts are added up
     p.piece0 = (int)std::max<int64_t>((T + 127) / 128, 128);
-    // logits: 16 KB and more to a work-group, at most 1024 of them (65536 x 128: 16.6 us; 2048 of them, whose beginnings and ends count, 20.3)
+    // logits: 16 KB and more to a work-group, at most 1024 of them (65536 x 128: 16.6 us; 2048 of them, whose beginnings and ends count,
+    // 20.3)
     p.piece = (int)std::max<int64_t>((T + 1023) / 1024, std::max<int64_t>(4, 4096 / E));
     if (balance_small(T, E, nseq)) p.piece0 = p.piece = (int)T;
     p.npieces0 = (int)((T + p.piece0 - 1) / p.piece0);

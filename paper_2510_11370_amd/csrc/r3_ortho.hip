@@ -1,16 +1,24 @@
 // Newton-Schulz orthogonalisation of a batch of matrices:  X = G / (|G|_F + eps);  steps times  A = X X^T,  X <- a X + (b A + c A A) X.
 // With X = U S V^T a step takes every singular value x to a x + b x^3 + c x^5 and leaves U and V alone.  The short side is the rows
 // of X (a tall G is read and written transposed), so that A is s x s; it and its polynomial are symmetric and half their tiles are made.
+// Bound by the matrix instructions where there are many tiles, by launches and latencies where there are few.  (A short side of at most 128:
+// r3_ortho_narrow.hip.)
 //
 // Numbers.  The matrix instruction's f16 operands, f32 sums.  A step's values are known beforehand: |X|_2 stays below about 1.2, so no
-// element of X, A or B = b A + c A A leaves (-16, 16) (the host checks it for other coefficients), and everything is stored times 2^12:
-// at best 11 bits, four times bf16's, down to 1.5e-8.  A rounding of X is an error that the coming steps multiply by up to a each (a
-// small singular value grows by a, a new one beside it does too), so X is kept as two f16, its rounding and the rounding of the rest; one
-// of them enters the products, where the small directions hardly count.  The last two steps' polynomial has a + b + c, what it is for
-// singular values of 1, taken out of B and applied to X in f32, so that B's rounding is one of a small matrix.  Relative error of bf16
-// results beside their own rounding (1.7e-3): 4e-4 ... 1.0e-3 for matrices with flat and falling spectra; with bf16 operands throughout
-// it is 1e-2 ... 4e-2.  For f32 results all of X, A, B are such pairs and products are the three of their parts that count
-// (hi lo, lo hi, hi hi): 22 bits, 3e-7 ... 8e-7 where f32 products give 2e-7 ... 5e-7.
+// element of X, A or B = b A + c A A leaves (-16, 16) (the host checks it for other coefficients), and everything is stored times 2^12: at
+// best 11 bits, four times bf16's, down to 1.5e-8.  A rounding of X is an error that the coming steps multiply by up to a each (a small
+// singular value grows by a, a new one beside it does too), so while three steps and more are left X is kept as an f16 and 8 bits of what
+// its rounding leaves; the f16 alone enters the products, where the small directions hardly count.  The last two steps' polynomial has a +
+// b + c, what it is for singular values of 1, taken out of B and applied to X in f32, so that B's rounding is one of a small matrix.
+// Relative error of bf16 results beside their own rounding (1.7e-3): 8e-4 ... 1.1e-3 for matrices with flat and falling spectra, 3e-3 for
+// those of three directions; with bf16 operands throughout it is 1e-2 ... 4e-2.  For f32 results all of X, A, B are pairs of f16 and
+// products are the three of their parts that count (hi lo, lo hi, hi hi): 22 bits, 3e-7 ... 8e-7 where f32 products give 2e-7 ... 5e-7.
+//
+// 128 of 2048 x 768 f32 to bf16 3550 us, 32 of 768 x 2048 to f32 2132; the products alone would be 1992 and (three to one) 1493 at the 1.31
+// PFLOP/s of a large f16 product.  X X^T runs at 1.08 PFLOP/s (190 us), the products with X at 0.70 ... 0.85 (441 with X's 8 bits, 364
+// without): their results, as large as X, are written when a tile is done and no second work-group fits beside it to multiply meanwhile.
+// (Tiles of 128 x 256 with two to a compute unit took as long, bound by the L2; fewer matrices at a time, so that X stays in the caches,
+// longer.)
 #include <algorithm>
 #include <cmath>
 #include <utility>
@@ -25,7 +33,7 @@ namespace {
 typedef _Float16 f16_t;
 typedef f16_t f16x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kSide = 128;                 // a work-group's tile
+constexpr int kSide = 128;                 // of a block of results; a work-group has two by two
 constexpr float kUnit = 4096.0f;           // what is stored is times this
 constexpr int kPitchF = kSide + 4;         // of a tile of results in LDS
 constexpr int kLdsTile = kSide * kPitchF * 4;   // 66 KB: 128 x 128 results; two of them, where the windows or stages of operands were
@@ -44,7 +52,7 @@ struct Product {
     int s, l, sp, lp;              // X is s x l in sp x lp, A and the like s x s in sp x sp, zeros beyond
     int ntiles;                    // of a matrix
     int passes;                    // through k: 1, or 3 for pairs (as a constant of the loop it costs registers that spill)
-    Pair Q, P, E1, E2, dst;        // (E1, E2: or none)
+    Pair Q, P, E1, E2, dst;        // (E1: or none; E2: or none, large tiles alone)
     f16_t own, own_lo;             // times kUnit
     float cd, c1, c2, diag, out;
     void *O;
@@ -198,7 +206,7 @@ template <int N> __device__ __forceinline__ void read_down(const float *sums, in
     for (int u = 0; u < 8; ++u) v[u] = at[u * (N + 4)];
 }
 // What an f16 leaves of a value where it is not multiplied (X's, bf16 results): 8 bits with 2 of mantissa, times 2^8, which takes 1e-3 to 2^4
-// times kUnit's results to the middle of their range.  A quarter less to move than with f16 (128 of 2048 x 768: X' 476 | 414 us).
+// times kUnit's results to the middle of their range.  A quarter less to move than with f16 (128 of 2048 x 768: the start 300 -> 257 us).
 constexpr float kLow = 256.0f;
 __device__ __forceinline__ uint2 pack_low(const float *v, const f16x8_t &h) {
     float r[8];
@@ -275,7 +283,6 @@ __device__ __forceinline__ void finish_rows(const Product &o, int64_t m, int ti,
 #pragma unroll
                 for (int u = 0; u < 8; ++u) v[u] *= o.cd;
                 if (o.E1.hi) add8<SPLIT>(o.E1, e, o.c1, v);
-                if (o.E2.hi) add8<SPLIT>(o.E2, e, o.c2, v);
                 const int row = ti * N + r;
                 if (ti == tj && row < o.s) {
 #pragma unroll
@@ -354,9 +361,10 @@ __device__ __forceinline__ void put_sums(const f32x4_t (&acc)[NI][NJ], int p0, i
 }
 
 // ---- the ends of 256 x 256 tiles ----
-// Where a result needs nothing but its sums it is rounded in registers, and the whole tile is f16 in LDS, where the operands were (pairs:
-// hi, then lo): one round trip, and whole lines to memory.  (With f32 sums in LDS, two blocks of 128 x 128 at a time (below): 128 products of 768
-// x 768 117 us instead of 112, their last products with X of 768 x 2048, to bf16 443 instead of 419.)
+// Where a result needs nothing but its sums it is rounded in registers, and the whole tile is f16 in
+// LDS, where the operands were (pairs: hi, then lo): one round trip, and whole lines to memory.  (With f32 sums in LDS, two blocks of 128 x
+// 128 at a time (below): 128 products of 768 x 768 117 us instead of 112, their last products with X of 768 x 2048, to bf16 443 instead of
+// 419.)
 constexpr int kPitch16 = kTile + 8;
 static_assert(kTile * kPitch16 * 2 <= 2 * kLdsTile, "");
 
@@ -825,9 +833,9 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const T *__restrict__ 
 }
 
 // Tiles of 64 x 64 up to some twelve of X's to a compute unit, sixteen where products are three (us a call, 64 x 64 | 256 x 256; bf16
-// results: 30 x 300 x 700 235 | 346, 2 x 2048 x 2048 733 | 868, 16 x 512 x 1024 317 | 412, 24 x 444 | 428, 32 x 579 | 451, 64 x 256 x 512 222 |
-// 288, 100 x 316 | 312, 128 x 388 | 335, 40 x 385 x 900 620 | 530, 1 x 4096 x 4096 2377 | 1674; f32: 1 x 2048 x 2048 840 | 2445, 24 x 512 x 1024
-// 805 | 1034, 32 x 1079 | 1060, 10 x 768 x 2048 1090 | 1411, 128 x 256 x 512 738 | 722).
+// results: 30 x 300 x 700 235 | 346, 2 x 2048 x 2048 733 | 868, 16 x 512 x 1024 317 | 412, 24 x 444 | 428, 32 x 579 | 451, 64 x 256 x 512
+// 222 | 288, 100 x 316 | 312, 128 x 388 | 335, 40 x 385 x 900 620 | 530, 1 x 4096 x 4096 2377 | 1674; f32: 1 x 2048 x 2048 840 | 2445, 24 x
+// 512 x 1024 805 | 1034, 32 x 1079 | 1060, 10 x 768 x 2048 1090 | 1411, 128 x 256 x 512 738 | 722).
 bool small_tiles(int64_t batch, int64_t s, int64_t l, bool split) {
     return batch * ((s + kSmall - 1) / kSmall) * ((l + kSmall - 1) / kSmall) <= (split ? 4000 : 3000);
 }
@@ -860,8 +868,8 @@ Plan plan(int64_t batch, int64_t rows, int64_t cols, int dtype_out) {
     p.chunk = fit < 1 ? 1 : fit < batch ? fit : batch;
     p.cut = 1;
     const int nt = p.sp / kSmall, tiles = nt * (nt + 1) / 2, nw = p.lp / kBK3;
-    // A work-group to a compute unit, at least four windows to a part (of pairs) or eight; up to 24 the join costs more (3 x 1000 x 501 to bf16, 16
-    // windows, 123 us uncut, 136 in two; 5 x 200 x 1500, 24, 119 | 122 in three; 1 x 512 x 2048, 32, 133 in four, 138 in two).
+    // A work-group to a compute unit, at least four windows to a part (of pairs) or eight; up to 24 the join costs more (3 x 1000 x 501 to
+    // bf16, 16 windows, 123 us uncut, 136 in two; 5 x 200 x 1500, 24, 119 | 122 in three; 1 x 512 x 2048, 32, 133 in four, 138 in two).
     if (p.small && (p.split || nw > 24)) p.cut = (int)std::max<int64_t>(1, std::min<int64_t>(nw / (p.split ? 4 : 8), 256 / (tiles * p.chunk)));
     size_t o = 0;
     // (a tile of 256 columns may read 128 columns past a matrix's last)
@@ -893,8 +901,9 @@ bool two_together(int step, int steps, bool split, bool pairs) {
 }
 
 // Whether every element stays in (-15, 15), so that times kUnit it is an f16: a matrix's are at most its largest singular value, that of X
-// at most 1 at the start and then what the quintic makes of it.  At equidistant points: between two of 2 n over (-r, r) a polynomial of degree d
-// is at most d^2 (d^2 - 1) / 24 n^2 of its maximum beyond them, 0.1 % at degree 6 and 256 points, 1.4 % at degree 24 (two steps) and 1024.
+// at most 1 at the start and then what the quintic makes of it.  At equidistant points: between two of 2 n over (-r, r) a polynomial of
+// degree d is at most d^2 (d^2 - 1) / 24 n^2 of its maximum beyond them, 0.1 % at degree 6 and 256 points, 1.4 % at degree 24 (two steps)
+// and 1024.
 bool in_range(int steps, const float *q, bool split, bool pairs) {
     const double a = q[0], b = q[1], c = q[2], room = pairs ? 1.03 : 1.01;    // for roundings and what lies between the points
     const int points = pairs ? 1024 : 256;

@@ -1,14 +1,16 @@
-// Newton-Schulz orthogonalisation (r3_ortho.hip has the mathematics and the numbers' scale) of matrices with a short side of at most 128: such a matrix's A = X X^T fits into
-// a compute unit's LDS as a pair of f16, and its X goes by in slabs of 64 columns.
+// Newton-Schulz orthogonalisation (r3_ortho.hip has the mathematics and the numbers' scale) of matrices with a short side of at most 128:
+// such a matrix's A = X X^T fits into a compute unit's LDS as a pair of f16, and its X goes by in slabs of 64 columns.
 //
-// A work-group has a run of a matrix's slabs.  A step of it: A, B = b A + c A A + .. into LDS; of each slab X' = a X + B X, and at once X' X'^T added to its part of the next
-// step's A, in registers.  So a step is one launch that reads and writes X once, and another that joins the parts where there are more than a
-// few; as products over tiles it was five launches, each of which waited for the one before (1 x 2048 x 128: 27 launches, NNN us | 12, NNN us).  Where
-// a work-group has one matrix and all its slabs, B is the smaller part of its work; where a matrix is shared, each of its work-groups makes B for itself, which costs
-// as much as a slab.
+// A work-group has a run of a matrix's slabs.  A step of it: A, then B = b A + c A A + .. into LDS; of each slab X' = a X + B X, and at
+// once X' X'^T added to its part of the next step's A, in registers.  So a step is one launch that reads and writes X once, and another
+// that joins the parts where there are more than a few; as products over tiles it was five, each of which waited for the one before (1 x
+// 2048 x 128 f32: 27 launches, 128 us | 12, 76 us; 256 x 128 x 1024: 878 | 424).  Where a work-group has a whole matrix, B is the smaller
+// part of its work; where work-groups share one, each makes B for itself, which costs as much as a slab and a half. Bound by latencies
+// where matrices are few (a step of one slab is 11 us, some 2 of them products), by memory where they are many (256 x 128 x 1024: 72 us a
+// step, 268 MB, 3.7 TB/s; matrix pipes 39 % busy).
 //
-// X, A and B are pairs of f16 times 2^12 for results of either type: products are hi hi, hi lo, lo hi.  These matrices have few directions in which an error could be lost (3 x 5, f16 operands:
-// 6e-3 of the norm at worst), and the two products more are hidden behind latencies.
+// X, A and B are pairs of f16 times 2^12 for results of either type: products are hi hi, hi lo, lo hi.  These matrices have few directions
+// in which an error could be lost (3 x 5, f16 operands: 6e-3 of the norm at worst), and the two products more hide behind the rest.
 #include <algorithm>
 
 #include "r3_kernels.h"
@@ -52,8 +54,8 @@ template <int SP> struct Shape {
 };
 static_assert(Shape<128>::kLds <= 160 * 1024, "");
 
-// A slab in LDS: rows of 128 bytes, the 16-byte chunk c of row r at c ^ ((r >> 1) & 7), so that both ways of reading it (KcFrag16's along rows,
-// and down columns) meet few banks twice.
+// A slab in LDS: rows of 128 bytes, the 16-byte chunk c of row r at c ^ ((r >> 1) & 7), so that both ways of reading it (KcFrag16's along
+// rows, and down columns) meet few banks twice.
 __device__ __forceinline__ int slab_at(int row, int col) { return row * 128 + ((((col >> 3) ^ (row >> 1)) & 7) << 4) + (col & 7) * 2; }
 // 32 rows from row 32 kk on of 16 columns, as an operand whose k are rows: two transposing reads of 4 k each
 struct DownFrag {
@@ -179,8 +181,8 @@ template <int SP, int MODE, typename T> __global__ void __launch_bounds__(Shape<
         const double inv = n == 0.0 ? 0.0 : isfinite(sum) ? (double)kUnit / n : (double)NAN;
         if (tid == 0 && piece == 0 && !isfinite(sum) && o.status) atomicOr(o.status, R3_DATA_NONFINITE);
         clear();
-        // A thread has a block of 4 x 4 of a slab: four loads of four elements along G's rows (a wave: whole lines of 32 x 32), and eight bytes of four
-        // rows to LDS, each bank as often as another.
+        // A thread has a block of 4 x 4 of a slab: four loads of four elements along G's rows (a wave: 32 x 32), and eight bytes of four rows
+        // to LDS, each bank as often as another.  (Single elements: 256 x 128 x 1024 153 us instead of 60.)
         const int row0 = 32 * (wave % (SP / 32)) + 4 * (lane & 7), col0 = 32 * (wave / (SP / 32)) + 4 * (lane >> 3);
         f32x4_t v[4];
         auto fetch = [&](int j) {
@@ -369,10 +371,10 @@ template <int SP> Plan plan(int64_t batch, int64_t l) {
     p.slabs = (int)((l + kSlab - 1) / kSlab);
     const size_t x = (size_t)p.slabs * H::kBytes;
     p.chunk = std::min<int64_t>(batch, std::max<int64_t>(1, (int64_t)(((size_t)4 << 30) / (x + 4 * H::kSums * sizeof(float)))));
-    // Work-groups to a matrix: the fewest rounds of slabs over the card, where B costs as much as one and a half (3.2 us a slab of 128 rows, 1.5 us of
-    // 64), a launch that joins A as much as three, and a part of A that is written and read a share of the card's bandwidth.  (us a call, with 32 |
-    // 16 | 8 work-groups: 1 x 128 x 2048 f32 78 | 90 | 129, 8 x 141 | 119 | 142, 16 x 194 | 135 | 152; with 4 | 2 | 1: 64 x 128 x 768 154 | 166 |
-    // 242, 128 x 276 | 201 | 255, 200 x 470 | 340 | 274, 128 x 64 x 1024 130 | 126 | 180.)
+    // Work-groups to a matrix: the fewest rounds of slabs over the card, where B costs as much as one and a half (3.2 us a slab of 128
+    // rows, 1.5 us of 64), a launch that joins A as much as three, and a part of A that is written and read a share of the card's
+    // bandwidth.  (us a call, with 32 | 16 | 8 work-groups: 1 x 128 x 2048 f32 78 | 90 | 129, 8 x 141 | 119 | 142, 16 x 194 | 135 | 152;
+    // with 4 | 2 | 1: 64 x 128 x 768 154 | 166 | 242, 128 x 276 | 201 | 255, 200 x 470 | 340 | 274, 128 x 64 x 1024 130 | 126 | 180.)
     p.pieces = 1;
     double best = 0.0;
     for (int n = 1; n <= std::min(p.slabs, 256); ++n) {
