@@ -1048,14 +1048,17 @@ hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int d
     double *part = (double *)(base + p.norm);
     const int64_t elems = rows * cols;
     const size_t eb = dtype_in == R3_BF16 ? 2 : 4, ob = dtype_out == R3_BF16 ? 2 : 4;
-    auto norms = [&](const char *g, int64_t nm) {
-        if (dtype_in == R3_BF16) ortho_norm_kernel<bf16_t><<<(unsigned)(nm * p.parts), 256, 0, s>>>((const bf16_t *)g, elems, p.parts, part);
-        else ortho_norm_kernel<float><<<(unsigned)(nm * p.parts), 256, 0, s>>>((const float *)g, elems, p.parts, part);
+    auto norms = [&](const char *g, int64_t nm, double *to) {
+        if (dtype_in == R3_BF16) ortho_norm_kernel<bf16_t><<<(unsigned)(nm * p.parts), 256, 0, s>>>((const bf16_t *)g, elems, p.parts, to);
+        else ortho_norm_kernel<float><<<(unsigned)(nm * p.parts), 256, 0, s>>>((const float *)g, elems, p.parts, to);
         return hipGetLastError();
     };
     if (p.narrow) {
-        const hipError_t e = norms((const char *)G, batch);
-        if (e != hipSuccess) return e;
+        constexpr int64_t kMost = 1 << 17;      // matrices to a launch: 2^31 threads at the most
+        for (int64_t m0 = 0; m0 < batch; m0 += kMost) {
+            const hipError_t e = norms((const char *)G + (size_t)m0 * elems * eb, std::min(kMost, batch - m0), part + m0 * p.parts);
+            if (e != hipSuccess) return e;
+        }
         NarrowCall c = {};
         c.batch = batch; c.s = p.s; c.l = p.l; c.steps = steps; c.norms = p.parts;
         c.transposed = rows > cols;
@@ -1081,7 +1084,7 @@ hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int d
         const char *g = (const char *)G + (size_t)m0 * elems * eb;
         const int side = p.small ? kSmall : kSide;
         const int64_t ntiles = nm * (p.sp / side) * (p.lp / side);
-        hipError_t e = norms(g, nm);
+        hipError_t e = norms(g, nm, part);
         if (e != hipSuccess) return e;
         auto start = [&](auto type) {
             typedef decltype(type) T;

@@ -90,6 +90,15 @@ def test_short_sides(b, r, c, src, to):
     assert torch.equal(big[rest], clean[rest])
 
 
+def test_more_matrices_than_a_launch_has_threads_for():
+    G = torch.empty(17_000_000, 1, 1, device=DEV).uniform_(0.5, 2.0).mul_(torch.where(torch.rand(17_000_000, 1, 1, device=DEV) < 0.5, -1.0, 1.0))
+    out = torch.full_like(G, 7.0)
+    r3.orthogonalize(G, out, steps=2)
+    want, tol = ref.orthogonalize(np.ones((1, 1)), steps=2)
+    # (1e-7 of 0.5 and more, by the steepest slope of two steps)
+    assert ((out * G.sign() - float(want[0, 0])).abs() <= tol + 2e-7 * 12).all()
+
+
 def test_what_one_step_alone_has_room_for():
     # two of these steps in one would need a matrix beyond the range of what products are made of
     G = _gradient(90, 300, 700, "f32", kind="flat")
