@@ -620,7 +620,48 @@ struct Balance {
     double *tot;               // groups that hold tokens, tokens
 };
 
-// The record's counts in each segment of piece p.  Ids that lie one behind the other are read 16 bytes at a time.
+// The record's counts of tokens b .. e - 1, to `to`.  Ids that lie one behind the other are read 16 bytes at a time.  COPIES: lanes that meet
+// in an expert have up to eight histograms, their counts of it in different banks, in kMaxE counts (a work-group's 240000 slots of 128 experts
+// 54 | 38 us a call, 32000 of 8 20 | 14; 4000 or 8000 of a piece's 0.5 longer, so pieces have one).
+template <int NT, bool COPIES, typename IdxT> __device__ __forceinline__ void balance_count(const Balance &a, int64_t b, int64_t e, int *hist, int32_t *to, bool &bad) {
+    const int copies = !COPIES ? 1 : a.E < kMaxE / 8 ? 8 : a.E < kMaxE / 4 ? 4 : a.E < kMaxE / 2 ? 2 : 1, apart = copies > 1 ? a.E + 1 : a.E;
+    for (int i = threadIdx.x; i < copies * apart; i += NT) hist[i] = 0;
+    __syncthreads();
+    int *mine = hist + (threadIdx.x & (copies - 1)) * apart;
+    const IdxT *idx = (const IdxT *)a.idx + b * a.stride;
+    const int n = b < e ? (int)(e - b) * a.K : 0;
+    auto one = [&](int id) {
+        if (id < a.E) atomicAdd(&mine[id], 1);
+        else bad = true;
+    };
+    if (a.stride == a.K) {
+        constexpr int kVec = 16 / (int)sizeof(IdxT);
+        const int head = (int)lesser(n, ((16 - (int)((uintptr_t)idx & 15)) & 15) / (int)sizeof(IdxT)), vecs = (n - head) / kVec;
+        for (int i = threadIdx.x; i < vecs; i += NT) {
+            const uint4 v = ((const uint4 *)(idx + head))[i];
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int u = 0; u < kVec; ++u) one((int)((w[u * (int)sizeof(IdxT) / 4] >> (8 * (int)sizeof(IdxT) * u % 32)) & ((1u << 8 * sizeof(IdxT)) - 1)));
+        }
+        const int rest = n - vecs * kVec;     // in front and behind
+        for (int i = threadIdx.x; i < rest; i += NT) one(idx[i < head ? i : i + vecs * kVec]);
+    } else {
+        for (int i = threadIdx.x; i < n; i += NT) {
+            const int t = i / a.K;
+            one(idx[(int64_t)t * a.stride + (i - t * a.K)]);
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.E; i += NT) {
+        int n = hist[i];
+        for (int k = 1; k < copies; ++k) n += hist[k * apart + i];
+        to[i] = n;
+    }
+}
+__device__ __forceinline__ void balance_report(const Balance &a, bool bad) {
+    if (a.status && bad) atomicOr(a.status, R3_DATA_IDX_RANGE);
+}
+// in each segment of piece p
 template <int NT, typename IdxT> __device__ void balance_counts(const Balance &a, int p, int *hist) {
     const int64_t lo = (int64_t)p * a.piece0, hi = lesser(lo + a.piece0, a.T);
     bool bad = false;
@@ -630,37 +671,11 @@ template <int NT, typename IdxT> __device__ void balance_counts(const Balance &a
         for (int q = q0; q <= q1; ++q) {
             const int64_t b = larger(lo, a.q.first(q)), e = lesser(hi, a.q.first(q + 1));
             if (b >= e) continue;
-            for (int i = threadIdx.x; i < a.E; i += NT) hist[i] = 0;
-            __syncthreads();
-            const IdxT *idx = (const IdxT *)a.idx + b * a.stride;
-            const int n = (int)(e - b) * a.K;
-            auto one = [&](int id) {
-                if (id < a.E) atomicAdd(&hist[id], 1);
-                else bad = true;
-            };
-            if (a.stride == a.K) {
-                constexpr int kVec = 16 / (int)sizeof(IdxT);
-                const int head = (int)lesser(n, ((16 - (int)((uintptr_t)idx & 15)) & 15) / (int)sizeof(IdxT)), vecs = (n - head) / kVec;
-                for (int i = threadIdx.x; i < vecs; i += NT) {
-                    const uint4 v = ((const uint4 *)(idx + head))[i];
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int u = 0; u < kVec; ++u) one((int)((w[u * (int)sizeof(IdxT) / 4] >> (8 * (int)sizeof(IdxT) * u % 32)) & ((1u << 8 * sizeof(IdxT)) - 1)));
-                }
-                const int rest = n - vecs * kVec;     // in front and behind
-                for (int i = threadIdx.x; i < rest; i += NT) one(idx[i < head ? i : i + vecs * kVec]);
-            } else {
-                for (int i = threadIdx.x; i < n; i += NT) {
-                    const int t = i / a.K;
-                    one(idx[(int64_t)t * a.stride + (i - t * a.K)]);
-                }
-            }
-            __syncthreads();
-            for (int i = threadIdx.x; i < a.E; i += NT) a.hist[(int64_t)(p + q) * a.E + i] = hist[i];
+            balance_count<NT, false, IdxT>(a, b, e, hist, a.hist + (int64_t)(p + q) * a.E, bad);
             __syncthreads();
         }
     }
-    if (a.status && bad) atomicOr(a.status, R3_DATA_IDX_RANGE);
+    balance_report(a, bad);
 }
 // groups and tokens, by one work-group
 template <int NT> __device__ void balance_totals(const Balance &a, double *room) {
@@ -678,6 +693,17 @@ template <typename IdxT> __global__ void __launch_bounds__(1024) balance_counts_
     __shared__ double room[1024 / kWave];
     balance_counts<1024, IdxT>(a, blockIdx.x, hist);
     if (blockIdx.x == 0) balance_totals<1024>(a, room);
+}
+
+// A work-group to a group, and nothing to join, where even one that holds all tokens is gone through soon enough.
+template <typename IdxT> __global__ void __launch_bounds__(1024) balance_whole_kernel(Balance a) {
+    __shared__ int hist[kMaxE];
+    __shared__ double room[1024 / kWave];
+    const int q = blockIdx.x;
+    bool bad = false;
+    balance_count<1024, true, IdxT>(a, a.q.first(q), a.q.first(q + 1), hist, a.counts + (int64_t)q * a.E, bad);
+    balance_report(a, bad);
+    if (q == 0) balance_totals<1024>(a, room);
 }
 
 // A group's counts of 16 experts, 16 threads to each, segments in turn and then the 16 sums in their order
@@ -922,6 +948,13 @@ template <typename IdxT, int L> __global__ void __launch_bounds__(kThreads) bala
 // One work-group up to 16 K logits of few groups.
 bool balance_small(int64_t T, int E, int nseq) { return E <= kSmallE && T * E <= 16384 && T <= 512 && nseq * E <= 1024; }
 
+// A work-group to a group saves the join of pieces: up to 32768 slots of one, 65536 of two, and 262144 of 32 and more, which seldom are one's (us
+// a call, pieces | whole: 4000 x 128, 8 slots 16.3 | 16.0, 1000 14.3 | 12.3; two groups of 8000 20.5 | 18.6, all in one 19.5 | 19.1; 64 of 32000
+// 31 | 24, all in one 28 | 42; 300 of 32000 x 64, 6 slots 34 | 22).
+bool balance_whole(int64_t T, int K, int nseq) {
+    return nseq <= 4096 && T * K <= 32768 * (int64_t)(nseq >= 32 ? 8 : std::min(nseq, 2));
+}
+
 struct BalancePlan {
     int piece0, npieces0, piece, npieces;
     size_t hist, psum, lsum, tot, counts, total;
@@ -985,10 +1018,15 @@ hipError_t launch_balance_loss(int T, int E, int K, const float *logits, int64_t
         else go(std::integral_constant<int, 64>{});
         return hipGetLastError();
     }
-    if (u8) balance_counts_kernel<uint8_t><<<p.npieces0, 1024, 0, s>>>(a);
-    else balance_counts_kernel<uint16_t><<<p.npieces0, 1024, 0, s>>>(a);
     const int64_t items = (int64_t)nseq * ((E + kColumns - 1) / kColumns), most = 1 << 20;
-    balance_join_kernel<<<(unsigned)std::min(items, most), kThreads, 0, s>>>(a);
+    if (balance_whole(T, K, nseq)) {
+        if (u8) balance_whole_kernel<uint8_t><<<nseq, 1024, 0, s>>>(a);
+        else balance_whole_kernel<uint16_t><<<nseq, 1024, 0, s>>>(a);
+    } else {
+        if (u8) balance_counts_kernel<uint8_t><<<p.npieces0, 1024, 0, s>>>(a);
+        else balance_counts_kernel<uint16_t><<<p.npieces0, 1024, 0, s>>>(a);
+        balance_join_kernel<<<(unsigned)std::min(items, most), kThreads, 0, s>>>(a);
+    }
     auto go = [&](auto l, auto v) { balance_tokens_kernel<decltype(l)::value, decltype(v)::value><<<p.npieces, kThreads, 0, s>>>(a); };
     typedef std::integral_constant<int, 64> wave;
     if (vecs <= 16) lanes([&](auto l) { go(l, std::integral_constant<int, 1>{}); });

@@ -245,6 +245,22 @@ def test_balance_loss(T, E, K, kind):
         assert torch.equal(alone["stats"], got["stats"]) and (k is None or torch.equal(alone[k], got[k])), k
 
 
+# on both sides of what a work-group to a group has the slots of, with as many histograms as an expert number leaves room for
+@pytest.mark.parametrize("T,E,K,kind", [(4096, 128, 8, "one"), (4097, 128, 8, "one"), (9000, 128, 8, "inside"), (9000, 511, 8, "empty"), (8000, 512, 8, "few"),
+                                        (16384, 8, 2, "none"), (16385, 8, 2, "none"), (520, 1023, 64, "none"), (500, 1024, 64, "inside"), (520, 2047, 64, "none"),
+                                        (500, 2048, 60, "many"), (700, 4096, 64, "empty"), (400, 4096, 64, "none"), (32768, 60, 8, "many"), (32769, 60, 8, "many")])
+def test_balance_loss_whole_groups_and_pieces(T, E, K, kind):
+    starts = _starts(kind, T)
+    z, idx = _routing(T, E, K)
+    got, status = _run_balance(z, idx, starts, stride=K + T % 2, balance_coef=0.3, z_coef=0.02)
+    assert status == 0
+    _check_balance(z, idx, starts, got, 0.3, 0.02)
+    idx[T // 2, 0] = E if E != 4096 else 5000
+    bad, status = _run_balance(z, idx, starts, balance_coef=0.3, z_coef=0.02)
+    got["counts"][torch.arange(len(got["counts"]), device=DEV)] -= bad["counts"]
+    assert status == r3.DATA_IDX_RANGE and got["counts"].sum().item() in (0, 1) and got["counts"].min().item() >= 0
+
+
 @pytest.mark.parametrize("kind,T", [("none", 70001), ("few", 30007), ("singles", 5000), ("many", 9001)])
 def test_balance_loss_over_many_pieces(kind, T):
     starts = _starts(kind, T)
