@@ -101,7 +101,7 @@ hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int d
 struct NarrowCall {
     int64_t batch;
     int s, l, steps, norms;
-    bool transposed;
+    bool transposed, pairs;      // pairs: there is room for two steps as one, where ortho_together says so
     const void *G;
     void *O, *ws;
     const double *norm;
@@ -112,6 +112,8 @@ struct NarrowCall {
 constexpr int kNarrowSide = 128;
 size_t ortho_narrow_ws_bytes(int64_t batch, int64_t s, int64_t l);
 hipError_t launch_ortho_narrow(const NarrowCall &c, int dtype_in, int dtype_out, hipStream_t s);
+// whether `step` and the next are taken together: at the start alone, or wherever two are left
+inline bool ortho_together(int step, int steps, bool all) { return all ? steps - step >= 2 : step == 0 && steps >= 3; }
 // what of step k's polynomial a + b A + c A A is taken out of the matrix and applied to X itself
 inline double ortho_apart(int k, int steps, const float *q) { return k >= steps - 2 ? (double)q[0] + q[1] + q[2] : (double)q[0]; }
 

@@ -896,38 +896,51 @@ Plan plan(int64_t batch, int64_t rows, int64_t cols, int dtype_out) {
 // no exactness: later a rounding of X enters the second product times a^2.  (Relative error beside the result's rounding, five steps,
 // random 256 x 768 / falling singular values / rank 3: apart 1.0e-3 / 7e-4 / 2.5e-3, the first two together the same, the first two pairs
 // 1.2e-3 / 1.6e-3 / 9e-3.)
-bool two_together(int step, int steps, bool split, bool pairs) {
-    return pairs && (split ? steps - step >= 2 : step == 0 && steps >= 3);
-}
+bool two_together(int step, int steps, bool all, bool pairs) { return pairs && ortho_together(step, steps, all); }
 
 // Whether every element stays in (-15, 15), so that times kUnit it is an f16: a matrix's are at most its largest singular value, that of X
 // at most 1 at the start and then what the quintic makes of it.  At equidistant points: between two of 2 n over (-r, r) a polynomial of
-// degree d is at most d^2 (d^2 - 1) / 24 n^2 of its maximum beyond them, 0.1 % at degree 6 and 256 points, 1.4 % at degree 24 (two steps)
-// and 1024.
-bool in_range(int steps, const float *q, bool split, bool pairs) {
-    const double a = q[0], b = q[1], c = q[2], room = pairs ? 1.03 : 1.01;    // for roundings and what lies between the points
-    const int points = pairs ? 1024 : 256;
+// degree d is at most d^2 (d^2 - 1) / 24 n^2 of its maximum beyond them, 1.3 % at degree 6 and 64 points, 21 % at degree 24 (two steps) and 256.
+bool in_range(int steps, const float *q, bool all, bool pairs) {
+    const double a = q[0], b = q[1], c = q[2];
+    // the largest of |values| (that are finite: |q| is below 2^128)
+    auto more = [](double v, double &most) {
+        v = v < 0.0 ? -v : v;
+        most = v > most ? v : most;
+    };
     double r = 1.0;
     for (int k = 0; k < steps;) {
-        const bool two = two_together(k, steps, split, pairs);
+        const bool two = two_together(k, steps, all, pairs);
+        const double out = ortho_apart(k, steps, q) * (two ? ortho_apart(k + 1, steps, q) : 1.0);
         double most = 0.0, next = 0.0;
-        for (int i = 0; i <= points; ++i) {
-            const double x = r * i / points, y = x * x, P = a + y * (b + y * c);
-            double all[6] = {x, y, P - a, 0.0, 0.0, 0.0}, to = x * P;
-            if (two) {
-                const double y1 = to * to, P1 = a + y1 * (b + y1 * c);
-                all[3] = P * y;
-                all[4] = y1;
-                all[5] = P1 - a;
-                all[2] = std::fmax(std::fabs(all[2]), std::fabs(P * P1 - ortho_apart(k, steps, q) * ortho_apart(k + 1, steps, q)));
-                to *= P1;
-            } else all[2] = P - ortho_apart(k, steps, q);
-            for (double v : all) most = std::fmax(most, std::fabs(v));
-            most = std::fmax(most, std::fabs(ortho_apart(k, steps, q) * (two ? ortho_apart(k + 1, steps, q) : 1.0)));
-            next = std::fmax(next, std::fabs(to));
+        for (int i = 0; i <= 64; ++i) {
+            const double x = r * i / 64, y = x * x, P = a + y * (b + y * c);
+            more(x, most);
+            more(y, most);
+            more(two ? P - a : P - out, most);
+            more(x * P, next);
         }
-        if (!(most * room < 15.0 && next * room < 15.0)) return false;
-        r = next * (pairs ? 1.015 : 1.001);
+        most *= 1.02;
+        next *= 1.02;
+        if (two) {
+            double pair = 0.0, last = 0.0;
+            for (int i = 0; i <= 256; ++i) {
+                const double x = r * i / 256, y = x * x, P = a + y * (b + y * c), y1 = x * P * (x * P), P1 = a + y1 * (b + y1 * c);
+                more(P * y, pair);
+                more(y1, pair);
+                more(P1 - a, pair);
+                more(P * P1 - out, pair);
+            }
+            for (int i = 0; i <= 64; ++i) {
+                const double x = next * i / 64, y = x * x;
+                more(x * (a + y * (b + y * c)), last);
+            }
+            more(pair * 1.25, most);
+            next = last * 1.02;
+        }
+        more(out, most);
+        if (!(most < 15.0 && next < 15.0)) return false;
+        r = next;
         k += two ? 2 : 1;
     }
     return true;
@@ -1062,6 +1075,7 @@ hipError_t launch_orthogonalize(int64_t batch, int64_t rows, int64_t cols, int d
         NarrowCall c = {};
         c.batch = batch; c.s = p.s; c.l = p.l; c.steps = steps; c.norms = p.parts;
         c.transposed = rows > cols;
+        c.pairs = in_range(steps, coef, dtype_out == R3_BF16, true);
         c.G = G; c.O = out; c.ws = base + p.X;
         c.norm = part;
         c.coef = coef;

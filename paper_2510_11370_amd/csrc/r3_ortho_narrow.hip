@@ -4,10 +4,15 @@
 // A work-group has a run of a matrix's slabs.  A step of it: A, then B = b A + c A A + .. into LDS; of each slab X' = a X + B X, and at
 // once X' X'^T added to its part of the next step's A, in registers.  So a step is one launch that reads and writes X once, and another
 // that joins the parts where there are more than a few; as products over tiles it was five, each of which waited for the one before (1 x
-// 2048 x 128 f32: 27 launches, 128 us | 12, 76 us; 256 x 128 x 1024: 878 | 424).  Where a work-group has a whole matrix, B is the smaller
-// part of its work; where work-groups share one, each makes B for itself, which costs as much as a slab and a half. Bound by latencies
-// where matrices are few (a step of one slab is 11 us, some 2 of them products), by memory where they are many (256 x 128 x 1024: 72 us a
-// step, 268 MB, 3.7 TB/s; matrix pipes 39 % busy).
+// 2048 x 128 f32: 27 launches, 128 us | 10, 75 us; 256 x 128 x 1024: 878 | 353).  Where a work-group has a whole matrix, B is the smaller
+// part of its work; where work-groups share one, each makes B for itself, which costs as much as a slab and a half.
+//
+// Two steps as one (r3_ortho.hip) are four products more of matrices that are in LDS, 12 us, for a pass over X and a join less: everywhere
+// for bf16 results (1 x 64 x 2048 54 -> 41 us, 128 x 100 x 700 211 -> 154); for f32 ones at the start alone (256 x 128 x 1024 411 -> 353),
+// as later pairs cost exactness (1 x 2048 x 128: 5.1e-6 of the result instead of 1.1e-6; f32 products 1.5e-6).
+//
+// Bound by latencies where matrices are few (a step of one slab is 10 us, some 2 of them products), by memory where they are many (256 x
+// 128 x 1024: 72 us a step, 268 MB, 3.7 TB/s; matrix pipes 39 % busy).
 //
 // X, A and B are pairs of f16 times 2^12 for results of either type: products are hi hi, hi lo, lo hi.  These matrices have few directions
 // in which an error could be lost (3 x 5, f16 operands: 6e-3 of the norm at worst), and the two products more hide behind the rest.
@@ -39,7 +44,8 @@ struct Narrow {
     int norms;                           // of a matrix: parts of |G|^2
     const double *norm;
     double eps;
-    float apart, rest, b, c, out;        // X' = apart X + (rest I + b A + c A A) X
+    bool two;                            // two steps: X'' = apart X + (rest I + a B + a B' + B' B) X, B' = b A' + c A' A', A' = (a + B) (a + B) A
+    float apart, rest, a, b, c, out;     // X' = apart X + (rest I + B) X, B = b A + c A A
     int32_t *status;
 };
 
@@ -48,7 +54,8 @@ template <int SP> struct Shape {
     static constexpr int kPlane = SP * kSlab * 2, kBytes = 2 * kPlane;           // hi or lo of a slab, both
     static constexpr int kPitch = SP * 2 + 16;                                   // bytes of a row of A or B
     static constexpr int kMatrix = SP * kPitch;                                  // hi or lo of it
-    static constexpr int kLds = 2 * kMatrix + 2 * kBytes;
+    static constexpr int kRoom = 2 * kBytes < 2 * kMatrix ? 2 * kMatrix : 2 * kBytes;     // two slabs, or before them a second matrix
+    static constexpr int kLds = 2 * kMatrix + kRoom;
     static constexpr int kGP = SP == 128 ? 4 : 2, kGQ = 2;                       // 16 x 16 tiles of a wave, of A: 64 x 32 or 32 x 32
     static constexpr int64_t kSums = SP * SP;
 };
@@ -120,7 +127,7 @@ template <int SP, int MODE, typename T> __global__ void __launch_bounds__(Shape<
     typedef Shape<SP> H;
     constexpr int NT = H::kThreads, kP = H::kGP, kQ = H::kGQ;
     extern __shared__ __align__(1024) char lds[];
-    char *const M = lds, *const S = lds + 2 * H::kMatrix;     // A or B; two slabs
+    char *const M = lds, *const S = lds + 2 * H::kMatrix;     // A, and what comes of it; two slabs
     const int64_t m = blockIdx.x / o.pieces, elems = (int64_t)o.s * o.l;
     const int piece = (int)(blockIdx.x - m * o.pieces);
     const int j0 = (int)((int64_t)o.slabs * piece / o.pieces), j1 = (int)((int64_t)o.slabs * (piece + 1) / o.pieces);
@@ -209,8 +216,7 @@ template <int SP, int MODE, typename T> __global__ void __launch_bounds__(Shape<
             store(j, slab);
         }
     } else {
-        load(j0, S + (j0 & 1) * H::kBytes);
-        // A
+        if (!o.two) load(j0, S + (j0 & 1) * H::kBytes);
 #pragma unroll
         for (int i = 0; i < kP; ++i)
 #pragma unroll
@@ -220,51 +226,81 @@ template <int SP, int MODE, typename T> __global__ void __launch_bounds__(Shape<
             for (int i = 0; i < kP; ++i)
 #pragma unroll
                 for (int j = 0; j < kQ; ++j) A[i][j] += *(const f32x4_t *)(o.A + sums_of(m * o.parts + k, i, j));
+        // a matrix to LDS; everybody has read what was there
+        auto put = [&](char *to, const f32x4_t (&v)[kP][kQ]) {
+#pragma unroll
+            for (int i = 0; i < kP; ++i)
+#pragma unroll
+                for (int j = 0; j < kQ; ++j) {
+                    float x[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) x[u] = v[i][j][u];
+                    put_pair(to + (gq + 16 * j + r) * H::kPitch + (gp + 16 * i + c4) * 2, H::kMatrix, x);
+                }
+        };
+        // v = x v + y P Q, of matrices in LDS that commute; everybody meets
+        auto product = [&](f32x4_t (&v)[kP][kQ], float x, float y, const char *P, const char *Q) {
+            f32x4_t large[kP][kQ], small[kP][kQ];
+#pragma unroll
+            for (int i = 0; i < kP; ++i)
+#pragma unroll
+                for (int j = 0; j < kQ; ++j) large[i][j] = small[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            __syncthreads();
+#pragma unroll
+            for (int kk = 0; kk < SP / 32; ++kk) {
+                bf16x8_t p[kP][2], q[kQ][2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int i = 0; i < kP; ++i) p[i][h] = row_frag<H::kPitch>(P + h * H::kMatrix, gp + 16 * i, kk);
+#pragma unroll
+                    for (int j = 0; j < kQ; ++j) q[j][h] = row_frag<H::kPitch>(Q + h * H::kMatrix, gq + 16 * j, kk);
+                }
+#pragma unroll
+                for (int j = 0; j < kQ; ++j)
+#pragma unroll
+                    for (int i = 0; i < kP; ++i) pair_mfma(large[i][j], small[i][j], p[i], q[j]);
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kP; ++i)
+#pragma unroll
+                for (int j = 0; j < kQ; ++j) {
+                    const f32x4_t s = (large[i][j] + small[i][j]) * (y * (1.0f / kUnit));
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) v[i][j][u] = fmaf(x, v[i][j][u], s[u]);
+                }
+        };
+        put(M, A);
+        if (o.two) {
+            f32x4_t B[kP][kQ];
+#pragma unroll
+            for (int i = 0; i < kP; ++i)
+#pragma unroll
+                for (int j = 0; j < kQ; ++j) B[i][j] = A[i][j];
+            product(B, o.b, o.c, M, M);       // B
+            put(S, B);
+            product(A, o.a, 1.0f, M, S);      // (a + B) A
+            put(M, A);
+            product(A, o.a, 1.0f, M, S);      // A'
+            put(M, A);
+            product(A, o.b, o.c, M, M);       // B'
+            put(M, A);
+#pragma unroll
+            for (int i = 0; i < kP; ++i)
+#pragma unroll
+                for (int j = 0; j < kQ; ++j) A[i][j] += B[i][j];
+            product(A, o.a, 1.0f, M, S);
+            load(j0, S + (j0 & 1) * H::kBytes);
+        } else product(A, o.b, o.c, M, M);
 #pragma unroll
         for (int i = 0; i < kP; ++i)
-#pragma unroll
-            for (int j = 0; j < kQ; ++j) {
-                float v[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = A[i][j][u];
-                put_pair(M + (gq + 16 * j + r) * H::kPitch + (gp + 16 * i + c4) * 2, H::kMatrix, v);
-            }
-        __syncthreads();
-        // B in its place
-        f32x4_t B[kP][kQ], Bs[kP][kQ];
-#pragma unroll
-        for (int i = 0; i < kP; ++i)
-#pragma unroll
-            for (int j = 0; j < kQ; ++j) B[i][j] = Bs[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int kk = 0; kk < SP / 32; ++kk) {
-            bf16x8_t p[kP][2], q[kQ][2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int i = 0; i < kP; ++i) p[i][h] = row_frag<H::kPitch>(M + h * H::kMatrix, gp + 16 * i, kk);
-#pragma unroll
-                for (int j = 0; j < kQ; ++j) q[j][h] = row_frag<H::kPitch>(M + h * H::kMatrix, gq + 16 * j, kk);
-            }
 #pragma unroll
             for (int j = 0; j < kQ; ++j)
 #pragma unroll
-                for (int i = 0; i < kP; ++i) pair_mfma(B[i][j], Bs[i][j], p[i], q[j]);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kP; ++i)
-#pragma unroll
-            for (int j = 0; j < kQ; ++j) {
-                float v[4];
-                const int row = gq + 16 * j + r;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    v[u] = fmaf(o.c, (B[i][j][u] + Bs[i][j][u]) * (1.0f / kUnit), o.b * A[i][j][u]);
-                    if (row == gp + 16 * i + c4 + u && row < o.s) v[u] += o.rest * kUnit;
-                }
-                put_pair(M + row * H::kPitch + (gp + 16 * i + c4) * 2, H::kMatrix, v);
-            }
+                for (int u = 0; u < 4; ++u)
+                    if (gq + 16 * j + r == gp + 16 * i + c4 + u && gq + 16 * j + r < o.s) A[i][j][u] += o.rest * kUnit;
+        put(M, A);
         if constexpr (MODE == kStep) clear();
         DownFrag down[2];
         down[0].init(xp);
@@ -408,7 +444,7 @@ template <int SP, typename IN, typename OUT> hipError_t run(const NarrowCall &c,
     o.eps = c.eps;
     o.out = c.scale / kUnit;
     o.status = c.status;
-    const float a = c.coef[0];
+    o.a = c.coef[0];
     o.b = c.coef[1];
     o.c = c.coef[2];
     hipError_t e = hipSuccess;
@@ -427,7 +463,12 @@ template <int SP, typename IN, typename OUT> hipError_t run(const NarrowCall &c,
         // `now`: the work-groups' sums; with many of them `other` is what they are joined into
         o.A_to = now;
         go(ortho_narrow_kernel<SP, kStart, IN>);
-        for (int k = 0; k < c.steps && e == hipSuccess; ++k) {
+        for (int k = 0; k < c.steps && e == hipSuccess;) {
+            o.two = c.pairs && ortho_together(k, c.steps, std::is_same<OUT, bf16_t>::value);
+            const double apart = ortho_apart(k, c.steps, c.coef) * (o.two ? ortho_apart(k + 1, c.steps, c.coef) : 1.0);
+            o.apart = (float)apart;
+            o.rest = (float)((double)o.a * (o.two ? o.a : 1.0) - apart);
+            k += o.two ? 2 : 1;
             o.parts = p.pieces;
             o.A = now;
             if (p.pieces > kFew) {
@@ -437,9 +478,7 @@ template <int SP, typename IN, typename OUT> hipError_t run(const NarrowCall &c,
                 o.A = other;
             } else std::swap(now, other);
             o.A_to = now;
-            o.apart = (float)ortho_apart(k, c.steps, c.coef);
-            o.rest = (float)((double)a - ortho_apart(k, c.steps, c.coef));
-            if (k + 1 < c.steps) go(ortho_narrow_kernel<SP, kStep, float>);
+            if (k < c.steps) go(ortho_narrow_kernel<SP, kStep, float>);
             else go(ortho_narrow_kernel<SP, kLast, OUT>);
         }
         if (e != hipSuccess) return e;
