@@ -597,7 +597,7 @@ namespace {
 //   ds_te = alpha / (groups N) p_te (f_e - sum_i f_i p_ti) + 2 zeta / tokens lse_t p_te
 // The counts come from the record alone, a byte or two to a slot, so they are made first and the logits are read once: a token's
 // probabilities give its part of the loss and its gradient at once.  HBM-bound where it counts: 65536 x 128 counts 4, join 3, tokens 16 us
-// (67 MB at 4.2 TB/s), finish 4; 131072 x 128 in 64 sequences 8 + 4 + 31 + 4; 3001 x 384 in 7 6 + 3 + 14 + 4, latencies.
+// (67 MB at 4.2 TB/s), finish 4; 131072 x 128 in 64 sequences 8 + 4 + 31 + 4; 3001 x 384 in 7 4 + 13 + 3, latencies.
 // ---------------------------------------------------------------------------------------------------------------------------------
 
 struct Balance {
