@@ -105,7 +105,8 @@ def _calls():
         o = dict(stats=f32(3), counts=torch.empty(nseq, E, dtype=torch.int32, device=DEV), probs=f32(nseq, E), dlogits=f32(T, E))
         ws = r3.balance_loss_workspace(L, nseq)
         out.append((lambda L=L, z=z, idx=idx, o=o, ws=ws, starts=starts: r3.balance_loss(L, z, idx, seq_start=starts, z_coef=0.01, ws=ws, **o), o))
-    for b, r, c, to in ((2, 100, 300, torch.float32), (24, 520, 600, torch.bfloat16), (40, 300, 700, torch.float32)):
+    for b, r, c, to in ((2, 100, 300, torch.float32), (24, 520, 600, torch.bfloat16), (40, 300, 700, torch.float32), (3, 900, 128, torch.bfloat16),
+                        (300, 60, 200, torch.bfloat16), (2, 130, 2000, torch.bfloat16)):
         G, o = rand(b, r, c), dict(O=torch.empty(b, r, c, dtype=to, device=DEV))
         ws = r3.orthogonalize_workspace(G, o["O"])
         out.append((lambda G=G, o=o, ws=ws: r3.orthogonalize(G, o["O"], ws=ws), o))
@@ -254,5 +255,17 @@ def test_past_2_to_31_elements():
     out = torch.empty_like(G)
     r3.orthogonalize(G, out)
     assert torch.equal(out[:29], out[-29:]) and torch.equal(out[:29], out[29 * 50:29 * 51])
+    want, tol = ref.orthogonalize(G[-1].double().cpu().numpy(), to="bf16")
+    assert np.linalg.norm(out[-1].double().cpu().numpy() - want) <= tol
+
+
+def test_short_sides_past_2_to_31_elements():
+    n, r, c = 17400, 121, 1030
+    assert n * r * c > 1 << 31
+    g = torch.Generator(device=DEV).manual_seed(2)
+    G = torch.randn(29, r, c, generator=g, device=DEV).bfloat16().repeat(600, 1, 1)
+    out = torch.empty_like(G)
+    r3.orthogonalize(G, out)
+    assert torch.equal(out[:29], out[-29:]) and torch.equal(out[:29], out[29 * 300:29 * 301])
     want, tol = ref.orthogonalize(G[-1].double().cpu().numpy(), to="bf16")
     assert np.linalg.norm(out[-1].double().cpu().numpy() - want) <= tol
