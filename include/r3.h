@@ -401,7 +401,8 @@ int r3_token_logprobs_backward(int64_t n, int64_t V, int dtype, const void *logi
  * weight_cap > 0; they and the coefficients finite, but for weight_cap, which may
  * be infinite.  n = 0 gives stats of 0.  n < 2^31 - 2^16.
  * No output, nor ws, may share bytes with another array.
- * ws: device workspace of r3_policy_loss_workspace_bytes(desc), 256-byte aligned.
+ * ws: device workspace of r3_policy_loss_workspace_bytes(desc), 256-byte aligned;
+ * enough with seq_start and without.
  */
 enum { R3_RATIO_TOKEN = 0, R3_RATIO_SEQUENCE = 1 };
 enum { R3_MEAN_TOKENS = 0, R3_MEAN_SEQUENCES = 1, R3_SUM = 2 };

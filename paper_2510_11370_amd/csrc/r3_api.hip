@@ -1,5 +1,6 @@
 // C ABI of the replayed MoE layer: argument checks, workspace carving and the
 // launch sequence of each call.  See include/r3.h for the contract.
+#include <algorithm>
 #include <atomic>
 #include <cfloat>
 #include <cstdlib>
@@ -574,8 +575,10 @@ static int check_policy(const r3_policy_desc *D) {
     return R3_OK;
 }
 
+// (whether there will be a seq_start is not known here, and either layout may be the larger: one sequence of many pieces has more parts than
+// several that are gone through whole)
 size_t r3_policy_loss_workspace_bytes(const r3_policy_desc *desc) {
-    return check_policy(desc) == R3_OK ? policy_loss_ws_bytes(desc->n, desc->nseq) : 0;
+    return check_policy(desc) == R3_OK ? std::max(policy_loss_ws_bytes(desc->n, desc->nseq), policy_loss_ws_bytes(desc->n, 1)) : 0;
 }
 
 int r3_policy_loss(const r3_policy_desc *desc, const float *logp, const float *logp_old, const float *logp_infer, const float *logp_ref,
@@ -589,9 +592,10 @@ int r3_policy_loss(const r3_policy_desc *desc, const float *logp, const float *l
     const void *words[] = {logp, logp_old, logp_infer, logp_ref, entropy, advantage, target, seq_start, dlogp, dentropy, stats, status_word};
     for (const void *p : words)
         if (!aligned(p, 4)) return R3_ERR_INVALID_ARG;
-    const size_t need = policy_loss_ws_bytes(D.n, D.nseq);
+    const int nseq = seq_start ? D.nseq : 1;
+    const size_t need = policy_loss_ws_bytes(D.n, nseq);
     if (!ws || ws_bytes < need || !aligned(ws, 256)) return R3_ERR_WORKSPACE;
-    const size_t word = (size_t)D.n * 4, seqs = (size_t)(seq_start ? D.nseq : 1) * 4;
+    const size_t word = (size_t)D.n * 4, seqs = (size_t)nseq * 4;
     const Span at[] = {{dlogp, word}, {dentropy, word}, {stats, 32}, {status_word, 4}, {ws, need}, {logp, word}, {logp_old, word}, {logp_infer, word},
                        {logp_ref, word}, {entropy, word}, {advantage, D.flags & R3_FLAG_SEQ_ADVANTAGE ? seqs : word}, {target, word}, {seq_start, seqs + 4}};
     if (any_overlap(at, 5)) return R3_ERR_INVALID_ARG;

@@ -1,0 +1,71 @@
+"""The losses and the orthogonalised update at the edges of what they document: workspaces of the size asked for and no more,
+terms that overflow where they do not count, sequences of every length side by side."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as ref
+from paper_2510_11370_amd import r3
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _near(got, want, tol, what):
+    got = got.cpu().double().numpy()
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (what, np.argwhere(bad)[:3].tolist(), got[bad][:3], want[bad][:3], np.broadcast_to(tol, got.shape)[bad][:3])
+
+
+def _policy(n, seed=0):
+    rng = np.random.default_rng(seed + n)
+    logp = -np.abs(rng.normal(0, 2, n))
+    a = {"logp": logp, "old": logp + rng.normal(0, 0.3, n), "adv": rng.normal(0, 1, n), "ref": logp + rng.normal(0, 0.4, n),
+         "entropy": np.abs(rng.normal(0, 1, n))}
+    a = {k: v.astype(np.float32) for k, v in a.items()}
+    a["target"] = np.where(rng.random(n) < 0.3, -1, 5).astype(np.int32)
+    return a
+
+
+def _run_policy(a, starts=None, nseq=None, ws=None, **kw):
+    """stats, dlogp, dentropy, the status word"""
+    n = len(a["logp"])
+    D = r3.policy_desc(n, nseq or (1 if starts is None else len(starts) - 1), **kw)
+    t = {k: torch.tensor(v, device=DEV) for k, v in a.items()}
+    o = {"stats": torch.full((8,), 77.0, device=DEV), "dlogp": torch.full((n,), 77.0, device=DEV), "dentropy": torch.full((n,), 77.0, device=DEV)}
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    r3.policy_loss(D, t["logp"], t["adv"], o["stats"], logp_old=t.get("old"), logp_infer=t.get("infer"), logp_ref=t.get("ref"),
+                   entropy=t.get("entropy"), target=t.get("target"),
+                   seq_start=None if starts is None else torch.tensor(starts, dtype=torch.int32, device=DEV), dlogp=o["dlogp"],
+                   dentropy=o["dentropy"], status=status, ws=ws if ws is None else ws(D))
+    return o, status.item()
+
+
+def _check_policy(a, starts=None, got=None, **kw):
+    got, status = _run_policy(a, starts, **kw) if got is None else got
+    c = {k: v if v.dtype.kind == "i" else v.astype(np.float64) for k, v in a.items()}
+    want = ref.policy_loss(starts=starts, **c, **kw)
+    for k in got:
+        _near(got[k], want[k], want["tol_" + k], k)
+    assert status == 0
+    return got
+
+
+@pytest.mark.parametrize("n,nseq", [(5000, 16), (65536, 64), (131072, 8), (131072, 213)])
+def test_a_descriptor_of_many_sequences_without_their_starts(n, nseq):
+    a, kw = _policy(n), dict(norm="sequences", kl_coef=0.05)
+    for ratio in ("token", "sequence"):
+        guarded = []
+
+        def ws(D):
+            need = r3.policy_loss_workspace(D).numel()
+            guarded.append((torch.full((need + 65536,), 171, dtype=torch.uint8, device=DEV), need))
+            return guarded[0][0][:need]
+
+        got = _run_policy(a, nseq=nseq, ws=ws, ratio=ratio, **kw)
+        full, need = guarded[0]
+        assert (full[need:] == 171).all()
+        _check_policy(a, got=got, ratio=ratio, **kw)
+        one, _ = _run_policy(a, ratio=ratio, **kw)
+        for k in one:
+            assert torch.equal(got[0][k], one[k]), k
