@@ -210,7 +210,9 @@ __device__ __forceinline__ SeqOut sequence_result(const Policy &a, const SegSum 
         o.up = up ? a.up : r;
         o.down = much ? a.dual : down ? a.down : r;
         o.cut = (up ? 1 : 0) | (down || much ? 2 : 0);
-        o.grad = (float)(-(double)r * ((up ? 0.0 : s.pos) + (down || much ? 0.0 : s.neg)) / (double)s.live);
+        // (nothing that the clip leaves free: no gradient, however large r is)
+        const double free = (up ? 0.0 : s.pos) + (down || much ? 0.0 : s.neg);
+        o.grad = free == 0.0 ? 0.0f : (float)(-(double)r * free / (double)s.live);
     }
     return o;
 }

@@ -69,3 +69,36 @@ def test_a_descriptor_of_many_sequences_without_their_starts(n, nseq):
         one, _ = _run_policy(a, ratio=ratio, **kw)
         for k in one:
             assert torch.equal(got[0][k], one[k]), k
+
+
+# one work-group has all tokens, a work-group to a sequence, pieces, and pieces of more sequences than LDS has places for
+LAYOUTS = [(120, 3), (900, 130), (30000, 12), (140000, 5), (9000, 4500)]
+
+
+def _even(n, nseq):
+    return np.linspace(0, n, nseq + 1).astype(int)
+
+
+@pytest.mark.parametrize("dual", [0.0, 3.0])
+@pytest.mark.parametrize("n,nseq", LAYOUTS)
+def test_clipped_sequences_whose_ratio_overflows(n, nseq, dual):
+    """Where clipping holds every token of a sequence it has no policy gradient, however far the ratio is."""
+    starts, a = _even(n, nseq), _policy(n)
+    del a["ref"], a["entropy"], a["target"]
+    kw = dict(ratio="sequence", norm="sequences", dual_clip=dual)
+    for q in (0, nseq - 1):
+        b, e = starts[q], starts[q + 1]
+        a["old"][b:e] = a["logp"][b:e] - np.float32(100)          # e^100 is beyond 32 bits
+        a["adv"][b:e] = np.abs(a["adv"][b:e]) * (1 if dual == 0 else np.where(np.arange(e - b) % 2, 1, -1))
+    got = _check_policy(a, starts, **kw)
+    held = np.zeros(n, dtype=bool)
+    held[:starts[1]] = held[starts[-2]:] = True
+    assert (got["dlogp"].cpu().numpy()[held] == 0).all()
+    # a token that the rollout's weights could not have drawn: the sequence's mean is infinite
+    a["old"][0] = -np.inf
+    far, status = _run_policy(a, starts, **kw)
+    assert status == 0 and all(torch.equal(far[k], got[k]) for k in got)
+    # held on one side alone: what is not held is told
+    if dual == 0:
+        a["adv"][starts[1] - 1] = -1.0
+        assert _run_policy(a, starts, **kw)[1] == r3.DATA_NONFINITE
