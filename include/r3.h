@@ -389,8 +389,9 @@ int r3_token_logprobs_backward(int64_t n, int64_t V, int dtype, const void *logi
  *       (sequences with live tokens * the sequence's live tokens)
  *       (R3_MEAN_SEQUENCES), scale (R3_SUM)
  *   dlogp = nu (-w A r [used = r] + kl_coef (1 - exp(q))); R3_RATIO_SEQUENCE: the
- *       first part is the mean over the sequence's live tokens; where clipping
- *       holds a token it has no part.   dentropy = -entropy_coef nu
+ *       first part is the mean over the sequence's live tokens.  A token that
+ *       clipping holds, or whose A is 0, adds nothing to it.
+ *   dentropy = -entropy_coef nu
  * Borders are compared in 64 bits.  Tokens that are not live get 0.
  * stats [8] f32: loss, sum nu (-w used A), sum nu k / scale, sum nu entropy /
  * scale, share of live tokens that clipping holds, mean w, live tokens, sequences

@@ -173,7 +173,7 @@ __device__ __forceinline__ SegSum segment_part(const Policy &a, int q, int64_t b
             const float wA = weight(a, k[u]) * k[u].A;
             if (k[u].A > 0.0f) s.pos += wA;
             else if (k[u].A < 0.0f) s.neg += wA;
-            else s.pos += wA * 0.0f;   // (a NaN stays one)
+            else if (k[u].A != 0.0f) s.pos += k[u].A;   // (a NaN; without an advantage the weight does not matter)
         }
     }
     return s;

@@ -102,3 +102,22 @@ def test_clipped_sequences_whose_ratio_overflows(n, nseq, dual):
     if dual == 0:
         a["adv"][starts[1] - 1] = -1.0
         assert _run_policy(a, starts, **kw)[1] == r3.DATA_NONFINITE
+
+
+@pytest.mark.parametrize("ratio", ["token", "sequence"])
+@pytest.mark.parametrize("n,nseq", LAYOUTS)
+def test_a_weight_that_overflows_where_the_advantage_is_zero(n, nseq, ratio):
+    starts, a = _even(n, nseq), _policy(n)
+    del a["target"]
+    a["infer"] = a["old"].copy()
+    at = [1, n // 2, n - 1]
+    a["adv"][at] = 0.0
+    kw = dict(ratio=ratio, norm="sequences", kl_coef=0.05, entropy_coef=0.01)
+    clean = _check_policy(a, starts, **kw)
+    for far in (-np.inf, -1e4):
+        a["infer"][at] = far
+        got, status = _run_policy(a, starts, **kw)
+        assert status == 0 and torch.isinf(got["stats"][5])
+        keep = torch.arange(8, device=DEV) != 5
+        assert torch.equal(got["stats"][keep], clean["stats"][keep])
+        assert torch.equal(got["dlogp"], clean["dlogp"]) and torch.equal(got["dentropy"], clean["dentropy"])
