@@ -140,6 +140,11 @@ __device__ __forceinline__ float weight(const Policy &a, const Token &k) {
     return a.infer ? __builtin_elementwise_minimum(expf(k.old - k.infer), a.cap) : 1.0f;   // (a NaN stays one)
 }
 
+// (without logp_old an infinite logp has d = 0, too; a NaN stays one)
+__device__ __forceinline__ double log_ratio(const Policy &a, const Token &k) {
+    return a.old || !isinf(k.x) ? (double)k.x - (double)k.old : 0.0;
+}
+
 // f(q, begin, end, all) for every segment of [lo, hi) of sequences q0 .. q1: all NT threads to each of a few, a wave to each of many
 template <int NT, class F> __device__ __forceinline__ void for_segments(const Seqs &s, int64_t lo, int64_t hi, int q0, int q1, F f) {
     const bool few = q1 - q0 < 4;
@@ -169,7 +174,7 @@ __device__ __forceinline__ SegSum segment_part(const Policy &a, int q, int64_t b
             if (!k[u].live) continue;
             ++s.live;
             if (!a.seq_ratio) continue;
-            s.d += (double)k[u].x - (double)k[u].old;
+            s.d += log_ratio(a, k[u]);
             const float wA = weight(a, k[u]) * k[u].A;
             if (k[u].A > 0.0f) s.pos += wA;
             else if (k[u].A < 0.0f) s.neg += wA;
@@ -337,7 +342,7 @@ struct PolicyPart {
                 cut = A > 0.0f ? s.cut & 1 : A < 0.0f ? s.cut & 2 : false;
                 g = s.grad;
             } else {
-                const double d = (double)k.x - (double)k.old;
+                const double d = log_ratio(a, k);
                 const float r = expf((float)d);
                 const bool up = d > a.log_up, down = d < a.log_down, over = d > a.log_dual;
                 used = A > 0.0f ? (up ? a.up : r) : over ? a.dual : down ? a.down : r;

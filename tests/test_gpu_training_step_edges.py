@@ -121,3 +121,18 @@ def test_a_weight_that_overflows_where_the_advantage_is_zero(n, nseq, ratio):
         keep = torch.arange(8, device=DEV) != 5
         assert torch.equal(got["stats"][keep], clean["stats"][keep])
         assert torch.equal(got["dlogp"], clean["dlogp"]) and torch.equal(got["dentropy"], clean["dentropy"])
+
+
+@pytest.mark.parametrize("ratio", ["token", "sequence"])
+@pytest.mark.parametrize("n,nseq", LAYOUTS)
+def test_on_the_policy_the_ratio_is_one_whatever_the_log_probability_is(n, nseq, ratio):
+    starts, a = _even(n, nseq), _policy(n)
+    a = {k: a[k] for k in ("logp", "adv", "target")}
+    kw = dict(ratio=ratio, norm="sequences")
+    clean = _check_policy(a, starts, **kw)
+    at = np.flatnonzero(a["target"] >= 0)[[0, 3, -1]]
+    a["logp"][at] = -np.inf
+    got, status = _run_policy(a, starts, **kw)
+    assert status == 0 and all(torch.equal(got[k], clean[k]) for k in got)
+    a["logp"][at[1]] = np.nan
+    assert _run_policy(a, starts, **kw)[1] == r3.DATA_NONFINITE
