@@ -396,7 +396,8 @@ int r3_token_logprobs_backward(int64_t n, int64_t V, int dtype, const void *logi
  * stats [8] f32: loss, sum nu (-w used A), sum nu k / scale, sum nu entropy /
  * scale, share of live tokens that clipping holds, mean w, live tokens, sequences
  * with live tokens (shares and means of nothing: 0).  Sums are made in 64 bits.
- * kl_coef needs logp_ref, entropy_coef needs entropy, unless they are 0.  dlogp,
+ * kl_coef needs logp_ref, entropy_coef needs entropy, unless they are 0: then the
+ * term is in the statistics alone, if its array is there.  dlogp,
  * dentropy [n]: may be NULL.  A live token whose loss or gradient is not finite
  * sets R3_DATA_NONFINITE.  0 <= clip_low <= 1, clip_high >= 0, dual_clip 0 or > 1,
  * weight_cap > 0; they and the coefficients finite, but for weight_cap, which may

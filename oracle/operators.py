@@ -233,7 +233,8 @@ def policy_loss(logp, adv, old=None, infer=None, ref=None, entropy=None, target=
             room[0] += abs(nu) * (np.abs(l) * (tr + tw + 12 * U)).sum()
             if ref is not None:
                 k = ref[g] - x
-                dl[g] -= beta * np.expm1(k)
+                if beta:      # (a term with coefficient 0 is a statistic alone)
+                    dl[g] -= beta * np.expm1(k)
                 tl[g] += abs(beta) * U * (8 * np.abs(np.expm1(k)) + np.exp(k) * np.abs(k))
                 parts[1] += nu * (np.expm1(k) - k).sum()
                 room[1] += abs(nu) * U * (12 * np.abs(np.expm1(k) - k) + 2 * np.abs(np.expm1(k) * k) + 4 * np.abs(k) * (np.abs(k) > 0.12)).sum()
@@ -249,7 +250,8 @@ def policy_loss(logp, adv, old=None, infer=None, ref=None, entropy=None, target=
             wroom += (w * tw).sum()
     one = max(N, 1)
     inv = 1 / scale if scale else 0.0
-    stats = np.array([parts[0] + beta * parts[1] - gamma * parts[2], parts[0], parts[1] * inv, parts[2] * inv, cuts / one, weights / one, N, S])
+    loss = parts[0] + (beta * parts[1] if beta else 0.0) - (gamma * parts[2] if gamma else 0.0)
+    stats = np.array([loss, parts[0], parts[1] * inv, parts[2] * inv, cuts / one, weights / one, N, S])
     tol = np.array([room[0] + abs(beta) * room[1] + abs(gamma) * room[2], room[0], room[1] * abs(inv), room[2] * abs(inv), 0.0, wroom / one, 0.0, 0.0])
     tol += 2 * U * np.abs(stats) + 1e-37
     return {"stats": stats, "dlogp": dl, "dentropy": dh, "tol_stats": tol, "tol_dlogp": tl + 1e-37, "tol_dentropy": th + 1e-37}

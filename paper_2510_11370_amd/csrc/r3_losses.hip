@@ -358,12 +358,14 @@ struct PolicyPart {
                 const double k3 = fabsf(x) < 0.125f ? y * y * (1.0 / 2 + y * (1.0 / 6 + y * (1.0 / 24 + y * (1.0 / 120 + y * (1.0 / 720 + y * (1.0 / 5040))))))
                                                     : (double)ex - y;
                 sum[1] += (double)nu * k3;
-                g = fmaf(-a.kl, ex, g);
-                l += a.kl * (float)k3;
+                if (a.kl != 0.0f) {      // (a term with coefficient 0 is a statistic alone)
+                    g = fmaf(-a.kl, ex, g);
+                    l += a.kl * (float)k3;
+                }
             }
             if (a.entropy) {
                 sum[2] += (double)nu * k.H;
-                l -= a.ent * k.H;
+                if (a.ent != 0.0f) l -= a.ent * k.H;
             }
             sum[3] += cut;
             sum[4] += w;
@@ -461,7 +463,7 @@ __global__ void __launch_bounds__(kThreads) policy_tokens_kernel(Policy a) {
 // the loss and its parts, from the sums
 __device__ __forceinline__ void policy_stats(const Policy &a, const double (&v)[kPolicySums], const PolicyTotals &all) {
     const double some = all.live > 0.0 ? all.live : 1.0, unit = a.scale != 0.0f ? 1.0 / a.scale : 0.0;
-    a.stats[0] = (float)(v[0] + (double)a.kl * v[1] - (double)a.ent * v[2]);
+    a.stats[0] = (float)(v[0] + (a.kl != 0.0f ? (double)a.kl * v[1] : 0.0) - (a.ent != 0.0f ? (double)a.ent * v[2] : 0.0));
     a.stats[1] = (float)v[0];
     a.stats[2] = (float)(v[1] * unit);
     a.stats[3] = (float)(v[2] * unit);

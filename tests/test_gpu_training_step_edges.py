@@ -136,3 +136,25 @@ def test_on_the_policy_the_ratio_is_one_whatever_the_log_probability_is(n, nseq,
     assert status == 0 and all(torch.equal(got[k], clean[k]) for k in got)
     a["logp"][at[1]] = np.nan
     assert _run_policy(a, starts, **kw)[1] == r3.DATA_NONFINITE
+
+
+@pytest.mark.parametrize("ratio", ["token", "sequence"])
+@pytest.mark.parametrize("n,nseq", LAYOUTS)
+def test_terms_that_are_only_watched(n, nseq, ratio):
+    """With a coefficient of 0 the KL and entropy terms are statistics: what overflows there stays there."""
+    starts, a = _even(n, nseq), _policy(n)
+    kw = dict(ratio=ratio, norm="tokens")
+    _check_policy(a, starts, **kw)
+    bare = {k: v for k, v in a.items() if k not in ("ref", "entropy")}
+    clean, _ = _run_policy(bare, starts, **kw)
+    at = np.flatnonzero(a["target"] >= 0)[[0, 3, -1]]
+    a["ref"][at] = a["logp"][at] + np.float32(200)
+    a["entropy"][at] = np.inf
+    got, status = _run_policy(a, starts, **kw)
+    assert status == 0 and torch.equal(got["dlogp"], clean["dlogp"]) and (got["dentropy"] == 0).all()
+    assert torch.isinf(got["stats"][2:4]).all()
+    keep = [0, 1, 4, 5, 6, 7]
+    assert torch.equal(got["stats"][keep], clean["stats"][keep])
+    # and with a coefficient they count
+    assert _run_policy(a, starts, kl_coef=0.1, **kw)[1] == r3.DATA_NONFINITE
+    assert _run_policy(a, starts, entropy_coef=0.1, **kw)[1] == r3.DATA_NONFINITE
