@@ -348,6 +348,28 @@ def _rows(what, name, t, dev, T, E):
     return t.data_ptr(), t.stride(0) if T > 1 else max(E, t.stride(0))
 
 
+def _record(what, D, idx, dev):
+    """Address of a record: T rows, desc's idx_token_stride elements apart (K if that is 0), of K ids side by side.  A tensor's rows are those of
+    its first dimension ([T,K] and columns of it, [T,L,K]), or of all but its last ([B,S,K]); one of one dimension may hold any."""
+    T, K = D.T, D.K
+    stride = D.idx_token_stride or K
+    if idx.get_device() != dev or idx.dtype is not idx_torch_dtype(D):
+        raise R3Error("%s: idx has to be the record of desc's type on cuda:%d" % (what, dev))
+    if stride == K and idx.shape == (T, K) and idx.is_contiguous():
+        return idx.data_ptr()
+    if idx.dim() == 1 and idx.is_contiguous() and idx.numel() >= (T - 1) * stride + K:
+        return idx.data_ptr()
+    if idx.dim() > 1:
+        for shape in [(idx.shape[0], -1)] + ([(-1, idx.shape[-1])] if idx.shape[0] != T else []):
+            try:
+                rows = idx.view(shape)
+            except RuntimeError:      # (no such rows, or not evenly apart)
+                continue
+            if rows.shape[0] >= T and rows.shape[1] >= K and (T == 1 or rows.stride(0) == stride) and (K == 1 or rows.stride(1) == 1):
+                return idx.data_ptr()
+    raise R3Error("%s: idx has to hold %d records of %d ids, %d elements apart" % (what, T, K, stride))
+
+
 def balance_loss(D, logits, idx, stats, counts=None, probs=None, dlogits=None, seq_start=None, balance_coef=0.01, z_coef=0.0, status=None,
                  ws=None):
     """Load-balance loss of the record idx (as replay_gate takes it) and z-loss of the router's logits [T,E] (rows may be strided):
@@ -359,10 +381,8 @@ def balance_loss(D, logits, idx, stats, counts=None, probs=None, dlogits=None, s
     ws = _workspace(w, ws, dev, lambda: balance_loss_workspace(D, nseq, logits.device))
     at, ld = _rows(w, "logits", logits, dev, D.T, D.E)
     dat, ldd = _rows(w, "dlogits", dlogits, dev, D.T, D.E)
-    if idx.get_device() != dev or idx.dtype is not idx_torch_dtype(D) or idx.numel() < D.T * D.K:
-        raise R3Error("%s: idx has to be the record of desc's type on cuda:%d" % (w, dev))
     _check(lib().r3_balance_loss(
-        C.byref(D), at, ld, idx.data_ptr(), _at(w, "seq_start", seq_start, dev, i, (nseq + 1,)), nseq, balance_coef, z_coef,
+        C.byref(D), at, ld, _record(w, D, idx, dev), _at(w, "seq_start", seq_start, dev, i, (nseq + 1,)), nseq, balance_coef, z_coef,
         _at(w, "counts", counts, dev, i, groups), _at(w, "probs", probs, dev, f, groups), _at(w, "stats", stats, dev, f, (3,)), dat, ldd,
         _at(w, "status", status, dev, i, (1,)), ws.data_ptr(), ws.numel(), _raw_stream(dev)), "r3_balance_loss")
 

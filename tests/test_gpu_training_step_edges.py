@@ -158,3 +158,25 @@ def test_terms_that_are_only_watched(n, nseq, ratio):
     # and with a coefficient they count
     assert _run_policy(a, starts, kl_coef=0.1, **kw)[1] == r3.DATA_NONFINITE
     assert _run_policy(a, starts, entropy_coef=0.1, **kw)[1] == r3.DATA_NONFINITE
+
+
+def test_records_of_several_layers_and_views_that_are_none():
+    T, E, K, L = 90, 20, 3, 4
+    g = torch.Generator().manual_seed(1)
+    z = torch.randn(T, E, generator=g).to(DEV)
+    rec = torch.randint(0, E, (T, L, K), generator=g).to(torch.uint8).to(DEV)
+
+    def run(idx, stride=0):
+        o = dict(stats=torch.empty(3, device=DEV), counts=torch.empty(1, E, dtype=torch.int32, device=DEV), dlogits=torch.empty(T, E, device=DEV))
+        r3.balance_loss(r3.desc(T, 8, E, K, 8, idx_token_stride=stride), z, idx, z_coef=0.1, **o)
+        return o
+
+    for layer in range(L):
+        want = run(rec[:, layer].contiguous())
+        assert torch.equal(want["counts"][0], torch.bincount(rec[:, layer].reshape(-1).int(), minlength=E).int())
+        for got in (run(rec[:, layer], L * K), run(rec.reshape(-1)[layer * K:], L * K), run(rec[:, layer].view(9, 10, K), L * K),
+                    run(rec[:, layer].contiguous().view(9, 10, K))):
+            assert all(torch.equal(got[k], want[k]) for k in want)
+    for idx, stride in ((rec[:, 1], 0), (rec, 0), (rec[:, 1].view(9, 10, K), 0), (rec[:, 1].contiguous(), L * K), (rec.reshape(-1)[1:][:(T - 1) * L * K + K - 1], L * K)):
+        with pytest.raises(r3.R3Error):
+            run(idx, stride)

@@ -3,6 +3,7 @@ needed: addresses are numbers, and each call is refused)."""
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_2510_11370_amd import build as hip_build
 from paper_2510_11370_amd import r3
@@ -30,3 +31,28 @@ def test_the_policy_loss_refuses_a_workspace_too_small_for_one_sequence(n, nseq)
     D = r3.policy_desc(n, nseq)
     at = A[:7] + [None] + A[8:13]                 # (no seq_start)
     assert r3.lib().r3_policy_loss(C.byref(D), *at, _policy_bytes(n, 1) - 1, None) == WORKSPACE
+
+
+def _record(shape, **desc):
+    D = r3.desc(6, 8, 16, 2, 8, **desc)
+    rec = shape if isinstance(shape, torch.Tensor) else torch.zeros(shape, dtype=torch.uint8)
+    return r3._record("call", D, rec, -1) == rec.data_ptr()
+
+
+def test_the_binding_looks_at_a_record_s_rows():
+    wide = torch.zeros(6, 5, dtype=torch.uint8)
+    layers = torch.zeros(6, 3, 2, dtype=torch.uint8)
+    # six tokens' records of two ids
+    for good, stride in (((6, 2), 0), ((12,), 0), ((2, 3, 2), 0), ((9, 2), 0), (wide[:, :2], 5), (wide[:, 3:], 5), (wide, 5), ((5 * 5 + 2,), 5),
+                         (layers[:, 0], 6), (layers[:, 2], 6), (layers, 6), (torch.zeros(2, 3, 4, 2, dtype=torch.uint8)[:, :, 1], 8)):
+        assert _record(good, idx_token_stride=stride), (good if isinstance(good, tuple) else good.shape, stride)
+    for bad, stride in ((wide[:, :2], 0), (wide, 0), (wide[:, 3:], 4), ((6, 2), 5), ((12,), 5), ((5 * 5 + 1,), 5), ((5, 2), 0), ((11,), 0), (layers[:, 0], 0), (layers, 2),
+                        (layers, 0), (layers[:, :, 0], 6), (wide.T, 0), (wide[:5, :2], 5), (torch.zeros(24, dtype=torch.uint8)[::2], 0),
+                        (torch.zeros(1, 2, dtype=torch.uint8).expand(6, 2), 0), (torch.zeros(6, 2, dtype=torch.uint16), 0), (torch.zeros(6, 2, dtype=torch.int64), 0)):
+        with pytest.raises(r3.R3Error):
+            _record(bad, idx_token_stride=stride)
+    # one token: its record alone counts
+    one = r3.desc(1, 8, 16, 2, 8, idx_token_stride=9)
+    r3._record("call", one, torch.zeros(1, 2, dtype=torch.uint8), -1)
+    with pytest.raises(r3.R3Error):
+        r3._record("call", one, torch.zeros(1, 1, dtype=torch.uint8), -1)
