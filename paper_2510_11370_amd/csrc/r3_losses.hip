@@ -955,7 +955,7 @@ template <typename IdxT, int L> __global__ void __launch_bounds__(kThreads) bala
 }
 
 // One work-group up to 16 K logits of few groups.
-bool balance_small(int64_t T, int E, int nseq) { return E <= kSmallE && T * E <= 16384 && T <= 512 && nseq * E <= 1024; }
+bool balance_small(int64_t T, int E, int nseq) { return E <= kSmallE && T * E <= 16384 && T <= 512 && (int64_t)nseq * E <= 1024; }
 
 // A work-group to a group saves the join of pieces: up to 32768 slots of one, 65536 of two, and 262144 of 32 and more, which seldom are one's (us
 // a call, pieces | whole: 4000 x 128, 8 slots 16.3 | 16.0, 1000 14.3 | 12.3; two groups of 8000 20.5 | 18.6, all in one 19.5 | 19.1; 64 of 32000

@@ -180,3 +180,25 @@ def test_records_of_several_layers_and_views_that_are_none():
     for idx, stride in ((rec[:, 1], 0), (rec, 0), (rec[:, 1].view(9, 10, K), 0), (rec[:, 1].contiguous(), L * K), (rec.reshape(-1)[1:][:(T - 1) * L * K + K - 1], L * K)):
         with pytest.raises(r3.R3Error):
             run(idx, stride)
+
+
+def test_far_more_groups_than_tokens():
+    # groups times experts is 2^31: beyond 32 bits, and no single work-group's
+    nseq, T, E = 1 << 23, 5, 256
+    g = torch.Generator().manual_seed(1)
+    z, idx = torch.randn(T, E, generator=g).to(DEV), torch.randint(0, E, (T, 2), generator=g).to(torch.uint8).to(DEV)
+    starts = torch.zeros(nseq + 1, dtype=torch.int32, device=DEV)
+    starts[nseq // 2:] = 2
+    starts[-1] = T
+    few = torch.tensor([0, 2, T], dtype=torch.int32, device=DEV)
+    got = []
+    for s in (starts, few):
+        o = dict(stats=torch.empty(3, device=DEV), dlogits=torch.empty(T, E, device=DEV), counts=torch.full((s.numel() - 1, E), 7, dtype=torch.int32, device=DEV))
+        r3.balance_loss(r3.desc(T, 8, E, 2, 8), z, idx, seq_start=s, z_coef=0.1, **o)
+        got.append(o)
+    a, b = got
+    assert torch.equal(a["counts"][nseq // 2 - 1], b["counts"][0]) and torch.equal(a["counts"][-1], b["counts"][1]) and a["counts"].sum().item() == 2 * T
+    want = ref.balance_loss(z.double().cpu().numpy(), idx.cpu().numpy(), np.array([0, 2, T]), 0.01, 0.1)
+    for o in got:
+        _near(o["stats"], want["stats"], want["tol_stats"], "stats")
+        _near(o["dlogits"], want["dlogits"], want["tol_dlogits"], "dlogits")

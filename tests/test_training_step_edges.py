@@ -56,3 +56,13 @@ def test_the_binding_looks_at_a_record_s_rows():
     r3._record("call", one, torch.zeros(1, 2, dtype=torch.uint8), -1)
     with pytest.raises(r3.R3Error):
         r3._record("call", one, torch.zeros(1, 1, dtype=torch.uint8), -1)
+
+
+def test_a_balance_workspace_grows_by_the_sequences_alone():
+    # one layout for more than a few groups: a row of slots, of probabilities and of counts to each, whatever nseq E is modulo 2^32
+    hip_build.build()
+    D = r3.desc(64, 8, 256, 2, 8)
+    size = lambda nseq: r3.lib().r3_balance_loss_workspace_bytes(C.byref(D), nseq)  # noqa: E731
+    at = [5000, 1 << 22, (1 << 23) - 1, 1 << 23, (1 << 23) + 1, 1 << 24, (1 << 24) + 8, 1 << 25, (1 << 31) - 65537]
+    for a, b in zip(at, at[1:]):
+        assert size(b) - size(a) == (b - a) * 3 * 256 * 4, (a, b)
