@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(kThreads) policy_segments_kernel(Policy a) {
         SegSum s = segment_part(a, q, b, e, all ? (int)threadIdx.x : lane_id(), all ? kThreads : kWave);
         if (all) over_block_sums<kThreads>(a, s, room);
         else over_wave_sums(a, s);
-        if ((all ? (int)threadIdx.x : lane_id()) == 0 && b < e) a.seg[p + q] = s;
+        if ((all ? (int)threadIdx.x : lane_id()) == 0 && b < e) a.seg[(int64_t)p + q] = s;
     });
 }
 
@@ -246,9 +246,9 @@ template <bool MANY> __global__ void __launch_bounds__(kThreads) policy_sequence
     __shared__ PolicyTotals room[kThreads / kWave];
     const int lane = lane_id(), wave = threadIdx.x / kWave;
     // where sequence q's segments are, and how many
-    auto segments = [&](int q, int &at, int &n) {
+    auto segments = [&](int q, int64_t &at, int &n) {
         const int64_t b = a.q.first(q), e = a.q.first(q + 1);
-        at = b < e ? (int)(b / a.piece) + q : 0;
+        at = b < e ? b / a.piece + q : 0;
         n = b < e ? (int)((e - 1) / a.piece) + q - at + 1 : 0;
     };
     PolicyTotals t = {0.0, 0.0};
@@ -257,7 +257,8 @@ template <bool MANY> __global__ void __launch_bounds__(kThreads) policy_sequence
         t.live += (double)s.live;
         t.seqs += s.live > 0;
     };
-    int at = 0, n = 0;
+    int64_t at = 0;
+    int n = 0;
     SegSum s = {0.0, 0.0, 0.0, 0};
     if constexpr (!MANY) {
         const int q = blockIdx.x * (kThreads / kWave) + wave;
@@ -274,7 +275,8 @@ template <bool MANY> __global__ void __launch_bounds__(kThreads) policy_sequence
         if (n <= kFew)
             for (int i = 0; i < n; ++i) add_sums(s, a.seg[at + i]);
         for (uint64_t many = __ballot(n > kFew); many; many &= many - 1) {
-            const int who = __builtin_ctzll(many), f = __shfl(at, who), m = __shfl(n, who);
+            const int who = __builtin_ctzll(many), m = __shfl(n, who);
+            const int64_t f = __shfl(at, who);
             SegSum w = {0.0, 0.0, 0.0, 0};
             for (int i = lane; i < m; i += kWave) add_sums(w, a.seg[f + i]);
             over_wave_sums(a, w);
@@ -552,7 +554,7 @@ PolicyPlan policy_plan(int64_t n, int nseq) {
     p.npieces = (int)((n + p.piece - 1) / p.piece);
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes, 256); return at; };
-    p.seg = take(p.whole ? 0 : (size_t)(p.npieces + nseq) * sizeof(SegSum));
+    p.seg = take(p.whole ? 0 : ((size_t)p.npieces + nseq) * sizeof(SegSum));
     p.seq = take((size_t)nseq * sizeof(SeqOut));
     p.tot = take((size_t)p.ntot * sizeof(PolicyTotals));
     p.part = take((size_t)p.npieces * kPolicySums * sizeof(double));
@@ -980,8 +982,8 @@ BalancePlan balance_plan(int64_t T, int E, int nseq) {
     p.npieces = (int)((T + p.piece - 1) / p.piece);
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes, 256); return at; };
-    p.hist = take((size_t)(p.npieces0 + nseq) * E * sizeof(int32_t));
-    p.psum = take((size_t)(p.npieces + nseq) * E * sizeof(float));
+    p.hist = take(((size_t)p.npieces0 + nseq) * E * sizeof(int32_t));
+    p.psum = take(((size_t)p.npieces + nseq) * E * sizeof(float));
     p.lsum = take((size_t)p.npieces * 2 * sizeof(double));
     p.tot = take(2 * sizeof(double));
     p.counts = take((size_t)nseq * E * sizeof(int32_t));

@@ -66,3 +66,12 @@ def test_a_balance_workspace_grows_by_the_sequences_alone():
     at = [5000, 1 << 22, (1 << 23) - 1, 1 << 23, (1 << 23) + 1, 1 << 24, (1 << 24) + 8, 1 << 25, (1 << 31) - 65537]
     for a, b in zip(at, at[1:]):
         assert size(b) - size(a) == (b - a) * 3 * 256 * 4, (a, b)
+
+
+def test_a_policy_workspace_grows_with_the_sequences_up_to_their_limit():
+    hip_build.build()
+    n = (1 << 31) - 65537
+    at = [1 << 20, 1 << 24, 1 << 28, 1 << 30, (1 << 31) - (1 << 19), (1 << 31) - (1 << 17), (1 << 31) - 65537]
+    slopes = [(_policy_bytes(n, b) - _policy_bytes(n, a)) / (b - a) for a, b in zip(at, at[1:])]
+    # (four arrays, each rounded up to 256 bytes, over 2^16 sequences and more)
+    assert max(slopes) - min(slopes) <= 2 * 4 * 256 / 65536, slopes
