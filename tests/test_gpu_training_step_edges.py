@@ -202,3 +202,22 @@ def test_far_more_groups_than_tokens():
     for o in got:
         _near(o["stats"], want["stats"], want["tol_stats"], "stats")
         _near(o["dlogits"], want["dlogits"], want["tol_dlogits"], "dlogits")
+
+
+@pytest.mark.parametrize("ratio", ["token", "sequence"])
+@pytest.mark.parametrize("norm", ["tokens", "sequences"])
+def test_long_sequences_among_many_short_ones(ratio, norm):
+    # more sequences than a wave has lanes for, most of none or one token; some of many pieces, side by side and alone, first and last
+    rng = np.random.default_rng(5)
+    lens = rng.integers(0, 2, 5000)
+    for q, n in {0: 3000, 64: 100000, 65: 5000, 66: 2500, 67: 2047, 127: 2049, 130: 12345, 191: 2600, 2000: 513, 4095: 30000, 4096: 2561, 4999: 40000}.items():
+        lens[q] = n
+    starts = np.concatenate([[17], 17 + np.cumsum(lens)])
+    n = starts[-1] + 9
+    a = _policy(n, seed=3)
+    a["target"][starts[65]:starts[66]] = -1          # a long one without a live token
+    kw = dict(ratio=ratio, norm=norm, kl_coef=0.05, entropy_coef=0.01, scale=0.5)
+    got = _check_policy(a, starts, **kw)
+    again, _ = _run_policy(a, starts, **kw)
+    assert all(torch.equal(got[k], again[k]) for k in got)
+    assert got["stats"][7] == sum((a["target"][b:e] >= 0).any() for b, e in zip(starts, starts[1:]))
