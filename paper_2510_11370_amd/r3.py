@@ -409,6 +409,8 @@ def orthogonalize(G, out, steps=5, coef=None, eps=1e-7, scale=1.0, status=None, 
     A = X X^T, from X = G / (|G| + eps).  coef: (a, b, c).  out: G's shape, bfloat16 or float32 (more exact); may be G.
     ws: orthogonalize_workspace(G, out); made here if it is not given."""
     w = "orthogonalize"
+    if coef is not None and len(coef) != 3:
+        raise R3Error("%s: coef is three numbers (a, b, c)" % w)
     b, r, c, src, to = _matrices(w, G, out)
     dev = _device(w, G)
     ws = _workspace(w, ws, dev, lambda: orthogonalize_workspace(G, out))

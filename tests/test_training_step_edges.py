@@ -75,3 +75,10 @@ def test_a_policy_workspace_grows_with_the_sequences_up_to_their_limit():
     slopes = [(_policy_bytes(n, b) - _policy_bytes(n, a)) / (b - a) for a, b in zip(at, at[1:])]
     # (four arrays, each rounded up to 256 bytes, over 2^16 sequences and more)
     assert max(slopes) - min(slopes) <= 2 * 4 * 256 / 65536, slopes
+
+
+def test_the_binding_wants_three_coefficients():
+    G = torch.zeros(3, 4)
+    for coef in ((), (1.5,), (1.5, -0.5), (1.5, -0.5, 0.0, 0.0)):
+        with pytest.raises(r3.R3Error, match="three"):
+            r3.orthogonalize(G, G, coef=coef)
