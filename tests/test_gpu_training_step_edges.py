@@ -221,3 +221,65 @@ def test_long_sequences_among_many_short_ones(ratio, norm):
     again, _ = _run_policy(a, starts, **kw)
     assert all(torch.equal(got[k], again[k]) for k in got)
     assert got["stats"][7] == sum((a["target"][b:e] >= 0).any() for b, e in zip(starts, starts[1:]))
+
+
+# ---- orthogonalised updates ----
+
+def _matrices(kind, b, r, c, seed=0):
+    g = torch.Generator().manual_seed(seed + 37 * r + c)
+    if kind == "flat":
+        return torch.randn(b, r, c, generator=g)
+    if kind == "rank 3":
+        return torch.randn(b, r, 3, generator=g) @ torch.randn(b, 3, c, generator=g)
+    low = min(r, c) // 4
+    return (torch.randn(b, r, low, generator=g) * torch.arange(1, low + 1).pow(-0.7)) @ torch.randn(b, low, c, generator=g) + 0.3 * torch.randn(b, r, c, generator=g)
+
+
+def _steps(G, dtype):
+    """Five steps of the short side's products in `dtype`, and each product's operands with it"""
+    X = G.astype(dtype) if G.shape[0] <= G.shape[1] else G.T.astype(dtype)
+    X = (X / (np.linalg.norm(X.astype(np.float64)) + 1e-7)).astype(dtype)
+    a, b, c = (np.float32(v).astype(dtype) for v in ref.QUINTIC)
+    for _ in range(5):
+        A = X @ X.T
+        X = a * X + (b * A + c * (A @ A)) @ X
+    return X if G.shape[0] <= G.shape[1] else X.T
+
+
+@pytest.mark.parametrize("kind", ["flat", "falling", "rank 3"])
+# a short side of 128 and less, tiles of 64 x 64, tiles of 256 x 256
+@pytest.mark.parametrize("b,r,c", [(3, 100, 700), (2, 900, 128), (3, 256, 768), (2, 700, 300), (100, 256, 768), (90, 700, 300)])
+def test_f32_results_are_as_exact_as_f32_products(b, r, c, kind):
+    """Each rounding of the same steps in f32 has one here that is at most four times as large: a pair's last place is 2^-22 of a value where an
+    f32's is 2^-24, and sums are f32 in both.  So the error is at most four times theirs (with operands of two bits less it would be sixteen
+    times)."""
+    G = _matrices(kind, b, r, c)
+    out = torch.empty(b, r, c, device=DEV)
+    r3.orthogonalize(G.to(DEV), out)
+    for i in (0, b // 2, b - 1):
+        want = _steps(G[i].numpy(), np.float64)
+        f32 = np.linalg.norm(_steps(G[i].numpy(), np.float32) - want)
+        off = np.linalg.norm(out[i].double().cpu().numpy() - want)
+        assert off <= 4 * f32, (i, off, f32, np.linalg.norm(want))
+
+
+@pytest.mark.parametrize("b,r,c", [(110, 130, 640), (70, 300, 700), (50, 700, 400), (64, 257, 1000), (12, 1100, 1300)])
+def test_f32_results_of_many_bf16_gradients(b, r, c):
+    G = _matrices("falling", b, r, c, seed=1).bfloat16()
+    big = torch.full((b + 1, r, c), 77.0, device=DEV)
+    r3.orthogonalize(G.to(DEV), big[:b], scale=1.5)
+    assert (big[b:] == 77).all()
+    for i in (0, 1, b // 2, b - 1):
+        want, tol = ref.orthogonalize(G[i].double().numpy(), scale=1.5)
+        assert np.linalg.norm(big[i].double().cpu().numpy() - want) <= tol, i
+    # the same numbers as f32 gradients
+    wide = torch.empty(b, r, c, device=DEV)
+    r3.orthogonalize(G.float().to(DEV), wide, scale=1.5)
+    assert torch.equal(wide, big[:b])
+    G[b // 3, r - 1, c - 1] = float("nan")
+    G[0] = 0.0
+    clean, status = big[:b].clone(), torch.zeros(1, dtype=torch.int32, device=DEV)
+    r3.orthogonalize(G.to(DEV), big[:b], scale=1.5, status=status)
+    assert status.item() == r3.DATA_NONFINITE and torch.isnan(big[b // 3]).all() and (big[0] == 0).all()
+    rest = [i for i in range(1, b) if i != b // 3]
+    assert torch.equal(big[rest], clean[rest])
