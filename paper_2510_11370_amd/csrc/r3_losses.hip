@@ -101,7 +101,7 @@ struct Policy {
     Seqs q;
     int piece, npieces;
     int norm;
-    bool seq_ratio, adv_seq;
+    bool seq_ratio, adv_seq, kl_counts, ent_counts;
     const float *logp, *old, *infer, *ref, *entropy, *adv;
     const int32_t *target;
     float *dlogp, *dentropy, *stats;
@@ -175,10 +175,9 @@ __device__ __forceinline__ SegSum segment_part(const Policy &a, int q, int64_t b
             ++s.live;
             if (!a.seq_ratio) continue;
             s.d += log_ratio(a, k[u]);
-            const float wA = weight(a, k[u]) * k[u].A;
-            if (k[u].A > 0.0f) s.pos += wA;
-            else if (k[u].A < 0.0f) s.neg += wA;
-            else if (k[u].A != 0.0f) s.pos += k[u].A;   // (a NaN; without an advantage the weight does not matter)
+            const float wA = k[u].A == 0.0f ? 0.0f : weight(a, k[u]) * k[u].A;   // (without an advantage the weight does not matter)
+            if (k[u].A < 0.0f) s.neg += wA;
+            else s.pos += wA;      // (or a NaN)
         }
     }
     return s;
@@ -353,22 +352,27 @@ struct PolicyPart {
             }
             float l = A == 0.0f ? 0.0f : -wA * used;
             sum[0] += (double)nu * l;
-            if (a.ref) {
-                const float x = k.ref - k.x, ex = expm1f(x);
-                // e^x - 1 - x: its leading terms where they cancel (the next is 2e-10 of them)
+            // e^x - 1 - x: its leading terms where they cancel (the next is 2e-10 of them)
+            auto third = [](float x, float ex) {
                 const double y = x;
-                const double k3 = fabsf(x) < 0.125f ? y * y * (1.0 / 2 + y * (1.0 / 6 + y * (1.0 / 24 + y * (1.0 / 120 + y * (1.0 / 720 + y * (1.0 / 5040))))))
-                                                    : (double)ex - y;
+                return fabsf(x) < 0.125f ? y * y * (1.0 / 2 + y * (1.0 / 6 + y * (1.0 / 24 + y * (1.0 / 120 + y * (1.0 / 720 + y * (1.0 / 5040))))))
+                                         : (double)ex - y;
+            };
+            // (a term with coefficient 0 is a statistic alone; a branch inside one that counts costs 1 M tokens 1.4 us)
+            if (a.kl_counts) {
+                const float x = k.ref - k.x, ex = expm1f(x);
+                const double k3 = third(x, ex);
                 sum[1] += (double)nu * k3;
-                if (a.kl != 0.0f) {      // (a term with coefficient 0 is a statistic alone)
-                    g = fmaf(-a.kl, ex, g);
-                    l += a.kl * (float)k3;
-                }
+                g = fmaf(-a.kl, ex, g);
+                l += a.kl * (float)k3;
+            } else if (a.ref) {
+                const float x = k.ref - k.x;
+                sum[1] += (double)nu * third(x, expm1f(x));
             }
-            if (a.entropy) {
+            if (a.ent_counts) {
                 sum[2] += (double)nu * k.H;
-                if (a.ent != 0.0f) l -= a.ent * k.H;
-            }
+                l -= a.ent * k.H;
+            } else if (a.entropy) sum[2] += (double)nu * k.H;
             sum[3] += cut;
             sum[4] += w;
             g *= nu;
@@ -465,7 +469,7 @@ __global__ void __launch_bounds__(kThreads) policy_tokens_kernel(Policy a) {
 // the loss and its parts, from the sums
 __device__ __forceinline__ void policy_stats(const Policy &a, const double (&v)[kPolicySums], const PolicyTotals &all) {
     const double some = all.live > 0.0 ? all.live : 1.0, unit = a.scale != 0.0f ? 1.0 / a.scale : 0.0;
-    a.stats[0] = (float)(v[0] + (a.kl != 0.0f ? (double)a.kl * v[1] : 0.0) - (a.ent != 0.0f ? (double)a.ent * v[2] : 0.0));
+    a.stats[0] = (float)(v[0] + (a.kl_counts ? (double)a.kl * v[1] : 0.0) - (a.ent_counts ? (double)a.ent * v[2] : 0.0));
     a.stats[1] = (float)v[0];
     a.stats[2] = (float)(v[1] * unit);
     a.stats[3] = (float)(v[2] * unit);
@@ -583,6 +587,7 @@ hipError_t launch_policy_loss(const r3_policy_desc &D, const float *logp, const 
     a.log_up = std::log1p((double)D.clip_high);
     a.log_down = D.clip_low < 1.0f ? std::log1p(-(double)D.clip_low) : -INFINITY;
     a.log_dual = D.dual_clip > 0.0f ? std::log((double)D.dual_clip) : INFINITY;
+    a.kl_counts = D.kl_coef != 0.0f; a.ent_counts = D.entropy_coef != 0.0f;
     a.cap = D.weight_cap; a.kl = D.kl_coef; a.ent = D.entropy_coef; a.scale = D.scale;
     a.seg = (SegSum *)(base + p.seg); a.seq = (SeqOut *)(base + p.seq); a.tot = (PolicyTotals *)(base + p.tot); a.part = (double *)(base + p.part);
     a.ntot = p.ntot;
