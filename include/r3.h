@@ -446,6 +446,9 @@ int r3_policy_loss(const r3_policy_desc *desc, const float *logp, const float *l
  * with ldd = ld; otherwise no output, nor ws, may lie between another array's
  * first element and its last.  T * max(ld, ldd) <= 2^48.
  * A token's gradient is the same bits whatever the other groups' logits are.
+ * Exponential, logarithm and reciprocal are the hardware's, each within a unit in
+ * the last place; sums over a row are f32, those over tokens 64 bits but for the
+ * probabilities' of a piece of a group.
  * ws: device workspace of r3_balance_loss_workspace_bytes(), 256-byte aligned.
  */
 size_t r3_balance_loss_workspace_bytes(const r3_layer_desc *desc, int nseq);
@@ -468,9 +471,11 @@ int r3_balance_loss(const r3_layer_desc *desc, const float *logits, int64_t ld, 
  * G and out: dense [batch, rows, cols], dtype R3_BF16 or R3_F32 each.  The
  * products' operands are f16 numbers with f32 sums; for dtype_out R3_F32, and
  * where rows or cols are at most 128, they are sums of two such, 22 bits.
- * Relative to each matrix (2-norm) a bf16 result is off by about 1e-3 beside its
- * own rounding, an f32 one by 1e-6, as f32 products are (three times as much
- * where most of G is within rounding of a few dimensions).
+ * Errors of five steps, relative to each result in the Frobenius norm, beside a
+ * bf16 result's own rounding (1.7e-3): bf16 1e-3 where many directions count, 8e-3
+ * where G has one to four (it is spread over all the others: 2e-3 in the 2-norm),
+ * with a side of at most 128 less than 1e-4; f32 3e-6, and 1e-4 with one to four
+ * directions (6e-6 and 2e-5 in the 2-norm), as the same steps in f32 have.
  * A matrix of zeros gives zeros.  A NaN or an infinity in a matrix makes its
  * result NaN and sets R3_DATA_NONFINITE; the other matrices are as without it.
  * A matrix's bits do not depend on what the call's other matrices hold, but may

@@ -80,7 +80,8 @@ template <int NT, typename T> __device__ __forceinline__ T block_sum(T v, T *roo
 // Which side of a border a token lies on is decided on d in 64 bits, where the difference of two floats is exact.  Two passes (the first
 // reads only `target` unless ratios are a sequence's): tokens' weights need the numbers of live tokens.  Nothing but loads: the card is
 // never busy, launches and their latencies are the time up to some 100 K tokens (us: one work-group's 1531 tokens 10, 64 K in 64 sequences
-// 5 + 8.5 + 3, 1 M in 2048 with all terms 12.5 + 4 + 17 + 4, where the 17 move 38 MB at 2.2 TB/s).  The sums' last launch as the end of the
+// 5 + 8.5 + 3, 1 M in 2048 with all terms 12.5 + 4 + 17 + 4, where the 17 move 38 MB at 2.2 TB/s; the 12.5 read 4 MB, a piece's sequences one after
+// another, each two trips for its borders and targets and a sum with two barriers).  The sums' last launch as the end of the
 // tokens' (the last work-group to come adds all up): no faster at 64 K, 27 us instead of 21 at 1 M, as many counters' turns.
 // ---------------------------------------------------------------------------------------------------------------------------------
 
@@ -977,7 +978,8 @@ struct BalancePlan {
 };
 BalancePlan balance_plan(int64_t T, int E, int nseq) {
     BalancePlan p;
-    // counts: at most 128 work-groups of 1024 threads, so that few parts are added up
+    // counts: at most 128 work-groups of 1024 threads, as one group's join adds up a part of each.  (Many groups have few parts each whatever the
+    // limit is: half of the card idles then, 7.8 us for the 1 MB of 131072 x 8 in 64.)
     p.piece0 = (int)std::max<int64_t>((T + 127) / 128, 128);
     // logits: 16 KB and more to a work-group, at most 1024 of them (65536 x 128: 16.6 us; 2048 of them, whose beginnings and ends count,
     // 20.3)

@@ -10,9 +10,12 @@
 // singular value grows by a, a new one beside it does too), so while three steps and more are left X is kept as an f16 and 8 bits of what
 // its rounding leaves; the f16 alone enters the products, where the small directions hardly count.  The last two steps' polynomial has a +
 // b + c, what it is for singular values of 1, taken out of B and applied to X in f32, so that B's rounding is one of a small matrix.
-// Relative error of bf16 results beside their own rounding (1.7e-3): 8e-4 ... 1.1e-3 for matrices with flat and falling spectra, 3e-3 for
-// those of three directions; with bf16 operands throughout it is 1e-2 ... 4e-2.  For f32 results all of X, A, B are pairs of f16 and
-// products are the three of their parts that count (hi lo, lo hi, hi hi): 22 bits, 3e-7 ... 8e-7 where f32 products give 2e-7 ... 5e-7.
+// Relative error of bf16 results in the Frobenius norm, beside their own rounding (1.7e-3), at 256 x 768 and 768 x 2048: 7e-4 ... 1.1e-3 for
+// matrices with flat and falling spectra; 4e-3, 5e-3, 4e-3, 7.5e-3 for those of four, three, two and one directions, where what X's 8 bits leave
+// grows by a in every other direction (simulated with 11 bits: 3e-3; in the 2-norm, rounding included, all four are 9e-4 ... 1.8e-3); with bf16
+// operands throughout it is 1e-2 ... 4e-2.  For f32 results all of X, A, B are pairs of f16 and products are the three of their parts that count
+// (hi lo, lo hi, hi hi): 22 bits, 1.3e-6 ... 3e-6 and, of few directions, 2.4e-5 ... 8.2e-5, where the same steps in f32 on a CPU have 1.6e-6 ...
+// 2.4e-5 and 2.5e-5 ... 1.2e-4.
 //
 // 128 of 2048 x 768 f32 to bf16 3550 us, 32 of 768 x 2048 to f32 2132; the products alone would be 1992 and (three to one) 1493 at the 1.31
 // PFLOP/s of a large f16 product.  X X^T runs at 1.08 PFLOP/s (190 us), the products with X at 0.70 ... 0.85 (441 with X's 8 bits, 364
@@ -206,7 +209,8 @@ template <int N> __device__ __forceinline__ void read_down(const float *sums, in
     for (int u = 0; u < 8; ++u) v[u] = at[u * (N + 4)];
 }
 // What an f16 leaves of a value where it is not multiplied (X's, bf16 results): 8 bits with 2 of mantissa, times 2^8, which takes 1e-3 to 2^4
-// times kUnit's results to the middle of their range.  A quarter less to move than with f16 (128 of 2048 x 768: the start 300 -> 257 us).
+// times kUnit's results to the middle of their range.  A quarter less to move than with f16 (128 of 2048 x 768: the start 300 -> 257 us), for
+// less exactness in matrices of few directions (above).
 constexpr float kLow = 256.0f;
 __device__ __forceinline__ uint2 pack_low(const float *v, const f16x8_t &h) {
     float r[8];
@@ -893,9 +897,9 @@ Plan plan(int64_t batch, int64_t rows, int64_t cols, int dtype_out) {
 // Steps taken together: X'' = Q X with Q = (a + b A' + c A' A') (a + b A + c A A) and A' = (a + b A + c A A)^2 A, without X' between them:
 // five products of s x s instead of two, and a product with X and an X X^T less.  On small tiles that is as many launches, which are what
 // counts there, and steps stay apart.  Else for f32 results wherever two steps are left; for bf16 ones at the start alone, where it costs
-// no exactness: later a rounding of X enters the second product times a^2.  (Relative error beside the result's rounding, five steps,
-// random 256 x 768 / falling singular values / rank 3: apart 1.0e-3 / 7e-4 / 2.5e-3, the first two together the same, the first two pairs
-// 1.2e-3 / 1.6e-3 / 9e-3.)
+// no exactness: later a rounding of X enters the second product times a^2.  (Simulated with 11 bits of X's rest, Frobenius norm, five
+// steps, random 256 x 768 / falling singular values / rank 3: apart 1.1e-3 / 8e-4 / 3.0e-3, the first two together the same, the first two pairs
+// 1.3e-3 / 1.6e-3 / 9e-3.)
 bool two_together(int step, int steps, bool all, bool pairs) { return pairs && ortho_together(step, steps, all); }
 
 // Whether every element stays in (-15, 15), so that times kUnit it is an f16: a matrix's are at most its largest singular value, that of X
