@@ -401,7 +401,7 @@ int r3_token_logprobs_backward(int64_t n, int64_t V, int dtype, const void *logi
  * dentropy [n]: may be NULL.  A live token whose loss or gradient is not finite
  * sets R3_DATA_NONFINITE.  0 <= clip_low <= 1, clip_high >= 0, dual_clip 0 or > 1,
  * weight_cap > 0; they and the coefficients finite, but for weight_cap, which may
- * be infinite.  n = 0 gives stats of 0.  n < 2^31 - 2^16.
+ * be infinite.  n = 0 gives stats of 0.  n, nseq < 2^31 - 2^16.
  * No output, nor ws, may share bytes with another array.
  * ws: device workspace of r3_policy_loss_workspace_bytes(desc), 256-byte aligned;
  * enough with seq_start and without.
@@ -444,7 +444,7 @@ int r3_policy_loss(const r3_policy_desc *desc, const float *logp, const float *l
  * Of desc T, E, K, idx and idx_token_stride are used.  Rows are ld elements apart
  * (ld, ldd >= E; they may start at any element).  dlogits may be logits itself
  * with ldd = ld; otherwise no output, nor ws, may lie between another array's
- * first element and its last.  T * max(ld, ldd) <= 2^48.
+ * first element and its last.  T * max(ld, ldd) <= 2^48, nseq < 2^31 - 2^16.
  * A token's gradient is the same bits whatever the other groups' logits are.
  * Exponential, logarithm and reciprocal are the hardware's, each within a unit in
  * the last place; sums over a row are f32, those over tokens 64 bits but for the
